@@ -208,6 +208,79 @@ int lrsa_attn_decode(const lrsa_params_t* params, const void* cache, size_t cach
                      void* cuda_stream);
 
 /*
+ * Selection by accumulated attention weight, an alternative to the lag score of Eq. 4-8 (the paper has no counterpart: its
+ * selection does not look at queries).  A window's tokens are kept by the attention that they received while they were
+ * seen uncompressed.
+ *
+ * lrsa_attn_weights: weight[b, hkv, j] = sum over the query heads of group hkv and the queries t >= j that see position
+ * j >= S uncompressed (j >= S + n_c*L in the notation of lrsa_attn_fwd) of exp(scale * q_t k_j - LSE[t]); 0 for sinks, which
+ * are never candidates.  With the LSE of lrsa_attn_fwd these are the attention weights of that forward.  fp32 accumulation.
+ * No gradient: like the selection of lrsa_score_select, the one made from it is held constant.
+ *   Q in : bf16 [B, Hq, N, d];  K in : bf16 [B, Hkv, N, d];  LSE in : fp32 [B, Hq, N];  weight out : fp32 [B, Hkv, N]
+ *   workspace: 256 bytes (status word)
+ *
+ * lrsa_weight_select: of every scored window the top_k positions of largest weight, for lrsa_attn_fwd / lrsa_attn_bwd.  Equal
+ * weights keep the lower position, NaN ranks below every number.  Windows and layout as in lrsa_score_select; it needs no workspace.
+ *   weight in : fp32 [B, Hkv, N] (any values);  idx out : int32 [B, Hkv, W_sel, top_k], ascending inside a window
+ */
+int lrsa_attn_weights(const lrsa_params_t* params, const void* Q, const void* K, const float* LSE, float* weight,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+int lrsa_weight_select(const lrsa_params_t* params, const float* weight, int32_t* idx, void* cuda_stream);
+
+/*
+ * The store: the condensed cache of the calls above as tensors of the caller, with two choices.  The kept rows may be held
+ * in 8 bits, and windows may be cut by accumulated attention weight.  Restrictions of the cache hold (n_dense_prev = 1, no
+ * packed batches; every batch element has the same number of tokens).  With w_cap and rows_per_window from lrsa_store_shape,
+ * rows_per_window = top_k rounded up to a multiple of `block`:
+ *   k_list, v_list   [B, Hkv, w_cap * rows_per_window, d], of list_type: row j of window w at w * rows_per_window + j.  The
+ *                    rows behind the top_k of a window are written as zero and never seen.
+ *   k_scale, v_scale fp32 [B, Hkv, w_cap * rows_per_window / block] (8-bit types): a row stands for code * scale.  scale is
+ *                    the largest magnitude of the block's rows over 448 (e4m3) or 127 (int8), rounded up to eight
+ *                    significant bits (2^-126 at least; 1 for a block of zeros), and the code is value / scale rounded to
+ *                    nearest, ties to even.  A block that holds an infinity or a NaN stands for NaN as a whole.
+ *   k_recent, v_recent bf16 [B, Hkv, S + 2*lag, d]: the sinks, then the ring, position p >= S at row S + (p - S) mod (2*lag)
+ *   weight           fp32 [B, Hkv, 2*lag] (LRSA_KEEP_WEIGHT): what the ring's tokens have gathered, by the same index
+ *   idx              int32 [B, Hkv, w_cap, top_k]: the kept positions
+ * list pointers and idx may be NULL when w_cap is 0, the scales for LRSA_LIST_BF16, weight for LRSA_KEEP_LAG.
+ *
+ * lrsa_store_append: as lrsa_cache_append.  When a window leaves the ring it is cut to top_k rows, by the lag score or by
+ * weight (equal weights keep the lower position), and their blocks are written, once.  w_new (LRSA_KEEP_WEIGHT only,
+ * otherwise NULL): fp32 [B, Hkv, n_new], the weight that the new tokens enter with (that of lrsa_attn_weights for a prompt);
+ * NULL: zero, for a call that compresses no window of its own tokens (LRSA_ERR_INVALID_ARG otherwise).
+ *
+ * lrsa_store_decode: as lrsa_attn_decode, over the store.  With LRSA_KEEP_WEIGHT the attention weights of the query, summed over the
+ * heads of a group, are added to those of the ring's tokens.  Arithmetic: codes, Q and K products are exact, sums and
+ * softmax fp32; the probabilities are rounded to 11 bits in front of 8-bit rows and to 8 bits (bf16) in front of bf16 rows.
+ *
+ * lrsa_store_rows: what the kept rows of windows 0 .. n_windows - 1 stand for, fp32 [B, Hkv, n_windows * top_k, d] each.
+ */
+typedef enum lrsa_list_type { LRSA_LIST_BF16 = 0, LRSA_LIST_E4M3 = 1, LRSA_LIST_INT8 = 2 } lrsa_list_type;
+typedef enum lrsa_keep { LRSA_KEEP_LAG = 0, LRSA_KEEP_WEIGHT = 1 } lrsa_keep;
+typedef struct lrsa_store {
+  int32_t list_type;   /* lrsa_list_type */
+  int32_t block;       /* list rows that share a scale: 16, 32, 64 or 128 (also for bf16, where it only places the windows) */
+  int32_t keep;        /* lrsa_keep */
+  int32_t reserved;
+  void* k_list;        /* DEVICE pointers, aligned to 16 bytes (scales, weight, idx: 4) */
+  void* v_list;
+  float* k_scale;
+  float* v_scale;
+  void* k_recent;
+  void* v_recent;
+  float* weight;
+  int32_t* idx;
+} lrsa_store_t;
+int lrsa_store_shape(const lrsa_params_t* params, const lrsa_store_t* store, int32_t* w_cap, int32_t* rows_per_window,
+                     size_t* workspace_bytes);   /* reads list_type, block and keep only */
+int lrsa_store_append(const lrsa_params_t* params, const lrsa_store_t* store, const void* k_new, const void* v_new,
+                      const float* w_new, int32_t n_prev, int32_t n_new, void* workspace, size_t workspace_bytes,
+                      void* cuda_stream);
+int lrsa_store_decode(const lrsa_params_t* params, const lrsa_store_t* store, const void* q, int32_t n_tokens, void* o,
+                      float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int lrsa_store_rows(const lrsa_params_t* params, const lrsa_store_t* store, int32_t n_windows, float* k, float* v,
+                    void* cuda_stream);
+
+/*
  * Reads the status word that the last call using `workspace` left there.  Synchronises
  * `cuda_stream`.  Returns LRSA_OK, LRSA_ERR_TIMEOUT, or LRSA_ERR_CUDA if the copy failed.
  */

@@ -37,6 +37,11 @@ class lrsa_params_t(ctypes.Structure):
                                                            ("o_residual", ctypes.c_void_p)]
 
 
+class lrsa_store_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("list_type", "block", "keep", "reserved")] + \
+               [(n, ctypes.c_void_p) for n in ("k_list", "v_list", "k_scale", "v_scale", "k_recent", "v_recent", "weight", "idx")]
+
+
 @dataclass(frozen=True)
 class Params:
     """Mirror of ``lrsa_params_t`` (Section 3.2: sink size S, lag L, kept tokens K = r*L)."""
@@ -120,6 +125,16 @@ def lib() -> ctypes.CDLL:
         L.lrsa_cache_kept.argtypes = [pp, vp, ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(i32)]
         L.lrsa_attn_decode.argtypes = [pp, vp, sz, vp, i32, vp, fp, vp, sz, vp]
         for name in ("lrsa_cache_bytes", "lrsa_cache_append", "lrsa_cache_kept", "lrsa_attn_decode"):
+            getattr(L, name).restype = ctypes.c_int
+        sp = ctypes.POINTER(lrsa_store_t)
+        L.lrsa_attn_weights.argtypes = [pp, vp, vp, fp, fp, vp, sz, vp]
+        L.lrsa_weight_select.argtypes = [pp, fp, i32p, vp]
+        L.lrsa_store_shape.argtypes = [pp, sp, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
+        L.lrsa_store_append.argtypes = [pp, sp, vp, vp, fp, i32, i32, vp, sz, vp]
+        L.lrsa_store_decode.argtypes = [pp, sp, vp, i32, vp, fp, vp, sz, vp]
+        L.lrsa_store_rows.argtypes = [pp, sp, i32, fp, fp, vp]
+        for name in ("lrsa_attn_weights", "lrsa_weight_select", "lrsa_store_shape", "lrsa_store_append", "lrsa_store_decode",
+                     "lrsa_store_rows"):
             getattr(L, name).restype = ctypes.c_int
         L.lrsa_workspace_status.argtypes = [vp, vp]
         L.lrsa_score_select_static_status.argtypes = [vp]
@@ -264,6 +279,47 @@ def lrsa_attn_bwd(params: Params, Q, K, V, O, dO, LSE, idx, dQ=None, dK=None, dV
     return dQ, dK, dV
 
 
+def _expect(where, name, t, shape, dtype):
+    """Raises LRSA_ERR_INVALID_ARG unless `t` is a contiguous tensor of this shape and type on the current device."""
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise LrsaError(1, f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
+                           f"{tuple(t.shape)}{'' if t.is_contiguous() else ' (strided)'}")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise LrsaError(1, f"{where}: {name} must be on the current device, got {t.device}")
+
+
+def lrsa_attn_weights(params: Params, Q, K, LSE, weight=None, workspace=None, stream=None):
+    """The attention weight that every position gathers from the queries that see it uncompressed: fp32 [B,Hkv,N], summed
+    over the query heads of a group.  `LSE`: that of lrsa_attn_fwd on the same Q and K."""
+    p, where = params, "lrsa_attn_weights"
+    _expect(where, "Q", Q, (p.batch, p.n_q_heads, p.seq_len, p.head_dim), torch.bfloat16)
+    _expect(where, "K", K, (p.batch, p.n_kv_heads, p.seq_len, p.head_dim), torch.bfloat16)
+    _expect(where, "LSE", LSE, (p.batch, p.n_q_heads, p.seq_len), torch.float32)
+    if weight is None:
+        weight = torch.empty((p.batch, p.n_kv_heads, p.seq_len), dtype=torch.float32, device=Q.device)
+    else:
+        _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32)
+    if workspace is None:
+        workspace = new_workspace(256, Q.device)
+    _check(lib().lrsa_attn_weights(params.ref(), _p(Q), _p(K), _p(LSE), _p(weight), _p(workspace), workspace.numel(),
+                                   _stream(stream)), where)
+    return weight
+
+
+def lrsa_weight_select(params: Params, weight, idx=None, stream=None):
+    """The top_k heaviest positions of every scored window: idx int32 [B,Hkv,W_sel,K], for lrsa_attn_fwd and lrsa_attn_bwd in
+    the place of lrsa_score_select's."""
+    p, where = params, "lrsa_weight_select"
+    _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32)
+    shape = (p.batch, p.n_kv_heads, lrsa_num_sel_windows(params), p.top_k)
+    if idx is None:
+        idx = torch.empty(shape, dtype=torch.int32, device=weight.device)
+    else:
+        _expect(where, "idx", idx, shape, torch.int32)
+    _check(lib().lrsa_weight_select(params.ref(), _p(weight), _p(idx), _stream(stream)), where)
+    return idx
+
+
 def lrsa_workspace_status(workspace, stream=None) -> int:
     return lib().lrsa_workspace_status(_p(workspace), _stream(stream))
 
@@ -335,6 +391,101 @@ class KVCache:
         n = self.params.batch * self.params.n_kv_heads * wcap.value * self.params.top_k
         return self.buf[off:off + 4 * n].view(torch.int32).view(self.params.batch, self.params.n_kv_heads, wcap.value,
                                                                  self.params.top_k)
+
+    def windows_compressed(self) -> int:
+        p = self.params
+        if self.n_tokens <= p.n_sink:
+            return 0
+        return max((self.n_tokens - 1 - p.n_sink) // p.lag - 1, 0)
+
+    def status(self, stream=None) -> int:
+        return lrsa_workspace_status(self.ws, stream)
+
+
+class KVStore:
+    """Condensed KV cache of one layer as plain tensors (see lrsa_store_t in the C header), for inference.  `dtype` of the
+    kept rows: torch.bfloat16, torch.float8_e4m3fn or torch.int8, 8 bits with one scale per `block` rows and head.  `keep`: the rule
+    by which a window is cut, "lag" (lrsa_score_select's) or "weight" (the attention weight its tokens have gathered: what
+    they entered with, and what decode adds).  The tensors may be read and written between calls; two stores share nothing."""
+
+    TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.int8: 2}
+    RULES = {"lag": 0, "weight": 1}
+
+    def __init__(self, params: Params, dtype=torch.float8_e4m3fn, block: int = 64, keep: str = "weight", device="cuda"):
+        if dtype not in self.TYPES or keep not in self.RULES:
+            raise LrsaError(1, f"KVStore: dtype {dtype}, keep {keep!r}")
+        self.params, self.dtype, self.block, self.keep = params, dtype, block, keep
+        self.n_tokens = 0
+        st = lrsa_store_t(self.TYPES[dtype], block, self.RULES[keep], 0)
+        wcap, rows, ws = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_size_t(0)
+        _check(lib().lrsa_store_shape(params.ref(), ctypes.byref(st), ctypes.byref(wcap), ctypes.byref(rows),
+                                      ctypes.byref(ws)), "lrsa_store_shape")
+        p, self.rows_per_window = params, rows.value
+        heads, n = (p.batch, p.n_kv_heads), wcap.value * rows.value
+
+        def zeros(*shape, dtype=torch.float32):
+            return torch.zeros(heads + shape, dtype=dtype, device=device)
+
+        self.k_list, self.v_list = (zeros(n, p.head_dim, dtype=dtype) for _ in "kv")
+        self.k_scale, self.v_scale = (None, None) if dtype == torch.bfloat16 else (zeros(n // block) for _ in "kv")
+        self.k_recent, self.v_recent = (zeros(p.n_sink + 2 * p.lag, p.head_dim, dtype=torch.bfloat16) for _ in "kv")
+        self.weight = zeros(2 * p.lag) if keep == "weight" else None
+        self.idx = zeros(wcap.value, p.top_k, dtype=torch.int32)
+        self.ws = new_workspace(ws.value, device)
+
+    def _struct(self):
+        return lrsa_store_t(self.TYPES[self.dtype], self.block, self.RULES[self.keep], 0, _p(self.k_list), _p(self.v_list),
+                            _p(self.k_scale), _p(self.v_scale), _p(self.k_recent), _p(self.v_recent), _p(self.weight),
+                            _p(self.idx))
+
+    def append(self, k_new, v_new, w_new=None, stream=None):
+        """k_new, v_new: bf16 [B, Hkv, n_new, d].  w_new (keep="weight"): fp32 [B, Hkv, n_new], the weight that the tokens enter
+        with (lrsa_attn_weights of a prompt); none: zero, unless the call compresses a window of its own tokens."""
+        p, where = self.params, "lrsa_store_append"
+        n_new = k_new.shape[2] if k_new.dim() == 4 else 0
+        shape = (p.batch, p.n_kv_heads, n_new, p.head_dim)
+        _expect(where, "k_new", k_new, shape, torch.bfloat16)
+        _expect(where, "v_new", v_new, shape, torch.bfloat16)
+        if w_new is not None:
+            _expect(where, "w_new", w_new, shape[:3], torch.float32)
+        st = self._struct()
+        _check(lib().lrsa_store_append(p.ref(), ctypes.byref(st), _p(k_new), _p(v_new), _p(w_new), self.n_tokens, n_new,
+                                       _p(self.ws), self.ws.numel(), _stream(stream)), where)
+        self.n_tokens += n_new
+
+    def decode(self, q, o=None, lse=None, stream=None):
+        """q: bf16 [B, Hq, d], the query of the last token in the store.  Returns (o, lse); with keep="weight" the weights of
+        the ring's tokens grow by those of the query."""
+        p, where = self.params, "lrsa_store_decode"
+        shape = (p.batch, p.n_q_heads, p.head_dim)
+        _expect(where, "q", q, shape, torch.bfloat16)
+        if o is None:
+            o = torch.empty_like(q)
+        else:
+            _expect(where, "o", o, shape, torch.bfloat16)
+        if lse is None:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+        else:
+            _expect(where, "lse", lse, shape[:2], torch.float32)
+        st = self._struct()
+        _check(lib().lrsa_store_decode(p.ref(), ctypes.byref(st), _p(q), self.n_tokens, _p(o), _p(lse), _p(self.ws),
+                                       self.ws.numel(), _stream(stream)), where)
+        return o, lse
+
+    def rows(self, k=None, v=None, stream=None):
+        """What the kept rows of the windows compressed so far stand for: (k, v), fp32 [B, Hkv, windows * top_k, d]."""
+        p, n = self.params, self.windows_compressed()
+        shape = (p.batch, p.n_kv_heads, n * p.top_k, p.head_dim)
+        out = []
+        for name, t in (("k", k), ("v", v)):
+            if t is None:
+                t = torch.empty(shape, dtype=torch.float32, device=self.k_list.device)
+            else:
+                _expect("lrsa_store_rows", name, t, shape, torch.float32)
+            out.append(t)
+        st = self._struct()
+        _check(lib().lrsa_store_rows(p.ref(), ctypes.byref(st), n, _p(out[0]), _p(out[1]), _stream(stream)), "lrsa_store_rows")
+        return tuple(out)
 
     def windows_compressed(self) -> int:
         p = self.params

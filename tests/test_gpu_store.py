@@ -1,0 +1,367 @@
+"""The store: rows kept by weight or by the lag score, in bf16 or 8 bits, and decode attention over them, against fp64."""
+import math
+
+import pytest
+import torch
+
+from paper_2506_11498_b200 import lrsa
+from tests import store_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+P = lrsa.Params
+E4M3, INT8, BF16 = torch.float8_e4m3fn, torch.int8, torch.bfloat16
+
+
+def tokens(p, seed, offset=2.0):
+    g = torch.Generator().manual_seed(seed)
+    K = (torch.randn(p.batch, p.n_kv_heads, p.seq_len, p.head_dim, generator=g)
+         + offset * torch.randn(1, p.n_kv_heads, 1, p.head_dim, generator=g)).bfloat16()
+    V = torch.randn(K.shape, generator=g).bfloat16()
+    Q = torch.randn(p.batch, p.n_q_heads, p.seq_len, p.head_dim, generator=g).bfloat16()
+    w = torch.empty(K.shape[:3]).log_normal_(0, 2, generator=g)
+    return Q, K, V, w
+
+
+def check_state(store, want):
+    """Kept positions, kept rows and recent rows are exact."""
+    p, c = store.params, want.idx.shape[2]
+    assert store.windows_compressed() == c and store.status() == 0
+    assert torch.equal(store.idx[:, :, :c].cpu().long(), want.idx)
+    k, v = (x.double().cpu() for x in store.rows())
+    for got, exact in ((k, want.k_rows), (v, want.v_rows)):
+        assert torch.equal(got.nan_to_num(7e30), exact.nan_to_num(7e30))
+    n, S, L = want.n, p.n_sink, p.lag
+    at = torch.arange(min(S + c * L, n), n)
+    for got, all_rows in ((store.k_recent, want.K), (store.v_recent, want.V)):
+        got = got.double().cpu()
+        assert torch.equal(got[:, :, :min(S, n)], all_rows[:, :, :min(S, n)])
+        if len(at):
+            assert torch.equal(got[:, :, S + (at - S) % (2 * L)], all_rows[:, :, at])
+    return at
+
+
+#        B Hq Hkv   N            d    L    K   S  type  block keep  steps
+CASES = [
+    (P(2, 4, 2, 4 + 5 * 128 + 77, 128, 128, 32, 4), E4M3, 16, "weight", (1, 1, 2, 37, 128, 300, 5, 1)),
+    (P(1, 4, 4, 16 + 6 * 64, 64, 64, 16, 16), INT8, 16, "weight", (7, 64, 1, 129)),
+    (P(1, 7, 1, 3 + 4 * 200 + 50, 128, 200, 50, 3), INT8, 64, "weight", (250, 1, 1, 199, 403)),       # K ends inside a block
+    (P(1, 2, 2, 6 * 96, 64, 96, 24, 0), E4M3, 32, "lag", (96, 96, 1, 95, 200)),                      # no sinks
+    (P(1, 4, 2, 4 + 7 * 128 + 3, 128, 128, 64, 4), E4M3, 64, "weight", (4 + 7 * 128 + 3,)),          # a prompt at once
+    (P(1, 4, 2, 4 + 7 * 128 + 3, 128, 128, 77, 4), BF16, 32, "weight", (500, 300, 1)),
+    (P(1, 20, 1, 4 + 3 * 128 + 50, 128, 128, 32, 4), INT8, 32, "weight", (200, 1, 150, 87)),         # more than 16 heads a group
+    (P(2, 40, 1, 2 + 3 * 64 + 9, 64, 64, 16, 2), E4M3, 16, "weight", (100, 1, 1, 101)),
+    (P(1, 9, 1, 2 + 5 * 40 + 9, 64, 40, 40, 2), BF16, 16, "lag", (33, 50, 1)),                       # every row kept
+    (P(1, 16, 1, 5 + 5 * 33, 128, 33, 1, 5), E4M3, 128, "weight", (3, 31, 1)),                       # one row kept
+    (P(1, 2, 1, 2 + 3 * 4608 + 100, 64, 4608, 100, 2), E4M3, 128, "lag", (5000, 4608, 1, 4000)),     # long windows
+    (P(17, 2, 2, 4 + 4 * 64 + 9, 64, 64, 16, 4), INT8, 16, "weight", (1, 70, 64, 90)),               # many heads
+]
+
+
+@pytest.mark.parametrize("p,dtype,block,keep,steps", CASES, ids=[f"{i}_{str(c[1])[6:]}_{c[3]}" for i, c in enumerate(CASES)])
+def test_growth_and_decode(p, dtype, block, keep, steps):
+    Q, K, V, w = tokens(p, p.seq_len)
+    dev = [x.cuda() for x in (Q, K, V, w)]
+    store, want = lrsa.KVStore(p, dtype=dtype, block=block, keep=keep), ref.Store(p, dtype, block, keep)
+    i = 0
+    while store.n_tokens < p.seq_len:
+        lo = store.n_tokens
+        n = min(steps[i % len(steps)], p.seq_len - lo)
+        i += 1
+        enters = keep == "weight" and n > 1          # single tokens enter with no weight
+        store.append(dev[1][:, :, lo:lo + n].contiguous(), dev[2][:, :, lo:lo + n].contiguous(),
+                     dev[3][:, :, lo:lo + n].contiguous() if enters else None)
+        if keep == "weight":
+            # gathered weights are fp32 here and fp64 there: the reference selects by the same numbers, checked below
+            c = store.windows_compressed()
+            sel = store.idx[:, :, :c].cpu().long()
+            for x in range(want.idx.shape[2], c):
+                a = p.n_sink + x * p.lag
+                if a + p.lag <= want.n:               # the window was in the ring: its weights were checked by the last decode
+                    want.w[:, :, a:a + p.lag] = ring_weight(before, p, a, p.lag)
+        want.append(K[:, :, lo:lo + n], V[:, :, lo:lo + n], w[:, :, lo:lo + n] if enters else None,
+                    store.idx[:, :, :store.windows_compressed()].cpu())
+        at = check_state(store, want)
+        q = Q[:, :, lo + n - 1]
+        if keep == "weight" and len(at):
+            want.w[:, :, at] = ring_weight(store.weight, p, int(at[0]), len(at))
+        o, lse = store.decode(q.cuda())
+        assert store.status() == 0
+        (eo, to), (el, tl), (eg, tg) = want.decode(q)
+        ref.within(f"o at {lo + n}", o, eo, to)
+        ref.within(f"lse at {lo + n}", lse, el, tl)
+        if keep == "weight":
+            if len(at):
+                got = ring_weight(store.weight, p, int(at[0]), len(at))
+                ref.within(f"weight at {lo + n}", got, want.w[:, :, at], tg + 2.0 ** -24 * want.w[:, :, at])
+            before = store.weight.clone()
+    if keep == "lag":
+        idx, _ = lrsa.lrsa_score_select(p, dev[1], dev[2])
+        c = store.windows_compressed()
+        assert torch.equal(store.idx[:, :, :c], idx[:, :, :c])
+
+
+def ring_weight(weight, p, first, n):
+    """fp64 weights of positions first .. first + n - 1 out of a ring [B, Hkv, 2L]."""
+    return weight.double().cpu()[:, :, (torch.arange(first, first + n) - p.n_sink) % (2 * p.lag)]
+
+
+def test_a_prompt_and_its_answer():
+    """The calls together, as they are used: forward of a prompt, weights, the prompt enters the store cut by them, then
+    tokens are generated until two more windows have been cut by what decode gathered."""
+    p = P(1, 8, 2, 4 + 7 * 128, 128, 128, 32, 4)
+    n0 = 4 + 5 * 128 + 60
+    Q, K, V, _ = tokens(p, 9)
+    dev = [x.cuda() for x in (Q, K, V)]
+    prompt = P(1, 8, 2, n0, 128, 128, 32, 4)
+    q, k, v = (x[:, :, :n0].contiguous() for x in dev)
+    idx, _ = lrsa.lrsa_score_select(prompt, k, v)
+    w = lrsa.lrsa_attn_weights(prompt, q, k, lrsa.lrsa_attn_fwd(prompt, q, k, v, idx)[1])
+    store, want = lrsa.KVStore(p, dtype=E4M3, block=32, keep="weight"), ref.Store(p, E4M3, 32, "weight")
+    store.append(k, v, w)
+    want.append(K[:, :, :n0], V[:, :, :n0], w.cpu())
+    sel = lrsa.lrsa_weight_select(prompt, w)
+    assert store.windows_compressed() == 4 and torch.equal(store.idx[:, :, :4], sel[:, :, :4])
+    for t in range(n0, p.seq_len):
+        cut = (t - 4) % 128 == 0
+        if cut:                                        # the reference cuts by the weights that decode has gathered, in fp32
+            lo = 4 + (want.idx.shape[2]) * 128
+            want.w[:, :, lo:lo + 128] = ring_weight(store.weight, p, lo, 128)
+        store.append(*(x[:, :, t:t + 1].contiguous() for x in dev[1:]))
+        want.append(K[:, :, t:t + 1], V[:, :, t:t + 1])
+        o, lse = store.decode(dev[0][:, :, t].contiguous())
+        (eo, to), (el, tl), (_, tg) = want.decode(Q[:, :, t])
+        if t % 17 == 0 or cut:
+            ref.within(f"o at {t}", o, eo, to)
+            ref.within(f"lse at {t}", lse, el, tl)
+            first = 4 + want.idx.shape[2] * 128
+            # every decode since adds its own roundings: none is larger than this one's bound by more than the number of them
+            ref.within(f"weight at {t}", ring_weight(store.weight, p, first, t + 1 - first), want.w[:, :, first:],
+                       256 * 2.0 ** -18 * want.w[:, :, first:].clamp_min(1.0))
+    check_state(store, want)
+    assert want.idx.shape[2] == 5
+
+
+def fill(p, dtype, block, keep, n, seed, device="cuda"):
+    """A store that holds n random tokens, made by writing its tensors, and its fp64 twin."""
+    g = torch.Generator(device=device).manual_seed(seed)
+    store, want = lrsa.KVStore(p, dtype=dtype, block=block, keep=keep), ref.Store(p, dtype, block, keep)
+    c = max((n - 1 - p.n_sink) // p.lag - 1, 0) if n > p.n_sink else 0
+    heads, kp = (p.batch, p.n_kv_heads), store.rows_per_window
+    for name in "kv":
+        x = torch.randn(*heads, c, p.top_k, p.head_dim, generator=g, device=device)
+        if dtype != BF16:
+            scale = torch.exp2(torch.randint(-9, -3, heads + (c, kp // block), generator=g, device=device).float())
+            x = (x * 40).round().clamp(-127, 127) if dtype == INT8 else (x * 100).clamp(-448, 448).to(E4M3).float()
+            getattr(store, name + "_scale")[:, :, :c * kp // block] = scale.flatten(2)
+            setattr(want, name + "_scale", scale.repeat_interleave(block, 3)[:, :, :, :p.top_k].flatten(2).double().cpu())
+            rows = x * scale.repeat_interleave(block, 3)[:, :, :, :p.top_k, None]
+        else:
+            rows = x = x.bfloat16().float()
+        getattr(store, name + "_list")[:, :, :c * kp].unflatten(2, (c, kp))[:, :, :, :p.top_k] = x.to(dtype)
+        recent = torch.randn(*heads, p.n_sink + 2 * p.lag, p.head_dim, generator=g, device=device).bfloat16()
+        getattr(store, name + "_recent").copy_(recent)
+        setattr(want, name + "_rows", rows.flatten(2, 3).double().cpu())
+        full = torch.zeros(*heads, n, p.head_dim, dtype=torch.float64)
+        at = torch.arange(min(p.n_sink + c * p.lag, n), n)
+        full[:, :, :p.n_sink] = recent[:, :, :min(p.n_sink, n)].double().cpu()
+        full[:, :, at] = recent.double().cpu()[:, :, p.n_sink + (at - p.n_sink) % (2 * p.lag)]
+        setattr(want, name.upper(), full)
+    want.idx = torch.zeros(*heads, c, p.top_k, dtype=torch.long)
+    want.w = torch.zeros(*heads, n, dtype=torch.float64)
+    store.n_tokens = n
+    return store, want
+
+
+@pytest.mark.parametrize("dtype", [E4M3, INT8, BF16], ids=["e4m3", "int8", "bf16"])
+@pytest.mark.parametrize("B,Hq,Hkv,d,L,K,S,n,block", [
+    (1, 4, 4, 64, 512, 128, 16, 1, 64), (1, 7, 1, 128, 64, 16, 4, 4, 16), (2, 8, 8, 64, 100, 17, 0, 100, 32),
+    (1, 28, 4, 128, 1024, 256, 4, 31743, 64),           # clusters of many CTAs
+    (1, 8, 1, 64, 4096, 4096, 4, 126975, 128),          # one head, a long list: several clusters and the merge
+    (1, 16, 2, 128, 2048, 2048, 0, 80000, 16),          # the same with two head groups
+    (1, 24, 1, 128, 1024, 1024, 4, 60000, 64),          # and with two passes over the heads
+    (16, 28, 4, 128, 256, 64, 4, 5000, 64),             # small CTAs
+    (3, 5, 1, 64, 333, 83, 7, 6000, 128),
+])
+def test_decode_of_large_and_odd_stores(dtype, B, Hq, Hkv, d, L, K, S, n, block):
+    p = P(B, Hq, Hkv, n + 5 + S, d, L, K, S)
+    store, want = fill(p, dtype, block, "weight", n, seed=n)
+    q = torch.randn(B, Hq, d, generator=torch.Generator().manual_seed(n)).bfloat16()
+    o, lse = store.decode(q.cuda())
+    o2, lse2 = store.decode(q.cuda())
+    assert store.status() == 0 and torch.equal(o, o2) and torch.equal(lse, lse2)
+    (eo, to), (el, tl), (eg, tg) = want.decode(q)
+    ref.within("o", o, eo, to)
+    ref.within("lse", lse, el, tl)
+    first = S + want.idx.shape[2] * L
+    if n > first:
+        got = ring_weight(store.weight, p, first, n - first)
+        ref.within("weight", got, 2 * eg, 2 * tg + 2.0 ** -23 * eg)
+    assert int((store.weight != 0).sum()) <= B * Hkv * max(n - first, 0)      # other tokens' weights stay
+    plain = lrsa.KVStore(p, dtype=dtype, block=block, keep="lag")
+    for name in ("k_list", "v_list", "k_scale", "v_scale", "k_recent", "v_recent"):
+        setattr(plain, name, getattr(store, name))
+    plain.n_tokens = n
+    o3, lse3 = plain.decode(q.cuda())
+    assert torch.equal(o, o3) and torch.equal(lse, lse3)
+
+
+@pytest.mark.parametrize("dtype", [E4M3, INT8], ids=["e4m3", "int8"])
+@pytest.mark.parametrize("what", ["v_scales", "k_small", "q_large", "q_small", "q_zero", "spread"])
+def test_decode_over_the_range_of_scales(dtype, what):
+    """Scales that differ by 2^40 between blocks, queries near the ends of bf16, scores that are far apart."""
+    p = P(1, 4, 2, 2000, 128, 128, 64, 4)
+    store, want = fill(p, dtype, 32, "weight", 1900, seed=5)
+    q = torch.randn(1, 4, 128, generator=torch.Generator().manual_seed(5)).bfloat16()
+    c = want.idx.shape[2]
+    if what == "v_scales":
+        f = torch.exp2(torch.arange(store.v_scale.shape[2]) % 5 * 10.0 - 20)
+        store.v_scale *= f.cuda()
+        f = f[:c * 2].repeat_interleave(32).double()
+        want.v_rows *= f[:, None]
+        want.v_scale *= f
+    elif what == "k_small":
+        store.k_scale *= 2.0 ** -100
+        want.k_rows *= 2.0 ** -100
+    elif what == "spread":
+        store.k_scale *= 16.0
+        want.k_rows *= 16.0
+    else:
+        q = q * {"q_large": 2.0 ** 60, "q_small": 2.0 ** -120, "q_zero": 0.0}[what]
+        if what == "q_large":
+            store.k_scale *= 2.0 ** -60
+            want.k_rows *= 2.0 ** -60
+            store.k_recent.zero_()
+            want.K.zero_()
+    o, lse = store.decode(q.cuda())
+    (eo, to), (el, tl), _ = want.decode(q)
+    ref.within("o", o, eo, to)
+    ref.within("lse", lse, el, tl)
+
+
+def test_values_that_are_not_finite():
+    """A block with an infinity or a NaN stands for NaN; other heads, and blocks that a query does not see, are not touched."""
+    p = P(1, 4, 2, 4 + 6 * 64, 64, 64, 32, 4)
+    Q, K, V, w = tokens(p, 3)
+    K[0, 0, 4 + 70, 5] = math.inf                 # window 1 of head 0
+    V[0, 0, 4 + 2 * 64 + 3, 7] = math.nan         # window 2
+    w[:, :, 4 + 70] = w[:, :, 4 + 2 * 64 + 3] = 1e9      # both kept
+    n = 4 + 4 * 64 + 1                            # windows 0, 1, 2 compressed
+    for dtype in (E4M3, INT8):
+        store, want = lrsa.KVStore(p, dtype=dtype, block=16), ref.Store(p, dtype, 16, "weight")
+        store.append(*(x[:, :, :n].cuda().contiguous() for x in (K, V, w)))
+        want.append(K[:, :, :n], V[:, :, :n], w[:, :, :n])
+        check_state(store, want)
+        k, v = store.rows()
+        assert int(k.isnan().sum()) == 16 * 64 and int(v.isnan().sum()) == 16 * 64 and not k[:, 1].isnan().any()
+        o, lse = store.decode(Q[:, :, n - 1].cuda().contiguous())
+        assert o[:, :2].isnan().all() and lse[:, :2].isnan().all()
+        (eo, to), (el, tl), _ = want.decode(Q[:, :, n - 1])
+        ref.within("o", o[:, 2:], eo[:, 2:], to[:, 2:])
+        ref.within("lse", lse[:, 2:], el[:, 2:], tl[:, 2:])
+    # a ring row that no query sees any more, and list rows of windows not compressed yet, may hold anything
+    store, want = fill(p, E4M3, 16, "weight", n, seed=2)
+    store.k_scale[:, :, 3 * 2:] = math.nan
+    store.v_scale[:, :, 3 * 2:] = math.nan
+    seen = 4 + (torch.arange(4 + 3 * 64, n) - 4) % 128
+    hidden = torch.ones(store.k_recent.shape[2], dtype=torch.bool)
+    hidden[:4] = hidden[seen] = False
+    store.k_recent[:, :, hidden.cuda()] = math.nan
+    store.v_recent[:, :, hidden.cuda()] = math.inf
+    o, lse = store.decode(Q[:, :, 0].cuda().contiguous())
+    (eo, to), (el, tl), _ = want.decode(Q[:, :, 0])
+    ref.within("o", o, eo, to)
+    ref.within("lse", lse, el, tl)
+
+
+def test_quantization_edges():
+    """Blocks of zeros, of one value, of subnormals, of values on the borders between codes."""
+    p = P(1, 1, 1, 6 * 16 + 1, 64, 16, 16, 0)
+    K = torch.zeros(1, 1, p.seq_len, 64)
+    K[:, :, 16:32] = 448.0 * (1 - 2 * (torch.arange(64) % 2))
+    K[:, :, 32:48] = 2.0 ** -130 * torch.arange(64)
+    border = torch.arange(1, 64) + 0.5
+    K[:, :, 48:64, 0] = 127.0
+    K[:, :, 48:64, 1:] = border                       # ties of int8 at scale 1
+    K[:, :, 64:80, 0] = 448.0
+    K[:, :, 64:80, 1:] = (16 + torch.arange(63)) * 0.5     # ties of e4m3 at scale 1
+    K = K.bfloat16()
+    V = (K.flip(3) * -1).contiguous()
+    for dtype in (E4M3, INT8):
+        store, want = lrsa.KVStore(p, dtype=dtype, block=16), ref.Store(p, dtype, 16, "weight")
+        store.append(K.cuda(), V.cuda(), torch.ones(1, 1, p.seq_len, device="cuda"))
+        want.append(K, V, torch.ones(1, 1, p.seq_len))
+        check_state(store, want)
+        assert torch.equal(store.k_scale[0, 0].double().cpu(), ref.held(K[0, 0, :80], dtype, 16)[1][:5]) and store.k_scale[0, 0, 0] == 1
+
+
+def test_two_stores_on_two_streams_and_in_graphs():
+    p = P(2, 8, 2, 3000, 128, 256, 64, 4)
+    made = [fill(p, t, 64, "weight", 2800, seed=s) for t, s in ((E4M3, 1), (INT8, 2))]
+    qs = [torch.randn(2, 8, 128, generator=torch.Generator().manual_seed(s)).bfloat16().cuda() for s in (1, 2)]
+    want = []
+    for (store, _), q in zip(made, qs):
+        o, lse = store.decode(q)
+        want.append((o.clone(), lse.clone(), store.weight.clone()))
+        store.weight.zero_()
+    streams = [torch.cuda.Stream() for _ in made]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(3):
+        for (store, _), q, s in zip(made, qs, streams):
+            with torch.cuda.stream(s):
+                outs.append(store.decode(q))
+    torch.cuda.synchronize()
+    for i, (o, lse) in enumerate(outs):
+        assert torch.equal(o, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
+    for (store, _), w in zip(made, want):
+        assert (store.weight - 3 * w[2]).abs().max() <= 2.0 ** -22 * 3 * float(w[2].max())
+        store.weight.zero_()
+    torch.cuda.synchronize()
+    graphs, res = [], []
+    for (store, _), q in zip(made, qs):      # each store has a workspace of its own
+        graph = torch.cuda.CUDAGraph()
+        o, lse = torch.empty_like(q), torch.empty(2, 8, device="cuda")
+        with torch.cuda.graph(graph):
+            store.decode(q, o=o, lse=lse)
+        graphs.append(graph)
+        res.append((o, lse))
+    for graph in graphs:
+        graph.replay()
+    torch.cuda.synchronize()
+    for (store, _), w, r in zip(made, want, res):
+        assert torch.equal(r[0], w[0]) and torch.equal(r[1], w[1]) and torch.equal(store.weight, w[2])
+
+
+def test_refusals():
+    p = P(1, 4, 2, 1000, 128, 128, 32, 4)
+    store = lrsa.KVStore(p)
+    k = torch.zeros(1, 2, 8, 128, dtype=BF16, device="cuda")
+    w = torch.zeros(1, 2, 8, device="cuda")
+    q = torch.zeros(1, 4, 128, dtype=BF16, device="cuda")
+    with pytest.raises(lrsa.LrsaError):            # nothing in it
+        store.decode(q)
+    for bad in ((k.float(), k, None), (k, k[:, :, :7], None), (k, k, w.double()), (k, k, w[:, :, :4]), (k.cpu(), k, None),
+                (k[:, :, ::2], k[:, :, ::2], None), (k[0], k[0], None), (k[:, :1], k[:, :1], None), (k[:, :, :0], k[:, :, :0], None)):
+        with pytest.raises(lrsa.LrsaError) as e:
+            store.append(*bad)
+        assert e.value.status == 1 and store.n_tokens == 0
+    store.n_tokens = 996                           # beyond the capacity
+    with pytest.raises(lrsa.LrsaError) as e:
+        store.append(k, k)
+    assert e.value.status == 1
+    store.n_tokens = 500
+    for bad in (q.float(), q[:, :2], q[None], q.cpu()):
+        with pytest.raises(lrsa.LrsaError) as e:
+            store.decode(bad)
+        assert e.value.status == 1
+    with pytest.raises(lrsa.LrsaError):
+        store.decode(q, o=torch.empty(1, 4, 64, dtype=BF16, device="cuda"))
+    store.n_tokens = 0
+    prompt = torch.zeros(1, 2, 700, 128, dtype=BF16, device="cuda")
+    with pytest.raises(lrsa.LrsaError) as e:       # cuts windows of its own tokens, by weights that nobody gave
+        store.append(prompt, prompt)
+    assert e.value.status == 1
+    with pytest.raises(lrsa.LrsaError) as e:       # weights for a store that does not keep them
+        lrsa.KVStore(p, keep="lag").append(k, k, w)
+    assert e.value.status == 1
