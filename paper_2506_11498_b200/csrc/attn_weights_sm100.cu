@@ -12,6 +12,8 @@
 // the partial sums in the order of the ranks (no atomics: repeats are equal bit by bit).
 #include <math.h>
 
+#include <type_traits>
+
 #include "attn_common_sm100.h"
 #include "infer_sm100.h"
 
@@ -219,29 +221,35 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
       if (!ok) break;
       tc_fence_after_sync();
       const float4* nl2 = reinterpret_cast<const float4*>(st_nl2 + b * kTile + wg * 64);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      // two forms of the loop: a test per element in it costs more than the exponentials (a branch for every four: 586 us)
+      auto half = [&](int h, auto hidden) {
         uint32_t s[32];
         tmem_ld32(S_addr + b * kTile + h * 32, s);
         tmem_wait_ld();
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
           const float4 nl = nl2[8 * h + v];
-          float e[4];
-          f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * v]), __uint_as_float(s[4 * v + 1])), c2, f2_pack(nl.x, nl.y)), e[0], e[1]);
-          f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * v + 2]), __uint_as_float(s[4 * v + 3])), c2, f2_pack(nl.z, nl.w)), e[2], e[3]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] = ex2(e[i]);
-          if (masked) {   // (a selection: what a hidden query holds, NaN or infinity, does not enter)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int col = 32 * h + 4 * v + i;
-              if (col < lo || col >= hi) e[i] = 0.f;
-            }
+          for (int z = 0; z < 2; ++z) {
+            const int i = 4 * v + 2 * z;
+            const uint64_t x = f2_fma(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, z ? f2_pack(nl.z, nl.w) : f2_pack(nl.x, nl.y));
+            float e0, e1;
+            f2_unpack(x, e0, e1);
+            e0 = ex2(e0);
+            e1 = ex2(e1);
+            // (a selection: what a hidden query holds, NaN or infinity, does not enter)
+            if (decltype(hidden)::value && (32 * h + i < lo || 32 * h + i >= hi)) e0 = 0.f;
+            if (decltype(hidden)::value && (32 * h + i + 1 < lo || 32 * h + i + 1 >= hi)) e1 = 0.f;
+            acc[z] = f2_add(acc[z], f2_pack(e0, e1));
           }
-          acc[0] = f2_add(acc[0], f2_pack(e[0], e[1]));
-          acc[1] = f2_add(acc[1], f2_pack(e[2], e[3]));
         }
+      };
+      if (masked) {
+        half(0, std::true_type());
+        half(1, std::true_type());
+      } else {
+        half(0, std::false_type());
+        half(1, std::false_type());
       }
       tc_fence_before_sync();
       mbar_arrive(s_empty + 8 * b);
@@ -272,11 +280,16 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
   if (tid == 0 && ctl.abort) atomicExch(a.status, (int)LRSA_ERR_TIMEOUT);
 }
 
-// CTAs that share a key tile: so many that every slot has one, while each keeps some pairs to itself.
+// CTAs that share a key tile.  Two CTAs run on an SM; a CTA's start and end cost about four pairs.
 int weights_split(long long items, long long pairs) {
-  int c = 1;
-  while (c < 8 && items * c < 2 * kSms && pairs >= items * c * 8) c *= 2;
-  return c;
+  int best = 1;
+  double least = -1;
+  for (int c = 1; c <= 8; c *= 2) {
+    const long long waves = (items * c + 2 * kSms - 1) / (2 * kSms);
+    const double cost = waves * ((double)pairs / (items * c) + 4);
+    if (least < 0 || cost < least) { least = cost; best = c; }
+  }
+  return best;
 }
 
 template <int D, int NSEQ>
