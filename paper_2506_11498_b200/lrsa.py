@@ -99,7 +99,7 @@ class Params:
 
 
 _lib = None
-_call = None   # the module of csrc/pycall.c, the two calls of a generated token without ctypes, or what stands for it
+_call = None   # the module of csrc/pycall.c, the short calls without ctypes, or what stands for it
 
 
 def lib() -> ctypes.CDLL:
@@ -154,12 +154,15 @@ def lib() -> ctypes.CDLL:
 
 
 class _CtypesCalls:
-    """The helper module's two calls where there is none for this interpreter (about 1 us a call more)."""
+    """The helper module's calls where there is none for this interpreter (about 1 us a call more)."""
 
     def __init__(self, L):
         at = ctypes.POINTER(lrsa_params_t)
-        self.cache_append = lambda params, *args: L.lrsa_cache_append(ctypes.cast(params, at), *args)
-        self.attn_decode = lambda params, *args: L.lrsa_attn_decode(ctypes.cast(params, at), *args)
+        for name in ("cache_append", "attn_decode", "attn_weights", "weight_select"):
+            setattr(self, name, lambda params, *args, f=getattr(L, "lrsa_" + name): f(ctypes.cast(params, at), *args))
+        for name in ("store_append", "store_decode", "store_rows"):    # eleven arguments make a store
+            setattr(self, name, lambda params, *args, f=getattr(L, "lrsa_" + name):
+                    f(ctypes.cast(params, at), ctypes.byref(lrsa_store_t(*args[:3], 0, *args[3:11])), *args[11:]))
 
 
 def _token_calls(L):
@@ -279,44 +282,71 @@ def lrsa_attn_bwd(params: Params, Q, K, V, O, dO, LSE, idx, dQ=None, dK=None, dV
     return dQ, dK, dV
 
 
-def _expect(where, name, t, shape, dtype):
-    """Raises LRSA_ERR_INVALID_ARG unless `t` is a contiguous tensor of this shape and type on the current device."""
-    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
-        raise LrsaError(1, f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} "
-                           f"{tuple(t.shape)}{'' if t.is_contiguous() else ' (strided)'}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _device(where, name, t) -> int:
+    """The index of the current device, on which `t` has to be."""
+    dev = t.get_device()      # -1: not a GPU's
+    if dev < 0 or dev != torch.cuda.current_device():
         raise LrsaError(1, f"{where}: {name} must be on the current device, got {t.device}")
+    return dev
+
+
+def _expect(where, name, t, shape, dtype, dev):
+    """Raises LRSA_ERR_INVALID_ARG unless `t` is a contiguous tensor of this shape and type on device `dev`."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        raise LrsaError(1, f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev}, got "
+                           f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' (strided)'}")
+
+
+def _stream_of(stream, dev):
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
+
+
+def _calls():
+    if _call is None:
+        lib()
+    return _call
 
 
 def lrsa_attn_weights(params: Params, Q, K, LSE, weight=None, workspace=None, stream=None):
     """The attention weight that every position gathers from the queries that see it uncompressed: fp32 [B,Hkv,N], summed
     over the query heads of a group.  `LSE`: that of lrsa_attn_fwd on the same Q and K."""
-    p, where = params, "lrsa_attn_weights"
-    _expect(where, "Q", Q, (p.batch, p.n_q_heads, p.seq_len, p.head_dim), torch.bfloat16)
-    _expect(where, "K", K, (p.batch, p.n_kv_heads, p.seq_len, p.head_dim), torch.bfloat16)
-    _expect(where, "LSE", LSE, (p.batch, p.n_q_heads, p.seq_len), torch.float32)
+    p, where, call = params, "lrsa_attn_weights", _calls()
+    dev = _device(where, "Q", Q)
+    _expect(where, "Q", Q, (p.batch, p.n_q_heads, p.seq_len, p.head_dim), torch.bfloat16, dev)
+    _expect(where, "K", K, (p.batch, p.n_kv_heads, p.seq_len, p.head_dim), torch.bfloat16, dev)
+    _expect(where, "LSE", LSE, (p.batch, p.n_q_heads, p.seq_len), torch.float32, dev)
     if weight is None:
         weight = torch.empty((p.batch, p.n_kv_heads, p.seq_len), dtype=torch.float32, device=Q.device)
     else:
-        _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32)
+        _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32, dev)
     if workspace is None:
         workspace = new_workspace(256, Q.device)
-    _check(lib().lrsa_attn_weights(params.ref(), _p(Q), _p(K), _p(LSE), _p(weight), _p(workspace), workspace.numel(),
-                                   _stream(stream)), where)
+    cp = p.struct()
+    status = call.attn_weights(ctypes.addressof(cp), Q.data_ptr(), K.data_ptr(), LSE.data_ptr(), weight.data_ptr(),
+                               workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev))
+    if status:
+        _check(status, where)
     return weight
 
 
 def lrsa_weight_select(params: Params, weight, idx=None, stream=None):
     """The top_k heaviest positions of every scored window: idx int32 [B,Hkv,W_sel,K], for lrsa_attn_fwd and lrsa_attn_bwd in
     the place of lrsa_score_select's."""
-    p, where = params, "lrsa_weight_select"
-    _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32)
-    shape = (p.batch, p.n_kv_heads, lrsa_num_sel_windows(params), p.top_k)
+    p, where, call = params, "lrsa_weight_select", _calls()
+    dev = _device(where, "weight", weight)
+    _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32, dev)
+    n = lrsa_num_sel_windows(p) if p.cu_seqlens or p.lag < 1 else max((p.seq_len - p.n_sink) // p.lag - 1, 0)
+    shape = (p.batch, p.n_kv_heads, n, p.top_k)
     if idx is None:
         idx = torch.empty(shape, dtype=torch.int32, device=weight.device)
     else:
-        _expect(where, "idx", idx, shape, torch.int32)
-    _check(lib().lrsa_weight_select(params.ref(), _p(weight), _p(idx), _stream(stream)), where)
+        _expect(where, "idx", idx, shape, torch.int32, dev)
+    cp = p.struct()
+    status = call.weight_select(ctypes.addressof(cp), weight.data_ptr(), idx.data_ptr(), _stream_of(stream, dev))
+    if status:
+        _check(status, where)
     return idx
 
 
@@ -415,8 +445,9 @@ class KVStore:
         if dtype not in self.TYPES or keep not in self.RULES:
             raise LrsaError(1, f"KVStore: dtype {dtype}, keep {keep!r}")
         self.params, self.dtype, self.block, self.keep = params, dtype, block, keep
+        self._type, self._rule = self.TYPES[dtype], self.RULES[keep]
         self.n_tokens = 0
-        st = lrsa_store_t(self.TYPES[dtype], block, self.RULES[keep], 0)
+        st = lrsa_store_t(self._type, block, self._rule, 0)
         wcap, rows, ws = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_size_t(0)
         _check(lib().lrsa_store_shape(params.ref(), ctypes.byref(st), ctypes.byref(wcap), ctypes.byref(rows),
                                       ctypes.byref(ws)), "lrsa_store_shape")
@@ -432,60 +463,74 @@ class KVStore:
         self.weight = zeros(2 * p.lag) if keep == "weight" else None
         self.idx = zeros(wcap.value, p.top_k, dtype=torch.int32)
         self.ws = new_workspace(ws.value, device)
+        self._lse = torch.empty((p.batch, p.n_q_heads), dtype=torch.float32, device=device)   # what an lse looks like
 
-    def _struct(self):
-        return lrsa_store_t(self.TYPES[self.dtype], self.block, self.RULES[self.keep], 0, _p(self.k_list), _p(self.v_list),
-                            _p(self.k_scale), _p(self.v_scale), _p(self.k_recent), _p(self.v_recent), _p(self.weight),
-                            _p(self.idx))
+    def _parts(self):
+        """The store as the calls of csrc/pycall.c take it: type, block, rule, addresses."""
+        scale_k, scale_v, weight = self.k_scale, self.v_scale, self.weight
+        return (self._type, self.block, self._rule, self.k_list.data_ptr(), self.v_list.data_ptr(),
+                None if scale_k is None else scale_k.data_ptr(), None if scale_v is None else scale_v.data_ptr(),
+                self.k_recent.data_ptr(), self.v_recent.data_ptr(), None if weight is None else weight.data_ptr(),
+                self.idx.data_ptr())
 
     def append(self, k_new, v_new, w_new=None, stream=None):
         """k_new, v_new: bf16 [B, Hkv, n_new, d].  w_new (keep="weight"): fp32 [B, Hkv, n_new], the weight that the tokens enter
         with (lrsa_attn_weights of a prompt); none: zero, unless the call compresses a window of its own tokens."""
-        p, where = self.params, "lrsa_store_append"
+        p, where, call = self.params, "lrsa_store_append", _calls()
         n_new = k_new.shape[2] if k_new.dim() == 4 else 0
         shape = (p.batch, p.n_kv_heads, n_new, p.head_dim)
-        _expect(where, "k_new", k_new, shape, torch.bfloat16)
-        _expect(where, "v_new", v_new, shape, torch.bfloat16)
+        dev = _device(where, "k_new", k_new)
+        _expect(where, "k_new", k_new, shape, torch.bfloat16, dev)
+        _expect(where, "v_new", v_new, shape, torch.bfloat16, dev)
         if w_new is not None:
-            _expect(where, "w_new", w_new, shape[:3], torch.float32)
-        st = self._struct()
-        _check(lib().lrsa_store_append(p.ref(), ctypes.byref(st), _p(k_new), _p(v_new), _p(w_new), self.n_tokens, n_new,
-                                       _p(self.ws), self.ws.numel(), _stream(stream)), where)
+            _expect(where, "w_new", w_new, shape[:3], torch.float32, dev)
+        cp, ws = p.struct(), self.ws
+        status = call.store_append(ctypes.addressof(cp), *self._parts(), k_new.data_ptr(), v_new.data_ptr(), _p(w_new),
+                                   self.n_tokens, n_new, ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        if status:
+            _check(status, where)
         self.n_tokens += n_new
 
     def decode(self, q, o=None, lse=None, stream=None):
         """q: bf16 [B, Hq, d], the query of the last token in the store.  Returns (o, lse); with keep="weight" the weights of
         the ring's tokens grow by those of the query."""
-        p, where = self.params, "lrsa_store_decode"
+        p, where, call, like = self.params, "lrsa_store_decode", _calls(), self._lse
         shape = (p.batch, p.n_q_heads, p.head_dim)
-        _expect(where, "q", q, shape, torch.bfloat16)
+        dev = _device(where, "q", q)
+        _expect(where, "q", q, shape, torch.bfloat16, dev)
         if o is None:
             o = torch.empty_like(q)
         else:
-            _expect(where, "o", o, shape, torch.bfloat16)
+            _expect(where, "o", o, shape, torch.bfloat16, dev)
         if lse is None:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty_like(like)
         else:
-            _expect(where, "lse", lse, shape[:2], torch.float32)
-        st = self._struct()
-        _check(lib().lrsa_store_decode(p.ref(), ctypes.byref(st), _p(q), self.n_tokens, _p(o), _p(lse), _p(self.ws),
-                                       self.ws.numel(), _stream(stream)), where)
+            _expect(where, "lse", lse, like.shape, torch.float32, dev)
+        cp, ws = p.struct(), self.ws
+        status = call.store_decode(ctypes.addressof(cp), *self._parts(), q.data_ptr(), self.n_tokens, o.data_ptr(),
+                                   lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        if status:
+            _check(status, where)
         return o, lse
 
     def rows(self, k=None, v=None, stream=None):
         """What the kept rows of the windows compressed so far stand for: (k, v), fp32 [B, Hkv, windows * top_k, d]."""
-        p, n = self.params, self.windows_compressed()
+        p, n, where, call = self.params, self.windows_compressed(), "lrsa_store_rows", _calls()
         shape = (p.batch, p.n_kv_heads, n * p.top_k, p.head_dim)
-        out = []
-        for name, t in (("k", k), ("v", v)):
-            if t is None:
-                t = torch.empty(shape, dtype=torch.float32, device=self.k_list.device)
-            else:
-                _expect("lrsa_store_rows", name, t, shape, torch.float32)
-            out.append(t)
-        st = self._struct()
-        _check(lib().lrsa_store_rows(p.ref(), ctypes.byref(st), n, _p(out[0]), _p(out[1]), _stream(stream)), "lrsa_store_rows")
-        return tuple(out)
+        dev = _device(where, "the store", self.k_list)
+        if k is None:
+            k = torch.empty(shape, dtype=torch.float32, device=self.k_list.device)
+        else:
+            _expect(where, "k", k, shape, torch.float32, dev)
+        if v is None:
+            v = torch.empty_like(k)
+        else:
+            _expect(where, "v", v, shape, torch.float32, dev)
+        cp = p.struct()
+        status = call.store_rows(ctypes.addressof(cp), *self._parts(), n, k.data_ptr(), v.data_ptr(), _stream_of(stream, dev))
+        if status:
+            _check(status, where)
+        return k, v
 
     def windows_compressed(self) -> int:
         p = self.params
