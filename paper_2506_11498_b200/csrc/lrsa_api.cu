@@ -20,18 +20,18 @@ static __global__ void room_kernel() {}
 // 8.7K keys 17.9 us instead of 10.7 with clusters of eight, 32/8 heads, d = 128, 9.5K keys 26.1 instead of 16.6.)
 // Where the GPUs of a process differ, the first one's numbers make the plans.
 static ClusterRoom ask_room() {
-  ClusterRoom room;
+  ClusterRoom room = {};
   const bool ok = cudaFuncSetAttribute(room_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10) == cudaSuccess &&
                   cudaFuncSetAttribute(room_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
   for (int p = 0; p < 3; ++p)
-    for (int c = 0; c < 5; ++c) {
+    for (int c = 1; c <= 16; ++c) {
       cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(1 << c);
+      cfg.gridDim = dim3(c);
       cfg.blockDim = dim3(128);
       cfg.dynamicSmemBytes = (200 << 10) >> p;
       cudaLaunchAttribute attr;
       attr.id = cudaLaunchAttributeClusterDimension;
-      attr.val.clusterDim.x = 1 << c;
+      attr.val.clusterDim.x = c;
       attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;

@@ -142,14 +142,13 @@ cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, dim3 block, size_t s
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-// lrsa_api.cu : clusters of 2^c CTAs that the device runs at a time with 2^p CTAs on an SM, n[p][c].
+// lrsa_api.cu : clusters of c CTAs (at most 16) that the device runs at a time with 2^p CTAs on an SM, n[p][c].
 struct ClusterRoom {
-  int n[3][5];
+  int n[3][17];
   int at_once(int per_sm, int cluster) const {
-    int p = 0, c = 0;
+    int p = 0;
     while ((1 << p) < per_sm) ++p;
-    while ((1 << c) < cluster) ++c;
-    return n[p][c];
+    return n[p][cluster];
   }
 };
 const ClusterRoom& cluster_room();

@@ -244,13 +244,36 @@ struct StoreDecodeArgs {
   int Hq, Hkv, G, Gp, L2, rows_list, recent, S;
   int K, Kp, gpw, n_groups, shift;      // 16-row groups per window and in all; log2 of the block
   int n_recent, n_front, ring0;         // recent keys: n_front sink rows, then the ring from ring row ring0 on (wrapping)
-  int list_blocks, blocks, n_split, n_group;
+  int list_blocks, recent_blocks, n_split, n_group;
   float scale_log2;
 };
 
-__device__ __forceinline__ uint2 ld_stream8(const void* p) {
+// Rows reach a warp through a ring of its own in shared memory, filled by asynchronous 16-byte copies: kRing stages of kStage bytes.
+// The 16-byte chunks of every 128 bytes lie in an order in which neither the lanes' reads of K nor those of V meet in a bank
+// (kBytes: of a row; row counts from the start of the stage).
+constexpr int kRing = 3, kStage = 4096;
+template <int kBytes>
+__device__ __forceinline__ uint32_t swizzled(int row, int byte) {   // byte within the row, a multiple of 8
+  const uint32_t at = row * kBytes + byte;
+  if constexpr (kBytes == 64) return at ^ (at >> 7 & 3) << 5;
+  if constexpr (kBytes == 128) return at ^ ((row & 1) << 6 ^ (row >> 1 & 3) << 5);
+  return at ^ (((row ^ row >> 1) & 1) << 6 | (row >> 2 & 1) << 4);
+}
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint2 lds8(uint32_t p) {
   uint2 v;
-  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 lds16(uint32_t p) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p) : "memory");
   return v;
 }
 __device__ __forceinline__ void mma_16816_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -295,20 +318,24 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
 template <int D, int NH, int T>
 __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel(const __grid_constant__ StoreDecodeArgs a) {
   constexpr bool k8 = T != LRSA_LIST_BF16;
-  constexpr int UR = 128 / D;               // 16-key groups per block of recent rows
-  constexpr int UL = k8 ? 256 / D : UR;     // of list rows
+  constexpr int UL = 128 / D;               // 16-row groups per block
   constexpr int KC = D / 32;                // 16-byte chunks of a bf16 row per lane
   constexpr int KC8 = D / 64;               // of an 8-bit row
   constexpr int VC = D / 64;                // 16-byte chunks of V per lane, bf16
   constexpr int MT = D / 16;                // channel tiles of the output: tile f holds channels g*D/8 + 2f, + 1
-  constexpr int kSlots = dec_max_warps(NH) / 2;
+  constexpr int kSlot = 8 * (D + 4);        // floats of a warp's O in the merge
   constexpr float kLift = 7.f;              // 8 + 7 < 16: no half overflows between two raises of the maxima
-  __shared__ __align__(16) float sm_o[kSlots][8][D + 4];
-  __shared__ float sm_m[kSlots][8], sm_l[kSlots][8], sm_r[kSlots][8];
+  // The rings; behind the loops, in the same place, the O of half of the warps [8 heads][D + 4] each and the CTA's [8][D].
+  extern __shared__ __align__(128) unsigned char dec_smem[];
+  float* sm_o = reinterpret_cast<float*>(dec_smem);
+  float* fin_o = sm_o + (blockDim.x >> 6) * kSlot;
+  __shared__ float sm_m[kDecMaxWarps / 2][8], sm_l[kDecMaxWarps / 2][8], sm_r[kDecMaxWarps / 2][8];
   __shared__ __align__(16) uint4 sm_q[NH][KC][32];                    // bf16
   __shared__ __align__(16) uint4 sm_h[k8 ? NH : 1][k8 ? 2 * KC8 : 1][32];   // halves
+  __shared__ __align__(8) float sm_scale[k8 ? kDecMaxWarps : 1][kRing * 2 * UL];   // of the groups of a stage: K, V
   __shared__ float sm_qs[8 * NH];                                     // what the halves are multiplied by
-  __shared__ float fin_o[8][D], fin_m[8], fin_l[8], fin_r[8];         // the CTA's result, read by the cluster
+  __shared__ float fin_m[8], fin_l[8], fin_r[8];                      // with fin_o the CTA's result, read by the cluster
+  __shared__ float all_m[kDecMaxSplits][8], all_l[kDecMaxSplits][8], all_r[kDecMaxSplits][8], sum_m[8], sum_l[8];   // the cluster's
   __shared__ float sm_lse[8 * NH];                                    // of the pass, in the log2 domain
   const int bh = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nw = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
@@ -330,44 +357,138 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
     }
     return (size_t)r * (D * 2);
   };
-  // first row and visible rows of 16-row group `gi` of the list
-  auto group_row = [&](int gi, int& n) {
-    const int w = gi / a.gpw, j = (gi - w * a.gpw) * 16;
-    n = gi < a.n_groups ? min(16, a.K - j) : 0;
-    return gi < a.n_groups ? w * a.Kp + j : 0;
-  };
   const int nx = a.n_split * a.n_group;
-  const int blk0 = (int)((long long)a.blocks * blockIdx.x / nx), blk1 = (int)((long long)a.blocks * (blockIdx.x + 1) / nx);
+  // This CTA's blocks: an even share of the list's (l0 ...) and of the recent rows' (r0 ...), which are twice the bytes.  Block v
+  // of the CTA is list block l0 + v for v < nl, then recent block r0 + v - nl.
+  const int x = blockIdx.x, l0 = (int)((long long)a.list_blocks * x / nx), nl = (int)((long long)a.list_blocks * (x + 1) / nx) - l0;
+  const int r0 = (int)((long long)a.recent_blocks * x / nx), nr = (int)((long long)a.recent_blocks * (x + 1) / nx) - r0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (blockIdx.x == 0 && bh == 0 && tid == 0) *a.status = 0;
 
+  // The warp takes the CTA's blocks warp, warp + nw, ...  The first n_list of them are 8-bit blocks of the list, a stage each (K and
+  // V), the others bf16 rows (first of a bf16 list), a stage for K and one for V.
+  const int n_blk = max(0, (nl + nr - warp + nw - 1) / nw), n_list = k8 ? max(0, (nl - warp + nw - 1) / nw) : 0;
+  const int n_stages = n_list + 2 * (n_blk - n_list);
+  // Place of a 16-row group in the list: group j of a window.  A cursor goes from block to block without a division.
+  struct Cursor { int w, j; };
+  const int step = nw * UL, step_w = step / a.gpw, step_j = step - step_w * a.gpw;
+  auto cursor_at = [&](int group) {
+    Cursor c;
+    c.w = group / a.gpw;
+    c.j = group - c.w * a.gpw;
+    return c;
+  };
+  auto advance = [&](Cursor& c) {
+    c.w += step_w;
+    c.j += step_j;
+    if (c.j >= a.gpw) { c.j -= a.gpw; ++c.w; }
+  };
+  // first row of the group `u` places behind the cursor; beyond the last group `last`: of the first
+  auto group_row = [&](Cursor c, int u, bool there) {
+    c.j += u;
+    if (c.j >= a.gpw) { c.j -= a.gpw; ++c.w; }   // (UL <= 2 and a window has a group at least)
+    return there ? c.w * a.Kp + c.j * 16 : 0;
+  };
+  auto group_rows = [&](Cursor c, int u, bool there) {   // its visible rows
+    c.j += u;
+    if (c.j >= a.gpw) c.j -= a.gpw;
+    return there ? min(16, a.K - c.j * 16) : 0;
+  };
+  const uint32_t ring = ptx::smem_u32(dec_smem) + warp * (kRing * kStage), meta = ptx::smem_u32(sm_scale[k8 ? warp : 0]);
+  int f_stage = 0, f_slot = 0, f_v = warp;   // the next stage to ask for, its slot, its block
+  Cursor f_at = cursor_at((l0 + warp) * UL);
+  // what this lane copies of a stage: 16 bytes of rows lane / chunks-per-row, ...
+  const uint32_t own8 = swizzled<D>(lane / (D / 16), lane % (D / 16) * 16), own16 = swizzled<2 * D>(lane / (D / 8), lane % (D / 8) * 16);
+  auto fetch = [&]() {
+    const uint32_t dst = ring + f_slot * kStage;
+    if (f_stage < n_list) {
+#pragma unroll
+      for (int u = 0; u < UL; ++u) {
+        const int row = group_row(f_at, u, (l0 + f_v) * UL + u < a.n_groups);
+        const unsigned char *pk = kl + (size_t)row * D + lane * 16, *pv = vl + (size_t)row * D + lane * 16;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {   // 512 bytes each: 4 rows (d = 128), 8 rows (64)
+          const uint32_t to = dst + u * 16 * D + ((D == 128 && (k & 1)) ? own8 ^ 64 : own8) + k * 512;
+          copy_async16(to, pk + k * 512);
+          copy_async16(to + kStage / 2, pv + k * 512);
+        }
+        if (lane < 2) copy_async4(meta + (f_slot * 2 * UL + 2 * u + lane) * 4, (lane ? vs : ks) + (row >> a.shift));
+      }
+      advance(f_at);
+      f_v += nw;
+    } else if (f_stage < n_stages) {
+      const bool is_v = (f_stage - n_list) & 1, in_list = !k8 && f_v < nl;
+      constexpr int kRows = 512 / (2 * D);   // rows per 512 bytes
+      const int key0 = (r0 + f_v - nl) * (16 * UL);
+      const unsigned char* src = in_list ? (is_v ? vl : kl) : (is_v ? vr : kr);
+      // the block's rows one behind the other?
+      int first = key0 - a.n_front + a.ring0;
+      if (first >= a.L2) first -= a.L2;
+      const bool run = !in_list && key0 >= a.n_front && key0 + 16 * UL <= a.n_recent && first + 16 * UL <= a.L2;
+      const unsigned char* base = src + (size_t)(a.S + first) * (2 * D) + lane * 16;
+#pragma unroll
+      for (int k = 0; k < kStage / 512; ++k) {
+        const int r = lane / (D / 8) + kRows * k;
+        const unsigned char* from = base + k * 512;
+        if (!run) {
+          const size_t at = in_list ? (size_t)(group_row(f_at, r >> 4, (l0 + f_v) * UL + (r >> 4) < a.n_groups) + (r & 15)) * (2 * D) : recent_row(key0 + r);
+          from = src + at + lane % (D / 8) * 16;
+        }
+        copy_async16(dst + swizzled<2 * D>(r, lane % (D / 8) * 16), from);
+      }
+      if (is_v) { f_v += nw; advance(f_at); }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ++f_stage;
+    f_slot = f_slot == kRing - 1 ? 0 : f_slot + 1;
+  };
+  int slot = 0;   // of the stage that is read next
+  // waits for the next stage, asks for the one kRing - 1 behind it
+  auto stage = [&]() {
+    __syncwarp();   // every lane has read the stage in front, whose place is filled now
+    fetch();
+    asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+    __syncwarp();   // the stage is there for all lanes
+    const int at = slot;
+    slot = slot == kRing - 1 ? 0 : slot + 1;
+    return at;
+  };
+
   for (int g0 = 0; g0 < a.G; g0 += 8 * NH) {
-    __syncthreads();
+    __syncthreads();   // the rings are idle: what the merge left there has been read
+    f_stage = f_slot = slot = 0;
+    f_v = warp;
+    f_at = cursor_at((l0 + warp) * UL);
+    for (int i = 0; i < kRing - 1; ++i) fetch();
     // Q of the pass as the B operand: chunk t + 4j of a lane's head, as it takes the chunks of every key row
     for (int hd = warp; hd < 8 * NH; hd += nw) {
       constexpr int PL = D / 32;   // channels per lane
       const int c0 = lane * PL, li = (hd & 7) * 4;
-      __nv_bfloat16 x[PL];
+      uint32_t x[PL / 2] = {};   // pairs of channels
+      if (g0 + hd < a.G) {
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + ((size_t)b * a.Hq + hkv * a.G + g0 + hd) * D + c0);
 #pragma unroll
-      for (int e = 0; e < PL; ++e)
-        x[e] = g0 + hd < a.G ? a.q[((size_t)b * a.Hq + hkv * a.G + g0 + hd) * D + c0 + e] : __float2bfloat16(0.f);
-      __nv_bfloat16* qb = reinterpret_cast<__nv_bfloat16*>(&sm_q[hd >> 3][c0 / 8 / 4][li + c0 / 8 % 4]) + c0 % 8;
+        for (int e = 0; e < PL / 2; ++e) x[e] = src[e];
+      }
+      uint32_t* qb = reinterpret_cast<uint32_t*>(&sm_q[hd >> 3][c0 / 8 / 4][li + c0 / 8 % 4]) + c0 % 8 / 2;
 #pragma unroll
-      for (int e = 0; e < PL; ++e) qb[e] = x[e];
+      for (int e = 0; e < PL / 2; ++e) qb[e] = x[e];
       if constexpr (k8) {
         uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < PL; ++e) most = max(most, (uint32_t)__bfloat16_as_ushort(x[e]) & 0x7fffu);
+        for (int e = 0; e < PL / 2; ++e) most = max(most, max(x[e] & 0x7fffu, x[e] >> 16 & 0x7fffu));
         most = __reduce_max_sync(0xffffffffu, most);
         // exponent of the largest element to 14; infinities, NaN and zero stay what they are
         const int e8 = (int)(most >> 7);
         const int up = most == 0 || most >= 0x7f80u ? 0 : 14 - (max(e8, 1) - 127);
-        const float f1 = exp2f((float)(up / 2)), f2 = exp2f((float)(up - up / 2));   // 2^up may exceed the range
-        __half* qh = reinterpret_cast<__half*>(&sm_h[hd >> 3][c0 / 64 * 2 + c0 % 16 / 8][li + c0 / 16 % 4]) + c0 % 8;
+        auto two_to = [](int n) { return __int_as_float((n + 127) << 23); };   // n in [-126, 127]
+        const float f1 = two_to(up / 2), f2 = two_to(up - up / 2);   // 2^up may exceed the range
+        uint32_t* qh = reinterpret_cast<uint32_t*>(&sm_h[hd >> 3][c0 / 64 * 2 + c0 % 16 / 8][li + c0 / 16 % 4]) + c0 % 8 / 2;
 #pragma unroll
-        for (int e = 0; e < PL; ++e) qh[e] = __float2half(__bfloat162float(x[e]) * f1 * f2);
-        if (lane == 0) sm_qs[hd] = exp2f((float)(-up));
+        for (int e = 0; e < PL / 2; ++e)
+          qh[e] = pack_f16(__uint_as_float(x[e] << 16) * f1 * f2, __uint_as_float(x[e] & 0xffff0000u) * f1 * f2);
+        if (lane == 0) sm_qs[hd] = two_to(-(up / 2)) * two_to(-(up - up / 2));
       }
     }
     __syncthreads();
@@ -401,45 +522,41 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
         }
       }
     };
-    int blk = blk0 + warp;
+    int v = warp;
+    Cursor at = cursor_at((l0 + warp) * UL);
     if constexpr (k8) {
-      for (; blk < min(blk1, a.list_blocks); blk += nw) {
-        uint4 kq[UL][2][KC8];
-        uint32_t vq[UL][4][D / 32];   // D / 8 codes of a V row
+      float qc[NH][2];   // what takes a product of halves to the log2 domain, but for the scale
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) qc[h][e] = sm_qs[8 * h + 2 * t + e] * a.scale_log2;
+      // this lane's places in a stage: K row g, chunk t; V row 2t, its D / 8 channels
+      const uint32_t k_at = swizzled<D>(g, t * 16), v_at = swizzled<D>(2 * t, g * (D / 8)) + kStage / 2;
+      for (int i = 0; i < n_list; ++i, v += nw) {
         int nvis[UL];
         float fk[UL], lv[UL];
+        const int sl = stage();
+        const uint32_t buf = ring + sl * kStage;
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
-          const int row = group_row(blk * UL + u, nvis[u]);
-          fk[u] = ks[row >> a.shift];
-          lv[u] = vs[row >> a.shift];
-          const unsigned char* p = kl + (size_t)row * D;
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < KC8; ++j) kq[u][i][j] = ld_stream(p + (g + 8 * i) * D + (t + 4 * j) * 16);
-          p = vl + (size_t)row * D;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const unsigned char* pv = p + (2 * t + (i & 1) + 8 * (i >> 1)) * D + g * (D / 8);
-            if constexpr (D == 128) {
-              const uint4 v = ld_stream(pv);
-              vq[u][i][0] = v.x; vq[u][i][1] = v.y; vq[u][i][2] = v.z; vq[u][i][3] = v.w;
-            } else {
-              const uint2 v = ld_stream8(pv);
-              vq[u][i][0] = v.x; vq[u][i][1] = v.y;
-            }
-          }
+          nvis[u] = group_rows(at, u, (l0 + v) * UL + u < a.n_groups);
+          const uint2 f = lds8(meta + (sl * 2 * UL + 2 * u) * 4);
+          fk[u] = __uint_as_float(f.x);
+          lv[u] = __uint_as_float(f.y);
         }
-#pragma unroll
-        for (int u = 0; u < UL; ++u) lv[u] = __log2f(lv[u]);
+        advance(at);
         float s[NH][UL][4];
 #pragma unroll
         for (int h = 0; h < NH; ++h)
 #pragma unroll
           for (int u = 0; u < UL; ++u) s[h][u][0] = s[h][u][1] = s[h][u][2] = s[h][u][3] = 0.f;
 #pragma unroll
-        for (int j = 0; j < KC8; ++j)
+        for (int j = 0; j < KC8; ++j) {
+          uint4 kq[UL][2];
+#pragma unroll
+          for (int u = 0; u < UL; ++u)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) kq[u][z] = lds16(buf + u * 16 * D + (j ? k_at ^ 64 : k_at) + 8 * D * z);   // (d = 64: one chunk)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint4 q[NH];
@@ -447,8 +564,8 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
             for (int h = 0; h < NH; ++h) q[h] = sm_h[h][2 * j + c][lane];
 #pragma unroll
             for (int u = 0; u < UL; ++u) {
-              const uint32_t w0 = c ? kq[u][0][j].z : kq[u][0][j].x, w1 = c ? kq[u][1][j].z : kq[u][1][j].x;
-              const uint32_t w2 = c ? kq[u][0][j].w : kq[u][0][j].y, w3 = c ? kq[u][1][j].w : kq[u][1][j].y;
+              const uint32_t w0 = c ? kq[u][0].z : kq[u][0].x, w1 = c ? kq[u][1].z : kq[u][1].x;
+              const uint32_t w2 = c ? kq[u][0].w : kq[u][0].y, w3 = c ? kq[u][1].w : kq[u][1].y;
               uint32_t a0, a1, a2, a3;
               widen<T>(w0, a0, a2);
               widen<T>(w1, a1, a3);
@@ -460,16 +577,39 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
               for (int h = 0; h < NH; ++h) mma_16816_f16(s[h][u], a0, a1, a2, a3, q[h].z, q[h].w);
             }
           }
-        uint32_t pb[NH][UL][2];
+        }
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
-          const float c0 = sm_qs[8 * h + 2 * t] * a.scale_log2, c1 = sm_qs[8 * h + 2 * t + 1] * a.scale_log2;
+#pragma unroll
+          for (int u = 0; u < UL; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s[h][u][e] = g + 8 * (e >> 1) < nvis[u] ? s[h][u][e] * (fk[u] * qc[h][e & 1]) : -INFINITY;
+        }
+        uint32_t pb[NH][UL][2];
+        uint32_t vq[UL][4][D / 32];   // D / 8 codes of a V row
+#pragma unroll
+        for (int u = 0; u < UL; ++u) {
+          lv[u] = __log2f(lv[u]);
+#pragma unroll
+          for (int i2 = 0; i2 < 4; ++i2) {
+            const uint32_t pv = buf + u * 16 * D + (i2 & 1 ? (v_at ^ 64) + (D == 128 ? 128 : 0) : v_at) + (i2 >> 1) * 8 * D;   // (d = 64: two rows in 128 bytes)
+            if constexpr (D == 128) {
+              const uint4 v = lds16(pv);
+              vq[u][i2][0] = v.x; vq[u][i2][1] = v.y; vq[u][i2][2] = v.z; vq[u][i2][3] = v.w;
+            } else {
+              const uint2 v = lds8(pv);
+              vq[u][i2][0] = v.x; vq[u][i2][1] = v.y;
+            }
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
           float mx[2] = {-INFINITY, -INFINITY}, mr[2] = {-INFINITY, -INFINITY};
 #pragma unroll
           for (int u = 0; u < UL; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              s[h][u][e] = g + 8 * (e >> 1) < nvis[u] ? s[h][u][e] * (fk[u] * (e & 1 ? c1 : c0)) : -INFINITY;
               mx[e & 1] = fmaxf(mx[e & 1], s[h][u][e]);
               mr[e & 1] = fmaxf(mr[e & 1], s[h][u][e] + lv[u]);
             }
@@ -491,73 +631,74 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
 #pragma unroll
         for (int u = 0; u < UL; ++u)
 #pragma unroll
-          for (int i = 0; i < D / 32; ++i) {   // four channels: tiles 2i, 2i + 1
+          for (int f = 0; f < D / 32; ++f) {   // four channels: tiles 2f, 2f + 1
             uint32_t x[2][4];                  // [rows 2t, 2t+1 | + 8][channel]: pairs of keys
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
-              widen<T>(__byte_perm(vq[u][2 * z][i], vq[u][2 * z + 1][i], 0x5140), x[z][0], x[z][1]);
-              widen<T>(__byte_perm(vq[u][2 * z][i], vq[u][2 * z + 1][i], 0x7362), x[z][2], x[z][3]);
+              widen<T>(__byte_perm(vq[u][2 * z][f], vq[u][2 * z + 1][f], 0x5140), x[z][0], x[z][1]);
+              widen<T>(__byte_perm(vq[u][2 * z][f], vq[u][2 * z + 1][f], 0x7362), x[z][2], x[z][3]);
             }
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-              mma_16816_f16(o[h][2 * i], x[0][0], x[0][1], x[1][0], x[1][1], pb[h][u][0], pb[h][u][1]);
-              mma_16816_f16(o[h][2 * i + 1], x[0][2], x[0][3], x[1][2], x[1][3], pb[h][u][0], pb[h][u][1]);
+              mma_16816_f16(o[h][2 * f], x[0][0], x[0][1], x[1][0], x[1][1], pb[h][u][0], pb[h][u][1]);
+              mma_16816_f16(o[h][2 * f + 1], x[0][2], x[0][3], x[1][2], x[1][3], pb[h][u][0], pb[h][u][1]);
             }
           }
       }
     }
-    for (; blk < blk1; blk += nw) {
+    for (; v < nl + nr; v += nw) {
       // bf16: recent rows, or rows of a bf16 list
-      const bool in_list = !k8 && blk < a.list_blocks;
-      uint4 kq[UR][2][KC], vq[UR][4][VC];
-      int nvis[UR], key0[UR];
+      const bool in_list = !k8 && v < nl;
+      int nvis[UL], key0[UL];
 #pragma unroll
-      for (int u = 0; u < UR; ++u) {
-        int row = 0;
-        if (in_list) {
-          row = group_row(blk * UR + u, nvis[u]);
-        } else {
-          key0[u] = ((blk - a.list_blocks) * UR + u) * 16;
-          nvis[u] = a.n_recent - key0[u];
-        }
+      for (int u = 0; u < UL; ++u) {
+        key0[u] = ((r0 + v - nl) * UL + u) * 16;
+        nvis[u] = a.n_recent - key0[u];
+        if (in_list) nvis[u] = group_rows(at, u, (l0 + v) * UL + u < a.n_groups);
+      }
+      if (!k8) advance(at);
+      float s[NH][UL][4];
+      {
+        const uint32_t buf = ring + stage() * kStage;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const unsigned char* p = in_list ? kl + (size_t)(row + g + 8 * i) * (D * 2) : kr + recent_row(key0[u] + g + 8 * i);
+        for (int h = 0; h < NH; ++h)
 #pragma unroll
-          for (int j = 0; j < KC; ++j) kq[u][i][j] = ld_stream(p + (t + 4 * j) * 16);
-        }
+          for (int u = 0; u < UL; ++u) s[h][u][0] = s[h][u][1] = s[h][u][2] = s[h][u][3] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int k = 2 * t + (i & 1) + 8 * (i >> 1);
-          const unsigned char* p = in_list ? vl + (size_t)(row + k) * (D * 2) : vr + recent_row(key0[u] + k);
+        for (int j = 0; j < KC; ++j) {
+          uint4 q[NH];
 #pragma unroll
-          for (int j = 0; j < VC; ++j) vq[u][i][j] = ld_stream(p + g * (D / 4) + j * 16);
+          for (int h = 0; h < NH; ++h) q[h] = sm_q[h][j][lane];
+#pragma unroll
+          for (int u = 0; u < UL; ++u) {
+            const uint4 k0 = lds16(buf + swizzled<D * 2>(16 * u + g, (t + 4 * j) * 16));
+            const uint4 k1 = lds16(buf + swizzled<D * 2>(16 * u + g + 8, (t + 4 * j) * 16));
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+              mma_16816(s[h][u], k0.x, k1.x, k0.y, k1.y, q[h].x, q[h].y);
+              mma_16816(s[h][u], k0.z, k1.z, k0.w, k1.w, q[h].z, q[h].w);
+            }
+          }
         }
       }
+      uint32_t pb[NH][UL][2];
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
-        float s[UR][4], mx[2] = {-INFINITY, -INFINITY};
+        float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int u = 0; u < UR; ++u) {
-          s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.f;
-#pragma unroll
-          for (int j = 0; j < KC; ++j) {
-            const uint4 q = sm_q[h][j][lane];
-            mma_16816(s[u], kq[u][0][j].x, kq[u][1][j].x, kq[u][0][j].y, kq[u][1][j].y, q.x, q.y);
-            mma_16816(s[u], kq[u][0][j].z, kq[u][1][j].z, kq[u][0][j].w, kq[u][1][j].w, q.z, q.w);
-          }
+        for (int u = 0; u < UL; ++u) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[u][e] = g + 8 * (e >> 1) < nvis[u] ? s[u][e] * a.scale_log2 : -INFINITY;
-            mx[e & 1] = fmaxf(mx[e & 1], s[u][e]);
+            s[h][u][e] = g + 8 * (e >> 1) < nvis[u] ? s[h][u][e] * a.scale_log2 : -INFINITY;
+            mx[e & 1] = fmaxf(mx[e & 1], s[h][u][e]);
           }
           if (a.weight && !in_list) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int key = key0[u] + g + 8 * i;
+            for (int z = 0; z < 2; ++z) {
+              const int key = key0[u] + g + 8 * z;
               if (key >= a.n_front && key < a.n_recent && g0 + 8 * h + 2 * t < a.Gp)
                 *reinterpret_cast<float2*>(a.scores + ((size_t)bh * a.L2 + key - a.n_front) * a.Gp + g0 + 8 * h + 2 * t) =
-                    make_float2(s[u][2 * i], s[u][2 * i + 1]);
+                    make_float2(s[h][u][2 * z], s[h][u][2 * z + 1]);
             }
           }
         }
@@ -566,37 +707,65 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
         const float rm[2] = {m[h][0] == -INFINITY ? 0.f : m[h][0], m[h][1] == -INFINITY ? 0.f : m[h][1]};
         const float rr[2] = {r[h][0] == -INFINITY ? 0.f : r[h][0] - kLift, r[h][1] == -INFINITY ? 0.f : r[h][1] - kLift};
 #pragma unroll
-        for (int u = 0; u < UR; ++u) {
+        for (int u = 0; u < UL; ++u) {
           float p[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            l[h][e & 1] += ptx::ex2(s[u][e] - rm[e & 1]);
-            p[e] = ptx::ex2(s[u][e] - rr[e & 1]);
+            l[h][e & 1] += ptx::ex2(s[h][u][e] - rm[e & 1]);
+            p[e] = ptx::ex2(s[h][u][e] - rr[e & 1]);
           }
-          const uint32_t b0 = transpose_8x8(ptx::pack_bf16(p[0], p[1])), b1 = transpose_8x8(ptx::pack_bf16(p[2], p[3]));
-#pragma unroll
-          for (int j = 0; j < VC; ++j)
-#pragma unroll
-            for (int f = 0; f < 4; ++f) {
-              auto w = [&](int i) { return f == 0 ? vq[u][i][j].x : f == 1 ? vq[u][i][j].y : f == 2 ? vq[u][i][j].z : vq[u][i][j].w; };
-              mma_16816(o[h][4 * j + f], __byte_perm(w(0), w(1), 0x5410), __byte_perm(w(0), w(1), 0x7632),
-                        __byte_perm(w(2), w(3), 0x5410), __byte_perm(w(2), w(3), 0x7632), b0, b1);
-            }
+          pb[h][u][0] = transpose_8x8(ptx::pack_bf16(p[0], p[1]));
+          pb[h][u][1] = transpose_8x8(ptx::pack_bf16(p[2], p[3]));
         }
       }
+      const uint32_t buf = ring + stage() * kStage;
+#pragma unroll
+      for (int u = 0; u < UL; ++u)
+#pragma unroll
+        for (int j = 0; j < VC; ++j) {
+          uint4 vr4[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) vr4[z] = lds16(buf + swizzled<D * 2>(16 * u + 2 * t + (z & 1) + 8 * (z >> 1), g * (D / 4) + j * 16));
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            auto w = [&](int z) { return f == 0 ? vr4[z].x : f == 1 ? vr4[z].y : f == 2 ? vr4[z].z : vr4[z].w; };
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+              mma_16816(o[h][4 * j + f], __byte_perm(w(0), w(1), 0x5410), __byte_perm(w(0), w(1), 0x7632),
+                        __byte_perm(w(2), w(3), 0x5410), __byte_perm(w(2), w(3), 0x7632), pb[h][u][0], pb[h][u][1]);
+          }
+        }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     // Merge the warps: the upper half hands its state to the lower half, then all threads add what is left.
     const int half = nw / 2;
     const bool upper = warp >= half;
     const int slot = upper ? warp - half : warp;
     const int group = blockIdx.x / a.n_split, rank = blockIdx.x - group * a.n_split;
+    // The keys of the ring whose scores this CTA has stored: k0 + tid, + blockDim.x, ... below k1.  What the first of them needs is on
+    // its way while the cluster meets.
+    const bool weigh = a.weight && a.n_group == 1;
+    const int k0 = max(a.n_front, r0 * UL * 16), k1 = weigh ? min(a.n_recent, (r0 + nr) * UL * 16) : 0, n_heads = min(8 * NH, a.G - g0);
+    float4 sc[2 * NH];
+    float gathered = 0.f;
+    auto weight_of = [&](int key) {
+      int at = key - a.n_front + a.ring0;
+      if (at >= a.L2) at -= a.L2;
+      return a.weight + (size_t)bh * a.L2 + at;
+    };
+    auto load_scores = [&](int key) {
+      const float4* src = reinterpret_cast<const float4*>(a.scores + ((size_t)bh * a.L2 + key - a.n_front) * a.Gp + g0);
+#pragma unroll
+      for (int i = 0; i < 2 * NH; ++i) sc[i] = 4 * i < n_heads ? src[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+      gathered = *weight_of(key);
+    };
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
       float lh[2], mh[2], rh[2];
       auto put = [&]() {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float* dst = sm_o[slot][2 * t + e] + g * (D / 8);
+          float* dst = sm_o + slot * kSlot + (2 * t + e) * (D + 4) + g * (D / 8);
 #pragma unroll
           for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[h][i][e], o[h][i][e + 2]);
           if (g == 0) { sm_m[slot][2 * t + e] = mh[e]; sm_l[slot][2 * t + e] = lh[e]; sm_r[slot][2 * t + e] = rh[e]; }
@@ -623,7 +792,7 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
           const float f0 = part_of(rh[e], rn), f1 = part_of(ro, rn);
           mh[e] = mn;
           rh[e] = rn;
-          const float* srcp = sm_o[slot][2 * t + e] + g * (D / 8);
+          const float* srcp = sm_o + slot * kSlot + (2 * t + e) * (D + 4) + g * (D / 8);
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             const float2 v = *reinterpret_cast<const float2*>(srcp + 2 * i);
@@ -642,105 +811,185 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
         for (int w = 0; w < half; ++w) { M = fmaxf(M, sm_m[w][hd]); R = fmaxf(R, sm_r[w][hd]); }
         float ov = 0.f, ls = 0.f;
         for (int w = 0; w < half; ++w) {
-          ov = fmaf(sm_o[w][hd][c], part_of(sm_r[w][hd], R), ov);
+          ov = fmaf(sm_o[w * kSlot + hd * (D + 4) + c], part_of(sm_r[w][hd], R), ov);
           ls = fmaf(sm_l[w][hd], part_of(sm_m[w][hd], M), ls);
         }
-        fin_o[hd][c] = ov;
+        fin_o[hd * D + c] = ov;
         if (c == 0) { fin_m[hd] = M; fin_l[hd] = ls; fin_r[hd] = R; }
       }
+      if (h == NH - 1 && k0 + tid < k1) load_scores(k0 + tid);   // (stored ahead of the barriers above)
       cluster_sync();
-      // the CTAs of the cluster share the elements of the output; every CTA wants the log-sums of all heads for its weights
-      auto total = [&](int hd, float& M, float& ls) {
-        M = -INFINITY; ls = 0.f;
-#pragma unroll 4
-        for (int k = 0; k < a.n_split; ++k) M = fmaxf(M, ld_cluster(&fin_m[hd], k));
-#pragma unroll 4
-        for (int k = 0; k < a.n_split; ++k) ls = fmaf(ld_cluster(&fin_l[hd], k), M == -INFINITY ? 0.f : exp2f(ld_cluster(&fin_m[hd], k) - M), ls);
-      };
+      // The maxima and sums of the CTAs of the cluster, into this one's shared memory; then the CTAs share the elements of the
+      // output.  (Every CTA wants the log-sums of all heads for its weights.)
+      for (int i = tid; i < 8 * a.n_split; i += blockDim.x) {
+        const int k = i >> 3, hd = i & 7;
+        if (hd < ng) {
+          all_m[k][hd] = ld_cluster(&fin_m[hd], k);
+          all_l[k][hd] = ld_cluster(&fin_l[hd], k);
+          all_r[k][hd] = ld_cluster(&fin_r[hd], k);
+        }
+      }
+      __syncthreads();
+      if (tid < 8 * 32) {   // a warp per head (or several), a lane per CTA
+        for (int hd = warp; hd < ng; hd += min(nw, 8)) {
+          const float mk = lane < a.n_split ? all_m[lane][hd] : -INFINITY, rk = lane < a.n_split ? all_r[lane][hd] : -INFINITY;
+          float M = mk, R = rk;
+#pragma unroll
+          for (int x = 8; x; x >>= 1) {
+            M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+            R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, x));
+          }
+          float ls = lane < a.n_split ? all_l[lane][hd] * part_of(mk, M) : 0.f;
+#pragma unroll
+          for (int x = 8; x; x >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, x);
+          // O in units of 2^M: R - M is the scale of the V rows that carry the weight
+          const float to = R == -INFINITY ? 0.f : exp2f(R - M);
+          if (lane < a.n_split) all_r[lane][hd] = part_of(rk, R) * to;
+          if (lane == 0) { sum_m[hd] = M; sum_l[hd] = ls; sm_lse[8 * h + hd] = M + log2f(ls); }
+        }
+      }
+      __syncthreads();
       for (int i = rank * blockDim.x + tid; i < ng * D; i += a.n_split * blockDim.x) {
         const int hd = i / D, c = i % D;
-        float M, ls, R = -INFINITY, ov = 0.f;
-        total(hd, M, ls);
-#pragma unroll 4
-        for (int k = 0; k < a.n_split; ++k) R = fmaxf(R, ld_cluster(&fin_r[hd], k));
-#pragma unroll 4
-        for (int k = 0; k < a.n_split; ++k) ov = fmaf(ld_cluster(&fin_o[hd][c], k), R == -INFINITY ? 0.f : exp2f(ld_cluster(&fin_r[hd], k) - R), ov);
-        // O in units of 2^M: R - M is the scale of the V rows that carry the weight
-        ov *= R == -INFINITY ? 0.f : exp2f(R - M);
+        float ov = 0.f;
+#pragma unroll 8
+        for (int k = 0; k < a.n_split; ++k) ov = fmaf(ld_cluster(&fin_o[hd * D + c], k), all_r[k][hd], ov);
         if (a.n_group > 1) {
           float* dst = a.part + (((size_t)bh * a.n_group + group) * a.G + g0 + 8 * h + hd) * (D + 2);
           dst[c] = ov;
-          if (c == 0) { dst[D] = M; dst[D + 1] = ls; }
+          if (c == 0) { dst[D] = sum_m[hd]; dst[D + 1] = sum_l[hd]; }
           continue;
         }
         const size_t head = (size_t)b * a.Hq + hkv * a.G + g0 + 8 * h + hd;
-        a.o[head * D + c] = __float2bfloat16(ov / ls);
-        if (c == 0 && a.lse) a.lse[head] = (M + log2f(ls)) * 0.6931471805599453f;
+        a.o[head * D + c] = __float2bfloat16(ov / sum_l[hd]);
+        if (c == 0 && a.lse) a.lse[head] = sm_lse[8 * h + hd] * 0.6931471805599453f;
       }
-      if (a.weight && a.n_group == 1 && tid < ng) {
-        float M, ls;
-        total(tid, M, ls);
-        sm_lse[8 * h + tid] = M + log2f(ls);
+      if (h == NH - 1) {
+        for (int key = k0 + tid; key < k1; key += blockDim.x) {
+          if (key != k0 + tid) load_scores(key);
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 2 * NH; ++i) {
+            const float y[4] = {sc[i].x, sc[i].y, sc[i].z, sc[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (4 * i + e < n_heads) sum += ptx::ex2(y[e] - sm_lse[4 * i + e]);
+          }
+          *weight_of(key) = gathered + sum;
+        }
       }
       cluster_sync();   // the other CTAs have read this one's result: it may be overwritten, or the CTA may leave
-    }
-    if (a.weight && a.n_group == 1) {
-      // (the barriers above have ordered the scores of the CTA's warps before these reads)
-      const int ng = min(8 * NH, a.G - g0);
-      const int k0 = max(a.n_front, (max(blk0, a.list_blocks) - a.list_blocks) * UR * 16), k1 = min(a.n_recent, (blk1 - a.list_blocks) * UR * 16);
-      for (int key = k0 + tid; key < k1; key += blockDim.x) {
-        const float* sc = a.scores + ((size_t)bh * a.L2 + key - a.n_front) * a.Gp + g0;
-        float sum = 0.f;
-        for (int hd = 0; hd < ng; ++hd) sum += ptx::ex2(sc[hd] - sm_lse[hd]);
-        int at = key - a.n_front + a.ring0;
-        if (at >= a.L2) at -= a.L2;
-        a.weight[(size_t)bh * a.L2 + at] += sum;
-      }
     }
   }
 }
 
-// The weights where a head has several clusters: log-sums are the merge kernel's.  A thread takes a key.
-__global__ void __launch_bounds__(128) store_weight_kernel(const StoreDecodeArgs a, const float* lse) {
-  const int bh = blockIdx.y, key = a.n_front + blockIdx.x * 128 + threadIdx.x;
+// Where a head has several clusters: their results are merged, and the weights formed with the log-sums.  Grid (chunks of the ring's
+// keys, BHkv); every CTA forms the log-sums of the group's heads, and the CTAs share the elements of the output and the keys.
+template <int D>
+__global__ void __launch_bounds__(128) store_finish_kernel(const __grid_constant__ StoreDecodeArgs a) {
+  extern __shared__ float fin_smem[];
+  float *lse2 = fin_smem, *inv = lse2 + a.G, *f = inv + a.G;   // per head: log-sum (log2 domain), 1 / sum; factor of every cluster
+  const int bh = blockIdx.y, tid = threadIdx.x, b = bh / a.Hkv, hkv = bh % a.Hkv;
+  const size_t head0 = (size_t)b * a.Hq + hkv * a.G;
+  const float* part = a.part + (size_t)bh * a.n_group * a.G * (D + 2);
   wait_for_front();
-  if (key >= a.n_recent) return;
-  const float* sc = a.scores + ((size_t)bh * a.L2 + key - a.n_front) * a.Gp;
-  const float* ls = lse + (size_t)(bh / a.Hkv) * a.Hq + (bh % a.Hkv) * a.G;
-  float sum = 0.f;
-  for (int hd = 0; hd < a.G; ++hd) sum += ptx::ex2(sc[hd] - ls[hd] * 1.4426950408889634f);
+  for (int hd = tid; hd < a.G; hd += 128) {
+    float M = -INFINITY, ls = 0.f;
+    for (int k = 0; k < a.n_group; ++k) M = fmaxf(M, __ldcg(part + ((size_t)k * a.G + hd) * (D + 2) + D));
+    for (int k = 0; k < a.n_group; ++k) {
+      const float* p = part + ((size_t)k * a.G + hd) * (D + 2) + D;
+      const float m = __ldcg(p), x = m == -INFINITY ? 0.f : exp2f(m - M);
+      f[k * a.G + hd] = x;
+      ls = fmaf(__ldcg(p + 1), x, ls);
+    }
+    lse2[hd] = M + log2f(ls);
+    inv[hd] = 1.f / ls;
+    if (a.lse && blockIdx.x == 0) a.lse[head0 + hd] = lse2[hd] * 0.6931471805599453f;
+  }
+  __syncthreads();
+  for (int i = blockIdx.x * 128 + tid; i < a.G * D; i += gridDim.x * 128) {
+    const int hd = i / D, c = i % D;
+    float ov = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < a.n_group; ++k) ov = fmaf(__ldcg(part + ((size_t)k * a.G + hd) * (D + 2) + c), f[k * a.G + hd], ov);
+    a.o[head0 * D + i] = __float2bfloat16(ov * inv[hd]);
+  }
+  const int key = a.n_front + blockIdx.x * 128 + tid;
+  if (!a.weight || key >= a.n_recent) return;
+  const float4* sc = reinterpret_cast<const float4*>(a.scores + ((size_t)bh * a.L2 + key - a.n_front) * a.Gp);
   int at = key - a.n_front + a.ring0;
   if (at >= a.L2) at -= a.L2;
-  a.weight[(size_t)bh * a.L2 + at] += sum;
+  float* w = a.weight + (size_t)bh * a.L2 + at;
+  float sum = *w;
+  for (int i = 0; 4 * i < a.G; ++i) {
+    const float4 x = __ldcg(sc + i);
+    const float y[4] = {x.x, x.y, x.z, x.w};
+    for (int e = 0; e < 4 && 4 * i + e < a.G; ++e) sum += ptx::ex2(y[e] - lse2[4 * i + e]);
+  }
+  *w = sum;
+}
+
+// How the blocks are dealt out: `groups` clusters of `splits` CTAs a (batch, KV head) pair, two CTAs on an SM (of 8 warps, 4 with two head
+// groups), by a model of the time in cycles: a warp takes about 2400 for a block, with all warps of the SM at work 170 for each (the
+// memory's rate and about the issue rate); start and merge take 4000, the kernel behind several clusters and their traffic 20 000.
+// us, warps x splits x groups (each with 2 to 3 us for setting the weights back): sixteen sequences of 28/4 heads at 32K (e4m3)
+// 8x4x1 37.8, 16x2x1 37.1, 4x8x1 39.3, 4x6x1 45.2, 4x1x9 62; one of them 8x16x1 16.9, 16x16x1 17.1 to 22, 8x8x1 19.0, 8x8x2 20.6; at 120K
+// 16x16x1 23.5, 8x16x2 27.2, 8x9x8 34; four of 32/8 at 120K (int8) 8x8x1 112, 16x4x1 111, 8x1x9 119, 8x9x1 (two waves of
+// clusters) 150; four of 8/8, d = 64, at 66K 8x8x1 25.4, 16x4x1 26.3, 16x2x2 29.3, 8x9x1 35.3.
+DecodePlan store_plan(const Geom& g, int blocks, int max_splits = kDecMaxSplits) {
+  const int nh = g.G > 8 ? 2 : 1, warps = dec_max_warps(nh) / 2;
+  DecodePlan best = {nh, warps, blocks, 1, 1};
+  const unsigned BH = (unsigned)g.B * g.Hkv;
+  const ClusterRoom& room = cluster_room();
+  unsigned long long least = ~0ull;
+  for (int s = 1; s <= max_splits; ++s) {
+    const unsigned at_once = room.at_once(2, s);
+    // one cluster for a pair, or as many as run at a time
+    const unsigned fit = BH > 2 * kSms ? 1 : at_once / BH < kDecMaxGroups ? at_once / BH : kDecMaxGroups;
+    for (unsigned grp = 1; grp == 1 || grp <= fit; grp = grp == 1 && fit > 1 ? fit : kDecMaxGroups + 1) {
+      const unsigned n = s * grp;
+      if (n > 1 && (n - 1) * warps >= (unsigned)blocks) break;
+      const unsigned clusters = BH * grp, waves = (clusters + at_once - 1) / at_once;
+      const unsigned on_sm = ((clusters < at_once ? clusters : at_once) * s + kSms - 1) / kSms;
+      const unsigned rounds = (blocks + n * warps - 1) / (n * warps), busy = 170 * on_sm * warps;
+      const unsigned long long cost = (unsigned long long)waves * (rounds * (busy > 2400 ? busy : 2400) + 4000) + (grp > 1 ? 20000 : 0);
+      if (cost <= least) { least = cost; best.splits = s; best.groups = grp; }
+    }
+  }
+  return best;
 }
 
 template <int D, int NH, int T>
 cudaError_t launch_store_decode_t(StoreDecodeArgs& a, const DecodePlan& pl, int BHkv, cudaStream_t st) {
   auto kern = store_decode_kernel<D, NH, T>;
+  // rings, or what the merge puts there: half of the warps' O and the CTA's
+  const int merge = (pl.warps / 2 * 8 * (D + 4) + 8 * D) * 4, rings = pl.warps * kRing * kStage;
+  const int smem = merge > rings ? merge : rings;
+  const cudaError_t es = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (es != cudaSuccess) return es;
   if (pl.splits > 8) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
   }
-  return launch_dependent(kern, dim3(pl.splits * pl.groups, BHkv), dim3(pl.warps * 32), 0, st, pl.splits, a);
+  return launch_dependent(kern, dim3(pl.splits * pl.groups, BHkv), dim3(pl.warps * 32), smem, st, pl.splits, a);
 }
 
 template <int T>
 cudaError_t launch_store_decode(const Geom& g, StoreDecodeArgs& a, const DecodePlan& pl, cudaStream_t st) {
   const int BHkv = g.B * g.Hkv;
-  a.n_split = pl.splits; a.n_group = pl.groups; a.blocks = pl.blocks;
+  a.n_split = pl.splits; a.n_group = pl.groups;
   if (g.d == 128) return pl.nh == 1 ? launch_store_decode_t<128, 1, T>(a, pl, BHkv, st) : launch_store_decode_t<128, 2, T>(a, pl, BHkv, st);
   return pl.nh == 1 ? launch_store_decode_t<64, 1, T>(a, pl, BHkv, st) : launch_store_decode_t<64, 2, T>(a, pl, BHkv, st);
 }
 
 // Parts of the workspace.
-struct StoreWs { size_t part, lse, scores, total; };
+struct StoreWs { size_t part, scores, total; };
 StoreWs store_ws(const Geom& g, const StoreGeom& o) {
   StoreWs w;
   const size_t BH = (size_t)g.B * g.Hkv;
   size_t off = sizeof(WsHeader);
-  // several clusters for a head only below 592 CTAs of 16 warps (deal_blocks)
-  w.part = off; off += align_up(BH <= 4 * (size_t)kSms * 4 ? BH * kDecMaxGroups * g.G * (g.d + 2) * sizeof(float) : 0, 256);
-  w.lse = off; off += align_up((size_t)g.B * g.Hq * sizeof(float), 256);
+  // several clusters for a head only where they run at a time (store_plan)
+  w.part = off; off += align_up(BH <= 2 * (size_t)kSms ? BH * kDecMaxGroups * g.G * (g.d + 2) * sizeof(float) : 0, 256);
   w.scores = off; off += o.by_weight ? align_up(BH * 2 * g.L * ((g.G + 7) / 8 * 8) * sizeof(float), 256) : 0;
   w.total = off;
   return w;
@@ -912,10 +1161,10 @@ int lrsa_store_decode(const lrsa_params_t* params, const lrsa_store_t* store, co
     a.ring0 = (nc * g.L) % (2 * g.L);
   }
   a.scale_log2 = g.scale * 1.4426950408889634f;
-  const int ul = o.type == LRSA_LIST_BF16 ? 128 / g.d : 256 / g.d, ur = 128 / g.d;
-  a.list_blocks = (a.n_groups + ul - 1) / ul;
-  const int blocks = a.list_blocks + (a.n_recent + 16 * ur - 1) / (16 * ur);
-  DecodePlan pl = deal_blocks(g, blocks);
+  const int ur = 128 / g.d;   // 16-row groups per block
+  a.list_blocks = (a.n_groups + ur - 1) / ur;
+  a.recent_blocks = (a.n_recent + 16 * ur - 1) / (16 * ur);
+  DecodePlan pl = store_plan(g, a.list_blocks + a.recent_blocks);
   auto launch = [&](const DecodePlan& p) {
     return o.type == LRSA_LIST_E4M3 ? launch_store_decode<LRSA_LIST_E4M3>(g, a, p, st)
            : o.type == LRSA_LIST_INT8 ? launch_store_decode<LRSA_LIST_INT8>(g, a, p, st)
@@ -924,20 +1173,18 @@ int lrsa_store_decode(const lrsa_params_t* params, const lrsa_store_t* store, co
   cudaError_t e = launch(pl);
   if (e != cudaSuccess && pl.splits > 8) {   // clusters of 16 are not portable: a part of a GPU may not have room for them
     (void)cudaGetLastError();
-    pl = deal_blocks(g, blocks, 8);
+    pl = store_plan(g, a.list_blocks + a.recent_blocks, 8);
     e = launch(pl);
   }
   LRSA_CUDA_CHECK(e);
   launch_counter().n++;
   if (pl.groups > 1) {
-    float* ls = a.weight && !lse ? reinterpret_cast<float*>(ws + lay.lse) : lse;
-    auto merge = g.d == 128 ? decode_merge_kernel<128, 1> : decode_merge_kernel<64, 1>;
-    LRSA_CUDA_CHECK(launch_dependent(merge, dim3(g.B * g.Hq), dim3(g.d), 0, st, 1, (const float*)a.part, a.o, ls, g.Hq, g.Hkv, g.G, pl.groups));
+    const int keys = a.weight ? a.n_recent - a.n_front : 0, chunks = keys > 128 ? (keys + 127) / 128 : 1;
+    const size_t smem = (size_t)(2 + pl.groups) * g.G * sizeof(float);
+    auto finish = g.d == 128 ? store_finish_kernel<128> : store_finish_kernel<64>;
+    if (smem > 48 * 1024) return LRSA_ERR_UNSUPPORTED;   // (more than 682 heads of a group)
+    LRSA_CUDA_CHECK(launch_dependent(finish, dim3(chunks, g.B * g.Hkv), dim3(128), smem, st, 1, a));
     launch_counter().n++;
-    if (a.weight && a.n_recent > a.n_front) {
-      LRSA_CUDA_CHECK(launch_dependent(store_weight_kernel, dim3((a.n_recent - a.n_front + 127) / 128, g.B * g.Hkv), dim3(128), 0, st, 1, a, (const float*)ls));
-      launch_counter().n++;
-    }
   }
   return LRSA_OK;
 }
