@@ -244,7 +244,8 @@ struct StoreDecodeArgs {
   int Hq, Hkv, G, Gp, L2, rows_list, recent, S;
   int K, Kp, gpw, n_groups, shift;      // 16-row groups per window and in all; log2 of the block
   int n_recent, n_front, ring0;         // recent keys: n_front sink rows, then the ring from ring row ring0 on (wrapping)
-  int list_blocks, recent_blocks, n_split, n_group;
+  int list_share, list_rest, recent_share, recent_rest;   // blocks of a CTA; so many CTAs have one more
+  int n_split, n_group;
   float scale_log2;
 };
 
@@ -282,6 +283,12 @@ __device__ __forceinline__ void mma_16816_f16(float (&d)[4], uint32_t a0, uint32
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// this CTA's variable at `p` as CTA `rank` of the cluster has it
+__device__ __forceinline__ void st_cluster(const float* p, int rank, float v) {
+  uint32_t addr;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(ptx::smem_u32(p)), "r"(rank));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -316,7 +323,7 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
 // stored, and when the cluster has its maximum and sum, each CTA adds exp2(score - lse) over the heads to the weights of
 // the keys that were its own: one owner per key, no atomics.  Several clusters per head: store_weight_kernel does it.
 template <int D, int NH, int T>
-__global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel(const __grid_constant__ StoreDecodeArgs a) {
+__global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel(const __grid_constant__ StoreDecodeArgs a) {
   constexpr bool k8 = T != LRSA_LIST_BF16;
   constexpr int UL = 128 / D;               // 16-row groups per block
   constexpr int KC = D / 32;                // 16-byte chunks of a bf16 row per lane
@@ -325,20 +332,23 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
   constexpr int MT = D / 16;                // channel tiles of the output: tile f holds channels g*D/8 + 2f, + 1
   constexpr int kSlot = 8 * (D + 4);        // floats of a warp's O in the merge
   constexpr float kLift = 7.f;              // 8 + 7 < 16: no half overflows between two raises of the maxima
-  // The rings; behind the loops, in the same place, the O of half of the warps [8 heads][D + 4] each and the CTA's [8][D].
+  constexpr int kWarps = dec_max_warps(NH) / 2;
+  // The rings; behind the loops, in the same place, the O of the warps [8 heads][D + 4] each.
   extern __shared__ __align__(128) unsigned char dec_smem[];
   float* sm_o = reinterpret_cast<float*>(dec_smem);
-  float* fin_o = sm_o + (blockDim.x >> 6) * kSlot;
-  __shared__ float sm_m[kDecMaxWarps / 2][8], sm_l[kDecMaxWarps / 2][8], sm_r[kDecMaxWarps / 2][8];
+  __shared__ float sm_m[kWarps][8], sm_l[kWarps][8], sm_r[kWarps][8], sm_f[kWarps][8];
+  // What the CTAs of the cluster write here: their maxima and sums, and their part of the outputs that are this one's.  The head groups
+  // take turns (a CTA writes those of group h + 1 when all have read those of group h - 1).
+  __shared__ float in_mlr[NH][kDecMaxSplits][3][8], in_o[NH][8 * D + kDecMaxSplits];
   __shared__ __align__(16) uint4 sm_q[NH][KC][32];                    // bf16
   __shared__ __align__(16) uint4 sm_h[k8 ? NH : 1][k8 ? 2 * KC8 : 1][32];   // halves
-  __shared__ __align__(8) float sm_scale[k8 ? kDecMaxWarps : 1][kRing * 2 * UL];   // of the groups of a stage: K, V
+  __shared__ __align__(8) float sm_scale[k8 ? kWarps : 1][kRing * 2 * UL];   // of the groups of a stage: K, V
   __shared__ float sm_qs[8 * NH];                                     // what the halves are multiplied by
-  __shared__ float fin_m[8], fin_l[8], fin_r[8];                      // with fin_o the CTA's result, read by the cluster
-  __shared__ float all_m[kDecMaxSplits][8], all_l[kDecMaxSplits][8], all_r[kDecMaxSplits][8], sum_m[8], sum_l[8];   // the cluster's
+  __shared__ float all_f[kDecMaxSplits][8], sum_m[8], sum_l[8];       // factor of a CTA's O, maximum and sum of the cluster
   __shared__ float sm_lse[8 * NH];                                    // of the pass, in the log2 domain
   const int bh = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int nw = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
+  constexpr int nw = kWarps, kThreads = 32 * kWarps;
+  const int g = lane >> 2, t = lane & 3;
   const int b = bh / a.Hkv, hkv = bh % a.Hkv;
   const unsigned char* kl = a.k_list + (size_t)bh * a.rows_list * (k8 ? D : 2 * D);
   const unsigned char* vl = a.v_list + (size_t)bh * a.rows_list * (k8 ? D : 2 * D);
@@ -357,11 +367,11 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
     }
     return (size_t)r * (D * 2);
   };
-  const int nx = a.n_split * a.n_group;
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (waited for before anything is written to another CTA)
   // This CTA's blocks: an even share of the list's (l0 ...) and of the recent rows' (r0 ...), which are twice the bytes.  Block v
   // of the CTA is list block l0 + v for v < nl, then recent block r0 + v - nl.
-  const int x = blockIdx.x, l0 = (int)((long long)a.list_blocks * x / nx), nl = (int)((long long)a.list_blocks * (x + 1) / nx) - l0;
-  const int r0 = (int)((long long)a.recent_blocks * x / nx), nr = (int)((long long)a.recent_blocks * (x + 1) / nx) - r0;
+  const int x = blockIdx.x, l0 = a.list_share * x + min(x, a.list_rest), nl = a.list_share + (x < a.list_rest);
+  const int r0 = a.recent_share * x + min(x, a.recent_rest), nr = a.recent_share + (x < a.recent_rest);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (blockIdx.x == 0 && bh == 0 && tid == 0) *a.status = 0;
@@ -737,11 +747,9 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
-    // Merge the warps: the upper half hands its state to the lower half, then all threads add what is left.
-    const int half = nw / 2;
-    const bool upper = warp >= half;
-    const int slot = upper ? warp - half : warp;
+    // Merge: the warps through shared memory, the CTAs by writing into one another's.
     const int group = blockIdx.x / a.n_split, rank = blockIdx.x - group * a.n_split;
+    const int share = (8 * D + a.n_split - 1) / a.n_split;   // elements of the output that are a CTA's
     // The keys of the ring whose scores this CTA has stored: k0 + tid, + blockDim.x, ... below k1.  What the first of them needs is on
     // its way while the cluster meets.
     const bool weigh = a.weight && a.n_group == 1;
@@ -761,99 +769,67 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
     };
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
-      float lh[2], mh[2], rh[2];
-      auto put = [&]() {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float* dst = sm_o + slot * kSlot + (2 * t + e) * (D + 4) + g * (D / 8);
-#pragma unroll
-          for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[h][i][e], o[h][i][e + 2]);
-          if (g == 0) { sm_m[slot][2 * t + e] = mh[e]; sm_l[slot][2 * t + e] = lh[e]; sm_r[slot][2 * t + e] = rh[e]; }
-        }
-      };
+      auto part_of = [](float from, float to) { return from == -INFINITY ? 0.f : exp2f(from - to); };
+      const int ng = min(8, a.G - g0 - 8 * h);
+      __syncthreads();   // the rings, or the last group's O, have been read
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        mh[e] = m[h][e];
-        rh[e] = r[h][e] - kLift;
-        lh[e] = l[h][e];
+        float* dst = sm_o + warp * kSlot + (2 * t + e) * (D + 4) + g * (D / 8);
 #pragma unroll
-        for (int y = 4; y < 32; y <<= 1) lh[e] += __shfl_xor_sync(0xffffffffu, lh[e], y);
+        for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[h][i][e], o[h][i][e + 2]);
+        float lh = l[h][e];
+#pragma unroll
+        for (int y = 4; y < 32; y <<= 1) lh += __shfl_xor_sync(0xffffffffu, lh, y);
+        if (g == 0) { sm_m[warp][2 * t + e] = m[h][e]; sm_l[warp][2 * t + e] = lh; sm_r[warp][2 * t + e] = r[h][e] - kLift; }
       }
-      auto part_of = [](float from, float to) { return from == -INFINITY ? 0.f : exp2f(from - to); };
-      __syncthreads();   // the buffer is free
-      if (upper) put();
+      if (h == 0 && g0 == 0) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");   // every CTA of the cluster has started
       __syncthreads();
-      if (!upper) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float mo = sm_m[slot][2 * t + e], mn = fmaxf(mh[e], mo);
-          const float ro = sm_r[slot][2 * t + e], rn = fmaxf(rh[e], ro);
-          lh[e] = lh[e] * part_of(mh[e], mn) + sm_l[slot][2 * t + e] * part_of(mo, mn);
-          const float f0 = part_of(rh[e], rn), f1 = part_of(ro, rn);
-          mh[e] = mn;
-          rh[e] = rn;
-          const float* srcp = sm_o + slot * kSlot + (2 * t + e) * (D + 4) + g * (D / 8);
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            const float2 v = *reinterpret_cast<const float2*>(srcp + 2 * i);
-            o[h][i][e] = o[h][i][e] * f0 + v.x * f1;
-            o[h][i][e + 2] = o[h][i][e + 2] * f0 + v.y * f1;
-          }
-        }
-        __syncwarp();   // every lane has read the slot before it is overwritten
-        put();
-      }
-      __syncthreads();
-      const int ng = min(8, a.G - g0 - 8 * h);
-      for (int i = tid; i < ng * D; i += blockDim.x) {
-        const int hd = i / D, c = i % D;
-        float M = -INFINITY, R = -INFINITY;
-        for (int w = 0; w < half; ++w) { M = fmaxf(M, sm_m[w][hd]); R = fmaxf(R, sm_r[w][hd]); }
-        float ov = 0.f, ls = 0.f;
-        for (int w = 0; w < half; ++w) {
-          ov = fmaf(sm_o[w * kSlot + hd * (D + 4) + c], part_of(sm_r[w][hd], R), ov);
-          ls = fmaf(sm_l[w][hd], part_of(sm_m[w][hd], M), ls);
-        }
-        fin_o[hd * D + c] = ov;
-        if (c == 0) { fin_m[hd] = M; fin_l[hd] = ls; fin_r[hd] = R; }
-      }
       if (h == NH - 1 && k0 + tid < k1) load_scores(k0 + tid);   // (stored ahead of the barriers above)
-      cluster_sync();
-      // The maxima and sums of the CTAs of the cluster, into this one's shared memory; then the CTAs share the elements of the
-      // output.  (Every CTA wants the log-sums of all heads for its weights.)
-      for (int i = tid; i < 8 * a.n_split; i += blockDim.x) {
-        const int k = i >> 3, hd = i & 7;
-        if (hd < ng) {
-          all_m[k][hd] = ld_cluster(&fin_m[hd], k);
-          all_l[k][hd] = ld_cluster(&fin_l[hd], k);
-          all_r[k][hd] = ld_cluster(&fin_r[hd], k);
+      if (tid < 8 * nw) {
+        const int hd = tid & 7, w = tid >> 3;
+        float M = -INFINITY, R = -INFINITY, ls = 0.f;
+#pragma unroll
+        for (int k = 0; k < nw; ++k) { M = fmaxf(M, sm_m[k][hd]); R = fmaxf(R, sm_r[k][hd]); }
+#pragma unroll
+        for (int k = 0; k < nw; ++k) ls = fmaf(sm_l[k][hd], part_of(sm_m[k][hd], M), ls);
+        sm_f[w][hd] = part_of(sm_r[w][hd], R);
+        for (int k = w; k < a.n_split; k += nw) {
+          st_cluster(&in_mlr[h][rank][0][hd], k, M);
+          st_cluster(&in_mlr[h][rank][1][hd], k, ls);
+          st_cluster(&in_mlr[h][rank][2][hd], k, R);
         }
       }
       __syncthreads();
-      if (tid < 8 * 32) {   // a warp per head (or several), a lane per CTA
-        for (int hd = warp; hd < ng; hd += min(nw, 8)) {
-          const float mk = lane < a.n_split ? all_m[lane][hd] : -INFINITY, rk = lane < a.n_split ? all_r[lane][hd] : -INFINITY;
-          float M = mk, R = rk;
-#pragma unroll
-          for (int x = 8; x; x >>= 1) {
-            M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
-            R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, x));
-          }
-          float ls = lane < a.n_split ? all_l[lane][hd] * part_of(mk, M) : 0.f;
-#pragma unroll
-          for (int x = 8; x; x >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, x);
-          // O in units of 2^M: R - M is the scale of the V rows that carry the weight
-          const float to = R == -INFINITY ? 0.f : exp2f(R - M);
-          if (lane < a.n_split) all_r[lane][hd] = part_of(rk, R) * to;
-          if (lane == 0) { sum_m[hd] = M; sum_l[hd] = ls; sm_lse[8 * h + hd] = M + log2f(ls); }
-        }
-      }
-      __syncthreads();
-      for (int i = rank * blockDim.x + tid; i < ng * D; i += a.n_split * blockDim.x) {
-        const int hd = i / D, c = i % D;
+      for (int i = tid; i < ng * D; i += kThreads) {
+        const int hd = i / D, c = i % D, owner = i / share;
         float ov = 0.f;
-#pragma unroll 8
-        for (int k = 0; k < a.n_split; ++k) ov = fmaf(ld_cluster(&fin_o[hd * D + c], k), all_r[k][hd], ov);
+#pragma unroll
+        for (int w = 0; w < nw; ++w) ov = fmaf(sm_o[w * kSlot + hd * (D + 4) + c], sm_f[w][hd], ov);
+        st_cluster(&in_o[h][rank * share + i - owner * share], owner, ov);
+      }
+      cluster_sync();
+      for (int hd = warp; hd < ng; hd += nw) {   // a warp per head, a lane per CTA
+        const bool there = lane < a.n_split;
+        const float mk = there ? in_mlr[h][lane][0][hd] : -INFINITY, rk = there ? in_mlr[h][lane][2][hd] : -INFINITY;
+        float M = mk, R = rk;
+#pragma unroll
+        for (int y = 8; y; y >>= 1) {
+          M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, y));
+          R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, y));
+        }
+        float ls = there ? in_mlr[h][lane][1][hd] * part_of(mk, M) : 0.f;
+#pragma unroll
+        for (int y = 8; y; y >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, y);
+        // O in units of 2^M: R - M is the scale of the V rows that carry the weight
+        if (there) all_f[lane][hd] = R == -INFINITY ? 0.f : part_of(rk, R) * exp2f(R - M);
+        if (lane == 0) { sum_m[hd] = M; sum_l[hd] = ls; sm_lse[8 * h + hd] = M + log2f(ls); }
+      }
+      __syncthreads();
+      for (int j = tid; j < share && rank * share + j < ng * D; j += kThreads) {
+        const int i = rank * share + j, hd = i / D, c = i % D;
+        float ov = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < a.n_split; ++k) ov = fmaf(in_o[h][k * share + j], all_f[k][hd], ov);
         if (a.n_group > 1) {
           float* dst = a.part + (((size_t)bh * a.n_group + group) * a.G + g0 + 8 * h + hd) * (D + 2);
           dst[c] = ov;
@@ -865,7 +841,7 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
         if (c == 0 && a.lse) a.lse[head] = sm_lse[8 * h + hd] * 0.6931471805599453f;
       }
       if (h == NH - 1) {
-        for (int key = k0 + tid; key < k1; key += blockDim.x) {
+        for (int key = k0 + tid; key < k1; key += kThreads) {
           if (key != k0 + tid) load_scores(key);
           float sum = 0.f;
 #pragma unroll
@@ -878,7 +854,6 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 32, 1) store_decode_kernel
           *weight_of(key) = gathered + sum;
         }
       }
-      cluster_sync();   // the other CTAs have read this one's result: it may be overwritten, or the CTA may leave
     }
   }
 }
@@ -962,9 +937,7 @@ DecodePlan store_plan(const Geom& g, int blocks, int max_splits = kDecMaxSplits)
 template <int D, int NH, int T>
 cudaError_t launch_store_decode_t(StoreDecodeArgs& a, const DecodePlan& pl, int BHkv, cudaStream_t st) {
   auto kern = store_decode_kernel<D, NH, T>;
-  // rings, or what the merge puts there: half of the warps' O and the CTA's
-  const int merge = (pl.warps / 2 * 8 * (D + 4) + 8 * D) * 4, rings = pl.warps * kRing * kStage;
-  const int smem = merge > rings ? merge : rings;
+  const int merge = pl.warps * 8 * (D + 4) * 4, rings = pl.warps * kRing * kStage, smem = merge > rings ? merge : rings;
   const cudaError_t es = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (es != cudaSuccess) return es;
   if (pl.splits > 8) {
@@ -975,9 +948,12 @@ cudaError_t launch_store_decode_t(StoreDecodeArgs& a, const DecodePlan& pl, int 
 }
 
 template <int T>
-cudaError_t launch_store_decode(const Geom& g, StoreDecodeArgs& a, const DecodePlan& pl, cudaStream_t st) {
+cudaError_t launch_store_decode(const Geom& g, StoreDecodeArgs& a, const DecodePlan& pl, int list_blocks, int recent_blocks, cudaStream_t st) {
   const int BHkv = g.B * g.Hkv;
   a.n_split = pl.splits; a.n_group = pl.groups;
+  const int n = pl.splits * pl.groups;
+  a.list_share = list_blocks / n; a.list_rest = list_blocks % n;
+  a.recent_share = recent_blocks / n; a.recent_rest = recent_blocks % n;
   if (g.d == 128) return pl.nh == 1 ? launch_store_decode_t<128, 1, T>(a, pl, BHkv, st) : launch_store_decode_t<128, 2, T>(a, pl, BHkv, st);
   return pl.nh == 1 ? launch_store_decode_t<64, 1, T>(a, pl, BHkv, st) : launch_store_decode_t<64, 2, T>(a, pl, BHkv, st);
 }
@@ -1162,18 +1138,17 @@ int lrsa_store_decode(const lrsa_params_t* params, const lrsa_store_t* store, co
   }
   a.scale_log2 = g.scale * 1.4426950408889634f;
   const int ur = 128 / g.d;   // 16-row groups per block
-  a.list_blocks = (a.n_groups + ur - 1) / ur;
-  a.recent_blocks = (a.n_recent + 16 * ur - 1) / (16 * ur);
-  DecodePlan pl = store_plan(g, a.list_blocks + a.recent_blocks);
+  const int list_blocks = (a.n_groups + ur - 1) / ur, recent_blocks = (a.n_recent + 16 * ur - 1) / (16 * ur);
+  DecodePlan pl = store_plan(g, list_blocks + recent_blocks);
   auto launch = [&](const DecodePlan& p) {
-    return o.type == LRSA_LIST_E4M3 ? launch_store_decode<LRSA_LIST_E4M3>(g, a, p, st)
-           : o.type == LRSA_LIST_INT8 ? launch_store_decode<LRSA_LIST_INT8>(g, a, p, st)
-                                      : launch_store_decode<LRSA_LIST_BF16>(g, a, p, st);
+    return o.type == LRSA_LIST_E4M3 ? launch_store_decode<LRSA_LIST_E4M3>(g, a, p, list_blocks, recent_blocks, st)
+           : o.type == LRSA_LIST_INT8 ? launch_store_decode<LRSA_LIST_INT8>(g, a, p, list_blocks, recent_blocks, st)
+                                      : launch_store_decode<LRSA_LIST_BF16>(g, a, p, list_blocks, recent_blocks, st);
   };
   cudaError_t e = launch(pl);
   if (e != cudaSuccess && pl.splits > 8) {   // clusters of 16 are not portable: a part of a GPU may not have room for them
     (void)cudaGetLastError();
-    pl = store_plan(g, a.list_blocks + a.recent_blocks, 8);
+    pl = store_plan(g, list_blocks + recent_blocks, 8);
     e = launch(pl);
   }
   LRSA_CUDA_CHECK(e);
