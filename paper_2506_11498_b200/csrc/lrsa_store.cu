@@ -10,6 +10,7 @@
 // A window leaves the ring when the first token of the chunk after the next one arrives, as in lrsa_infer.cu.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <limits.h>
 
 #include "infer_sm100.h"
 #include "weight_select.h"
@@ -54,7 +55,7 @@ int check_store(const lrsa_store_t* s, const StoreGeom& o) {
 }
 
 // ---- growing the store ----
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256;   // 512 where a block of the list takes as many
 
 struct StoreRows {
   const __nv_bfloat16 *k_new, *v_new;   // [BH][n_new][d], token p at row p - p_first
@@ -67,30 +68,36 @@ struct StoreRows {
   int* status;                          // cleared when not null
   int n_new, p_first, S, L, K, Kp, Wcap, rows_list, recent, block;
   int n_sink, p0, n_ins;                // new tokens [p_first, + n_sink) and [p0, + n_ins) go to the recent rows
-  int w0, n_win, from_ring;             // kept rows of windows [w0, + n_win), out of the ring or out of the new tokens
+  int w0, n_win, ring_below;            // kept rows of windows [w0, + n_win): positions below ring_below are in the ring
   int copy_blocks, list_blocks;         // thread blocks per (batch, KV head)
+  int lanes;                            // threads that share a block of the list: four 16-byte chunks each
 };
 
-// The least bf16 that is not below x (finite, positive); infinities and NaN stay.  With eight bits in the scale the quotient
-// of a bf16 value and the scale lies at least 2^-17 (relative) away from every rounding border of the codes that it does
-// not hit exactly, so a correctly rounded fp32 quotient gives the code of the exact one.
+// The least bf16 that is not below x (finite, positive); infinities and NaN stay.
 __device__ __forceinline__ float scale_up(float x) {
   return x < INFINITY ? __uint_as_float((__float_as_uint(x) + 0xffffu) & 0xffff0000u) : x;
+}
+// value / scale as exactly as its code needs.  Value and scale have eight significant bits, a border between two codes at most
+// eight: a quotient that is not on a border is at least 2^-16 (relative) away from it.  The product with the rounded
+// reciprocal is within 2^-22 of the quotient, and rounded to 19 bits it is on the border exactly when the quotient is, and on its side
+// otherwise.  (A division takes eight instructions more for every element.)
+__device__ __forceinline__ float quotient(float x, float inv) {
+  return __uint_as_float((__float_as_uint(x * inv) + 0x10u) & 0xffffffe0u);
 }
 
 // Tokens into the recent rows, and blocks of kept rows into the list.  Bound by the rows it moves: a copied row is read and
 // written once; a kept row is read once (gathered by position, whole lines), held in registers while the block's largest
 // magnitude is found, and written once in 8 bits.
 template <int D, int T>
-__global__ void __launch_bounds__(kRowThreads) store_rows_kernel(const __grid_constant__ StoreRows a) {
+__global__ void __launch_bounds__(512) store_rows_kernel(const __grid_constant__ StoreRows a) {
   constexpr int CPR = D / 8;                // 16-byte chunks per bf16 row
-  __shared__ uint32_t s_max[kRowThreads / 32];
+  __shared__ uint32_t s_max[16];
   const int tid = threadIdx.x, per = a.copy_blocks + a.list_blocks;
   const int bh = blockIdx.x / per, blk = blockIdx.x % per;
   wait_for_front();
   if (a.status && blockIdx.x == 0 && tid == 0) *a.status = 0;
   if (blk < a.copy_blocks) {
-    const int item = blk * (kRowThreads / CPR) + tid / CPR, ch = tid % CPR;
+    const int item = blk * (blockDim.x / CPR) + tid / CPR, ch = tid % CPR;
     if (item >= a.n_sink + a.n_ins) return;
     const int p = item < a.n_sink ? a.p_first + item : a.p0 + (item - a.n_sink);
     const int at = p < a.S ? p : a.S + (p - a.S) % (2 * a.L);
@@ -102,38 +109,35 @@ __global__ void __launch_bounds__(kRowThreads) store_rows_kernel(const __grid_co
       a.weight[(size_t)bh * 2 * a.L + (at - a.S)] = a.w_new ? a.w_new[(size_t)bh * a.n_new + (p - a.p_first)] : 0.f;
     return;
   }
-  // a block of K (even) or of V (odd)
-  const int lb = (blk - a.copy_blocks) >> 1, row0 = lb * a.block;   // first row, from window w0's first on
-  const bool is_v = (blk - a.copy_blocks) & 1;
-  const int w = a.w0 + row0 / a.Kp, j0 = row0 % a.Kp;
+  // several blocks of K (even) or of V (odd), each by a.lanes threads
+  const int in = tid & (a.lanes - 1), item = (blk - a.copy_blocks) * (blockDim.x / a.lanes) + tid / a.lanes;
+  const int per_win = a.Kp / a.block, lb = item >> 1;
+  const bool there = lb < a.n_win * per_win, is_v = item & 1;
+  const int win = there ? lb / per_win : 0, j0 = there ? (lb - win * per_win) * a.block : 0, w = a.w0 + win;
   const int32_t* idx = a.idx + ((size_t)bh * a.Wcap + w) * a.K;
-  const __nv_bfloat16* src = a.from_ring ? (is_v ? a.v_recent : a.k_recent) + (size_t)bh * a.recent * D
-                                         : (is_v ? a.v_new : a.k_new) + (size_t)bh * a.n_new * D;
-  constexpr int kMost = 128 * CPR / kRowThreads;   // chunks per thread of the largest block
-  uint4 x[kMost];
+  const __nv_bfloat16 *ring = (is_v ? a.v_recent : a.k_recent) + (size_t)bh * a.recent * D, *fresh = (is_v ? a.v_new : a.k_new) + (size_t)bh * a.n_new * D;
+  uint4 x[4];
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < kMost; ++i) {
-    const int c = i * kRowThreads + tid, r = c / CPR;
+  for (int i = 0; i < 4; ++i) {
+    const int c = i * a.lanes + in, r = c / CPR;
     x[i] = make_uint4(0, 0, 0, 0);
-    if (r < a.block && j0 + r < a.K) {
+    if (there && j0 + r < a.K) {
       const int pos = idx[j0 + r];
-      const int at = a.from_ring ? a.S + (pos - a.S) % (2 * a.L) : pos - a.p_first;
-      x[i] = *reinterpret_cast<const uint4*>(src + (size_t)at * D + (c % CPR) * 8);
+      const __nv_bfloat16* row = pos < a.ring_below ? ring + (size_t)(a.S + (pos - a.S) % (2 * a.L)) * D : fresh + (size_t)(pos - a.p_first) * D;
+      x[i] = *reinterpret_cast<const uint4*>(row + (c % CPR) * 8);
     }
   }
   const size_t out_row = (size_t)bh * a.rows_list + (size_t)w * a.Kp + j0;
   if constexpr (T == LRSA_LIST_BF16) {
     __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(is_v ? a.v_list : a.k_list) + out_row * D;
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-      const int c = i * kRowThreads + tid;
-      if (c / CPR < a.block) reinterpret_cast<uint4*>(dst)[c] = x[i];
-    }
+    for (int i = 0; i < 4; ++i)
+      if (there) reinterpret_cast<uint4*>(dst)[i * a.lanes + in] = x[i];
   } else {
     // largest magnitude: bits without the sign are ordered like the values, infinities and NaN above all
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
+    for (int i = 0; i < 4; ++i) {
       const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) most = max(most, max(u[e] & 0x7fffu, (u[e] >> 16) & 0x7fffu));
@@ -141,47 +145,53 @@ __global__ void __launch_bounds__(kRowThreads) store_rows_kernel(const __grid_co
     most = __reduce_max_sync(0xffffffffu, most);
     if ((tid & 31) == 0) s_max[tid >> 5] = most;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kRowThreads / 32; ++i) most = max(most, s_max[i]);
+    if (!there) return;
+    const int warp0 = tid / a.lanes * (a.lanes / 32);   // of the threads that share the block
+    for (int i = 0; i < a.lanes / 32; ++i) most = max(most, s_max[warp0 + i]);
     const float limit = T == LRSA_LIST_E4M3 ? 448.f : 127.f;
     const float scale = most ? fmaxf(scale_up(__fdiv_rn(__uint_as_float(most << 16), limit)), 1.17549435e-38f) : 1.f;
-    if (tid == 0) {
+    if (in == 0) {
       // NaN in a block must not become the floor's 2^-126 (fmaxf drops it): its rows then all stand for NaN, as they do for an infinity
       const bool nan = most > 0x7f80u;
       (is_v ? a.v_scale : a.k_scale)[out_row / a.block] = nan ? NAN : scale;
     }
     unsigned char* dst = static_cast<unsigned char*>(is_v ? a.v_list : a.k_list) + out_row * D;
     const bool finite = most < 0x7f80u;
+    const float inv = 1.f / scale;
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-      const int c = i * kRowThreads + tid;
-      if (c / CPR >= a.block) continue;
+    for (int i = 0; i < 4; ++i) {
+      const int c = i * a.lanes + in;
       const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
       uint32_t code[4];   // two codes each
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float lo = __fdiv_rn(__uint_as_float(u[e] << 16), scale), hi = __fdiv_rn(__uint_as_float(u[e] & 0xffff0000u), scale);
-        if constexpr (T == LRSA_LIST_E4M3)
+        const float lo = quotient(__uint_as_float(u[e] << 16), inv), hi = quotient(__uint_as_float(u[e] & 0xffff0000u), inv);
+        if constexpr (T == LRSA_LIST_E4M3) {
           code[e] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
-        else
-          code[e] = (__float2int_rn(lo) & 0xff) | (__float2int_rn(hi) & 0xff) << 8;
-        if (!finite) code[e] = 0;
+        } else {   // rounded to whole numbers in the low bits of the sum
+          code[e] = __byte_perm(__float_as_uint(lo + 12582912.f), __float_as_uint(hi + 12582912.f), 0x0040);
+        }
       }
-      reinterpret_cast<uint2*>(dst)[c] = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
+      const uint2 y = make_uint2(__byte_perm(code[0], code[1], 0x5410), __byte_perm(code[2], code[3], 0x5410));
+      reinterpret_cast<uint2*>(dst)[c] = finite ? y : make_uint2(0, 0);
     }
   }
 }
 
 int launch_store_rows(StoreRows a, const StoreGeom& o, int BH, int d, cudaStream_t st) {
-  const int rpb = kRowThreads / (d / 8);
+  a.lanes = o.block * (d / 8) / 4;   // 32 ... 512
+  // few blocks: one a thread block (a window of 512 out of the ring, 16 pairs: 4.7 us instead of 6.7)
+  const bool few = (long long)BH * a.n_win * (o.Kp / o.block) * 2 * a.lanes < 2LL * kSms * kRowThreads;
+  const int threads = a.lanes > kRowThreads ? a.lanes : !few ? kRowThreads : a.lanes > 64 ? a.lanes : 64;
+  const int rpb = threads / (d / 8), bpb = threads / a.lanes;
   a.copy_blocks = (a.n_sink + a.n_ins + rpb - 1) / rpb;
-  a.list_blocks = a.n_win * (o.Kp / o.block) * 2;
+  a.list_blocks = (a.n_win * (o.Kp / o.block) * 2 + bpb - 1) / bpb;
   const long long grid = (long long)BH * (a.copy_blocks + a.list_blocks);
   if (grid == 0) return LRSA_OK;
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   auto kern = d == 128 ? (o.type == LRSA_LIST_E4M3 ? store_rows_kernel<128, LRSA_LIST_E4M3> : o.type == LRSA_LIST_INT8 ? store_rows_kernel<128, LRSA_LIST_INT8> : store_rows_kernel<128, LRSA_LIST_BF16>)
                        : (o.type == LRSA_LIST_E4M3 ? store_rows_kernel<64, LRSA_LIST_E4M3> : o.type == LRSA_LIST_INT8 ? store_rows_kernel<64, LRSA_LIST_INT8> : store_rows_kernel<64, LRSA_LIST_BF16>);
-  LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)grid), dim3(kRowThreads), 0, st, 1, a));
+  LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)grid), dim3(threads), 0, st, 1, a));
   launch_counter().n++;
   return LRSA_OK;
 }
@@ -190,44 +200,52 @@ int launch_store_rows(StoreRows a, const StoreGeom& o, int BH, int d, cudaStream
 struct StoreReadArgs {
   const void *k_list, *v_list;
   const float *k_scale, *v_scale;
-  float *k, *v;          // [BH][n][d]
-  int n, K, Kp, rows_list, block;   // n = kept rows
+  float *k, *v;          // [BH][n_windows * K][d]
+  int n_windows, chunks, K, Kp, rows_list, shift;   // thread blocks per window; log2 of the block
 };
 
-// A thread takes 16 channels of a kept row (bound by the fp32 rows it writes).
+// A thread takes four channels of each of four rows, so that a warp writes whole lines: bound by the fp32 rows it writes.
 template <int D, int T>
-__global__ void __launch_bounds__(256) store_read_kernel(const StoreReadArgs a) {
-  constexpr int CPR = D / 16;
-  const int bh = blockIdx.y, r = blockIdx.x * (256 / CPR) + threadIdx.x / CPR, ch = threadIdx.x % CPR;
-  const bool is_v = blockIdx.z;
-  wait_for_front();
-  if (r >= a.n) return;
-  const size_t row = (size_t)bh * a.rows_list + (size_t)(r / a.K) * a.Kp + r % a.K;
-  float4* out = reinterpret_cast<float4*>((is_v ? a.v : a.k) + ((size_t)bh * a.n + r) * D + ch * 16);
+__global__ void __launch_bounds__(256) store_read_kernel(const __grid_constant__ StoreReadArgs a) {
+  constexpr int LPR = D / 4, RPS = 256 / LPR;   // lanes a row, rows a step
+  const int w = blockIdx.x / a.chunks, chunk = blockIdx.x - w * a.chunks, bh = blockIdx.y >> 1, ch = threadIdx.x % LPR * 4;
+  const bool is_v = blockIdx.y & 1;
+  const int j0 = chunk * (4 * RPS) + threadIdx.x / LPR;   // row of the window
+  const size_t row0 = (size_t)bh * a.rows_list + (size_t)w * a.Kp;
+  float* out = (is_v ? a.v : a.k) + (((size_t)bh * a.n_windows + w) * a.K) * D + ch;
   const void* list = is_v ? a.v_list : a.k_list;
-  float x[16];
-  if constexpr (T == LRSA_LIST_BF16) {
-    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(list) + row * D + ch * 16);
+  wait_for_front();
+  uint2 u[4];
+  float scale[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint4 u = src[h];
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { x[8 * h + 2 * e] = __uint_as_float(w[e] << 16); x[8 * h + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
-    }
-  } else {
-    const float scale = (is_v ? a.v_scale : a.k_scale)[row / a.block];
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(list) + row * D + ch * 16);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const uint32_t c = w[e / 4] >> (8 * (e % 4)) & 0xffu;
-      x[e] = scale * (T == LRSA_LIST_INT8 ? (float)(int8_t)c
-                                          : __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)c, __NV_E4M3))));
+  for (int i = 0; i < 4; ++i) {
+    const int j = min(j0 + i * RPS, a.K - 1);
+    if constexpr (T == LRSA_LIST_BF16) {
+      u[i] = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(list) + (row0 + j) * D + ch);
+      scale[i] = 1.f;
+    } else {
+      u[i] = make_uint2(*reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(list) + (row0 + j) * D + ch), 0);
+      scale[i] = (is_v ? a.v_scale : a.k_scale)[(row0 + j) >> a.shift];
     }
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) out[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+  for (int i = 0; i < 4; ++i) {
+    const int j = j0 + i * RPS;
+    if (j >= a.K) break;
+    float x[4];
+    if constexpr (T == LRSA_LIST_BF16) {
+      x[0] = __uint_as_float(u[i].x << 16); x[1] = __uint_as_float(u[i].x & 0xffff0000u);
+      x[2] = __uint_as_float(u[i].y << 16); x[3] = __uint_as_float(u[i].y & 0xffff0000u);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t c = u[i].x >> (8 * e) & 0xffu;
+        x[e] = scale[i] * (T == LRSA_LIST_INT8 ? (float)(int8_t)c
+                                               : __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)c, __NV_E4M3))));
+      }
+    }
+    *reinterpret_cast<float4*>(out + (size_t)j * D) = make_float4(x[0], x[1], x[2], x[3]);
+  }
 }
 
 // ---- decode attention ----
@@ -1033,23 +1051,12 @@ int lrsa_store_append(const lrsa_params_t* params, const lrsa_store_t* store, co
   // The status word is cleared by the first kernel of the call (a memset in front of a scoring kernel that cannot).
   int* status = &static_cast<WsHeader*>(workspace)->status;
   bool cleared = false;
-  // Selects windows [w0, + n): out of the ring (one window), or out of the new tokens.
-  auto select = [&](int w0, int n, bool ring) -> int {
-    const int tok0 = ring ? (w0 % 2) * g.L : g.S + w0 * g.L - n_prev;
-    if (o.by_weight) {
-      WeightSelectArgs a = {};
-      a.weight = ring ? store->weight : w_new;
-      a.row = ring ? 2 * g.L : n_new;
-      a.idx = store->idx; a.status = cleared ? nullptr : status; a.L = g.L; a.K = g.K; a.Wtot = o.Wcap; a.n = 1;
-      if ((long long)BH * n > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
-      a.item0[1] = BH * n; a.windows[0] = n; a.first[0] = tok0; a.woff[0] = w0; a.emit0[0] = g.S + w0 * g.L;
-      cleared = true;
-      return launch_weight_select(a, st);
-    }
+  // Lag rule: selects windows [w0, + n), out of the ring (one window) or out of the new tokens.
+  auto score = [&](int w0, int n, bool ring) -> int {
     Geom s = g;
     s.S = 0; s.T = 0; s.W = n + 1; s.C = n + 1; s.Wsel = n; s.Wtot = o.Wcap; s.woff = w0; s.emit_off = g.S + w0 * g.L;
     s.N = s.Nrow = ring ? o.recent : n_new;
-    s.tok0 = ring ? g.S + tok0 : tok0;
+    s.tok0 = ring ? g.S + (w0 % 2) * g.L : g.S + w0 * g.L - n_prev;
     s.win_stride = ring && w0 % 2 ? -g.L : g.L;
     const bool self = !cleared && score_select_clears_status(s);
     if (!cleared && !self) {
@@ -1068,28 +1075,45 @@ int lrsa_store_append(const lrsa_params_t* params, const lrsa_store_t* store, co
   int pos = n_prev;                                     // tokens before it are in the store
   int c = pos > g.S ? (pos - g.S + g.L - 1) / g.L : 0;  // next chunk whose first token has not arrived yet
   if (c < 2) c = 2;
-  // Chunk start after chunk start while the window c-2 that leaves the ring holds tokens of earlier calls (at most two): the
-  // tokens up to it enter the ring, the window is cut, its kept rows join the list before its half is overwritten.
-  for (; (long long)g.S + (long long)c * g.L < end && g.S + (c - 2) * g.L < n_prev; ++c) {
+  // Lag rule: chunk start after chunk start while the window c-2 that leaves the ring holds tokens of earlier calls (at most two).
+  // The tokens up to it enter the ring, the window is scored with its successor there, its kept rows join the list before its
+  // half is overwritten.
+  for (; !o.by_weight && (long long)g.S + (long long)c * g.L < end && g.S + (c - 2) * g.L < n_prev; ++c) {
     const int w = c - 2;
     rows.p0 = pos; rows.n_ins = g.S + c * g.L - pos; rows.n_win = 0;
     if ((rc = move_rows()) != LRSA_OK) return rc;
-    if ((rc = select(w, 1, true)) != LRSA_OK) return rc;
-    rows.n_ins = 0; rows.w0 = w; rows.n_win = 1; rows.from_ring = 1;
+    if ((rc = score(w, 1, true)) != LRSA_OK) return rc;
+    rows.n_ins = 0; rows.w0 = w; rows.n_win = 1; rows.ring_below = INT_MAX;
     if ((rc = move_rows()) != LRSA_OK) return rc;
     pos = g.S + c * g.L;
   }
   rows.n_win = 0;
   rows.p0 = pos; rows.n_ins = end - pos;
   if ((long long)g.S + (long long)c * g.L < end) {
-    // Windows c-2 .. c_last-2 lie in the new tokens as a whole: one selection for all of them, then one launch for their
-    // kept rows, the sinks and the tokens that stay in the ring.
+    // Windows c-2 .. c_last-2, one selection for all of them, then their kept rows, the sinks and the tokens that stay in the ring.
+    // By the lag rule they lie in the new tokens as a whole, by weight the first ones may be in the ring.
     const int w0 = c - 2, nw = (end - 1 - g.S) / g.L - c + 1;
-    if ((rc = select(w0, nw, false)) != LRSA_OK) return rc;
+    if (o.by_weight) {
+      WeightSelectArgs a = {};
+      a.weight = w_new; a.row = n_new; a.ring = store->weight; a.ring_below = n_prev; a.ring_first = g.S; a.ring_len = 2 * g.L;
+      a.idx = store->idx; a.status = status; a.L = g.L; a.K = g.K; a.Wtot = o.Wcap; a.n = 1;
+      if ((long long)BH * nw > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
+      a.item0[1] = BH * nw; a.windows[0] = nw; a.first[0] = g.S + w0 * g.L - n_prev; a.woff[0] = w0; a.emit0[0] = g.S + w0 * g.L;
+      cleared = true;
+      rc = launch_weight_select(a, st);
+    } else {
+      rc = score(w0, nw, false);
+    }
+    if (rc != LRSA_OK) return rc;
+    rows.w0 = w0; rows.n_win = nw; rows.ring_below = n_prev;
+    if (g.S + w0 * g.L < n_prev) {   // rows of the ring have to be read before tokens take their places
+      rows.n_ins = 0;
+      if ((rc = move_rows()) != LRSA_OK) return rc;
+      rows.n_win = 0;
+    }
     rows.n_sink = pos < g.S ? g.S - pos : 0;
     rows.p0 = end - 2 * g.L > pos ? end - 2 * g.L : pos;
     rows.n_ins = end - rows.p0;
-    rows.w0 = w0; rows.n_win = nw; rows.from_ring = 0;
   }
   return move_rows();
 }
@@ -1176,14 +1200,16 @@ int lrsa_store_rows(const lrsa_params_t* params, const lrsa_store_t* store, int3
   if (!k || !v || mis(k, 16) || mis(v, 16)) return LRSA_ERR_INVALID_ARG;
   rc = check_store(store, o);
   if (rc != LRSA_OK) return rc;
-  if ((long long)g.B * g.Hkv > 65535) return LRSA_ERR_UNSUPPORTED;   // grid rows
+  if ((long long)g.B * g.Hkv > 32767) return LRSA_ERR_UNSUPPORTED;   // grid rows
   StoreReadArgs a = {};
   a.k_list = store->k_list; a.v_list = store->v_list; a.k_scale = store->k_scale; a.v_scale = store->v_scale; a.k = k; a.v = v;
-  a.n = n_windows * g.K; a.K = g.K; a.Kp = o.Kp; a.rows_list = o.rows_list; a.block = o.block;
+  const int rows = 4 * 256 / (g.d / 4);   // of a thread block
+  a.n_windows = n_windows; a.chunks = (g.K + rows - 1) / rows; a.K = g.K; a.Kp = o.Kp; a.rows_list = o.rows_list;
+  while ((1 << a.shift) < o.block) ++a.shift;
+  if ((long long)n_windows * a.chunks > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   auto kern = g.d == 128 ? (o.type == LRSA_LIST_E4M3 ? store_read_kernel<128, LRSA_LIST_E4M3> : o.type == LRSA_LIST_INT8 ? store_read_kernel<128, LRSA_LIST_INT8> : store_read_kernel<128, LRSA_LIST_BF16>)
                          : (o.type == LRSA_LIST_E4M3 ? store_read_kernel<64, LRSA_LIST_E4M3> : o.type == LRSA_LIST_INT8 ? store_read_kernel<64, LRSA_LIST_INT8> : store_read_kernel<64, LRSA_LIST_BF16>);
-  const int rpb = 256 / (g.d / 16);
-  LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)((a.n + rpb - 1) / rpb), g.B * g.Hkv, 2), dim3(256), 0,
+  LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)n_windows * a.chunks, g.B * g.Hkv * 2), dim3(256), 0,
                                    static_cast<cudaStream_t>(cuda_stream), 1, a));
   launch_counter().n++;
   return LRSA_OK;

@@ -33,9 +33,11 @@ __global__ void __launch_bounds__(kThreads) weight_select_kernel(const __grid_co
   if (a.status && blockIdx.x == 0 && tid == 0) *a.status = 0;
   const float* src = a.weight + (size_t)bh * a.row + a.first[sq] + (long long)w * L;
   uint32_t kmin = 0xffffffffu, kmax = 0u;
+  const int pos0 = a.emit0[sq] + w * L;
 #pragma unroll 8
   for (int i = tid; i < L; i += kThreads) {
-    float x = src[i] + 0.f;                // -0 and 0 are the same weight
+    const float* at = a.ring && pos0 + i < a.ring_below ? a.ring + (size_t)bh * a.ring_len + (pos0 + i - a.ring_first) % a.ring_len : src + i;
+    float x = *at + 0.f;                   // -0 and 0 are the same weight
     if (x != x) x = -INFINITY;             // NaN is kept last
     const uint32_t k = order_key(x);
     key[i] = k;
@@ -117,7 +119,6 @@ __global__ void __launch_bounds__(kThreads) weight_select_kernel(const __grid_co
     if (j < warp) before += above_eq[j];
   int gt = before & 0xffff, eq = before >> 16;
   int32_t* out = a.idx + ((size_t)bh * a.Wtot + a.woff[sq] + w) * a.K;
-  const int pos0 = a.emit0[sq] + w * L;
   const uint32_t lower = (1u << lane) - 1u;
   for (int i = i0; i < i1; i += 32) {
     const bool in = i + lane < i1;

@@ -8,6 +8,8 @@ namespace lrsa {
 constexpr int kSelectSeqs = 16;   // sequences of a launch
 struct WeightSelectArgs {
   const float* weight;   // [B*Hkv][row]
+  const float* ring;     // when not null, positions below ring_below are here: [B*Hkv][ring_len], position p at (p - ring_first) % ring_len
+  int ring_below, ring_first, ring_len;
   int32_t* idx;          // [B*Hkv][Wtot][K]
   int* status;           // cleared when not null
   long long row;
