@@ -90,18 +90,6 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort = &ctl.abort;
 
-  if (tid == 0) {
-    ctl.abort = (smem0 & 1023u) ? 1 : 0;   // the swizzled tiles need the alignment
-    mbar_init(k_full, 1);
-    for (int i = 0; i < NQ; ++i) { mbar_init(q_full + 8 * i, 1); mbar_init(q_empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(s_full + 8 * i, 2);   // the product and the statistics
-      mbar_init(s_empty + 8 * i, 32 * Cfg::kSoftWarps);
-    }
-    fence_barrier_init();
-  }
-  if (warp == 1) { tmem_alloc(smem_u32(&ctl.tmem_base), Cfg::kCols); tmem_relinquish(); }
-
   // ---- which tile, which part of its pairs ----
   const int rank = blockIdx.x % a.split;
   int item = blockIdx.x / a.split, sq = 0;
@@ -117,11 +105,36 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
   const int cc = first_compressed_chunk(w, p.ndp, p.Wsel, p.C);
   const int qend = cc >= p.C ? p.N : min(p.N, p.S + cc * p.L);
   const int nq = qend > row0 ? (qend - row0 + kTile - 1) / kTile : 0;
-  const int it0 = (int)((long long)a.G * nq * rank / a.split), n = (int)((long long)a.G * nq * (rank + 1) / a.split) - it0;
+  const int all = a.G * nq, per = all / a.split, rest = all - per * a.split;
+  const int it0 = per * rank + min(rank, rest), n = per + (rank < rest);
   const int hq0 = (bh / a.Hkv) * a.Hq + (bh % a.Hkv) * a.G;
   // pair i: query tile nq-1 - i/G (from the last query backwards) of head i % G of the group
   const int qt0 = nq - 1 - it0 / a.G, hd0 = it0 % a.G;
-  if (tid == 0) { prefetch_tensormap(&maps.q[sq]); prefetch_tensormap(&maps.k[sq]); }
+  auto load_q = [&](int slot, int qt, int hd) {
+    mbar_expect_tx(q_full + 8 * slot, Cfg::kTileBytes);
+    for (int h = 0; h < Cfg::kSub; ++h)
+      tma_load_3d(sQ + slot * Cfg::kTileBytes + h * Cfg::kSubBytes, &maps.q[sq], h * 64, row0 + qt * kTile, hq0 + hd, q_full + 8 * slot);
+  };
+  if (tid == 0) {
+    prefetch_tensormap(&maps.q[sq]); prefetch_tensormap(&maps.k[sq]);
+    ctl.abort = (smem0 & 1023u) ? 1 : 0;   // the swizzled tiles need the alignment
+    mbar_init(k_full, 1);
+    for (int i = 0; i < NQ; ++i) { mbar_init(q_full + 8 * i, 1); mbar_init(q_empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + 8 * i, 2);   // the product and the statistics
+      mbar_init(s_empty + 8 * i, 32 * Cfg::kSoftWarps);
+    }
+    fence_barrier_init();
+    // K_j and the first Q are on their way while the other warps get their tensor memory
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (n > 0 && !ctl.abort) {
+      mbar_expect_tx(k_full, Cfg::kTileBytes);
+      for (int h = 0; h < Cfg::kSub; ++h) tma_load_3d(sK + h * Cfg::kSubBytes, &maps.k[sq], h * 64, row0, bh, k_full);
+      load_q(0, qt0, hd0);
+    }
+  }
+  if (warp == 1) { tmem_alloc(smem_u32(&ctl.tmem_base), Cfg::kCols); tmem_relinquish(); }
+
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -134,18 +147,14 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
   } else if (warp == 0) {
     // ---------------- TMA producer ----------------
     if (lane == 0 && n > 0) {
-      mbar_expect_tx(k_full, Cfg::kTileBytes);
-      for (int h = 0; h < Cfg::kSub; ++h) tma_load_3d(sK + h * Cfg::kSubBytes, &maps.k[sq], h * 64, row0, bh, k_full);
-      int qt = qt0, hd = hd0, sl = 0, ph = 0, issued = 0;
+      int qt = qt0, hd = hd0, sl = 1, ph = 0, issued = 1;   // (the first step's loads are on their way)
       bool ok = true;
-      for (int it = 0; it < n; ++it) {
+      for (int it = 1; it < n; ++it) {
+        if (++hd == a.G) { hd = 0; --qt; }
         if (it >= NQ) ok = mbar_wait(q_empty + 8 * sl, ph ^ 1, abort);
         if (!ok) break;
-        mbar_expect_tx(q_full + 8 * sl, Cfg::kTileBytes);
-        for (int h = 0; h < Cfg::kSub; ++h)
-          tma_load_3d(sQ + sl * Cfg::kTileBytes + h * Cfg::kSubBytes, &maps.q[sq], h * 64, row0 + qt * kTile, hq0 + hd, q_full + 8 * sl);
+        load_q(sl, qt, hd);
         ++issued;
-        if (++hd == a.G) { hd = 0; --qt; }
         if (++sl == NQ) { sl = 0; ph ^= 1; }
       }
       if (!ok) {   // give the loads in flight a bounded chance to land before shared memory is released
@@ -292,13 +301,16 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
   if (tid == 0 && ctl.abort) atomicExch(a.status, (int)LRSA_ERR_TIMEOUT);
 }
 
-// CTAs that share a key tile.  Two CTAs run on an SM; a CTA's start and end cost about four pairs.
+// CTAs that share a key tile, by the time in steps (two CTAs on an SM; start and end of a CTA cost about five): the work spread over
+// the slots, and half of the last CTA.  us at 1 | 2 | 4 | 8: 8/8 heads, d = 64, 4K tokens 14 | 17 | 26 | 46; 28/4, d = 128: 1777 (windows of 512)
+// 48 | 31 | 26 | 27, 4K 52 | 48 | 48 | 55, 8K (1024) 169 | 137 | 133 | 154, 16K 274 | 248 | 255 | 304, 32K 522 | 512 | 543 | 603; 16/2, d = 64, two
+// sequences of 11K (windows of 333) 52 | 50 | 61 | 93; 32/8, 20K (512) 191 | 193 | 237 | 359.
 int weights_split(long long items, long long pairs) {
+  const double n = (double)pairs / items, slots = 2 * kSms;
   int best = 1;
   double least = -1;
   for (int c = 1; c <= 8; c *= 2) {
-    const long long waves = (items * c + 2 * kSms - 1) / (2 * kSms);
-    const double cost = waves * ((double)pairs / (items * c) + 4);
+    const double cost = items * (n + 5.0 * c) / slots + 0.5 * (n / c + 5.0);
     if (least < 0 || cost < least) { least = cost; best = c; }
   }
   return best;
@@ -322,7 +334,8 @@ int launch_weights_t(const Geom& whole, const SeqBatch& b, const __nv_bfloat16* 
     a.tok0[s] = g.tok0;
     a.item0[s] = (int)items;
     items += BHkv * a.plan[s].n_tiles;
-    pairs += BHkv * a.plan[s].n_tiles * (long long)(((g.L + g.L * (g.ndp ? 1 : 0)) / kTile + 1) * g.G);
+    const long long L = g.N - g.S < g.L ? g.N - g.S : g.L;   // a tile is seen by half a window's queries, and by the next window's
+    pairs += BHkv * a.plan[s].n_tiles * (((g.ndp ? 3 : 1) * L / (2 * kTile) + 1) * g.G);
     if (items > 0x7fffffffLL / 8) return LRSA_ERR_UNSUPPORTED;
     a.item0[s + 1] = (int)items;
   }
