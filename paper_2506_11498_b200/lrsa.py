@@ -187,6 +187,7 @@ def _check(status: int, where: str):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # (a tensor on a GPU is in hand)
 
 
 def _p(t):
@@ -285,7 +286,7 @@ def lrsa_attn_bwd(params: Params, Q, K, V, O, dO, LSE, idx, dQ=None, dK=None, dV
 def _device(where, name, t) -> int:
     """The index of the current device, on which `t` has to be."""
     dev = t.get_device()      # -1: not a GPU's
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _current_device():
         raise LrsaError(1, f"{where}: {name} must be on the current device, got {t.device}")
     return dev
 
@@ -464,6 +465,7 @@ class KVStore:
         self.idx = zeros(wcap.value, p.top_k, dtype=torch.int32)
         self.ws = new_workspace(ws.value, device)
         self._lse = torch.empty((p.batch, p.n_q_heads), dtype=torch.float32, device=device)   # what an lse looks like
+        self._q_shape = torch.Size((p.batch, p.n_q_heads, p.head_dim))
 
     def _parts(self):
         """The store as the calls of csrc/pycall.c take it: type, block, rule, addresses."""
@@ -494,19 +496,18 @@ class KVStore:
     def decode(self, q, o=None, lse=None, stream=None):
         """q: bf16 [B, Hq, d], the query of the last token in the store.  Returns (o, lse); with keep="weight" the weights of
         the ring's tokens grow by those of the query."""
-        p, where, call, like = self.params, "lrsa_store_decode", _calls(), self._lse
-        shape = (p.batch, p.n_q_heads, p.head_dim)
+        where, call, like = "lrsa_store_decode", _call or _calls(), self._lse
         dev = _device(where, "q", q)
-        _expect(where, "q", q, shape, torch.bfloat16, dev)
+        _expect(where, "q", q, self._q_shape, torch.bfloat16, dev)
         if o is None:
             o = torch.empty_like(q)
         else:
-            _expect(where, "o", o, shape, torch.bfloat16, dev)
+            _expect(where, "o", o, self._q_shape, torch.bfloat16, dev)
         if lse is None:
             lse = torch.empty_like(like)
         else:
             _expect(where, "lse", lse, like.shape, torch.float32, dev)
-        cp, ws = p.struct(), self.ws
+        cp, ws = self.params.struct(), self.ws
         status = call.store_decode(ctypes.addressof(cp), *self._parts(), q.data_ptr(), self.n_tokens, o.data_ptr(),
                                    lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
         if status:
