@@ -34,16 +34,23 @@ __global__ void __launch_bounds__(kThreads) weight_select_kernel(const __grid_co
   const float* src = a.weight + (size_t)bh * a.row + a.first[sq] + (long long)w * L;
   uint32_t kmin = 0xffffffffu, kmax = 0u;
   const int pos0 = a.emit0[sq] + w * L;
-#pragma unroll 8
-  for (int i = tid; i < L; i += kThreads) {
-    const float* at = a.ring && pos0 + i < a.ring_below ? a.ring + (size_t)bh * a.ring_len + (pos0 + i - a.ring_first) % a.ring_len : src + i;
-    float x = *at + 0.f;                   // -0 and 0 are the same weight
+  auto take = [&](float x, int i) {
+    x += 0.f;                              // -0 and 0 are the same weight
     if (x != x) x = -INFINITY;             // NaN is kept last
     const uint32_t k = order_key(x);
     key[i] = k;
     kmin = min(kmin, k);
     kmax = max(kmax, k);
+  };
+  // tokens [0, in_ring) of the window are in the ring, wherever it wraps
+  const int in_ring = a.ring ? min(L, max(a.ring_below - pos0, 0)) : 0;
+  if (in_ring > 0) {
+    const float* ring = a.ring + (size_t)bh * a.ring_len;
+    const int at = (pos0 - a.ring_first) % a.ring_len;
+    for (int i = tid; i < in_ring; i += kThreads) take(ring[at + i < a.ring_len ? at + i : at + i - a.ring_len], i);
   }
+#pragma unroll 8
+  for (int i = in_ring + tid; i < L; i += kThreads) take(src[i], i);
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   kmax = __reduce_max_sync(0xffffffffu, kmax);
   if (lane == 0) { kred[0][warp] = kmin; kred[1][warp] = kmax; }
