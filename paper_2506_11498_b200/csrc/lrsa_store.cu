@@ -12,6 +12,8 @@
 #include <cuda_fp8.h>
 #include <limits.h>
 
+#include <type_traits>
+
 #include "infer_sm100.h"
 #include "weight_select.h"
 
@@ -55,7 +57,7 @@ int check_store(const lrsa_store_t* s, const StoreGeom& o) {
 }
 
 // ---- growing the store ----
-constexpr int kRowThreads = 256;   // 512 where a block of the list takes as many
+constexpr int kRowThreads = kSelThreads;
 
 struct StoreRows {
   const __nv_bfloat16 *k_new, *v_new;   // [BH][n_new][d], token p at row p - p_first
@@ -64,13 +66,14 @@ struct StoreRows {
   float* weight;                        // null: not kept
   void *k_list, *v_list;
   float *k_scale, *v_scale;
-  const int32_t* idx;                   // [BH][Wcap][K]
+  int32_t* idx;                         // [BH][Wcap][K]
   int* status;                          // cleared when not null
   int n_new, p_first, S, L, K, Kp, Wcap, rows_list, recent, block;
   int n_sink, p0, n_ins;                // new tokens [p_first, + n_sink) and [p0, + n_ins) go to the recent rows
   int w0, n_win, ring_below;            // kept rows of windows [w0, + n_win): positions below ring_below are in the ring
-  int copy_blocks, list_blocks;         // thread blocks per (batch, KV head)
-  int lanes;                            // threads that share a block of the list: four 16-byte chunks each
+  int BH, copy_blocks, list_blocks;     // thread blocks per (batch, KV head); store_cut_kernel: clusters that cut
+  int lanes;                            // threads that share a block of the list: M 16-byte chunks each
+  int split;                            // CTAs that share a window (store_cut_kernel)
 };
 
 // The least bf16 that is not below x (finite, positive); infinities and NaN stay.
@@ -85,45 +88,39 @@ __device__ __forceinline__ float quotient(float x, float inv) {
   return __uint_as_float((__float_as_uint(x * inv) + 0x10u) & 0xffffffe0u);
 }
 
-// Tokens into the recent rows, and blocks of kept rows into the list.  Bound by the rows it moves: a copied row is read and
-// written once; a kept row is read once (gathered by position, whole lines), held in registers while the block's largest
-// magnitude is found, and written once in 8 bits.
-template <int D, int T>
-__global__ void __launch_bounds__(512) store_rows_kernel(const __grid_constant__ StoreRows a) {
+// Token `item` of the copied ones into the recent rows: this thread's 16 bytes of K and of V, and its weight.
+template <int D>
+__device__ __forceinline__ void move_token(const StoreRows& a, int bh, int item, int ch) {
   constexpr int CPR = D / 8;                // 16-byte chunks per bf16 row
-  __shared__ uint32_t s_max[16];
-  const int tid = threadIdx.x, per = a.copy_blocks + a.list_blocks;
-  const int bh = blockIdx.x / per, blk = blockIdx.x % per;
-  wait_for_front();
-  if (a.status && blockIdx.x == 0 && tid == 0) *a.status = 0;
-  if (blk < a.copy_blocks) {
-    const int item = blk * (blockDim.x / CPR) + tid / CPR, ch = tid % CPR;
-    if (item >= a.n_sink + a.n_ins) return;
-    const int p = item < a.n_sink ? a.p_first + item : a.p0 + (item - a.n_sink);
-    const int at = p < a.S ? p : a.S + (p - a.S) % (2 * a.L);
-    const size_t src = ((size_t)bh * a.n_new + (p - a.p_first)) * CPR + ch, dst = ((size_t)bh * a.recent + at) * CPR + ch;
-    const uint4 k = reinterpret_cast<const uint4*>(a.k_new)[src], v = reinterpret_cast<const uint4*>(a.v_new)[src];
-    reinterpret_cast<uint4*>(a.k_recent)[dst] = k;
-    reinterpret_cast<uint4*>(a.v_recent)[dst] = v;
-    if (a.weight && ch == 0 && p >= a.S)
-      a.weight[(size_t)bh * 2 * a.L + (at - a.S)] = a.w_new ? a.w_new[(size_t)bh * a.n_new + (p - a.p_first)] : 0.f;
-    return;
-  }
-  // several blocks of K (even) or of V (odd), each by a.lanes threads
-  const int in = tid & (a.lanes - 1), item = (blk - a.copy_blocks) * (blockDim.x / a.lanes) + tid / a.lanes;
-  const int per_win = a.Kp / a.block, lb = item >> 1;
-  const bool there = lb < a.n_win * per_win, is_v = item & 1;
-  const int win = there ? lb / per_win : 0, j0 = there ? (lb - win * per_win) * a.block : 0, w = a.w0 + win;
+  if (item >= a.n_sink + a.n_ins) return;
+  const int p = item < a.n_sink ? a.p_first + item : a.p0 + (item - a.n_sink);
+  const int at = p < a.S ? p : a.S + (p - a.S) % (2 * a.L);
+  const size_t src = ((size_t)bh * a.n_new + (p - a.p_first)) * CPR + ch, dst = ((size_t)bh * a.recent + at) * CPR + ch;
+  const uint4 k = reinterpret_cast<const uint4*>(a.k_new)[src], v = reinterpret_cast<const uint4*>(a.v_new)[src];
+  reinterpret_cast<uint4*>(a.k_recent)[dst] = k;
+  reinterpret_cast<uint4*>(a.v_recent)[dst] = v;
+  if (a.weight && ch == 0 && p >= a.S)
+    a.weight[(size_t)bh * 2 * a.L + (at - a.S)] = a.w_new ? a.w_new[(size_t)bh * a.n_new + (p - a.p_first)] : 0.f;
+}
+
+// Blocks of kept rows of K (even items) or of V (odd) of window w into the list, each by a.lanes threads: block item / 2 of the
+// window.  A row is read once (gathered by position, whole lines), held in registers while the block's largest magnitude
+// is found, and written once.  s_max: a word for every warp.  All threads come here; there: this one has a block.
+template <int D, int T, int M>
+__device__ __forceinline__ void cut_block(const StoreRows& a, int bh, int w, int item, bool there, uint32_t* s_max) {
+  constexpr int CPR = D / 8;
+  const int tid = threadIdx.x, in = tid & (a.lanes - 1), j0 = there ? (item >> 1) * a.block : 0;
+  const bool is_v = item & 1;
   const int32_t* idx = a.idx + ((size_t)bh * a.Wcap + w) * a.K;
   const __nv_bfloat16 *ring = (is_v ? a.v_recent : a.k_recent) + (size_t)bh * a.recent * D, *fresh = (is_v ? a.v_new : a.k_new) + (size_t)bh * a.n_new * D;
-  uint4 x[4];
+  uint4 x[M];
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < M; ++i) {
     const int c = i * a.lanes + in, r = c / CPR;
     x[i] = make_uint4(0, 0, 0, 0);
     if (there && j0 + r < a.K) {
-      const int pos = idx[j0 + r];
+      const int pos = __ldcg(idx + j0 + r);   // (may be another CTA's of this kernel)
       const __nv_bfloat16* row = pos < a.ring_below ? ring + (size_t)(a.S + (pos - a.S) % (2 * a.L)) * D : fresh + (size_t)(pos - a.p_first) * D;
       x[i] = *reinterpret_cast<const uint4*>(row + (c % CPR) * 8);
     }
@@ -132,12 +129,12 @@ __global__ void __launch_bounds__(512) store_rows_kernel(const __grid_constant__
   if constexpr (T == LRSA_LIST_BF16) {
     __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(is_v ? a.v_list : a.k_list) + out_row * D;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < M; ++i)
       if (there) reinterpret_cast<uint4*>(dst)[i * a.lanes + in] = x[i];
   } else {
     // largest magnitude: bits without the sign are ordered like the values, infinities and NaN above all
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < M; ++i) {
       const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) most = max(most, max(u[e] & 0x7fffu, (u[e] >> 16) & 0x7fffu));
@@ -159,7 +156,7 @@ __global__ void __launch_bounds__(512) store_rows_kernel(const __grid_constant__
     const bool finite = most < 0x7f80u;
     const float inv = 1.f / scale;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < M; ++i) {
       const int c = i * a.lanes + in;
       const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
       uint32_t code[4];   // two codes each
@@ -178,22 +175,107 @@ __global__ void __launch_bounds__(512) store_rows_kernel(const __grid_constant__
   }
 }
 
-int launch_store_rows(StoreRows a, const StoreGeom& o, int BH, int d, cudaStream_t st) {
-  a.lanes = o.block * (d / 8) / 4;   // 32 ... 512
-  // few blocks: one a thread block (a window of 512 out of the ring, 16 pairs: 4.7 us instead of 6.7)
-  const bool few = (long long)BH * a.n_win * (o.Kp / o.block) * 2 * a.lanes < 2LL * kSms * kRowThreads;
-  const int threads = a.lanes > kRowThreads ? a.lanes : !few ? kRowThreads : a.lanes > 64 ? a.lanes : 64;
-  const int rpb = threads / (d / 8), bpb = threads / a.lanes;
-  a.copy_blocks = (a.n_sink + a.n_ins + rpb - 1) / rpb;
-  a.list_blocks = (a.n_win * (o.Kp / o.block) * 2 + bpb - 1) / bpb;
-  const long long grid = (long long)BH * (a.copy_blocks + a.list_blocks);
-  if (grid == 0) return LRSA_OK;
-  if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
-  auto kern = d == 128 ? (o.type == LRSA_LIST_E4M3 ? store_rows_kernel<128, LRSA_LIST_E4M3> : o.type == LRSA_LIST_INT8 ? store_rows_kernel<128, LRSA_LIST_INT8> : store_rows_kernel<128, LRSA_LIST_BF16>)
-                       : (o.type == LRSA_LIST_E4M3 ? store_rows_kernel<64, LRSA_LIST_E4M3> : o.type == LRSA_LIST_INT8 ? store_rows_kernel<64, LRSA_LIST_INT8> : store_rows_kernel<64, LRSA_LIST_BF16>);
-  LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)grid), dim3(threads), 0, st, 1, a));
+// Tokens into the recent rows, and kept rows into the list.  Bound by the rows it moves.
+template <int D, int T, int M>
+__global__ void __launch_bounds__(kRowThreads) store_rows_kernel(const __grid_constant__ StoreRows a) {
+  constexpr int CPR = D / 8;
+  __shared__ uint32_t s_max[kRowThreads / 32];
+  const int tid = threadIdx.x, per = a.copy_blocks + a.list_blocks;
+  const int bh = blockIdx.x / per, blk = blockIdx.x % per;
+  wait_for_front();
+  if (a.status && blockIdx.x == 0 && tid == 0) *a.status = 0;
+  if (blk < a.copy_blocks) {
+    move_token<D>(a, bh, blk * (blockDim.x / CPR) + tid / CPR, tid % CPR);
+    return;
+  }
+  const int item = (blk - a.copy_blocks) * (blockDim.x / a.lanes) + tid / a.lanes, per_win = a.Kp / a.block * 2;
+  const bool there = item < a.n_win * per_win;
+  const int win = there ? item / per_win : 0;
+  cut_block<D, T, M>(a, bh, a.w0 + win, item - win * per_win, there, s_max);
+}
+
+// By weight: selects windows [w0, + n_win) and moves their kept rows, a cluster of a.split CTAs a window (one selects, all move),
+// beside the tokens that enter the recent rows.  (As two kernels, one behind the other, a 32K
+// prompt and its read-back take 26.3 us instead of 23.9, a 9K prompt in five pieces 76 instead of 65.)
+template <int D, int T, int M>
+__global__ void __launch_bounds__(kRowThreads) store_cut_kernel(const __grid_constant__ StoreRows a) {
+  constexpr int CPR = D / 8;
+  extern __shared__ __align__(16) uint32_t cut_key[];
+  __shared__ SelectShared sh;
+  __shared__ uint32_t s_max[kRowThreads / 32];
+  const int tid = threadIdx.x, cluster = blockIdx.x / a.split, rank = blockIdx.x - cluster * a.split;
+  const int n_cut = a.list_blocks;                       // clusters that cut: one for each window of each (batch, KV head)
+  if (cluster < n_cut && rank == 0) select_clear(sh);
+  wait_for_front();
+  if (a.status && blockIdx.x == 0 && tid == 0) *a.status = 0;
+  if (cluster >= n_cut) {
+    const int blk = blockIdx.x - n_cut * a.split, bh = blk / a.copy_blocks;
+    if (bh < a.BH) move_token<D>(a, bh, (blk - bh * a.copy_blocks) * (kRowThreads / CPR) + tid / CPR, tid % CPR);
+    return;
+  }
+  const int bh = cluster / a.n_win, w = a.w0 + cluster - bh * a.n_win;
+  if (rank == 0) {
+    const int pos0 = a.S + w * a.L, in_ring = min(a.L, max(a.ring_below - pos0, 0));
+    select_window_by_weight(sh, cut_key, a.L, a.K, a.w_new + (size_t)bh * a.n_new + (pos0 - a.p_first), a.weight + ((size_t)bh * 2 + w % 2) * a.L,
+                            in_ring, a.idx + ((size_t)bh * a.Wcap + w) * a.K, pos0);
+  }
+  cluster_sync();   // the positions are in global memory for the CTAs of the cluster
+  const int at_once = kRowThreads / a.lanes, per_win = a.Kp / a.block * 2;
+  for (int i = rank * at_once; i < per_win; i += a.split * at_once) {
+    const int item = i + tid / a.lanes;
+    cut_block<D, T, M>(a, bh, w, item, item < per_win, s_max);
+    __syncthreads();   // the words of the warps are written again
+  }
+}
+
+template <int D, int T, int M>
+int launch_rows_t(const StoreRows& a, int threads, long long grid, size_t smem, cudaStream_t st, bool cut) {
+  auto rows = store_rows_kernel<D, T, M>;
+  auto cuts = store_cut_kernel<D, T, M>;
+  if (cut && smem > 38 * 1024) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cuts, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  LRSA_CUDA_CHECK(cut ? launch_dependent(cuts, dim3((unsigned)grid), dim3(threads), smem, st, a.split, a)
+                      : launch_dependent(rows, dim3((unsigned)grid), dim3(threads), 0, st, 1, a));
   launch_counter().n++;
   return LRSA_OK;
+}
+
+// `cut`: the windows are selected, by weight, in the same launch.
+int launch_store_rows(StoreRows a, const StoreGeom& o, int BH, int d, cudaStream_t st, bool cut) {
+  const int chunks = o.block * (d / 8);   // 16-byte chunks of a block: 128 ... 2048
+  const bool wide = chunks > 4 * kRowThreads;
+  a.lanes = chunks / (wide ? 8 : 4);      // 32 ... 256
+  a.BH = BH;
+  const int per_win = o.Kp / o.block * 2;
+  long long grid;
+  int threads = kRowThreads;
+  if (cut) {
+    const int at_once = kRowThreads / a.lanes, turns = (per_win + at_once - 1) / at_once;
+    a.split = 1;
+    while (a.split < 8 && a.split < turns && (long long)BH * a.n_win * a.split * 2 <= 4LL * kSms) a.split *= 2;
+    const int rpb = kRowThreads / (d / 8);
+    a.copy_blocks = (a.n_sink + a.n_ins + rpb - 1) / rpb;
+    if ((long long)BH * a.n_win > 0x7fffffffLL / 8) return LRSA_ERR_UNSUPPORTED;
+    a.list_blocks = BH * a.n_win;
+    grid = (long long)a.list_blocks * a.split + ((long long)BH * a.copy_blocks + a.split - 1) / a.split * a.split;
+  } else {
+    // few blocks: one a thread block (a window of 512 out of the ring, 16 pairs: 4.7 us instead of 6.7)
+    if ((long long)BH * a.n_win * per_win * a.lanes < 2LL * kSms * kRowThreads) threads = a.lanes > 64 ? a.lanes : 64;
+    const int rpb = threads / (d / 8), bpb = threads / a.lanes;
+    a.copy_blocks = (a.n_sink + a.n_ins + rpb - 1) / rpb;
+    a.list_blocks = (a.n_win * per_win + bpb - 1) / bpb;
+    grid = (long long)BH * (a.copy_blocks + a.list_blocks);
+  }
+  if (grid == 0) return LRSA_OK;
+  if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
+  const size_t smem = cut ? (size_t)a.L * 4 : 0;
+  auto launch = [&](auto type) -> int {
+    constexpr int T = decltype(type)::value;
+    if (d == 64) return launch_rows_t<64, T, 4>(a, threads, grid, smem, st, cut);
+    return wide ? launch_rows_t<128, T, 8>(a, threads, grid, smem, st, cut) : launch_rows_t<128, T, 4>(a, threads, grid, smem, st, cut);
+  };
+  return o.type == LRSA_LIST_E4M3   ? launch(std::integral_constant<int, LRSA_LIST_E4M3>())
+         : o.type == LRSA_LIST_INT8 ? launch(std::integral_constant<int, LRSA_LIST_INT8>())
+                                    : launch(std::integral_constant<int, LRSA_LIST_BF16>());
 }
 
 // ---- reading the list back ----
@@ -1066,11 +1148,11 @@ int lrsa_store_append(const lrsa_params_t* params, const lrsa_store_t* store, co
     cleared = true;
     return launch_score_select(&s, 1, ring ? rows.k_recent : rows.k_new, ring ? rows.v_recent : rows.v_new, store->idx, nullptr, workspace, st, self);
   };
-  auto move_rows = [&]() -> int {
+  auto move_rows = [&](bool cut = false) -> int {   // cut: windows are selected, by weight, in the same launch
     if (rows.n_sink + rows.n_ins + rows.n_win == 0) return LRSA_OK;
     rows.status = cleared ? nullptr : status;
     cleared = true;
-    return launch_store_rows(rows, o, BH, g.d, st);
+    return launch_store_rows(rows, o, BH, g.d, st, cut);
   };
   int pos = n_prev;                                     // tokens before it are in the store
   int c = pos > g.S ? (pos - g.S + g.L - 1) / g.L : 0;  // next chunk whose first token has not arrived yet
@@ -1093,29 +1175,18 @@ int lrsa_store_append(const lrsa_params_t* params, const lrsa_store_t* store, co
     // Windows c-2 .. c_last-2, one selection for all of them, then their kept rows, the sinks and the tokens that stay in the ring.
     // By the lag rule they lie in the new tokens as a whole, by weight the first ones may be in the ring.
     const int w0 = c - 2, nw = (end - 1 - g.S) / g.L - c + 1;
-    if (o.by_weight) {
-      WeightSelectArgs a = {};
-      a.weight = w_new; a.row = n_new; a.ring = store->weight; a.ring_below = n_prev; a.ring_first = g.S; a.ring_len = 2 * g.L;
-      a.idx = store->idx; a.status = status; a.L = g.L; a.K = g.K; a.Wtot = o.Wcap; a.n = 1;
-      if ((long long)BH * nw > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
-      a.item0[1] = BH * nw; a.windows[0] = nw; a.first[0] = g.S + w0 * g.L - n_prev; a.woff[0] = w0; a.emit0[0] = g.S + w0 * g.L;
-      cleared = true;
-      rc = launch_weight_select(a, st);
-    } else {
-      rc = score(w0, nw, false);
-    }
-    if (rc != LRSA_OK) return rc;
+    if (!o.by_weight && (rc = score(w0, nw, false)) != LRSA_OK) return rc;
     rows.w0 = w0; rows.n_win = nw; rows.ring_below = n_prev;
     if (g.S + w0 * g.L < n_prev) {   // rows of the ring have to be read before tokens take their places
       rows.n_ins = 0;
-      if ((rc = move_rows()) != LRSA_OK) return rc;
+      if ((rc = move_rows(o.by_weight)) != LRSA_OK) return rc;
       rows.n_win = 0;
     }
     rows.n_sink = pos < g.S ? g.S - pos : 0;
     rows.p0 = end - 2 * g.L > pos ? end - 2 * g.L : pos;
     rows.n_ins = end - rows.p0;
   }
-  return move_rows();
+  return move_rows(o.by_weight && rows.n_win > 0);
 }
 
 int lrsa_store_decode(const lrsa_params_t* params, const lrsa_store_t* store, const void* q, int32_t n_tokens, void* out_o,

@@ -295,6 +295,38 @@ def test_quantization_edges():
         assert torch.equal(store.k_scale[0, 0].double().cpu(), ref.held(K[0, 0, :80], dtype, 16)[1][:5]) and store.k_scale[0, 0, 0] == 1
 
 
+def test_offsets_beyond_32_bits():
+    """A list of more than 2^31 elements: every key scores zero, only the last window of the last head holds values."""
+    p = P(1, 8, 8, 2 + 570 * 4096, 128, 4096, 4096, 2)
+    store = lrsa.KVStore(p, dtype=INT8, block=128)
+    assert store.k_list.numel() > 2 ** 31
+    n = 2 + 569 * 4096 + 5                         # windows 0 .. 567 compressed
+    store.n_tokens = n
+    store.k_scale.fill_(1.0)
+    store.v_scale.fill_(0.5)
+    store.v_list[0, 7, 567 * 4096:568 * 4096] = 64
+    q = torch.randn(1, 8, 128, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    o, lse = store.decode(q)
+    keys = 568 * 4096 + 2 + 4096 + 5
+    assert store.status() == 0 and float(o[:, :7].abs().max()) == 0.0
+    assert ((o[0, 7].double() - 32.0 * 4096 / keys).abs() <= 2.0 ** -8 * 32.0 * 4096 / keys).all()
+    assert ((lse.double() - math.log(keys)).abs() <= 1e-5).all()
+    assert ((store.weight[:, :, :5].double() * keys - 1).abs() <= 1e-4).all()
+    k = torch.randn(1, 8, 4096, 128, generator=torch.Generator().manual_seed(2)).bfloat16()
+    w = torch.rand(1, 8, 4096, generator=torch.Generator().manual_seed(3))
+    del store, o, lse
+    wide = P(1, 8, 8, 2 + 571 * 4096, 128, 4096, 4096, 2)
+    big = lrsa.KVStore(wide, dtype=INT8, block=128)
+    big.n_tokens = 2 + 568 * 4096
+    big.append(k.cuda(), (-k).cuda(), w.cuda())
+    big.append(k.cuda(), (-k).cuda(), w.cuda())
+    big.append(k[:, :, :1].cuda(), k[:, :, :1].cuda())     # window 568 is cut: its rows lie behind 2^31 elements
+    assert big.windows_compressed() == 569
+    for rows, scale, x in ((big.k_list, big.k_scale, k), (big.v_list, big.v_scale, -k)):
+        got = rows[:, :, 568 * 4096:].double().cpu().unflatten(2, (-1, 128)) * scale[:, :, 568 * 32:].double().cpu()[..., None, None]
+        assert torch.equal(got.flatten(2, 3)[:, :, :4096], ref.held(x, INT8, 128)[0])
+
+
 def test_two_stores_on_two_streams_and_in_graphs():
     p = P(2, 8, 2, 3000, 128, 256, 64, 4)
     made = [fill(p, t, 64, "weight", 2800, seed=s) for t, s in ((E4M3, 1), (INT8, 2))]
