@@ -253,6 +253,9 @@ int lrsa_weight_select(const lrsa_params_t* params, const float* weight, int32_t
  * softmax fp32; the probabilities are rounded to 11 bits in front of 8-bit rows and to 8 bits (bf16) in front of bf16 rows.
  *
  * lrsa_store_rows: what the kept rows of windows 0 .. n_windows - 1 stand for, fp32 [B, Hkv, n_windows * top_k, d] each.
+ *
+ * Calls on one store are ordered, like calls on one workspace; different stores share nothing.  n_prev and n_tokens are values
+ * of the host: a captured call repeats them.
  */
 typedef enum lrsa_list_type { LRSA_LIST_BF16 = 0, LRSA_LIST_E4M3 = 1, LRSA_LIST_INT8 = 2 } lrsa_list_type;
 typedef enum lrsa_keep { LRSA_KEEP_LAG = 0, LRSA_KEEP_WEIGHT = 1 } lrsa_keep;

@@ -336,7 +336,6 @@ int launch_weights_t(const Geom& whole, const SeqBatch& b, const __nv_bfloat16* 
     items += BHkv * a.plan[s].n_tiles;
     const long long L = g.N - g.S < g.L ? g.N - g.S : g.L;   // a tile is seen by half a window's queries, and by the next window's
     pairs += BHkv * a.plan[s].n_tiles * (((g.ndp ? 3 : 1) * L / (2 * kTile) + 1) * g.G);
-    if (items > 0x7fffffffLL / 8) return LRSA_ERR_UNSUPPORTED;
     a.item0[s + 1] = (int)items;
   }
   a.n_seqs = b.n;
@@ -354,6 +353,11 @@ int launch_weights(const Geom& whole, const __nv_bfloat16* Q, const __nv_bfloat1
                    cudaStream_t st) {
   SeqBatch b;
   bool clear = true;
+  for (SeqBatches it(whole); it.next(&b);) {   // (windows of a few tokens can be too many tiles: found before anything is launched)
+    long long items = 0;
+    for (int s = 0; s < b.n; ++s) items += (long long)whole.B * whole.Hkv * make_wgt_plan(b.g[s]).n_tiles;
+    if (items > 0x7fffffffLL / 8) return LRSA_ERR_UNSUPPORTED;
+  }
   for (SeqBatches it(whole); it.next(&b); clear = false) {
     int rc;
     if (whole.d == 128)

@@ -139,6 +139,10 @@ struct DecodeArgs {
   float scale_log2;
 };
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -147,10 +151,12 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ uint4 ld_stream(const void* p) {   // read once: no place in L1
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
 }
+
 // Grid (n_group * n_split, BHkv), clusters of n_split CTAs of 4 to 16 warps.  One query token per (batch, head) over a few hundred to a few thousand keys
 // per KV head: the work is the transfer of K and V (two bytes per multiply-add of one head), so the kernel is built
 // around the loads.  A warp takes blocks of 2048 / D keys; it loads the block's K and V rows straight into the
@@ -586,6 +592,63 @@ __global__ void __launch_bounds__(kDecThreads) decode_split_kernel(const DecodeA
   }
 }
 
+// One CTA per (batch, query head): merges the partial results of its splits, or of its clusters.  kRows thread rows (one
+// for clusters, of which there are at most kDecMaxGroups) take alternate results, four at a time with all their loads issued before the
+// arithmetic (the kernel is a chain of L2 round trips otherwise), then the rows are merged through shared memory.
+constexpr int kMergeRows = 8;
+template <int D, int kRows>
+__global__ void __launch_bounds__(kRows * D) decode_merge_kernel(const float* part, __nv_bfloat16* o, float* lse, int Hq,
+                                                                  int Hkv, int G, int n_split) {
+  __shared__ float sm_m[kRows], sm_l[kRows], sm_o[kRows][D];
+  const int bhq = blockIdx.x, b = bhq / Hq, hq = bhq % Hq, hkv = hq / G, g = hq % G;
+  const int c = threadIdx.x % D, row = threadIdx.x / D;
+  const float* base = part + (((size_t)(b * Hkv + hkv) * n_split) * G + g) * (D + 2);
+  const size_t stride = (size_t)G * (D + 2);
+  float M = -INFINITY, acc = 0.f, l = 0.f;
+  constexpr int kBatch = 4;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial results of the kernel in front of this one
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  for (int s0 = row; s0 < n_split; s0 += kRows * kBatch) {
+    float ms[kBatch], vs[kBatch], ls[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int s = s0 + u * kRows;
+      const bool in = s < n_split;
+      ms[u] = in ? __ldcg(base + s * stride + D) : -INFINITY;
+      vs[u] = in ? __ldcg(base + s * stride + c) : 0.f;
+      ls[u] = in ? __ldcg(base + s * stride + D + 1) : 0.f;
+    }
+    float mn = M;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, ms[u]);
+    if (mn == -INFINITY) continue;
+    const float f0 = exp2f(M - mn);   // exp2f(-inf) = 0 while nothing has been merged
+    acc *= f0; l *= f0;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const float f = exp2f(ms[u] - mn);
+      acc = fmaf(vs[u], f, acc);
+      l = fmaf(ls[u], f, l);
+    }
+    M = mn;
+  }
+  sm_o[row][c] = acc;
+  if (c == 0) { sm_m[row] = M; sm_l[row] = l; }
+  __syncthreads();
+  if (row == 0) {
+    float Mt = -INFINITY;
+    for (int r = 0; r < kRows; ++r) Mt = fmaxf(Mt, sm_m[r]);
+    float at = 0.f, lt = 0.f;
+    for (int r = 0; r < kRows; ++r) {
+      const float f = sm_m[r] == -INFINITY ? 0.f : exp2f(sm_m[r] - Mt);
+      at = fmaf(sm_o[r][c], f, at);
+      lt = fmaf(sm_l[r], f, lt);
+    }
+    o[(size_t)bhq * D + c] = __float2bfloat16(at / lt);
+    if (c == 0 && lse) lse[bhq] = (Mt + log2f(lt)) * 0.6931471805599453f;
+  }
+}
+
 // Groups of more than eight query heads: the split kernel up to three of its CTAs an SM (what is resident), four when
 // decode_kernel goes over the keys more than once (more than 16 heads); beyond, decode_kernel's transfers are the better ones.  Its merge
 // has a CTA per query head: not for hundreds of them.  us, decode_kernel | split kernel (data as in that kernel's head):
@@ -598,8 +661,33 @@ bool use_split_kernel(const Geom& g, int n_keys) {
 }
 
 DecodePlan decode_plan(const Geom& g, int n_keys, int max_splits = kDecMaxSplits) {
+  DecodePlan p;
+  p.nh = g.G > 8 ? 2 : 1;
   const int per_block = 2048 / g.d;
-  return deal_blocks(g, (n_keys + per_block - 1) / per_block, max_splits);
+  const long long BH = (long long)g.B * g.Hkv;
+  p.blocks = n_keys > 0 ? (n_keys + per_block - 1) / per_block : 1;
+  // 16 warps (8 with two groups of heads) are resident per SM, as one large CTA or several small ones.  Large ones
+  // have fewer partial results to merge; small ones fill the SMs more evenly when every SM has several blocks per warp
+  // to do.  A round of blocks takes about 1.3 us, a CTA's start and merge as long as two, the second kernel as three; a
+  // cluster lies in one group of SMs (ClusterRoom).  (One sequence, 4 heads, d = 128: 9471 keys, one cluster for a
+  // head 17.7 us a token with 8 CTAs, 15.8 with 16; 66 000 keys 107 us with one cluster of 16, 34.5 with two.)
+  const int max_warps = dec_max_warps(p.nh);
+  p.warps = BH * p.blocks > 2LL * kSms * max_warps ? 4 : max_warps;
+  const int per_sm = max_warps / p.warps;
+  const ClusterRoom& room = cluster_room();
+  long long best = -1;
+  for (int s = 1; s <= max_splits; s *= 2) {
+    const long long at_once = room.at_once(per_sm, s);
+    for (int grp = 1; grp <= kDecMaxGroups; grp *= 2) {
+      const int n = s * grp;
+      if (n > 1 && ((n - 1) * p.warps >= p.blocks || BH * n > (long long)kSms * per_sm * 4)) break;
+      const long long waves = (BH * grp + at_once - 1) / at_once;
+      const int per_cta = (p.blocks + n - 1) / n;
+      const long long cost = waves * ((per_cta + p.warps - 1) / p.warps + 2) + (grp > 1 ? 3 : 0);
+      if (best < 0 || cost < best) { best = cost; p.splits = s; p.groups = grp; }
+    }
+  }
+  return p;
 }
 
 template <int D, int NH>

@@ -232,7 +232,7 @@ template <int D, int T, int M>
 int launch_rows_t(const StoreRows& a, int threads, long long grid, size_t smem, cudaStream_t st, bool cut) {
   auto rows = store_rows_kernel<D, T, M>;
   auto cuts = store_cut_kernel<D, T, M>;
-  if (cut && smem > 38 * 1024) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cuts, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  if (smem > kSelSmemFree) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cuts, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelSmemMax));
   LRSA_CUDA_CHECK(cut ? launch_dependent(cuts, dim3((unsigned)grid), dim3(threads), smem, st, a.split, a)
                       : launch_dependent(rows, dim3((unsigned)grid), dim3(threads), 0, st, 1, a));
   launch_counter().n++;
@@ -409,19 +409,25 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
   }
 }
 
-// Grid (n_group * n_split, BHkv), clusters of n_split CTAs: the plan, the lanes' places and the merge are those of
-// decode_kernel (lrsa_infer.cu).  The work is the transfer of the rows, one byte an element in the list and two in the recent
-// rows, so a warp takes 8 KB at a time in either: 256 / d groups of sixteen list rows, or half as many of recent rows,
-// loaded straight into the registers in which the warp-level products want them.
+// Grid (n_group * n_split, BHkv), clusters of n_split CTAs of eight warps (four with two groups of heads).  One query token per
+// (batch, head): the work is the transfer of the rows, one byte an element in the list and two in the recent rows, so a
+// warp takes 8 KB of K and V at a time of either, 256 / d groups of sixteen list rows or half as many of recent rows.  They come by
+// asynchronous copies into a ring of three stages per warp: two of them are on their way while the third is used, 128 KB an SM with
+// two CTAs (twelve warps' worth of registers would hold 96 KB, and leave none for the products).  The warp-level products take
+// the rows from there; as in decode_kernel (lrsa_infer.cu) which channel or key a lane's chunk stands for is the same on
+// both sides of a product, so that a lane reads 8 or 16 bytes at a time.
 //   List.  A code is widened to a half (exact) and multiplied as such.  Q is brought into the range of halves by a power of
 //     two per head (exact but for elements below 2^-28 of the head's largest).  The K scale of a group multiplies its scores.
 //     The V scale enters the exponent, p' = 2^(s + log2(scale) - m' + 7), with a running maximum m' of that sum: what is rounded
 //     to a half is at most 2^15 and 2^7 or more for the key that counts most, whatever the scales are, so a half's
 //     smallest step is 2^-31 of it; O is in units of 2^(m' - 7).  The sum of the weights has its own maximum m and is kept in fp32.
 //   Recent rows.  bf16 products with the bf16 Q, scale 1.
-// The maxima are raised only when they grew by more than 2^8 (then O is rescaled).  With `weight` the ring's scores are
-// stored, and when the cluster has its maximum and sum, each CTA adds exp2(score - lse) over the heads to the weights of
-// the keys that were its own: one owner per key, no atomics.  Several clusters per head: store_weight_kernel does it.
+// The maxima are raised only when they grew by more than 2^8 (then O is rescaled).  Every CTA takes an even share of the list's
+// blocks and one of the recent rows'.  The CTAs of a cluster write their maxima, sums and parts of O into one another's
+// shared memory, then meet once.  With `weight` the ring's scores are stored, and when the cluster has its maximum and sum, each CTA
+// adds exp2(score - lse) over the heads to the weights of the keys that were its own: one owner per key, no atomics.  Several
+// clusters per head: store_finish_kernel does both.
+// Bound by the rows it reads where there are many, by its start and merge where there are few (store_plan has the times).
 template <int D, int NH, int T>
 __global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel(const __grid_constant__ StoreDecodeArgs a) {
   constexpr bool k8 = T != LRSA_LIST_BF16;
@@ -1004,6 +1010,9 @@ __global__ void __launch_bounds__(128) store_finish_kernel(const __grid_constant
   *w = sum;
 }
 
+// Heads of a group whose factors store_finish_kernel has room for; where there are more, a pair has one cluster.
+constexpr int kFinishHeads = 48 * 1024 / (4 * (2 + kDecMaxGroups));
+
 // How the blocks are dealt out: `groups` clusters of `splits` CTAs a (batch, KV head) pair, two CTAs on an SM (of 8 warps, 4 with two head
 // groups), by a model of the time in cycles: a warp takes about 2400 for a block, with all warps of the SM at work 170 for each (the
 // memory's rate and about the issue rate); start and merge take 4000, the kernel behind several clusters and their traffic 20 000.
@@ -1020,7 +1029,7 @@ DecodePlan store_plan(const Geom& g, int blocks, int max_splits = kDecMaxSplits)
   for (int s = 1; s <= max_splits; ++s) {
     const unsigned at_once = room.at_once(2, s);
     // one cluster for a pair, or as many as run at a time
-    const unsigned fit = BH > 2 * kSms ? 1 : at_once / BH < kDecMaxGroups ? at_once / BH : kDecMaxGroups;
+    const unsigned fit = BH > 2 * kSms || g.G > kFinishHeads ? 1 : at_once / BH < kDecMaxGroups ? at_once / BH : kDecMaxGroups;
     for (unsigned grp = 1; grp == 1 || grp <= fit; grp = grp == 1 && fit > 1 ? fit : kDecMaxGroups + 1) {
       const unsigned n = s * grp;
       if (n > 1 && (n - 1) * warps >= (unsigned)blocks) break;
@@ -1155,7 +1164,7 @@ int lrsa_store_append(const lrsa_params_t* params, const lrsa_store_t* store, co
     return launch_store_rows(rows, o, BH, g.d, st, cut);
   };
   int pos = n_prev;                                     // tokens before it are in the store
-  int c = pos > g.S ? (pos - g.S + g.L - 1) / g.L : 0;  // next chunk whose first token has not arrived yet
+  int c = pos > g.S ? (pos - g.S - 1) / g.L + 1 : 0;    // next chunk whose first token has not arrived yet
   if (c < 2) c = 2;
   // Lag rule: chunk start after chunk start while the window c-2 that leaves the ring holds tokens of earlier calls (at most two).
   // The tokens up to it enter the ring, the window is scored with its successor there, its kept rows join the list before its
@@ -1252,7 +1261,6 @@ int lrsa_store_decode(const lrsa_params_t* params, const lrsa_store_t* store, co
     const int keys = a.weight ? a.n_recent - a.n_front : 0, chunks = keys > 128 ? (keys + 127) / 128 : 1;
     const size_t smem = (size_t)(2 + pl.groups) * g.G * sizeof(float);
     auto finish = g.d == 128 ? store_finish_kernel<128> : store_finish_kernel<64>;
-    if (smem > 48 * 1024) return LRSA_ERR_UNSUPPORTED;   // (more than 682 heads of a group)
     LRSA_CUDA_CHECK(launch_dependent(finish, dim3(chunks, g.B * g.Hkv), dim3(128), smem, st, 1, a));
     launch_counter().n++;
   }

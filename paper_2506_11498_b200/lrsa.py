@@ -324,6 +324,8 @@ def lrsa_attn_weights(params: Params, Q, K, LSE, weight=None, workspace=None, st
         _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32, dev)
     if workspace is None:
         workspace = new_workspace(256, Q.device)
+    else:
+        _device(where, "workspace", workspace)
     cp = p.struct()
     status = call.attn_weights(ctypes.addressof(cp), Q.data_ptr(), K.data_ptr(), LSE.data_ptr(), weight.data_ptr(),
                                workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev))
@@ -467,6 +469,12 @@ class KVStore:
         self._lse = torch.empty((p.batch, p.n_q_heads), dtype=torch.float32, device=device)   # what an lse looks like
         self._q_shape = torch.Size((p.batch, p.n_q_heads, p.head_dim))
 
+    def _device(self, where, name, t) -> int:
+        dev = _device(where, name, t)
+        if self._lse.get_device() != dev:
+            raise LrsaError(1, f"{where}: the store is on {self._lse.device}, {name} on {t.device}")
+        return dev
+
     def _parts(self):
         """The store as the calls of csrc/pycall.c take it: type, block, rule, addresses."""
         scale_k, scale_v, weight = self.k_scale, self.v_scale, self.weight
@@ -481,7 +489,7 @@ class KVStore:
         p, where, call = self.params, "lrsa_store_append", _calls()
         n_new = k_new.shape[2] if k_new.dim() == 4 else 0
         shape = (p.batch, p.n_kv_heads, n_new, p.head_dim)
-        dev = _device(where, "k_new", k_new)
+        dev = self._device(where, "k_new", k_new)
         _expect(where, "k_new", k_new, shape, torch.bfloat16, dev)
         _expect(where, "v_new", v_new, shape, torch.bfloat16, dev)
         if w_new is not None:
@@ -497,7 +505,7 @@ class KVStore:
         """q: bf16 [B, Hq, d], the query of the last token in the store.  Returns (o, lse); with keep="weight" the weights of
         the ring's tokens grow by those of the query."""
         where, call, like = "lrsa_store_decode", _call or _calls(), self._lse
-        dev = _device(where, "q", q)
+        dev = self._device(where, "q", q)
         _expect(where, "q", q, self._q_shape, torch.bfloat16, dev)
         if o is None:
             o = torch.empty_like(q)

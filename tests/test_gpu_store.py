@@ -327,6 +327,52 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(got.flatten(2, 3)[:, :, :4096], ref.held(x, INT8, 128)[0])
 
 
+@pytest.mark.parametrize("L,K", [(9729, 9729), (32767, 5000)])
+def test_long_windows(L, K):
+    """Windows whose weights take more shared memory than a kernel gets unasked, some of their tokens in the ring."""
+    p = P(1, 2, 2, 3 + 5 * L, 64, L, K, 3)
+    g = torch.Generator(device="cuda").manual_seed(L)
+    n = 3 + 4 * L + 9
+    k, v = (torch.randn(1, 2, n, 64, generator=g, device="cuda").bfloat16() for _ in "kv")
+    w = torch.rand(1, 2, n, generator=g, device="cuda")
+    store, at = lrsa.KVStore(p, dtype=E4M3, block=64), 3 + L + L // 2
+    store.append(k[:, :, :at].contiguous(), v[:, :, :at].contiguous(), w[:, :, :at].contiguous())
+    store.append(k[:, :, at:].contiguous(), v[:, :, at:].contiguous(), w[:, :, at:].contiguous())
+    assert store.windows_compressed() == 3 and store.status() == 0
+    sel = lrsa.lrsa_weight_select(P(1, 2, 2, n, 64, L, K, 3), w)
+    assert torch.equal(store.idx, sel)
+    for rows, x in zip(store.rows(), (k, v)):
+        for i in range(3):
+            kept = torch.gather(x, 2, sel[:, :, i, :, None].long().expand(-1, -1, -1, 64)).cpu()
+            assert torch.equal(rows[:, :, i * K:(i + 1) * K].double().cpu(), ref.held(kept, E4M3, 64)[0])
+
+
+def test_hundreds_of_heads_in_a_group():
+    """More heads than the merge of several clusters has room for: one cluster, and no call that is refused half way."""
+    p = P(1, 700, 1, 33010, 64, 512, 512, 2)
+    store, want = fill(p, INT8, 64, "weight", 33000, seed=700)
+    q = torch.randn(1, 700, 64, generator=torch.Generator().manual_seed(700)).bfloat16()
+    o, lse = store.decode(q.cuda())
+    (eo, to), (el, tl), (eg, tg) = want.decode(q)
+    ref.within("o", o, eo, to)
+    ref.within("lse", lse, el, tl)
+    first = 2 + want.idx.shape[2] * 512
+    ref.within("weight", ring_weight(store.weight, p, first, 33000 - first), eg, tg)
+
+
+def test_a_store_elsewhere_is_refused():
+    p = P(1, 4, 2, 1000, 128, 128, 32, 4)
+    store = lrsa.KVStore(p, device="cpu")
+    k = torch.zeros(1, 2, 8, 128, dtype=BF16, device="cuda")
+    with pytest.raises(lrsa.LrsaError) as e:
+        store.append(k, k)
+    assert e.value.status == 1 and store.n_tokens == 0
+    store.n_tokens = 8
+    with pytest.raises(lrsa.LrsaError) as e:
+        store.decode(torch.zeros(1, 4, 128, dtype=BF16, device="cuda"))
+    assert e.value.status == 1
+
+
 def test_two_stores_on_two_streams_and_in_graphs():
     p = P(2, 8, 2, 3000, 128, 256, 64, 4)
     made = [fill(p, t, 64, "weight", 2800, seed=s) for t, s in ((E4M3, 1), (INT8, 2))]
