@@ -54,7 +54,7 @@ __device__ __forceinline__ void select_window_by_weight(SelectShared& sh, uint32
     kmax = max(kmax, k);
   };
   for (int i = tid; i < in_ring; i += kSelThreads) take(ring[i], i);
-#pragma unroll 8
+#pragma unroll 16
   for (int i = in_ring + tid; i < L; i += kSelThreads) take(src[i], i);
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   kmax = __reduce_max_sync(0xffffffffu, kmax);
@@ -65,7 +65,7 @@ __device__ __forceinline__ void select_window_by_weight(SelectShared& sh, uint32
 
   // The leading bits that all keys share are fixed at once, then ten-bit digits from the highest differing bit on.  (The first digit
   // holds the exponents of the weights and little more: with eight bits hundreds of keys meet in a bin, and their additions
-  // take turns: 480 windows of 4096 tokens 18.3 us instead of XSELX.)
+  // take turns: 480 windows of 4096 tokens 14.6 us instead of 13.3.)
   const uint32_t diff = kmin ^ kmax;
   const int top = diff ? 31 - __clz(diff) : -1;
   uint32_t mask = top < 0 ? 0xffffffffu : top >= 31 ? 0u : ~((2u << top) - 1u), prefix = kmax & mask;
