@@ -113,18 +113,21 @@ __device__ __forceinline__ void cut_block(const StoreRows& a, int bh, int w, int
   const bool is_v = item & 1;
   const int32_t* idx = a.idx + ((size_t)bh * a.Wcap + w) * a.K;
   const __nv_bfloat16 *ring = (is_v ? a.v_recent : a.k_recent) + (size_t)bh * a.recent * D, *fresh = (is_v ? a.v_new : a.k_new) + (size_t)bh * a.n_new * D;
+  // (all positions, then all rows: one behind the other they would be M round trips)
+  int pos[M];
   uint4 x[M];
   uint32_t most = 0;
 #pragma unroll
+  for (int i = 0; i < M; ++i) pos[i] = __ldcg(idx + min(j0 + (i * a.lanes + in) / CPR, a.K - 1));   // (may be another CTA's of this kernel)
+  const int ring0 = a.S + (w & 1) * a.L - (a.S + w * a.L);   // from a position to its ring row
+#pragma unroll
   for (int i = 0; i < M; ++i) {
-    const int c = i * a.lanes + in, r = c / CPR;
-    x[i] = make_uint4(0, 0, 0, 0);
-    if (there && j0 + r < a.K) {
-      const int pos = __ldcg(idx + j0 + r);   // (may be another CTA's of this kernel)
-      const __nv_bfloat16* row = pos < a.ring_below ? ring + (size_t)(a.S + (pos - a.S) % (2 * a.L)) * D : fresh + (size_t)(pos - a.p_first) * D;
-      x[i] = *reinterpret_cast<const uint4*>(row + (c % CPR) * 8);
-    }
+    const __nv_bfloat16* row = pos[i] < a.ring_below ? ring + (size_t)(pos[i] + ring0) * D : fresh + (size_t)(pos[i] - a.p_first) * D;
+    x[i] = *reinterpret_cast<const uint4*>(row + (i * a.lanes + in) % CPR * 8);
   }
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+    if (j0 + (i * a.lanes + in) / CPR >= a.K) x[i] = make_uint4(0, 0, 0, 0);
   const size_t out_row = (size_t)bh * a.rows_list + (size_t)w * a.Kp + j0;
   if constexpr (T == LRSA_LIST_BF16) {
     __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(is_v ? a.v_list : a.k_list) + out_row * D;
@@ -143,8 +146,8 @@ __device__ __forceinline__ void cut_block(const StoreRows& a, int bh, int w, int
     if ((tid & 31) == 0) s_max[tid >> 5] = most;
     __syncthreads();
     if (!there) return;
-    const int warp0 = tid / a.lanes * (a.lanes / 32);   // of the threads that share the block
-    for (int i = 0; i < a.lanes / 32; ++i) most = max(most, s_max[warp0 + i]);
+    const int warps = a.lanes / 32;   // share the block (one to eight)
+    most = __reduce_max_sync(0xffffffffu, s_max[tid / a.lanes * warps + (tid & (warps - 1))]);
     const float limit = T == LRSA_LIST_E4M3 ? 448.f : 127.f;
     const float scale = most ? fmaxf(scale_up(__fdiv_rn(__uint_as_float(most << 16), limit)), 1.17549435e-38f) : 1.f;
     if (in == 0) {
@@ -154,7 +157,7 @@ __device__ __forceinline__ void cut_block(const StoreRows& a, int bh, int w, int
     }
     unsigned char* dst = static_cast<unsigned char*>(is_v ? a.v_list : a.k_list) + out_row * D;
     const bool finite = most < 0x7f80u;
-    const float inv = 1.f / scale;
+    const float inv = __frcp_rn(scale);
 #pragma unroll
     for (int i = 0; i < M; ++i) {
       const int c = i * a.lanes + in;
