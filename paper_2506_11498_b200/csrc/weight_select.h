@@ -1,6 +1,8 @@
 // The selection by accumulated weight, for the entry point and the store that keeps rows by it.
 #pragma once
 
+#include <type_traits>
+
 #include "lrsa_internal.h"
 
 namespace lrsa {
@@ -53,9 +55,23 @@ __device__ __forceinline__ void select_window_by_weight(SelectShared& sh, uint32
     kmin = min(kmin, k);
     kmax = max(kmax, k);
   };
-  for (int i = tid; i < in_ring; i += kSelThreads) take(ring[i], i);
-#pragma unroll 16
-  for (int i = in_ring + tid; i < L; i += kSelThreads) take(src[i], i);
+  // n tokens a thread, all loads ahead of their use; the last ones may not be there
+  auto load = [&](int i, auto n, auto whole) {
+    constexpr int kAhead = decltype(n)::value;
+    constexpr bool kWhole = decltype(whole)::value;
+    float x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = i + u * kSelThreads;
+      if (kWhole || j < L) x[u] = j < in_ring ? ring[j] : src[j];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (kWhole || i + u * kSelThreads < L) take(x[u], i + u * kSelThreads);
+  };
+  int at = tid;
+  for (; at - tid + 16 * kSelThreads <= L; at += 16 * kSelThreads) load(at, std::integral_constant<int, 16>(), std::true_type());
+  for (; at - tid < L; at += 4 * kSelThreads) load(at, std::integral_constant<int, 4>(), std::false_type());
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   kmax = __reduce_max_sync(0xffffffffu, kmax);
   if (lane == 0) { sh.kred[0][warp] = kmin; sh.kred[1][warp] = kmax; }
