@@ -419,7 +419,8 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
 // (batch, head): the work is the transfer of the rows, one byte an element in the list and two in the recent rows, so a
 // warp takes 8 KB of K and V at a time of either, 256 / d groups of sixteen list rows or half as many of recent rows.  They come by
 // asynchronous copies into a ring of three stages per warp: two of them are on their way while the third is used, 128 KB an SM with
-// two CTAs (twelve warps' worth of registers would hold 96 KB, and leave none for the products).  The warp-level products take
+// two CTAs.  (Loaded straight into registers, as in decode_kernel, the next ones have no room on their way: sixteen sequences of 28/4
+// heads at 32K 44.7 us instead of 37.8, four of 32/8 at 120K 134.6 instead of 111.4.)  The warp-level products take
 // the rows from there; as in decode_kernel (lrsa_infer.cu) which channel or key a lane's chunk stands for is the same on
 // both sides of a product, so that a lane reads 8 or 16 bytes at a time.
 //   List.  A code is widened to a half (exact) and multiplied as such.  Q is brought into the range of halves by a power of
@@ -430,10 +431,12 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
 //   Recent rows.  bf16 products with the bf16 Q, scale 1.
 // The maxima are raised only when they grew by more than 2^8 (then O is rescaled).  Every CTA takes an even share of the list's
 // blocks and one of the recent rows'.  The CTAs of a cluster write their maxima, sums and parts of O into one another's
-// shared memory, then meet once.  With `weight` the ring's scores are stored, and when the cluster has its maximum and sum, each CTA
+// shared memory, then meet once (reading from one another between two meetings: one sequence of 28/4 heads at 32K 16.8 us instead
+// of 15.4).  With `weight` the ring's scores are stored, and when the cluster has its maximum and sum, each CTA
 // adds exp2(score - lse) over the heads to the weights of the keys that were its own: one owner per key, no atomics.  Several
 // clusters per head: store_finish_kernel does both.
-// Bound by the rows it reads where there are many, by its start and merge where there are few (store_plan has the times).
+// Bound by the rows it reads where there are many (sixteen sequences at 32K, 189 MB: 35.4 us, 5.3 TB/s; four at 120K, 623 MB: 108 us in short
+// runs, 117 in long ones, 5.8 and 5.3 TB/s), by its start and merge where there are few.
 template <int D, int NH, int T>
 __global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel(const __grid_constant__ StoreDecodeArgs a) {
   constexpr bool k8 = T != LRSA_LIST_BF16;
