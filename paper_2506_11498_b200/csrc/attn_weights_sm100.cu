@@ -11,7 +11,7 @@
 // until the end.  Where there are few tiles a cluster of CTAs shares one, each takes a run of its pairs, and rank 0 adds
 // the partial sums in the order of the ranks (no atomics: repeats are equal bit by bit).
 // Bound by the unit that forms the exponentials, one a pair (32K tokens of 28/4 heads, d = 128, windows of 1024: 1.4e9 of them take
-// 297 us at 1965 MHz, the products 213; measured 495, that unit 77 % busy between its waits, the clock below its maximum);
+// 297 us at 1965 MHz, the products 213; measured 495, that unit 78 % busy by its counter);
 // short prompts by a tile's start and end (4K tokens of 8 heads, d = 64: 14 us, of which 5 are exponentials).
 #include <math.h>
 

@@ -123,7 +123,9 @@ __device__ __forceinline__ void cut_block(const StoreRows& a, int bh, int w, int
   const int ring0 = a.S + (w & 1) * a.L - (a.S + w * a.L);   // from a position to its ring row
 #pragma unroll
   for (int i = 0; i < M; ++i) {
-    const __nv_bfloat16* row = pos[i] < a.ring_below ? ring + (size_t)(pos[i] + ring0) * D : fresh + (size_t)(pos[i] - a.p_first) * D;
+    // (clamped: where a scoring kernel's wait ran out, the positions are what was there before)
+    const __nv_bfloat16* row = pos[i] < a.ring_below ? ring + (size_t)min((unsigned)(pos[i] + ring0), (unsigned)(a.recent - 1)) * D
+                                                     : fresh + (size_t)min((unsigned)(pos[i] - a.p_first), (unsigned)(a.n_new - 1)) * D;
     x[i] = *reinterpret_cast<const uint4*>(row + (i * a.lanes + in) % CPR * 8);
   }
 #pragma unroll

@@ -360,6 +360,32 @@ def test_hundreds_of_heads_in_a_group():
     ref.within("weight", ring_weight(store.weight, p, first, 33000 - first), eg, tg)
 
 
+def test_a_selection_that_ran_out_of_time():
+    """Long windows by the lag rule: a scoring kernel whose wait ends without an answer leaves no positions.  The status says so, the
+    rows are copied from inside the store all the same, and the next selection is whole."""
+    p = P(1, 2, 2, 2 + 6 * 4608, 64, 4608, 100, 2)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.randn(1, 2, 2 + 5 * 4608 + 1, 64, generator=g, device="cuda").bfloat16() for _ in "kv")
+    store, whole = (lrsa.KVStore(p, dtype=E4M3, block=32, keep="lag") for _ in "ab")
+    at = 2 + 4 * 4608
+    for s in (store, whole):
+        s.append(k[:, :, :at].contiguous(), v[:, :, :at].contiguous())
+    lrsa.lrsa_debug_set_wait_limit(-1)
+    try:
+        store.append(k[:, :, at:at + 1].contiguous(), v[:, :, at:at + 1].contiguous())      # window 2, out of the ring
+        assert store.status() == 5
+    finally:
+        lrsa.lrsa_debug_set_wait_limit(0)
+    whole.append(k[:, :, at:at + 1].contiguous(), v[:, :, at:at + 1].contiguous())
+    for s in (store, whole):
+        s.append(k[:, :, at + 1:].contiguous(), v[:, :, at + 1:].contiguous())
+        assert s.status() == 0 and s.windows_compressed() == 4
+    assert torch.equal(store.idx[:, :, [0, 1, 3]], whole.idx[:, :, [0, 1, 3]])
+    a, b = store.rows(), whole.rows()
+    for i in (0, 1, 3):
+        assert all(torch.equal(x[:, :, 100 * i:100 * i + 100], y[:, :, 100 * i:100 * i + 100]) for x, y in zip(a, b))
+
+
 def test_a_store_elsewhere_is_refused():
     p = P(1, 4, 2, 1000, 128, 128, 32, 4)
     store = lrsa.KVStore(p, device="cpu")
