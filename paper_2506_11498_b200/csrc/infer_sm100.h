@@ -40,6 +40,7 @@ __device__ __forceinline__ void cluster_sync() {
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+
 // How the keys of the (batch, KV head) pairs are dealt out: to `groups` clusters of `splits` CTAs of `warps` warps each.
 struct DecodePlan { int nh, warps, blocks, splits, groups; };
 constexpr int kDecMaxSplits = 16, kDecMaxGroups = 16;
