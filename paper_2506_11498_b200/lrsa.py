@@ -3,6 +3,10 @@
 Argument marshalling only: torch supplies device memory and streams, every step of the path
 runs in the library's CUDA kernels.  There is no fallback: if the shared library is missing
 the import of any entry point raises.
+
+A call runs on `stream`, by default the current one, and the caller orders that stream behind what made the
+inputs.  Results and workspaces that the caller does not give are made in the memory of that stream.  A device-side wait that
+runs out (LRSA_ERR_TIMEOUT) is told by lrsa_workspace_status on the workspace of the call: give one where that matters.
 """
 from __future__ import annotations
 
@@ -219,16 +223,33 @@ def new_workspace(nbytes: int, device="cuda") -> torch.Tensor:
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+def _made(stream, near, make, *args, **kw):
+    """make(*args, **kw), a tensor beside `near` that a call on `stream` makes for itself or returns, in memory of that stream.
+    The allocator orders the users of a block by the stream it was asked for on: a block of the current stream may still be in
+    use there when a call on another stream starts to write it, and a temporary that the call drops may be another tensor of
+    the current stream before the kernel has run."""
+    if stream is None or not near.is_cuda:
+        return make(*args, **kw)
+    here = torch.cuda.current_stream()
+    if not isinstance(stream, torch.cuda.Stream):     # another library's
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        t = make(*args, **kw)
+    t.record_stream(here)     # where the caller will use it, and drop it
+    return t
+
+
 def lrsa_score_select(params: Params, K, V, idx=None, score=None, workspace=None, stream=None,
                       want_score: bool = False):
     """Eq. 4-8 + top-K.  Returns (idx int32 [B,Hkv,W_sel,K], score or None)."""
     wsel = lrsa_num_sel_windows(params)
     if idx is None:
-        idx = torch.empty((params.batch, params.n_kv_heads, wsel, params.top_k), dtype=torch.int32, device=K.device)
+        idx = _made(stream, K, torch.empty, (params.batch, params.n_kv_heads, wsel, params.top_k), dtype=torch.int32, device=K.device)
     if score is None and want_score:
-        score = torch.empty((params.batch, params.n_kv_heads, wsel, params.lag), dtype=torch.float32, device=K.device)
+        score = _made(stream, K, torch.empty, (params.batch, params.n_kv_heads, wsel, params.lag), dtype=torch.float32,
+                      device=K.device)
     if workspace is None:
-        workspace = new_workspace(lrsa_workspace_bytes(params)[0], K.device)
+        workspace = _made(stream, K, new_workspace, lrsa_workspace_bytes(params)[0], K.device)
     _check(lib().lrsa_score_select(params.ref(), _p(K), _p(V), _p(idx), _p(score), _p(workspace),
                                    workspace.numel(), _stream(stream)), "lrsa_score_select")
     return idx, score
@@ -257,11 +278,11 @@ def lrsa_attn_fwd(params: Params, Q, K, V, idx, O=None, LSE=None, workspace=None
     """Eq. 3 under the chunked mask.  Returns (O bf16 [B,Hq,N,d], LSE fp32 [B,Hq,N]).  `o_residual` (bf16,
     shaped like O, optional) receives what the bf16 O cannot hold; lrsa_attn_bwd takes it to form dK more accurately."""
     if O is None:
-        O = torch.empty_like(Q)
+        O = _made(stream, Q, torch.empty_like, Q)
     if LSE is None:
-        LSE = Q.new_empty(Q.shape[:3], dtype=torch.float32)
+        LSE = _made(stream, Q, Q.new_empty, Q.shape[:3], dtype=torch.float32)
     if workspace is None:
-        workspace = new_workspace(lrsa_workspace_bytes(params)[1], Q.device)
+        workspace = _made(stream, Q, new_workspace, lrsa_workspace_bytes(params)[1], Q.device)
     _check(lib().lrsa_attn_fwd(params.ref(o_residual), _p(Q), _p(K), _p(V), _p(idx), _p(O), _p(LSE), _p(workspace),
                                workspace.numel(), _stream(stream)), "lrsa_attn_fwd")
     return O, LSE
@@ -271,13 +292,13 @@ def lrsa_attn_bwd(params: Params, Q, K, V, O, dO, LSE, idx, dQ=None, dK=None, dV
                   stream=None, o_residual=None):
     """Gradient of Eq. 3 with the mask constant.  Returns (dQ, dK, dV) in bf16."""
     if dQ is None:
-        dQ = torch.empty_like(Q)
+        dQ = _made(stream, Q, torch.empty_like, Q)
     if dK is None:
-        dK = torch.empty_like(K)
+        dK = _made(stream, Q, torch.empty_like, K)
     if dV is None:
-        dV = torch.empty_like(V)
+        dV = _made(stream, Q, torch.empty_like, V)
     if workspace is None:
-        workspace = new_workspace(lrsa_workspace_bytes(params)[2], Q.device)
+        workspace = _made(stream, Q, new_workspace, lrsa_workspace_bytes(params)[2], Q.device)
     _check(lib().lrsa_attn_bwd(params.ref(o_residual), _p(Q), _p(K), _p(V), _p(O), _p(dO), _p(LSE), _p(idx), _p(dQ),
                                _p(dK), _p(dV), _p(workspace), workspace.numel(), _stream(stream)), "lrsa_attn_bwd")
     return dQ, dK, dV
@@ -312,18 +333,19 @@ def _calls():
 
 def lrsa_attn_weights(params: Params, Q, K, LSE, weight=None, workspace=None, stream=None):
     """The attention weight that every position gathers from the queries that see it uncompressed: fp32 [B,Hkv,N], summed
-    over the query heads of a group.  `LSE`: that of lrsa_attn_fwd on the same Q and K."""
+    over the query heads of a group.  `LSE`: that of lrsa_attn_fwd on the same Q and K.  The status of the call stays in the
+    `workspace` that the caller gives (256 bytes, lrsa_workspace_status)."""
     p, where, call = params, "lrsa_attn_weights", _calls()
     dev = _device(where, "Q", Q)
     _expect(where, "Q", Q, (p.batch, p.n_q_heads, p.seq_len, p.head_dim), torch.bfloat16, dev)
     _expect(where, "K", K, (p.batch, p.n_kv_heads, p.seq_len, p.head_dim), torch.bfloat16, dev)
     _expect(where, "LSE", LSE, (p.batch, p.n_q_heads, p.seq_len), torch.float32, dev)
     if weight is None:
-        weight = torch.empty((p.batch, p.n_kv_heads, p.seq_len), dtype=torch.float32, device=Q.device)
+        weight = _made(stream, Q, torch.empty, (p.batch, p.n_kv_heads, p.seq_len), dtype=torch.float32, device=Q.device)
     else:
         _expect(where, "weight", weight, (p.batch, p.n_kv_heads, p.seq_len), torch.float32, dev)
     if workspace is None:
-        workspace = new_workspace(256, Q.device)
+        workspace = _made(stream, Q, new_workspace, 256, Q.device)
     else:
         _device(where, "workspace", workspace)
     cp = p.struct()
@@ -343,7 +365,7 @@ def lrsa_weight_select(params: Params, weight, idx=None, stream=None):
     n = lrsa_num_sel_windows(p) if p.cu_seqlens or p.lag < 1 else max((p.seq_len - p.n_sink) // p.lag - 1, 0)
     shape = (p.batch, p.n_kv_heads, n, p.top_k)
     if idx is None:
-        idx = torch.empty(shape, dtype=torch.int32, device=weight.device)
+        idx = _made(stream, weight, torch.empty, shape, dtype=torch.int32, device=weight.device)
     else:
         _expect(where, "idx", idx, shape, torch.int32, dev)
     cp = p.struct()
@@ -401,10 +423,13 @@ class KVCache:
     def decode(self, q, o=None, lse=None, stream=None):
         """q: bf16 [B, Hq, d], the query of the last token in the cache.  Returns (o, lse)."""
         if o is None:
-            o = torch.empty_like(q)
+            o = torch.empty_like(q) if stream is None else _made(stream, q, torch.empty_like, q)
         if lse is None:
             like = self._lse
-            lse = q.new_empty(q.shape[:2], dtype=torch.float32) if like is None else torch.empty_like(like)
+            if like is None:
+                lse = _made(stream, q, q.new_empty, q.shape[:2], dtype=torch.float32)
+            else:
+                lse = torch.empty_like(like) if stream is None else _made(stream, q, torch.empty_like, like)
         buf, ws = self.buf, self.ws
         cp = self.params.struct()
         if _call is None:
@@ -508,11 +533,11 @@ class KVStore:
         dev = self._device(where, "q", q)
         _expect(where, "q", q, self._q_shape, torch.bfloat16, dev)
         if o is None:
-            o = torch.empty_like(q)
+            o = torch.empty_like(q) if stream is None else _made(stream, q, torch.empty_like, q)
         else:
             _expect(where, "o", o, self._q_shape, torch.bfloat16, dev)
         if lse is None:
-            lse = torch.empty_like(like)
+            lse = torch.empty_like(like) if stream is None else _made(stream, q, torch.empty_like, like)
         else:
             _expect(where, "lse", lse, like.shape, torch.float32, dev)
         cp, ws = self.params.struct(), self.ws
@@ -528,11 +553,11 @@ class KVStore:
         shape = (p.batch, p.n_kv_heads, n * p.top_k, p.head_dim)
         dev = _device(where, "the store", self.k_list)
         if k is None:
-            k = torch.empty(shape, dtype=torch.float32, device=self.k_list.device)
+            k = _made(stream, self.k_list, torch.empty, shape, dtype=torch.float32, device=self.k_list.device)
         else:
             _expect(where, "k", k, shape, torch.float32, dev)
         if v is None:
-            v = torch.empty_like(k)
+            v = _made(stream, self.k_list, torch.empty_like, k)
         else:
             _expect(where, "v", v, shape, torch.float32, dev)
         cp = p.struct()
