@@ -244,7 +244,8 @@ def lrsa_score_select(params: Params, K, V, idx=None, score=None, workspace=None
     """Eq. 4-8 + top-K.  Returns (idx int32 [B,Hkv,W_sel,K], score or None)."""
     wsel = lrsa_num_sel_windows(params)
     if idx is None:
-        idx = _made(stream, K, torch.empty, (params.batch, params.n_kv_heads, wsel, params.top_k), dtype=torch.int32, device=K.device)
+        idx = _made(stream, K, torch.empty, (params.batch, params.n_kv_heads, wsel, params.top_k), dtype=torch.int32,
+                    device=K.device)
     if score is None and want_score:
         score = _made(stream, K, torch.empty, (params.batch, params.n_kv_heads, wsel, params.lag), dtype=torch.float32,
                       device=K.device)
@@ -464,10 +465,13 @@ class KVStore:
     """Condensed KV cache of one layer as plain tensors (see lrsa_store_t in the C header), for inference.  `dtype` of the
     kept rows: torch.bfloat16, torch.float8_e4m3fn or torch.int8, 8 bits with one scale per `block` rows and head.  `keep`: the rule
     by which a window is cut, "lag" (lrsa_score_select's) or "weight" (the attention weight its tokens have gathered: what
-    they entered with, and what decode adds).  The tensors may be read and written between calls; two stores share nothing."""
+    they entered with, and what decode adds).  The tensors may be read and written between calls, or replaced by others of
+    the same shape, type and device: anything else is refused by the next call.  Two stores share nothing."""
 
     TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.int8: 2}
     RULES = {"lag": 0, "weight": 1}
+    _TENSORS = ("k_list", "v_list", "k_scale", "v_scale", "k_recent", "v_recent", "weight", "idx")
+    _checked = None   # when the tensors were last looked at: addresses, and aliases so that no other memory can be there
 
     def __init__(self, params: Params, dtype=torch.float8_e4m3fn, block: int = 64, keep: str = "weight", device="cuda"):
         if dtype not in self.TYPES or keep not in self.RULES:
@@ -475,24 +479,57 @@ class KVStore:
         self.params, self.dtype, self.block, self.keep = params, dtype, block, keep
         self._type, self._rule = self.TYPES[dtype], self.RULES[keep]
         self.n_tokens = 0
+        want, ws = self._layout()
+        for name in self._TENSORS:
+            shape, kind = want[name]
+            setattr(self, name, None if shape is None else torch.zeros(shape, dtype=kind, device=device))
+        self.ws = new_workspace(ws, device)
+        self._lse = torch.empty((params.batch, params.n_q_heads), dtype=torch.float32, device=device)   # what an lse looks like
+        self._q_shape = torch.Size((params.batch, params.n_q_heads, params.head_dim))
+
+    def _layout(self):
+        """({tensor: (shape or None, type)}, bytes of workspace) as the library has them."""
+        p, block = self.params, self.block
         st = lrsa_store_t(self._type, block, self._rule, 0)
         wcap, rows, ws = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_size_t(0)
-        _check(lib().lrsa_store_shape(params.ref(), ctypes.byref(st), ctypes.byref(wcap), ctypes.byref(rows),
-                                      ctypes.byref(ws)), "lrsa_store_shape")
-        p, self.rows_per_window = params, rows.value
+        _check(lib().lrsa_store_shape(p.ref(), ctypes.byref(st), ctypes.byref(wcap), ctypes.byref(rows), ctypes.byref(ws)),
+               "lrsa_store_shape")
+        self.rows_per_window = rows.value
         heads, n = (p.batch, p.n_kv_heads), wcap.value * rows.value
+        kept = (heads + (n, p.head_dim), self.dtype)
+        scale = (None if self.dtype == torch.bfloat16 else heads + (n // block,), torch.float32)
+        recent = (heads + (p.n_sink + 2 * p.lag, p.head_dim), torch.bfloat16)
+        return {"k_list": kept, "v_list": kept, "k_scale": scale, "v_scale": scale, "k_recent": recent, "v_recent": recent,
+                "weight": (heads + (2 * p.lag,) if self.keep == "weight" else None, torch.float32),
+                "idx": (heads + (wcap.value, p.top_k), torch.int32)}, ws.value
 
-        def zeros(*shape, dtype=torch.float32):
-            return torch.zeros(heads + shape, dtype=dtype, device=device)
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name != "n_tokens":
+            object.__setattr__(self, "_checked", None)
 
-        self.k_list, self.v_list = (zeros(n, p.head_dim, dtype=dtype) for _ in "kv")
-        self.k_scale, self.v_scale = (None, None) if dtype == torch.bfloat16 else (zeros(n // block) for _ in "kv")
-        self.k_recent, self.v_recent = (zeros(p.n_sink + 2 * p.lag, p.head_dim, dtype=torch.bfloat16) for _ in "kv")
-        self.weight = zeros(2 * p.lag) if keep == "weight" else None
-        self.idx = zeros(wcap.value, p.top_k, dtype=torch.int32)
-        self.ws = new_workspace(ws.value, device)
-        self._lse = torch.empty((p.batch, p.n_q_heads), dtype=torch.float32, device=device)   # what an lse looks like
-        self._q_shape = torch.Size((p.batch, p.n_q_heads, p.head_dim))
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_checked"}   # (addresses of this process)
+
+    def _look(self, where):
+        """Raises LRSA_ERR_INVALID_ARG unless the store's tensors are what its kernels read and write."""
+        p, dev = self.params, self._lse.get_device()
+        if (self.TYPES.get(self.dtype), self.RULES.get(self.keep)) != (self._type, self._rule) or \
+                self._q_shape != (p.batch, p.n_q_heads, p.head_dim):
+            raise LrsaError(1, f"{where}: dtype, rule, heads and batch of a store are those that it was made with")
+        want, held = dict(self._layout()[0], ws=(tuple(self.ws.shape), torch.uint8)), []
+        for name, (shape, kind) in want.items():
+            t = getattr(self, name)
+            if shape is None and t is None:
+                continue
+            if shape is None or not isinstance(t, torch.Tensor) or t.device != self._lse.device:
+                what = "None" if shape is None else f"a tensor on {self._lse.device}"
+                raise LrsaError(1, f"{where}: {name} of the store must be {what}")
+            _expect(where, name + " of the store", t, shape, kind, dev)
+            if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
+                raise LrsaError(1, f"{where}: {name} of the store has lost its memory")
+            held.append(t.detach())
+        object.__setattr__(self, "_checked", (None, None, held))
 
     def _device(self, where, name, t) -> int:
         dev = _device(where, name, t)
@@ -500,13 +537,21 @@ class KVStore:
             raise LrsaError(1, f"{where}: the store is on {self._lse.device}, {name} on {t.device}")
         return dev
 
-    def _parts(self):
-        """The store as the calls of csrc/pycall.c take it: type, block, rule, addresses."""
-        scale_k, scale_v, weight = self.k_scale, self.v_scale, self.weight
-        return (self._type, self.block, self._rule, self.k_list.data_ptr(), self.v_list.data_ptr(),
-                None if scale_k is None else scale_k.data_ptr(), None if scale_v is None else scale_v.data_ptr(),
-                self.k_recent.data_ptr(), self.v_recent.data_ptr(), None if weight is None else weight.data_ptr(),
-                self.idx.data_ptr())
+    def _parts(self, where, ws):
+        """The store as the calls of csrc/pycall.c take it: type, block, rule, addresses.  The tensors are looked at when one
+        has been replaced, or lies elsewhere than it did (on every call that would take longer than the call).  ws: address of
+        the workspace."""
+        if self._checked is None:
+            self._look(where)
+        seen, scale_k, scale_v, weight = self._checked, self.k_scale, self.v_scale, self.weight
+        parts = (self._type, self.block, self._rule, self.k_list.data_ptr(), self.v_list.data_ptr(),
+                 None if scale_k is None else scale_k.data_ptr(), None if scale_v is None else scale_v.data_ptr(),
+                 self.k_recent.data_ptr(), self.v_recent.data_ptr(), None if weight is None else weight.data_ptr(),
+                 self.idx.data_ptr())
+        if parts != seen[0] or ws != seen[1]:
+            self._look(where)
+            object.__setattr__(self, "_checked", (parts, ws, self._checked[2]))
+        return parts
 
     def append(self, k_new, v_new, w_new=None, stream=None):
         """k_new, v_new: bf16 [B, Hkv, n_new, d].  w_new (keep="weight"): fp32 [B, Hkv, n_new], the weight that the tokens enter
@@ -520,8 +565,9 @@ class KVStore:
         if w_new is not None:
             _expect(where, "w_new", w_new, shape[:3], torch.float32, dev)
         cp, ws = p.struct(), self.ws
-        status = call.store_append(ctypes.addressof(cp), *self._parts(), k_new.data_ptr(), v_new.data_ptr(), _p(w_new),
-                                   self.n_tokens, n_new, ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        at = ws.data_ptr()
+        status = call.store_append(ctypes.addressof(cp), *self._parts(where, at), k_new.data_ptr(), v_new.data_ptr(), _p(w_new),
+                                   self.n_tokens, n_new, at, ws.numel(), _stream_of(stream, dev))
         if status:
             _check(status, where)
         self.n_tokens += n_new
@@ -541,8 +587,9 @@ class KVStore:
         else:
             _expect(where, "lse", lse, like.shape, torch.float32, dev)
         cp, ws = self.params.struct(), self.ws
-        status = call.store_decode(ctypes.addressof(cp), *self._parts(), q.data_ptr(), self.n_tokens, o.data_ptr(),
-                                   lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        at = ws.data_ptr()
+        status = call.store_decode(ctypes.addressof(cp), *self._parts(where, at), q.data_ptr(), self.n_tokens, o.data_ptr(),
+                                   lse.data_ptr(), at, ws.numel(), _stream_of(stream, dev))
         if status:
             _check(status, where)
         return o, lse
@@ -551,17 +598,18 @@ class KVStore:
         """What the kept rows of the windows compressed so far stand for: (k, v), fp32 [B, Hkv, windows * top_k, d]."""
         p, n, where, call = self.params, self.windows_compressed(), "lrsa_store_rows", _calls()
         shape = (p.batch, p.n_kv_heads, n * p.top_k, p.head_dim)
-        dev = _device(where, "the store", self.k_list)
+        dev = self._device(where, "the store", self._lse)
         if k is None:
-            k = _made(stream, self.k_list, torch.empty, shape, dtype=torch.float32, device=self.k_list.device)
+            k = _made(stream, self._lse, torch.empty, shape, dtype=torch.float32, device=self._lse.device)
         else:
             _expect(where, "k", k, shape, torch.float32, dev)
         if v is None:
-            v = _made(stream, self.k_list, torch.empty_like, k)
+            v = _made(stream, k, torch.empty_like, k)
         else:
             _expect(where, "v", v, shape, torch.float32, dev)
         cp = p.struct()
-        status = call.store_rows(ctypes.addressof(cp), *self._parts(), n, k.data_ptr(), v.data_ptr(), _stream_of(stream, dev))
+        status = call.store_rows(ctypes.addressof(cp), *self._parts(where, self.ws.data_ptr()), n, k.data_ptr(), v.data_ptr(),
+                                 _stream_of(stream, dev))
         if status:
             _check(status, where)
         return k, v
