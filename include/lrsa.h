@@ -220,7 +220,8 @@ int lrsa_attn_decode(const lrsa_params_t* params, const void* cache, size_t cach
  *   workspace: 256 bytes (status word)
  *
  * lrsa_weight_select: of every scored window the top_k positions of largest weight, for lrsa_attn_fwd / lrsa_attn_bwd.  Equal
- * weights keep the lower position, NaN ranks below every number.  Windows and layout as in lrsa_score_select; it needs no workspace.
+ * weights keep the lower position, NaN ranks below every number, -infinity among them.  Windows and layout as in
+ * lrsa_score_select; it needs no workspace.
  *   weight in : fp32 [B, Hkv, N] (any values);  idx out : int32 [B, Hkv, W_sel, top_k], ascending inside a window
  */
 int lrsa_attn_weights(const lrsa_params_t* params, const void* Q, const void* K, const float* LSE, float* weight,

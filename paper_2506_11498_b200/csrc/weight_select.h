@@ -48,9 +48,8 @@ __device__ __forceinline__ void select_window_by_weight(SelectShared& sh, uint32
   const uint4 zero = make_uint4(0, 0, 0, 0);
   uint32_t kmin = 0xffffffffu, kmax = 0u;
   auto take = [&](float x, int i) {
-    x += 0.f;                              // -0 and 0 are the same weight
-    if (x != x) x = -INFINITY;             // NaN is kept last
-    const uint32_t k = order_key(x);
+    x += 0.f;                                         // -0 and 0 are the same weight
+    const uint32_t k = x != x ? 0u : order_key(x);    // NaN is kept last, behind -infinity (0x007fffff)
     key[i] = k;
     kmin = min(kmin, k);
     kmax = max(kmax, k);

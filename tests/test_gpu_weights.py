@@ -177,3 +177,30 @@ def test_refusals():
     with pytest.raises(lrsa.LrsaError) as e:
         lrsa.lrsa_weight_select(p, w, idx=torch.zeros(1, 2, 3, 32, dtype=torch.int32, device="cuda"))
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("L,K", [(8, 5), (64, 50), (333, 300), (4096, 4000)])
+def test_nan_ranks_below_minus_infinity(L, K):
+    """More rows are kept than there are numbers: first every -infinity, wherever it stands, then the NaN of lowest position."""
+    p = P(1, 2, 2, 3 + 3 * L + 1, 64, L, K, 3)
+    g = torch.Generator().manual_seed(L)
+    w = torch.rand(1, 2, p.seq_len, generator=g)
+    kind = torch.rand(w.shape, generator=g)
+    w[kind < 0.6] = float("nan")
+    w[kind < 0.3] = -float("inf")
+    w[0, 0, 3:3 + L] = float("nan")                   # nothing but NaN; then one -infinity behind all of them
+    w[0, 1, 3:3 + L] = float("nan")
+    w[0, 1, 3 + L - 1] = -float("inf")
+    w.view(torch.int32)[0, 0, 3 + L:3 + 2 * L:2] |= -2 ** 31     # NaN of either sign
+    got = lrsa.lrsa_weight_select(p, w.cuda()).cpu()
+    store = lrsa.KVStore(p, block=16)
+    x = torch.zeros(1, 2, p.seq_len, 64, dtype=torch.bfloat16, device="cuda")
+    store.append(x, x, w.cuda())
+    for h in range(2):
+        for i in range(2):
+            a = 3 + i * L
+            part = w[0, h, a:a + L].tolist()
+            order = sorted(range(L), key=lambda j: (part[j] != part[j], -part[j] if part[j] == part[j] else 0.0, j))
+            want = torch.tensor(sorted(a + j for j in order[:K]), dtype=torch.int32)
+            assert torch.equal(got[0, h, i], want)
+            assert torch.equal(store.idx[0, h, i].cpu(), want)
