@@ -469,3 +469,32 @@ def test_refusals():
     with pytest.raises(lrsa.LrsaError) as e:       # weights for a store that does not keep them
         lrsa.KVStore(p, keep="lag").append(k, k, w)
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("keep", ["weight", "lag"])
+def test_more_heads_than_a_grid_has_rows(keep):
+    """65536 (batch, KV head) pairs: 64 different ones, repeated, against the small store that holds each once."""
+    few, many = (P(b, 32, 32, 4 + 3 * 16 + 2, 64, 16, 5, 4) for b in (2, 2048))
+    Q, K, V, w = tokens(few, 77)
+    small, want = lrsa.KVStore(few, dtype=E4M3, block=16, keep=keep), ref.Store(few, E4M3, 16, keep)
+    store = lrsa.KVStore(many, dtype=E4M3, block=16, keep=keep)
+    for lo, n in ((0, 4 + 2 * 16), (4 + 2 * 16, 1), (4 + 2 * 16 + 1, few.seq_len - 4 - 2 * 16 - 1)):
+        k, v, e = (x[:, :, lo:lo + n] for x in (K, V, w))
+        e = e if keep == "weight" else None
+        args = [x if x is None else x.cuda().contiguous() for x in (k, v, e)]
+        small.append(*args)
+        store.append(*(x if x is None else x.repeat((1024,) + (1,) * (x.dim() - 1)) for x in args))
+        want.append(k, v, e, small.idx[:, :, :small.windows_compressed()].cpu())
+    check_state(small, want)
+    assert store.status() == 0 and store.windows_compressed() == 2
+    for name in ("idx", "k_list", "v_list", "k_scale", "v_scale", "k_recent", "v_recent") + (("weight",) if keep == "weight" else ()):
+        a, b = getattr(store, name), getattr(small, name)
+        assert torch.equal(a.view(torch.uint8).view(1024, *b.view(torch.uint8).shape), b.view(torch.uint8).expand(1024, *b.view(torch.uint8).shape))
+    for got, rows in zip(store.rows(), small.rows()):
+        assert torch.equal(got.view(1024, *rows.shape), rows.expand(1024, *rows.shape))
+    q = Q[:, :, -1].contiguous()
+    o, lse = store.decode(q.cuda().repeat(1024, 1, 1))
+    assert store.status() == 0
+    (eo, to), (el, tl), _ = want.decode(q)
+    ref.within("o", o, eo.repeat(1024, 1, 1), to.repeat(1024, 1, 1))
+    ref.within("lse", lse, el.repeat(1024, 1), tl.repeat(1024, 1))
