@@ -498,3 +498,40 @@ def test_more_heads_than_a_grid_has_rows(keep):
     (eo, to), (el, tl), _ = want.decode(q)
     ref.within("o", o, eo.repeat(1024, 1, 1), to.repeat(1024, 1, 1))
     ref.within("lse", lse, el.repeat(1024, 1), tl.repeat(1024, 1))
+
+
+@pytest.mark.parametrize("given", [True, False], ids=["given", "zero"])
+@pytest.mark.parametrize("p,steps", [
+    (P(2, 4, 2, 5 + 9 * 48 + 7, 64, 48, 12, 5), (3, 1, 1, 40, 9, 48, 48, 96, 1, 30, 1)),     # sinks alone, then several turns of the ring
+    (P(1, 3, 3, 7 * 64 + 2, 128, 64, 64, 0), (130, 64, 1, 63, 64, 2, 100)),                  # no sinks
+    (P(1, 7, 1, 2 + 6 * 33, 64, 33, 8, 2), (2 + 33, 33, 34, 32, 17, 1)),
+])
+def test_weights_in_the_ring(p, steps, given):
+    """What append leaves of the gathered weights, to the bit: the new tokens' are those that were given (zero without), the earlier
+    tokens' are what they were, decode's additions among them."""
+    Q, K, V, w = (x.cuda() for x in tokens(p, 31))
+    store = lrsa.KVStore(p, dtype=INT8, block=16)
+    store.weight.fill_(-5.0)                  # a row that is not written would show
+    known, i = torch.zeros(p.batch, p.n_kv_heads, p.seq_len, device="cuda"), 0
+    while store.n_tokens < p.seq_len:
+        lo = store.n_tokens
+        n = min(steps[i % len(steps)], p.seq_len - lo)
+        i += 1
+        c = max((lo + n - 1 - p.n_sink) // p.lag - 1, 0) if lo + n > p.n_sink else 0
+        own = c > store.windows_compressed() and p.n_sink + c * p.lag > lo     # a window of the call's own tokens is cut
+        e = w[:, :, lo:lo + n].contiguous() if given or own else None
+        known[:, :, lo:lo + n] = 0.0 if e is None else e
+        store.append(K[:, :, lo:lo + n].contiguous(), V[:, :, lo:lo + n].contiguous(), e)
+        first = p.n_sink + c * p.lag
+        if lo + n > first:
+            at = torch.arange(first, lo + n, device="cuda")
+            row = (at - p.n_sink) % (2 * p.lag)
+            assert torch.equal(store.weight[:, :, row], known[:, :, at]), f"{lo} + {n}"
+            rest = store.weight.clone()
+            store.decode(Q[:, :, lo + n - 1].contiguous())
+            known[:, :, at] = store.weight[:, :, row]
+            assert (known[:, :, at] >= rest[:, :, row]).all() and (known[:, :, at] > rest[:, :, row]).any()
+            hidden = torch.ones(2 * p.lag, dtype=torch.bool, device="cuda")
+            hidden[row] = False
+            assert torch.equal(store.weight[:, :, hidden], rest[:, :, hidden])
+    assert store.status() == 0 and store.windows_compressed() >= 4
