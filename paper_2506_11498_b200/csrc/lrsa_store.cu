@@ -371,7 +371,10 @@ __device__ __forceinline__ uint32_t swizzled(int row, int byte) {   // byte with
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-
+// zeros unless `there` (src is an address that may be read, but is not)
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void copy_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -473,7 +476,7 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel
   const unsigned char* vr = reinterpret_cast<const unsigned char*>(a.v_recent) + (size_t)bh * a.recent * (D * 2);
   const float* ks = a.k_scale + (size_t)bh * (a.rows_list >> a.shift);
   const float* vs = a.v_scale + (size_t)bh * (a.rows_list >> a.shift);
-  // byte offset of recent key `key`'s row; beyond the end: the last one's (its probability is zero)
+  // byte offset of recent key `key`'s row; beyond the end: the last one's
   auto recent_row = [&](int key) {
     key = min(key, a.n_recent - 1);
     int r = key;
@@ -554,15 +557,19 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel
       if (first >= a.L2) first -= a.L2;
       const bool run = !in_list && key0 >= a.n_front && key0 + 16 * UL <= a.n_recent && first + 16 * UL <= a.L2;
       const unsigned char* base = src + (size_t)(a.S + first) * (2 * D) + lane * 16;
+      if (run) {
 #pragma unroll
-      for (int k = 0; k < kStage / 512; ++k) {
-        const int r = lane / (D / 8) + kRows * k;
-        const unsigned char* from = base + k * 512;
-        if (!run) {
-          const size_t at = in_list ? (size_t)(group_row(f_at, r >> 4, (l0 + f_v) * UL + (r >> 4) < a.n_groups) + (r & 15)) * (2 * D) : recent_row(key0 + r);
-          from = src + at + lane % (D / 8) * 16;
+        for (int k = 0; k < kStage / 512; ++k)
+          copy_async16(dst + swizzled<2 * D>(lane / (D / 8) + kRows * k, lane % (D / 8) * 16), base + k * 512);
+      } else {
+        // Rows behind the last one are zeros: their probability is zero, which an infinity must not meet.
+#pragma unroll
+        for (int k = 0; k < kStage / 512; ++k) {
+          const int r = lane / (D / 8) + kRows * k;
+          const bool there = in_list ? (l0 + f_v) * UL + (r >> 4) < a.n_groups : key0 + r < a.n_recent;
+          const size_t at = in_list ? (size_t)(group_row(f_at, r >> 4, there) + (r & 15)) * (2 * D) : recent_row(key0 + r);
+          copy_async16(dst + swizzled<2 * D>(r, lane % (D / 8) * 16), src + at + lane % (D / 8) * 16, there);
         }
-        copy_async16(dst + swizzled<2 * D>(r, lane % (D / 8) * 16), from);
       }
       if (is_v) { f_v += nw; advance(f_at); }
     }

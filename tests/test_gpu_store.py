@@ -535,3 +535,30 @@ def test_weights_in_the_ring(p, steps, given):
             hidden[row] = False
             assert torch.equal(store.weight[:, :, hidden], rest[:, :, hidden])
     assert store.status() == 0 and store.windows_compressed() >= 4
+
+
+@pytest.mark.parametrize("d,L,n", [(128, 128, 4 + 5 * 128 + 3), (64, 48, 4 + 5 * 48 + 45), (64, 48, 4 + 2 * 48 + 1), (64, 100, 3), (128, 100, 54)])
+@pytest.mark.parametrize("dtype", [E4M3, BF16], ids=["e4m3", "bf16"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_values_of_visible_rows_that_are_not_finite(dtype, d, L, n, bad):
+    """An infinity in a value that the query sees is one channel's infinity, wherever the row stands in its tile: not a NaN, and
+    nothing in the other channels."""
+    p = P(1, 6, 2, n + 7, d, L, 16, 4)
+    store, want = fill(p, dtype, 16, "weight", n, seed=n + d)
+    q = torch.randn(1, 6, d, generator=torch.Generator().manual_seed(n)).bfloat16()
+    (eo, to), (el, tl), _ = want.decode(q)
+    first = min(n, 4 + want.idx.shape[2] * L)
+    spots = [(store.v_recent, 0)] + [(store.v_recent, 4 + (t - 4) % (2 * L)) for t in {first, n - 1, (first + n) // 2} if t >= max(first, 4)]
+    if dtype == BF16 and want.idx.shape[2]:
+        spots += [(store.v_list, 0), (store.v_list, (want.idx.shape[2] - 1) * store.rows_per_window + 15)]
+    for rows, at in spots:
+        old = rows[0, 1, at, 9].clone()
+        rows[0, 1, at, 9] = bad
+        o, lse = store.decode(q.cuda())
+        rows[0, 1, at, 9] = old
+        ref.within("lse", lse, el, tl)
+        o = o.cpu()
+        hit = o[:, 3:, 9]
+        assert torch.equal(hit.nan_to_num(7.0, 8.0, 9.0), torch.full_like(hit, bad).nan_to_num(7.0, 8.0, 9.0)), f"row {at}: {hit}"
+        o[:, 3:, 9] = eo[:, 3:, 9].bfloat16()
+        ref.within("o", o, eo, to)
