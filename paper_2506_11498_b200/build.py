@@ -11,7 +11,7 @@ import sysconfig
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "liblrsa.so")
-# Python module over two of the library's calls, for the interpreter that builds it.  The binding works without it.
+# Python module over the library's short calls, for the interpreter that builds it.  The binding works without it.
 CALL = os.path.join(_HERE, "_lrsa_call" + importlib.machinery.EXTENSION_SUFFIXES[0])
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]

@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel
   int f_stage = 0, f_slot = 0, f_v = warp;   // the next stage to ask for, its slot, its block
   Cursor f_at = cursor_at((l0 + warp) * UL);
   // what this lane copies of a stage: 16 bytes of rows lane / chunks-per-row, ...
-  const uint32_t own8 = swizzled<D>(lane / (D / 16), lane % (D / 16) * 16), own16 = swizzled<2 * D>(lane / (D / 8), lane % (D / 8) * 16);
+  const uint32_t own8 = swizzled<D>(lane / (D / 16), lane % (D / 16) * 16);
   auto fetch = [&]() {
     const uint32_t dst = ring + f_slot * kStage;
     if (f_stage < n_list) {
