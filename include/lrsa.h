@@ -247,7 +247,9 @@ int lrsa_weight_select(const lrsa_params_t* params, const float* weight, int32_t
  * lrsa_store_append: as lrsa_cache_append.  When a window leaves the ring it is cut to top_k rows, by the lag score or by
  * weight (equal weights keep the lower position), and their blocks are written, once.  w_new (LRSA_KEEP_WEIGHT only,
  * otherwise NULL): fp32 [B, Hkv, n_new], the weight that the new tokens enter with (that of lrsa_attn_weights for a prompt);
- * NULL: zero, for a call that compresses no window of its own tokens (LRSA_ERR_INVALID_ARG otherwise).
+ * NULL: zero, for a call that compresses no window of its own tokens (LRSA_ERR_INVALID_ARG otherwise).  Only decode adds to the
+ * weights of tokens that are in the ring: the queries of a later append do not.  A prompt that arrives in pieces can have the
+ * weights of the whole prompt, once they are known.
  *
  * lrsa_store_decode: as lrsa_attn_decode, over the store.  With LRSA_KEEP_WEIGHT the attention weights of the query, summed over the
  * heads of a group, are added to those of the ring's tokens.  Arithmetic: codes, Q and K products are exact, sums and
@@ -256,7 +258,8 @@ int lrsa_weight_select(const lrsa_params_t* params, const float* weight, int32_t
  * lrsa_store_rows: what the kept rows of windows 0 .. n_windows - 1 stand for, fp32 [B, Hkv, n_windows * top_k, d] each.
  *
  * Calls on one store are ordered, like calls on one workspace; different stores share nothing.  n_prev and n_tokens are values
- * of the host: a captured call repeats them.
+ * of the host: a captured call repeats them.  A bf16 list by the lag score holds what the cache of the calls above holds, which is the
+ * faster one of the two.
  */
 typedef enum lrsa_list_type { LRSA_LIST_BF16 = 0, LRSA_LIST_E4M3 = 1, LRSA_LIST_INT8 = 2 } lrsa_list_type;
 typedef enum lrsa_keep { LRSA_KEEP_LAG = 0, LRSA_KEEP_WEIGHT = 1 } lrsa_keep;

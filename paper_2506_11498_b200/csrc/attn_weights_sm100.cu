@@ -11,8 +11,12 @@
 // until the end.  Where there are few tiles a cluster of CTAs shares one, each takes a run of its pairs, and rank 0 adds
 // the partial sums in the order of the ranks (no atomics: repeats are equal bit by bit).
 // Bound by the unit that forms the exponentials, one a pair (32K tokens of 28/4 heads, d = 128, windows of 1024: 1.4e9 of them take
-// 297 us at 1965 MHz, the products 213; measured 495, that unit 78 % busy by its counter);
-// short prompts by a tile's start and end (4K tokens of 8 heads, d = 64: 14 us, of which 5 are exponentials).
+// 297 us at 1965 MHz, the products 213; measured 480 to 503, at 1.68 GHz, that unit 78 % and the issue slots 40 % busy by their
+// counters); shorter prompts by tiles of unequal length on few places (4K tokens of 8 heads, d = 64: 14 us, 256 tiles on 296 places,
+// of which 5 are exponentials).
+// Rounding: the exponent is one fma of the score with -LSE * log2(e), itself rounded to fp32, and goes to ex2.approx (2^-22 relative):
+// an exponential costs one instruction of the unit that bounds the kernel.  A weight is within 1.1e-7 of its exact value
+// (32-bit torch operations: 4.6e-8), relative, at 32K.
 #include <math.h>
 
 #include <type_traits>
@@ -253,8 +257,8 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
           }
         }
       };
-      // A step that every lane sees whole goes straight through (a test per element costs more than the exponentials: a branch for every four,
-      // 586 us at 32K instead of 512); in the others sixteen columns at a time are left out, taken whole or tested.
+      // A step that every lane sees whole goes straight through (a test per element costs more than the exponentials: with a branch for every
+      // four, 32K took a seventh longer); in the others sixteen columns at a time are left out, taken whole or tested.
       if (!masked) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -305,9 +309,9 @@ lrsa_weights_kernel(const __grid_constant__ WgtMaps<NSEQ> maps, const __grid_con
 }
 
 // CTAs that share a key tile, by the time in steps (two CTAs on an SM; start and end of a CTA cost about five): the work spread over
-// the slots, and half of the last CTA.  us at 1 | 2 | 4 | 8: 8/8 heads, d = 64, 4K tokens 14 | 17 | 26 | 46; 28/4, d = 128: 1777 (windows of 512)
-// 48 | 31 | 26 | 27, 4K 52 | 48 | 48 | 55, 8K (1024) 169 | 137 | 133 | 154, 16K 274 | 248 | 255 | 304, 32K 522 | 512 | 543 | 603; 16/2, d = 64, two
-// sequences of 11K (windows of 333) 52 | 50 | 61 | 93; 32/8, 20K (512) 191 | 193 | 237 | 359.
+// the slots, and half of the last CTA.  us at 1 | 2 | 4 | 8: 8/8 heads, d = 64, 4K tokens 14 | 17 | 25 | 44; 28/4, d = 128: 1777 (windows of 512)
+// 48 | 31 | 25 | 25, 4K 51 | 47 | 47 | 53, 8K (1024) 168 | 135 | 131 | 149, 16K 271 | 240 | 250 | 292, 32K 503 | 482 | 508 | 581; 16/2, d = 64, two
+// sequences of 11K (windows of 333) 54 | 54 | 63 | 91; 32/8, 20K (512) 183 | 189 | 231 | 343.
 int weights_split(long long items, long long pairs) {
   const double n = (double)pairs / items, slots = 2 * kSms;
   int best = 1;

@@ -257,6 +257,9 @@ int launch_store_rows(StoreRows a, const StoreGeom& o, int BH, int d, cudaStream
   long long grid;
   int threads = kRowThreads;
   if (cut) {
+    // A CTA more for a window while its rows take several turns and the CTAs are few.  us of a prompt and its read-back, 1 | 2 | 4 | 8, * taken: 32K of
+    // 28/4 heads, windows of 1024 28.1 | 21.0 | 20.1* | 23.8; 65K of 32/8, half kept 107.5* | 106.6 | 114 | 132; 60K of 8/8, d = 64, windows of
+    // 2048 39.9 | 34.1* | 38.3 | 49; 30K of 28/4, windows of 4096 68.5 | 42.8 | 30.0 | 24.2*; 9K in five pieces 65 | 57* | 57 | 63.
     const int at_once = kRowThreads / a.lanes, turns = (per_win + at_once - 1) / at_once;
     a.split = 1;
     while (a.split < 8 && a.split < turns && (long long)BH * a.n_win * a.split * 2 <= 4LL * kSms) a.split *= 2;
@@ -425,7 +428,7 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
 // warp takes 8 KB of K and V at a time of either, 256 / d groups of sixteen list rows or half as many of recent rows.  They come by
 // asynchronous copies into a ring of three stages per warp: two of them are on their way while the third is used, 128 KB an SM with
 // two CTAs.  (Loaded straight into registers, as in decode_kernel, the next ones have no room on their way: sixteen sequences of 28/4
-// heads at 32K 44.7 us instead of 37.8, four of 32/8 at 120K 134.6 instead of 111.4.)  The warp-level products take
+// heads at 32K took 44.7 us instead of 37.8 then, four of 32/8 at 120K 134.6 instead of 111.4.)  The warp-level products take
 // the rows from there; as in decode_kernel (lrsa_infer.cu) which channel or key a lane's chunk stands for is the same on
 // both sides of a product, so that a lane reads 8 or 16 bytes at a time.
 //   List.  A code is widened to a half (exact) and multiplied as such.  Q is brought into the range of halves by a power of
@@ -433,15 +436,20 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
 //     The V scale enters the exponent, p' = 2^(s + log2(scale) - m' + 7), with a running maximum m' of that sum: what is rounded
 //     to a half is at most 2^15 and 2^7 or more for the key that counts most, whatever the scales are, so a half's
 //     smallest step is 2^-31 of it; O is in units of 2^(m' - 7).  The sum of the weights has its own maximum m and is kept in fp32.
-//   Recent rows.  bf16 products with the bf16 Q, scale 1.
+//   Recent rows, and a bf16 list.  bf16 products with the bf16 Q, scale 1; the probabilities are bf16 there, as the product asks for.
+//   Rounding.  The sums of the probabilities, and the weights, are formed before they are rounded.  A term of O is off by half a step of its
+//     probability, 2^-11 (halves) or 2^-8 (bf16) at most, either way: o is 1.8e-3 to 2.0e-3 (root mean square, relative) from the exact
+//     one where probabilities of 32 bits leave 1.65e-3, the rounding of o itself.  Two bf16 for a probability would be twice the products
+//     with V.  decode_kernel rounds alike.
 // The maxima are raised only when they grew by more than 2^8 (then O is rescaled).  Every CTA takes an even share of the list's
 // blocks and one of the recent rows'.  The CTAs of a cluster write their maxima, sums and parts of O into one another's
-// shared memory, then meet once (reading from one another between two meetings: one sequence of 28/4 heads at 32K 16.8 us instead
-// of 15.4).  With `weight` the ring's scores are stored, and when the cluster has its maximum and sum, each CTA
+// shared memory, then meet once (reading from one another between two meetings: one sequence of 28/4 heads at 32K, by weight and with its
+// host time, 16.8 us instead of 15.4).  With `weight` the ring's scores are stored, and when the cluster has its maximum and sum, each CTA
 // adds exp2(score - lse) over the heads to the weights of the keys that were its own: one owner per key, no atomics.  Several
 // clusters per head: store_finish_kernel does both.
-// Bound by the rows it reads where there are many (sixteen sequences at 32K, 189 MB: 35.4 us, 5.3 TB/s; four at 120K, 623 MB: 108 us in short
-// runs, 117 in long ones, 5.8 and 5.3 TB/s), by its start and merge where there are few.
+// Bound by the rows it reads where there are many (sixteen sequences at 32K, 189 MB: 33.8 us, 5.6 TB/s; four at 120K, 623 MB: 107 us in short
+// runs, 117 in long ones, 5.8 and 5.3 TB/s); where there are few by its start, two or three round trips to memory and the merge (one of 28/4
+// heads at 32K 8.6 us in a graph, of 8/8, d = 64, at 4K 5.0, by weight 9.4 and 5.4).
 template <int D, int NH, int T>
 __global__ void __launch_bounds__(dec_max_warps(NH) * 16, 2) store_decode_kernel(const __grid_constant__ StoreDecodeArgs a) {
   constexpr bool k8 = T != LRSA_LIST_BF16;
@@ -1034,10 +1042,10 @@ constexpr int kFinishHeads = 48 * 1024 / (4 * (2 + kDecMaxGroups));
 // How the blocks are dealt out: `groups` clusters of `splits` CTAs a (batch, KV head) pair, two CTAs on an SM (of 8 warps, 4 with two head
 // groups), by a model of the time in cycles: a warp takes about 2400 for a block, with all warps of the SM at work 170 for each (the
 // memory's rate and about the issue rate); start and merge take 4000, the kernel behind several clusters and their traffic 20 000.
-// us, warps x splits x groups (each with 2 to 3 us for setting the weights back): sixteen sequences of 28/4 heads at 32K (e4m3)
-// 8x4x1 37.8, 16x2x1 37.1, 4x8x1 39.3, 4x6x1 45.2, 4x1x9 62; one of them 8x16x1 16.9, 16x16x1 17.1 to 22, 8x8x1 19.0, 8x8x2 20.6; at 120K
-// 16x16x1 23.5, 8x16x2 27.2, 8x9x8 34; four of 32/8 at 120K (int8) 8x8x1 112, 16x4x1 111, 8x1x9 119, 8x9x1 (two waves of
-// clusters) 150; four of 8/8, d = 64, at 66K 8x8x1 25.4, 16x4x1 26.3, 16x2x2 29.3, 8x9x1 35.3.
+// us, splits x groups, * the plan that is taken: sixteen sequences of 28/4 heads at 32K (e4m3) 4x1* 34.0, 2x1 34.7, 3x1 37.2, 8x1 38.1, 6x1
+// 44.7, 1x1 57; one of them 16x1* 10.0, 12x1 10.8, 8x1 12.6, 8x2 17.8, 16x2 17.3, 4x4 19.3; four of 32/8 at 120K (int8) 8x1* 107, 2x4 113,
+// 1x9 117, 4x1 119, 16x1 127, 9x1 (two waves of clusters) 138; four of 8/8, d = 64, at 66K 8x1* 21.1, 4x1 26.2, 9x1 29.2, 16x1 31.0, 16x2 44.6.
+// Where one pair's list is long the model takes several clusters too early: one sequence of 28/4 at 127K 12x5* 27.7, 16x1 19.3, 16x2 25.8.
 DecodePlan store_plan(const Geom& g, int blocks, int max_splits = kDecMaxSplits) {
   const int nh = g.G > 8 ? 2 : 1, warps = dec_max_warps(nh) / 2;
   DecodePlan best = {nh, warps, blocks, 1, 1};

@@ -5,8 +5,8 @@
 namespace lrsa {
 namespace {
 
-// (Eight CTAs on an SM: those of the call behind it start beside the last ones, 480 windows of 4096 tokens 14.3 us in a run of calls
-// instead of 15.7 with six.)
+// (Eight CTAs on an SM: those of the call behind it start beside the last ones, 480 windows of 4096 tokens 13.3 to 14.3 us in a run of
+// calls instead of 15.6 with six.)
 __global__ void __launch_bounds__(kSelThreads, 8) weight_select_kernel(const __grid_constant__ WeightSelectArgs a) {
   extern __shared__ __align__(16) uint32_t key[];
   __shared__ SelectShared sh;

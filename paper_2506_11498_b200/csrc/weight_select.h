@@ -80,7 +80,7 @@ __device__ __forceinline__ void select_window_by_weight(SelectShared& sh, uint32
 
   // The leading bits that all keys share are fixed at once, then ten-bit digits from the highest differing bit on.  (The first digit
   // holds the exponents of the weights and little more: with eight bits hundreds of keys meet in a bin, and their additions
-  // take turns: 480 windows of 4096 tokens 14.6 us instead of 13.3.)
+  // take turns: 480 windows of 4096 tokens took a tenth longer.)
   const uint32_t diff = kmin ^ kmax;
   const int top = diff ? 31 - __clz(diff) : -1;
   uint32_t mask = top < 0 ? 0xffffffffu : top >= 31 ? 0u : ~((2u << top) - 1u), prefix = kmax & mask;

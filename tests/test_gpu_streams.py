@@ -112,3 +112,22 @@ def test_streams_of_another_library():
     got = call(other)[0]
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_side_stream_in_a_graph(name):
+    """Captured on a stream that joins the capture and leaves it again, replayed twice."""
+    call = calls()[name]
+    want = [x.clone() for x in call(None)]
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        s.wait_stream(torch.cuda.current_stream())
+        got = on(s, call)
+        kept = [x.clone() for x in got]
+    for _ in range(2):
+        for x in kept:
+            x.fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(kept, want))
