@@ -488,16 +488,20 @@ def test_more_heads_than_a_grid_has_rows(keep):
     check_state(small, want)
     assert store.status() == 0 and store.windows_compressed() == 2
     for name in ("idx", "k_list", "v_list", "k_scale", "v_scale", "k_recent", "v_recent") + (("weight",) if keep == "weight" else ()):
-        a, b = getattr(store, name), getattr(small, name)
-        assert torch.equal(a.view(torch.uint8).view(1024, *b.view(torch.uint8).shape), b.view(torch.uint8).expand(1024, *b.view(torch.uint8).shape))
+        a, b = (getattr(s, name).view(torch.uint8) for s in (store, small))
+        assert torch.equal(a.view(1024, *b.shape), b.expand(1024, *b.shape))
     for got, rows in zip(store.rows(), small.rows()):
         assert torch.equal(got.view(1024, *rows.shape), rows.expand(1024, *rows.shape))
     q = Q[:, :, -1].contiguous()
     o, lse = store.decode(q.cuda().repeat(1024, 1, 1))
     assert store.status() == 0
-    (eo, to), (el, tl), _ = want.decode(q)
+    (eo, to), (el, tl), (_, tg) = want.decode(q)
     ref.within("o", o, eo.repeat(1024, 1, 1), to.repeat(1024, 1, 1))
     ref.within("lse", lse, el.repeat(1024, 1), tl.repeat(1024, 1))
+    if keep == "weight":
+        first = 4 + 2 * 16
+        got, all_w = ring_weight(store.weight, many, first, few.seq_len - first), want.w[:, :, first:]
+        ref.within("weight", got, all_w.repeat(1024, 1, 1), (tg + 2.0 ** -24 * all_w).repeat(1024, 1, 1))
 
 
 @pytest.mark.parametrize("given", [True, False], ids=["given", "zero"])
