@@ -288,8 +288,92 @@ int lrsa_store_rows(const lrsa_params_t* params, const lrsa_store_t* store, int3
                     void* cuda_stream);
 
 /*
+ * Position rotation, and a cache in pages for sequences of different lengths (the paper has no counterpart: it takes rotated
+ * rows and one sequence).
+ *
+ * lrsa_rope_t: the angles, as tables of the caller, so that any base, scaling or interpolation is the caller's: fp32
+ * [n_pos, dim / 2] cosines and sines.  The first `dim` channels of a row are rotated in pairs (a, b): a' = a cos - b sin,
+ * b' = b cos + a sin; the pairs are (i, i + dim / 2), or (2i, 2i + 1) with `interleaved`.  dim is a multiple of 16, at most
+ * head_dim.  Arithmetic in fp32, rounded to bf16 once.
+ *
+ * lrsa_rotate: Q and K (either may be NULL) rotated; with `inverse` by the opposite angles, which is the gradient of the rotation:
+ * dQ, dK of lrsa_attn_bwd in, those of the unrotated Q, K out.  Out of place, or in place (the same pointer).
+ *   Q, Q_out : bf16 [B, Hq, N, d];  K, K_out : bf16 [B, Hkv, N, d]
+ *   positions: optional int32 [N] on the device.  NULL: the position of a token is its index in its sequence (packed batches too),
+ *              and n_pos covers the longest one.  A row whose given position is not in [0, n_pos) becomes NaN in the rotated channels.
+ */
+typedef struct lrsa_rope {
+  const float* cos;      /* DEVICE pointers, 16-byte aligned */
+  const float* sin;
+  int32_t n_pos;
+  int32_t dim;
+  int32_t interleaved;   /* 0 or 1 */
+  int32_t reserved;
+} lrsa_rope_t;
+int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void* Q_out, void* K_out, const lrsa_rope_t* rope,
+                const int32_t* positions, int32_t inverse, void* cuda_stream);
+
+/*
+ * The paged cache: the condensed cache (lrsa_cache_*) of many sequences of different lengths in pages of `page` rows (16, 32, 64
+ * or 128).  Every count lies on the device, so a captured call serves every later step; the caller keeps them, and deals out the pages.
+ *   k_pages, v_pages  bf16 [n_pages, Hkv, page, d]
+ *   table             int32 [n_seqs, table_width], page numbers.  With sp, lp, kp = S, lag, top_k over `page`, rounded up, the columns of a
+ *                     sequence are: sp for the sinks; 2 lp for the recent tokens, window w (positions S + w*lag ...) in the first lp of
+ *                     them when w is even, in the others when it is odd; kp for the kept rows of every window.  Rows behind the last of
+ *                     the sinks, of a window or of its kept rows are never read or written.  Entries that no token has reached are not read.
+ *   n_tokens          int32 [n_seqs], tokens in the cache
+ * A cache of n tokens is condensed for the token at position n: with c = (n - S) / lag, windows 0 .. c-2 are held by their kept rows (what
+ * lrsa_score_select keeps), window c-1 and the tokens behind it whole.  That is what the mask of Section 3.2 shows this token.
+ * params: n_dense_prev = 1, no packed batch; seq_len is the most tokens of a sequence; batch is not read.  Several sequences may share a
+ * page that they only read.
+ *
+ * New tokens are packed: those of sequence s are [cu_new[s], cu_new[s + 1]), cu_new int32 [n_seqs + 1] on the device, of rows with any
+ * strides (lrsa_rows_t; multiples of 8 elements, 16-byte aligned data).  n_new is the room for them (cu_new[n_seqs] may be less; what
+ * lies behind is left as it was).
+ *
+ * lrsa_paged_append: token i of a sequence is rotated for position n_tokens + i (rope NULL: it is rotated already), rounded to bf16, and
+ * enters the cache; windows that are to be condensed then are scored and cut, in the arithmetic of lrsa_score_select.  rows (optional,
+ * int32 [n_new]): new token i is row rows[i] of k_new and v_new, whose n_rows rows are then drafts of which some were accepted.
+ * n_tokens is not changed: all layers of a model see the same, and the caller adds to it when the last one is done.
+ *   k_new, v_new : bf16 [Hkv, n_rows, d];  kept (optional): int32 [n_seqs, Hkv, w_cap, top_k], the kept positions
+ *
+ * lrsa_paged_attend: attention of every sequence's new tokens, its next one or a tree of drafts, at most max_new (<= 128) of them, which
+ * are not in the cache.  parent (optional, int32 [n_new]): new token i continues new token parent[i] < i of its sequence, or (-1) the
+ * cache; NULL: token i continues token i - 1.  A token sees what the cache shows its next token, the new tokens that it continues, and itself;
+ * its position is n_tokens + the number of those that it continues.  q and k are rotated on the way (rope NULL: they are rotated already).
+ * A token deeper than the end of the chunk of the first one sees the cache as the first one does.
+ *   q, o : bf16 [Hq, n_new, d];  k, v : bf16 [Hkv, n_new, d];  lse (optional): fp32 [Hq, n_new]
+ *
+ * Counts, page numbers, rows and parents that cannot be used (out of range, more new tokens than max_new, beyond seq_len or beyond the
+ * rope's positions, which have to cover n_tokens + the new tokens of a sequence) are found on the device: lrsa_workspace_status
+ * returns LRSA_ERR_INVALID_ARG.  A sequence with bad counts is left out, whatever is read or written stays inside the tensors.
+ * The workspace's figure holds for both calls and any n_seqs.
+ */
+typedef struct lrsa_paged {
+  int32_t page, n_pages, n_seqs, table_width;
+  void* k_pages;             /* DEVICE pointers */
+  void* v_pages;
+  const int32_t* table;
+  const int32_t* n_tokens;
+} lrsa_paged_t;
+typedef struct lrsa_rows {
+  void* data;                /* DEVICE pointer to row (head 0, token 0) */
+  int64_t head_stride;       /* in elements */
+  int64_t token_stride;
+} lrsa_rows_t;
+int lrsa_paged_shape(const lrsa_params_t* params, int32_t page, int32_t* table_width, int32_t* w_cap, size_t* workspace_bytes);
+int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t* paged, const lrsa_rows_t* k_new, const lrsa_rows_t* v_new,
+                      int32_t n_rows, const int32_t* cu_new, int32_t n_new, const int32_t* rows, const lrsa_rope_t* rope, int32_t* kept,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+int lrsa_paged_attend(const lrsa_params_t* params, const lrsa_paged_t* paged, const lrsa_rows_t* q, const lrsa_rows_t* k,
+                      const lrsa_rows_t* v, const int32_t* cu_new, int32_t n_new, int32_t max_new, const int32_t* parent,
+                      const lrsa_rope_t* rope, const lrsa_rows_t* o, float* lse, void* workspace, size_t workspace_bytes,
+                      void* cuda_stream);
+
+/*
  * Reads the status word that the last call using `workspace` left there.  Synchronises
- * `cuda_stream`.  Returns LRSA_OK, LRSA_ERR_TIMEOUT, or LRSA_ERR_CUDA if the copy failed.
+ * `cuda_stream`.  Returns LRSA_OK, LRSA_ERR_TIMEOUT, LRSA_ERR_INVALID_ARG (counts or tables on the device, lrsa_paged_*), or
+ * LRSA_ERR_CUDA if the copy failed.
  */
 int lrsa_workspace_status(const void* workspace, void* cuda_stream);
 

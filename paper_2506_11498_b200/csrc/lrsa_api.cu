@@ -252,7 +252,7 @@ int lrsa_workspace_status(const void* workspace, void* cuda_stream) {
   if (cudaMemcpyAsync(&status, workspace, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess)
     return LRSA_ERR_CUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return LRSA_ERR_CUDA;
-  return status == 0 ? LRSA_OK : LRSA_ERR_TIMEOUT;
+  return status == LRSA_OK || status == LRSA_ERR_INVALID_ARG ? status : LRSA_ERR_TIMEOUT;
 }
 
 const char* lrsa_status_string(int status) {

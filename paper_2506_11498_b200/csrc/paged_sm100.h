@@ -1,0 +1,118 @@
+// What the kernels of the paged cache and the rotation share: the rotation of a row, where the rows of a sequence lie in its
+// pages, and which counts and tables on the device are usable.
+#pragma once
+
+#include "lrsa_internal.h"
+#include "sm100_ptx.h"
+
+namespace lrsa {
+
+// May be launched before the kernel in front of it has ended.
+__device__ __forceinline__ void wait_front() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// ---- rotation ----
+struct RopeArgs {
+  const float *cos, *sin;   // [n_pos][half]
+  int n_pos, half;          // half: rotated pairs of a row (a multiple of 8); 0: no rotation
+  int interleaved;          // pairs are neighbours (2i, 2i + 1) instead of (i, i + half)
+};
+// Checks and takes the caller's description (NULL: no rotation).  An lrsa_status.
+int make_rope(const lrsa_rope_t* rope, int d, RopeArgs* out);
+
+__device__ __forceinline__ float bf16_lo(uint32_t p) { return __uint_as_float(p << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
+
+// x c + y s' for the pair (x, y), s' = -sin for the first of a pair: one product rounded, one fused.  Written out, so that a row
+// is rotated to the same bits by every kernel (what a draft attends with is what the cache holds when it is accepted).
+__device__ __forceinline__ float turn(float x, float y, float c, float s) { return fmaf(x, c, __fmul_rn(y, s)); }
+
+// Chunk c (channels 8c .. 8c + 7) of the row at `row`, rotated for position pos and rounded to bf16.  All three loads of a chunk are 16 bytes
+// or more; the partner's chunk is another lane's and comes from L1.
+__device__ __forceinline__ uint4 rotated_chunk(const __nv_bfloat16* row, int c, int pos, const RopeArgs& r) {
+  const uint4 x = *reinterpret_cast<const uint4*>(row + 8 * c);
+  if (8 * c >= 2 * r.half) return x;
+  const float* cs = r.cos + (size_t)pos * r.half;
+  const float* sn = r.sin + (size_t)pos * r.half;
+  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+  uint32_t out[4];
+  if (r.interleaved) {
+    const float4 c4 = *reinterpret_cast<const float4*>(cs + 4 * c), s4 = *reinterpret_cast<const float4*>(sn + 4 * c);
+    const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float a = bf16_lo(xs[e]), b = bf16_hi(xs[e]);
+      out[e] = ptx::pack_bf16(turn(a, b, cc[e], -ss[e]), turn(b, a, cc[e], ss[e]));
+    }
+  } else {
+    const int m = r.half >> 3;
+    const bool first = c < m;
+    const int i = first ? c : c - m;
+    const uint4 y = *reinterpret_cast<const uint4*>(row + 8 * (first ? c + m : c - m));
+    const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 c4 = *reinterpret_cast<const float4*>(cs + 8 * i + 4 * h), s4 = *reinterpret_cast<const float4*>(sn + 8 * i + 4 * h);
+      const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int k = 2 * h + e;
+        const float s0 = first ? -ss[2 * e] : ss[2 * e], s1 = first ? -ss[2 * e + 1] : ss[2 * e + 1];
+        out[k] = ptx::pack_bf16(turn(bf16_lo(xs[k]), bf16_lo(ys[k]), cc[2 * e], s0), turn(bf16_hi(xs[k]), bf16_hi(ys[k]), cc[2 * e + 1], s1));
+      }
+    }
+  }
+  return make_uint4(out[0], out[1], out[2], out[3]);
+}
+
+// ---- pages ----
+// A sequence of the cache is a row of the page table:
+//   [0, sp)                      pages of the sinks
+//   [sp, sp + 2 lp)              two groups of lp pages: the uncompressed window w lies in group w mod 2
+//   [sp + 2 lp + w kp, ... kp)   the kept rows of window w
+// A cache of n tokens is condensed for the token at position n, the next one: of the windows in front of that token's chunk c all but
+// the last are cut to their kept rows (the mask of Section 3.2).  So cut(n) = max((n - S) / L - 1, 0) windows are, and at most 2 L tokens are whole.
+struct PageGeom {
+  int S, L, K, N;                // N: most tokens of a sequence
+  int shift, sp, lp, kp, width;  // page = 1 << shift rows
+  int n_pages, n_seqs, Hkv, w_cap;
+  const int32_t* table;          // [n_seqs][width]
+  const int32_t* n_tokens;       // [n_seqs]
+  const int32_t* cu;             // [n_seqs + 1]: where the new tokens of a sequence begin
+  int n_new;                     // new tokens that there is room for (cu[n_seqs] may be less)
+};
+// Checks the caller's description and fills everything but cu and n_new.  An lrsa_status.
+int make_pages(const lrsa_params_t* params, const lrsa_paged_t* paged, Geom* g, PageGeom* out);
+
+__device__ __forceinline__ int cut_windows(const PageGeom& a, int n) { return n >= a.S ? max((n - a.S) / a.L - 1, 0) : 0; }
+
+// The tokens of sequence s in the cache (n) and the new ones [tok0, tok0 + m); m = 0 where the counts on the device are not usable.
+// most: new tokens that a sequence may have; limit: tokens it may have together.
+struct SeqCounts { int n, tok0, m; bool ok; };
+__device__ __forceinline__ SeqCounts seq_counts(const PageGeom& a, int s, int most, int limit) {
+  SeqCounts q;
+  q.n = a.n_tokens[s];
+  q.tok0 = a.cu[s];
+  const int end = a.cu[s + 1];
+  q.ok = q.n >= 0 && q.n <= a.N && q.tok0 >= 0 && end >= q.tok0 && end <= a.n_new;
+  q.m = q.ok ? end - q.tok0 : 0;
+  if (q.m > most || q.m > limit - q.n) { q.ok = false; q.m = 0; }
+  if (!q.ok) q.n = q.tok0 = 0;
+  return q;
+}
+
+// Column of the table and row of that page of the uncompressed token at position p.
+__device__ __forceinline__ int token_column(const PageGeom& a, int p, int& row) {
+  int i = p, col = 0;
+  if (p >= a.S) {
+    const int w = (p - a.S) / a.L;
+    i = p - a.S - w * a.L;
+    col = a.sp + (w & 1) * a.lp;
+  }
+  row = i & ((1 << a.shift) - 1);
+  return col + (i >> a.shift);
+}
+
+}  // namespace lrsa

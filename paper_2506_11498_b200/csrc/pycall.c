@@ -136,7 +136,89 @@ static PyObject* store_rows(PyObject* self, PyObject* const* args, Py_ssize_t n)
   return PyLong_FromLong(rc);
 }
 
+/* five values make a rope: cos, sin, n_pos, dim, interleaved (no cos: none) */
+static const lrsa_rope_t* rope_of(PyObject* const* args, int i, lrsa_rope_t* r) {
+  r->cos = (const float*)PTR(i); r->sin = (const float*)PTR(i + 1);
+  r->n_pos = (int32_t)PyLong_AsLong(args[i + 2]); r->dim = (int32_t)PyLong_AsLong(args[i + 3]);
+  r->interleaved = (int32_t)PyLong_AsLong(args[i + 4]); r->reserved = 0;
+  return r->cos ? r : NULL;
+}
+/* eight make a paged cache: page, n_pages, n_seqs, table_width, k_pages, v_pages, table, n_tokens */
+static lrsa_paged_t paged_of(PyObject* const* args, int i) {
+  lrsa_paged_t p;
+  p.page = (int32_t)PyLong_AsLong(args[i]); p.n_pages = (int32_t)PyLong_AsLong(args[i + 1]);
+  p.n_seqs = (int32_t)PyLong_AsLong(args[i + 2]); p.table_width = (int32_t)PyLong_AsLong(args[i + 3]);
+  p.k_pages = PTR(i + 4); p.v_pages = PTR(i + 5); p.table = (const int32_t*)PTR(i + 6); p.n_tokens = (const int32_t*)PTR(i + 7);
+  return p;
+}
+/* three make rows: data, head stride, token stride */
+static lrsa_rows_t rows_of(PyObject* const* args, int i) {
+  lrsa_rows_t r;
+  r.data = PTR(i); r.head_stride = (int64_t)PyLong_AsLongLong(args[i + 1]); r.token_stride = (int64_t)PyLong_AsLongLong(args[i + 2]);
+  return r;
+}
+
+/* (params, q, k, q_out, k_out, rope ..., positions, inverse, stream) -> status */
+static PyObject* rotate(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  (void)self;
+  if (n != 13) return PyErr_Format(PyExc_TypeError, "rotate takes 13 arguments");
+  const lrsa_params_t* p = (const lrsa_params_t*)PTR(0);
+  void *q = PTR(1), *k = PTR(2), *qo = PTR(3), *ko = PTR(4), *pos = PTR(10), *st = PTR(12);
+  lrsa_rope_t r;
+  const lrsa_rope_t* rope = rope_of(args, 5, &r);
+  const int32_t inverse = (int32_t)PyLong_AsLong(args[11]);
+  if (PyErr_Occurred()) return NULL;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = lrsa_rotate(p, q, k, qo, ko, rope, (const int32_t*)pos, inverse, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (params, paged ..., k ..., v ..., n_rows, cu_new, n_new, rows, rope ..., kept, workspace, workspace_bytes, stream) -> status */
+static PyObject* paged_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  (void)self;
+  if (n != 28) return PyErr_Format(PyExc_TypeError, "paged_append takes 28 arguments");
+  const lrsa_params_t* p = (const lrsa_params_t*)PTR(0);
+  const lrsa_paged_t paged = paged_of(args, 1);
+  const lrsa_rows_t k = rows_of(args, 9), v = rows_of(args, 12);
+  const int32_t n_rows = (int32_t)PyLong_AsLong(args[15]), n_new = (int32_t)PyLong_AsLong(args[17]);
+  void *cu = PTR(16), *rows = PTR(18), *kept = PTR(24), *ws = PTR(25), *st = PTR(27);
+  lrsa_rope_t r;
+  const lrsa_rope_t* rope = rope_of(args, 19, &r);
+  const size_t ws_bytes = (size_t)arg(args, 26);
+  if (PyErr_Occurred()) return NULL;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = lrsa_paged_append(p, &paged, &k, &v, n_rows, (const int32_t*)cu, n_new, (const int32_t*)rows, rope, (int32_t*)kept, ws, ws_bytes, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (params, paged ..., q ..., k ..., v ..., cu_new, n_new, max_new, parent, rope ..., o ..., lse, workspace, workspace_bytes, stream) -> status */
+static PyObject* paged_attend(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  (void)self;
+  if (n != 34) return PyErr_Format(PyExc_TypeError, "paged_attend takes 34 arguments");
+  const lrsa_params_t* p = (const lrsa_params_t*)PTR(0);
+  const lrsa_paged_t paged = paged_of(args, 1);
+  const lrsa_rows_t q = rows_of(args, 9), k = rows_of(args, 12), v = rows_of(args, 15), o = rows_of(args, 27);
+  void *cu = PTR(18), *parent = PTR(21), *lse = PTR(30), *ws = PTR(31), *st = PTR(33);
+  const int32_t n_new = (int32_t)PyLong_AsLong(args[19]), max_new = (int32_t)PyLong_AsLong(args[20]);
+  lrsa_rope_t r;
+  const lrsa_rope_t* rope = rope_of(args, 22, &r);
+  const size_t ws_bytes = (size_t)arg(args, 32);
+  if (PyErr_Occurred()) return NULL;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = lrsa_paged_attend(p, &paged, &q, &k, &v, (const int32_t*)cu, n_new, max_new, (const int32_t*)parent, rope, &o, (float*)lse, ws, ws_bytes, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {
+    {"rotate", (PyCFunction)(void (*)(void))rotate, METH_FASTCALL, NULL},
+    {"paged_append", (PyCFunction)(void (*)(void))paged_append, METH_FASTCALL, NULL},
+    {"paged_attend", (PyCFunction)(void (*)(void))paged_attend, METH_FASTCALL, NULL},
     {"cache_append", (PyCFunction)(void (*)(void))cache_append, METH_FASTCALL, NULL},
     {"attn_decode", (PyCFunction)(void (*)(void))attn_decode, METH_FASTCALL, NULL},
     {"attn_weights", (PyCFunction)(void (*)(void))attn_weights, METH_FASTCALL, NULL},

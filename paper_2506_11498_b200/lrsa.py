@@ -46,6 +46,20 @@ class lrsa_store_t(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("k_list", "v_list", "k_scale", "v_scale", "k_recent", "v_recent", "weight", "idx")]
 
 
+class lrsa_rope_t(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("n_pos", "dim", "interleaved", "reserved")]
+
+
+class lrsa_paged_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("page", "n_pages", "n_seqs", "table_width")] + \
+               [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "table", "n_tokens")]
+
+
+class lrsa_rows_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
 @dataclass(frozen=True)
 class Params:
     """Mirror of ``lrsa_params_t`` (Section 3.2: sink size S, lag L, kept tokens K = r*L)."""
@@ -140,6 +154,13 @@ def lib() -> ctypes.CDLL:
         for name in ("lrsa_attn_weights", "lrsa_weight_select", "lrsa_store_shape", "lrsa_store_append", "lrsa_store_decode",
                      "lrsa_store_rows"):
             getattr(L, name).restype = ctypes.c_int
+        rp, gp, wp = ctypes.POINTER(lrsa_rope_t), ctypes.POINTER(lrsa_paged_t), ctypes.POINTER(lrsa_rows_t)
+        L.lrsa_rotate.argtypes = [pp, vp, vp, vp, vp, rp, i32p, i32, vp]
+        L.lrsa_paged_shape.argtypes = [pp, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
+        L.lrsa_paged_append.argtypes = [pp, gp, wp, wp, i32, vp, i32, vp, rp, vp, vp, sz, vp]
+        L.lrsa_paged_attend.argtypes = [pp, gp, wp, wp, wp, vp, i32, i32, vp, rp, wp, fp, vp, sz, vp]
+        for name in ("lrsa_rotate", "lrsa_paged_shape", "lrsa_paged_append", "lrsa_paged_attend"):
+            getattr(L, name).restype = ctypes.c_int
         L.lrsa_workspace_status.argtypes = [vp, vp]
         L.lrsa_score_select_static_status.argtypes = [vp]
         L.lrsa_score_select_static_status.restype = ctypes.c_int
@@ -167,6 +188,21 @@ class _CtypesCalls:
         for name in ("store_append", "store_decode", "store_rows"):    # eleven arguments make a store
             setattr(self, name, lambda params, *args, f=getattr(L, "lrsa_" + name):
                     f(ctypes.cast(params, at), ctypes.byref(lrsa_store_t(*args[:3], 0, *args[3:11])), *args[11:]))
+
+        def rope(cos, sin, *rest):
+            return ctypes.byref(lrsa_rope_t(cos, sin, *rest, 0)) if cos else None
+
+        def rows(*args):
+            return ctypes.byref(lrsa_rows_t(*args))
+
+        # the orders of csrc/pycall.c: eight values make a paged cache, three make rows, five a rope
+        self.rotate = lambda params, q, k, qo, ko, *args: L.lrsa_rotate(
+            ctypes.cast(params, at), q, k, qo, ko, rope(*args[:5]), *args[5:])
+        self.paged_append = lambda params, *a: L.lrsa_paged_append(
+            ctypes.cast(params, at), ctypes.byref(lrsa_paged_t(*a[:8])), rows(*a[8:11]), rows(*a[11:14]), *a[14:18], rope(*a[18:23]), *a[23:])
+        self.paged_attend = lambda params, *a: L.lrsa_paged_attend(
+            ctypes.cast(params, at), ctypes.byref(lrsa_paged_t(*a[:8])), rows(*a[8:11]), rows(*a[11:14]), rows(*a[14:17]), *a[17:21],
+            rope(*a[21:26]), rows(*a[26:29]), *a[29:])
 
 
 def _token_calls(L):
@@ -620,6 +656,193 @@ class KVStore:
         if self.n_tokens <= p.n_sink:
             return 0
         return max((self.n_tokens - 1 - p.n_sink) // p.lag - 1, 0)
+
+    def status(self, stream=None) -> int:
+        return lrsa_workspace_status(self.ws, stream)
+
+
+class Rope:
+    """The angles of a position rotation: cos, sin fp32 [positions, pairs], whatever base or scaling they were made with.  The first
+    2 * pairs channels of a row are rotated, pairs (i, i + pairs), or neighbours (2i, 2i + 1) where `interleaved`."""
+
+    def __init__(self, cos, sin, interleaved: bool = False):
+        for name, t in (("cos", cos), ("sin", sin)):
+            if t.dtype is not torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.data_ptr() % 16 or t.shape != cos.shape or \
+                    t.device != cos.device:
+                raise LrsaError(1, f"Rope: {name} must be a contiguous, 16-byte aligned float32 tensor [positions, pairs], the same for both")
+        if cos.shape[0] < 1 or cos.shape[1] < 8 or cos.shape[1] % 8:
+            raise LrsaError(1, f"Rope: {cos.shape[1]} pairs of {cos.shape[0]} positions (pairs: a multiple of 8)")
+        self.cos, self.sin, self.interleaved = cos.detach(), sin.detach(), bool(interleaved)
+        self._dev = cos.get_device()
+        self._args = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(self.interleaved))
+
+    @staticmethod
+    def of_base(base: float, dim: int, n_positions: int, interleaved: bool = False, device="cuda") -> "Rope":
+        """The usual table: pair i of `dim` channels turns by base ** (-2i / dim) a position.  Angles in 64 bits."""
+        f = float(base) ** (-torch.arange(0, dim, 2, dtype=torch.float64) / dim)
+        angle = torch.arange(n_positions, dtype=torch.float64)[:, None] * f
+        return Rope(angle.cos().float().to(device), angle.sin().float().to(device), interleaved)
+
+    def __getstate__(self):
+        return {"cos": self.cos, "sin": self.sin, "interleaved": self.interleaved}
+
+    def __setstate__(self, state):
+        self.__init__(**state)
+
+
+_NO_ROPE = (None, None, 0, 0, 0)
+
+
+def _rope_args(where, rope, dev):
+    if rope is None:
+        return _NO_ROPE
+    if rope._dev != dev:
+        raise LrsaError(1, f"{where}: the rope is on {rope.cos.device}")
+    return rope._args
+
+
+def lrsa_rotate(params: Params, Q, K, rope: Rope, positions=None, inverse: bool = False, Q_out=None, K_out=None, stream=None):
+    """Position rotation of Q [B,Hq,N,d] and K [B,Hkv,N,d] (either may be None), in front of lrsa_score_select and lrsa_attn_fwd;
+    inverse: its gradient, behind lrsa_attn_bwd.  positions: int32 [N]; none: a token's index in its sequence.  Q_out, K_out may be
+    Q, K themselves.  Returns (Q_out, K_out)."""
+    p, where, call = params, "lrsa_rotate", _calls()
+    first = Q if Q is not None else K
+    if first is None:
+        raise LrsaError(1, f"{where}: neither Q nor K")
+    dev, out = _device(where, "Q" if Q is not None else "K", first), []
+    for name, x, y, heads in (("Q", Q, Q_out, p.n_q_heads), ("K", K, K_out, p.n_kv_heads)):
+        if x is None:
+            if y is not None:
+                raise LrsaError(1, f"{where}: {name}_out without {name}")
+        else:
+            shape = (p.batch, heads, p.seq_len, p.head_dim)
+            _expect(where, name, x, shape, torch.bfloat16, dev)
+            if y is None:
+                y = _made(stream, x, torch.empty_like, x)
+            elif y is not x:
+                _expect(where, name + "_out", y, shape, torch.bfloat16, dev)
+        out.append(y)
+    if positions is not None:
+        _expect(where, "positions", positions, (p.seq_len,), torch.int32, dev)
+    cp = p.struct()
+    status = call.rotate(ctypes.addressof(cp), _p(Q), _p(K), _p(out[0]), _p(out[1]), *_rope_args(where, rope, dev), _p(positions),
+                         int(inverse), _stream_of(stream, dev))
+    if status:
+        _check(status, where)
+    return tuple(out)
+
+
+class PagedCache:
+    """Condensed KV cache of one layer for sequences of different lengths, in pages (lrsa_paged_* in the C header): k_pages and
+    v_pages, bf16 [n_pages, Hkv, page, d], which may be replaced by others of that shape, type and device.  What the layers of a
+    model share is the caller's, on the device: the page table (int32 [sequences, table_width]), the tokens in the cache (n_tokens, int32
+    [sequences]) and where the new tokens of a sequence begin (cu_new, int32 [sequences + 1]).  Neither call changes them, so a step is
+    attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status()."""
+
+    MOST_NEW = 128   # new tokens of a sequence in an attend
+
+    def __init__(self, params: Params, n_pages: int, page: int = 64, device="cuda"):
+        self.params, self.page, self.n_pages = params, page, n_pages
+        width, cap, ws = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_size_t(0)
+        _check(lib().lrsa_paged_shape(params.ref(), page, ctypes.byref(width), ctypes.byref(cap), ctypes.byref(ws)), "lrsa_paged_shape")
+        if n_pages < 1:
+            raise LrsaError(1, f"PagedCache: {n_pages} pages")
+        self.table_width, self.w_cap = width.value, cap.value
+        self._shape = torch.Size((n_pages, params.n_kv_heads, page, params.head_dim))
+        self.k_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
+        self.v_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
+        self.ws = new_workspace(ws.value, device)
+
+    def columns(self, n_tokens: int):
+        """Columns of the page table that a sequence of n_tokens has reached: those that need a page."""
+        p, size = self.params, self.page
+        sinks, ring, kept = (-(-x // size) for x in (p.n_sink, p.lag, p.top_k))
+        rest = max(n_tokens - p.n_sink, 0)
+        cols = list(range(-(-min(n_tokens, p.n_sink) // size)))
+        for g in range(2):
+            cols += range(sinks + g * ring, sinks + g * ring - (-min(max(rest - g * p.lag, 0), p.lag) // size))
+        first = sinks + 2 * ring
+        return cols + list(range(first, first + max(rest // p.lag - 1, 0) * kept))
+
+    def _pages(self, where, name, first, table, n_tokens, cu_new):
+        """(device, what csrc/pycall.c takes of the cache), when everything is what the kernels read and write."""
+        dev = _device(where, name, first)
+        k, v, ws = self.k_pages, self.v_pages, self.ws
+        if k.shape != self._shape or v.shape != self._shape or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or \
+                not k.is_contiguous() or not v.is_contiguous() or k.get_device() != dev or v.get_device() != dev or ws.get_device() != dev:
+            raise LrsaError(1, f"{where}: the pages of the cache must be contiguous bfloat16 tensors of shape {tuple(self._shape)}, they and the "
+                               f"workspace on cuda:{dev}")
+        n = table.shape[0] if table.dim() == 2 else 0
+        _expect(where, "table", table, (n, self.table_width), torch.int32, dev)
+        _expect(where, "n_tokens", n_tokens, (n,), torch.int32, dev)
+        _expect(where, "cu_new", cu_new, (n + 1,), torch.int32, dev)
+        return dev, (self.page, self.n_pages, n, self.table_width, k.data_ptr(), v.data_ptr(), table.data_ptr(), n_tokens.data_ptr())
+
+    def _rows(self, where, name, t, heads, n, dev):
+        """(address, strides) of rows [heads, n, d] with any strides between heads and tokens."""
+        if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.shape[0] != heads or t.shape[1] != n or t.shape[2] != self.params.head_dim or \
+                t.get_device() != dev:
+            raise LrsaError(1, f"{where}: {name} must be a bfloat16 tensor of shape {(heads, n, self.params.head_dim)} on cuda:{dev}, got "
+                               f"{t.dtype} {tuple(t.shape)} on {t.device}")
+        head, token, channel = t.stride()
+        head, token = head if heads > 1 else 0, token if n > 1 else 0
+        at = t.data_ptr()
+        if channel != 1 or head % 8 or token % 8 or at % 16:
+            raise LrsaError(1, f"{where}: the rows of {name} must be contiguous and 16-byte aligned, got strides {t.stride()}")
+        return at, head, token
+
+    def append(self, k_new, v_new, table, n_tokens, cu_new, rows=None, rope=None, kept=None, stream=None):
+        """The new tokens enter the cache: k_new, v_new bf16 [Hkv, tokens, d] with any strides, K rotated on the way unless rope is
+        None.  rows (int32): new token i is row rows[i] of k_new and v_new (the accepted ones of drafts).  kept (int32 [sequences, Hkv,
+        w_cap, top_k]) receives the kept positions of the windows that are cut."""
+        p, where, call = self.params, "lrsa_paged_append", _calls()
+        dev, pages = self._pages(where, "k_new", k_new, table, n_tokens, cu_new)
+        n_rows = k_new.shape[1] if k_new.dim() == 3 else 0
+        k, v = self._rows(where, "k_new", k_new, p.n_kv_heads, n_rows, dev), self._rows(where, "v_new", v_new, p.n_kv_heads, n_rows, dev)
+        n_new = n_rows
+        if rows is not None:
+            n_new = rows.shape[0] if rows.dim() == 1 else -1
+            _expect(where, "rows", rows, (n_new,), torch.int32, dev)
+        if kept is not None:
+            _expect(where, "kept", kept, (pages[2], p.n_kv_heads, self.w_cap, p.top_k), torch.int32, dev)
+        cp, ws = p.struct(), self.ws
+        status = call.paged_append(ctypes.addressof(cp), *pages, *k, *v, n_rows, cu_new.data_ptr(), n_new, _p(rows),
+                                   *_rope_args(where, rope, dev), _p(kept), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        if status:
+            _check(status, where)
+
+    def attend(self, q, k, v, table, n_tokens, cu_new, parent=None, rope=None, max_new=None, o=None, lse=None, stream=None):
+        """Attention of every sequence's next token, or of a tree of drafted ones, over the cache: q bf16 [Hq, tokens, d], k, v bf16
+        [Hkv, tokens, d] with any strides, not in the cache, rotated on the way unless rope is None.  parent (int32 [tokens]): which
+        token of its sequence each one continues, -1: the cache; none: the one in front of it.  max_new: the most tokens of a
+        sequence (at most 128; fewer than 17 rows, heads of a group times max_new, take the kernel for few).  Returns (o [Hq, tokens, d],
+        lse fp32 [Hq, tokens]); o lies in memory as q does, token by token or head by head."""
+        p, where, call = self.params, "lrsa_paged_attend", _calls()
+        dev, pages = self._pages(where, "q", q, table, n_tokens, cu_new)
+        n = q.shape[1] if q.dim() == 3 else 0
+        qa, ka, va = (self._rows(where, name, t, heads, n, dev) for name, t, heads in
+                      (("q", q, p.n_q_heads), ("k", k, p.n_kv_heads), ("v", v, p.n_kv_heads)))
+        if parent is not None:
+            _expect(where, "parent", parent, (n,), torch.int32, dev)
+        if o is None:
+            if n > 1 and qa[2] > qa[1]:     # token by token
+                o = _made(stream, q, torch.empty, (n, p.n_q_heads, p.head_dim), dtype=q.dtype, device=q.device).transpose(0, 1)
+            else:
+                o = _made(stream, q, torch.empty, (p.n_q_heads, n, p.head_dim), dtype=q.dtype, device=q.device)
+        oa = self._rows(where, "o", o, p.n_q_heads, n, dev)
+        if (p.n_q_heads > 1 and oa[1] < p.head_dim) or (n > 1 and oa[2] < p.head_dim):
+            raise LrsaError(1, f"{where}: rows of o overlap, strides {o.stride()}")
+        if lse is None:
+            lse = _made(stream, q, torch.empty, (p.n_q_heads, n), dtype=torch.float32, device=q.device)
+        else:
+            _expect(where, "lse", lse, (p.n_q_heads, n), torch.float32, dev)
+        cp, ws = p.struct(), self.ws
+        status = call.paged_attend(ctypes.addressof(cp), *pages, *qa, *ka, *va, cu_new.data_ptr(), n,
+                                   max(1, min(n, self.MOST_NEW)) if max_new is None else max_new, _p(parent), *_rope_args(where, rope, dev),
+                                   *oa, lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        if status:
+            _check(status, where)
+        return o, lse
 
     def status(self, stream=None) -> int:
         return lrsa_workspace_status(self.ws, stream)
