@@ -29,42 +29,67 @@ __device__ __forceinline__ float bf16_hi(uint32_t p) { return __uint_as_float(p 
 // is rotated to the same bits by every kernel (what a draft attends with is what the cache holds when it is accepted).
 __device__ __forceinline__ float turn(float x, float y, float c, float s) { return fmaf(x, c, __fmul_rn(y, s)); }
 
-// Chunk c (channels 8c .. 8c + 7) of the row at `row`, rotated for position pos and rounded to bf16.  All three loads of a chunk are 16 bytes
-// or more; the partner's chunk is another lane's and comes from L1.
-__device__ __forceinline__ uint4 rotated_chunk(const __nv_bfloat16* row, int c, int pos, const RopeArgs& r) {
+// Eight rotated channels in 32 bits: chunk c (channels 8c .. 8c + 7) of the row at `row`, for position pos; false: the chunk is not among the rotated
+// ones and y holds it as it is.  All loads are 16 bytes; the partner's chunk is another lane's too and comes from L1.
+__device__ __forceinline__ bool turned_channels(const __nv_bfloat16* row, int c, int pos, const RopeArgs& r, float (&y)[8]) {
   const uint4 x = *reinterpret_cast<const uint4*>(row + 8 * c);
-  if (8 * c >= 2 * r.half) return x;
+  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { y[2 * e] = bf16_lo(xs[e]); y[2 * e + 1] = bf16_hi(xs[e]); }
+  if (8 * c >= 2 * r.half) return false;
   const float* cs = r.cos + (size_t)pos * r.half;
   const float* sn = r.sin + (size_t)pos * r.half;
-  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-  uint32_t out[4];
   if (r.interleaved) {
     const float4 c4 = *reinterpret_cast<const float4*>(cs + 4 * c), s4 = *reinterpret_cast<const float4*>(sn + 4 * c);
     const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = bf16_lo(xs[e]), b = bf16_hi(xs[e]);
-      out[e] = ptx::pack_bf16(turn(a, b, cc[e], -ss[e]), turn(b, a, cc[e], ss[e]));
+      const float a = y[2 * e], b = y[2 * e + 1];
+      y[2 * e] = turn(a, b, cc[e], -ss[e]);
+      y[2 * e + 1] = turn(b, a, cc[e], ss[e]);
     }
   } else {
     const int m = r.half >> 3;
     const bool first = c < m;
     const int i = first ? c : c - m;
-    const uint4 y = *reinterpret_cast<const uint4*>(row + 8 * (first ? c + m : c - m));
-    const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
+    const uint4 v = *reinterpret_cast<const uint4*>(row + 8 * (first ? c + m : c - m));
+    const uint32_t vs[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float4 c4 = *reinterpret_cast<const float4*>(cs + 8 * i + 4 * h), s4 = *reinterpret_cast<const float4*>(sn + 8 * i + 4 * h);
       const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int k = 2 * h + e;
-        const float s0 = first ? -ss[2 * e] : ss[2 * e], s1 = first ? -ss[2 * e + 1] : ss[2 * e + 1];
-        out[k] = ptx::pack_bf16(turn(bf16_lo(xs[k]), bf16_lo(ys[k]), cc[2 * e], s0), turn(bf16_hi(xs[k]), bf16_hi(ys[k]), cc[2 * e + 1], s1));
+      for (int e = 0; e < 4; ++e) {
+        const int k = 4 * h + e;
+        y[k] = turn(y[k], e & 1 ? bf16_hi(vs[k >> 1]) : bf16_lo(vs[k >> 1]), cc[e], first ? -ss[e] : ss[e]);
       }
     }
   }
-  return make_uint4(out[0], out[1], out[2], out[3]);
+  return true;
+}
+__device__ __forceinline__ uint4 pack_channels(const float (&y)[8]) {
+  return make_uint4(ptx::pack_bf16(y[0], y[1]), ptx::pack_bf16(y[2], y[3]), ptx::pack_bf16(y[4], y[5]), ptx::pack_bf16(y[6], y[7]));
+}
+// The chunk rotated and rounded to bf16: what the cache holds.
+__device__ __forceinline__ uint4 rotated_chunk(const __nv_bfloat16* row, int c, int pos, const RopeArgs& r) {
+  float y[8];
+  turned_channels(row, c, pos, r, y);
+  return pack_channels(y);
+}
+// The chunk rotated, as the sum of two bf16: rounded, and what that leaves (2^-17 of a channel is lost).  For operands of products.
+__device__ __forceinline__ uint4 rotated_chunk(const __nv_bfloat16* row, int c, int pos, const RopeArgs& r, uint4& rest) {
+  float y[8];
+  turned_channels(row, c, pos, r, y);
+  const uint4 hi = pack_channels(y);
+  const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float a = y[2 * e] - bf16_lo(h[e]), b = y[2 * e + 1] - bf16_hi(h[e]);
+    y[2 * e] = fabsf(a) < INFINITY ? a : 0.f;           // (an infinity or NaN is all in the first)
+    y[2 * e + 1] = fabsf(b) < INFINITY ? b : 0.f;
+  }
+  rest = pack_channels(y);
+  return hi;
 }
 
 // ---- pages ----

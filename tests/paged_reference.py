@@ -69,10 +69,11 @@ def ancestors(parent, m):
     return sees
 
 
-def attend(q, k, v, sees, scale):
+def attend(q, k, v, sees, scale, rotated=False):
     """q [H, m, d], k, v [Hkv, n, d], sees [m, n] or [Hkv, m, n].  Returns o, lse, and bounds of what rounding may do to them: a probability
     is rounded to bf16 (half a step of each term), o to bf16; a score is a sum of d products in 32 bits (2^-24 of the terms' sum for
-    each addition), and enters the exponent of p and the log-sum."""
+    each addition), and enters the exponent of p and the log-sum.  rotated: queries and new keys are sums of two bf16 (half a step of half a
+    step, 2^-16, is lost of each, and their smaller parts' product)."""
     H, Hkv, d = q.shape[0], k.shape[0], q.shape[-1]
     o, lse, o_tol, lse_tol = [], [], [], []
     for h in range(H):
@@ -86,7 +87,7 @@ def attend(q, k, v, sees, scale):
         o.append(p @ v[kv])
         lse.append((top + np.log(total))[:, 0])
         terms = p @ np.abs(v[kv])
-        ds = (d + 4) * 2.0 ** -24 * (np.where(see, np.abs(q[h]) @ np.abs(k[kv]).T, 0) * scale).max(1) + 2.0 ** -21
+        ds = ((d + 4) * 2.0 ** -24 + (3 * HALF_STEP ** 2 if rotated else 0)) * (np.where(see, np.abs(q[h]) @ np.abs(k[kv]).T, 0) * scale).max(1) + 2.0 ** -21
         o_tol.append((HALF_STEP + 2 * ds[:, None] + 2.0 ** -18) * terms + HALF_STEP * (np.abs(o[-1]) + HALF_STEP * terms))
         lse_tol.append(ds + 2.0 ** -21 + 2.0 ** -23 * np.abs(lse[-1]))
     return tuple(np.stack(t) for t in (o, lse, o_tol, lse_tol))

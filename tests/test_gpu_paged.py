@@ -45,8 +45,8 @@ class Model:
         x = torch.randn((n, heads, self.p.head_dim) if token_major else (heads, n, self.p.head_dim), generator=self.gen).bfloat16()
         return x.transpose(0, 1) if token_major else x
 
-    def turned(self, x, pos):
-        return ref.rotate(x, pos, self.cos, self.sin, self.interleaved) if self.dim else x
+    def turned(self, x, pos, rounded=True):
+        return ref.rotate(x, pos, self.cos, self.sin, self.interleaved, rounded=rounded) if self.dim else x
 
     def reach(self, s, n):
         """Pages for a sequence of n tokens."""
@@ -86,7 +86,7 @@ class Model:
         p, n, w = self.p, self.n[s], ref.cut(self.p, self.n[s])
         if w == 0:
             return np.zeros((p.n_kv_heads, 0, p.top_k), int)
-        q = lrsa.Params(1, p.n_q_heads, p.n_kv_heads, n, p.head_dim, p.lag, p.top_k, p.n_sink)
+        q = lrsa.Params(1, p.n_q_heads, p.n_kv_heads, n, p.head_dim, p.lag, p.top_k, p.n_sink, std_ddof=p.std_ddof)
         K, V = (torch.from_numpy(x).bfloat16()[None].contiguous().cuda() for x in (self.K[s], self.V[s]))
         return lrsa.lrsa_score_select(q, K, V)[0][0, :, :w].cpu().numpy()
 
@@ -139,7 +139,7 @@ class Model:
             at += m
             sees = ref.ancestors(parents[s], m)
             pos = n + sees.sum(1) - 1
-            qs, ks, vs = self.turned(f64(q)[:, part], pos), self.turned(f64(k)[:, part], pos), f64(v)[:, part]
+            qs, ks, vs = self.turned(f64(q)[:, part], pos, False), self.turned(f64(k)[:, part], pos, False), f64(v)[:, part]
             idx = self.selected(s)
             keys, vals = [], []
             for h in range(p.n_kv_heads):
@@ -147,7 +147,7 @@ class Model:
                 keys.append(np.concatenate([self.K[s][h, seen], ks[h]]))
                 vals.append(np.concatenate([self.V[s][h, seen], vs[h]]))
             old = np.ones((m, keys[0].shape[0] - m), bool)
-            want = ref.attend(qs, np.stack(keys), np.stack(vals), np.concatenate([old, sees], 1), scale)
+            want = ref.attend(qs, np.stack(keys), np.stack(vals), np.concatenate([old, sees], 1), scale, rotated=self.dim > 0)
             for name, got, x, tol in (("o", f64(o)[:, part], want[0], want[2]), ("lse", f64(lse)[:, part], want[1], want[3])):
                 err = np.abs(got - x)
                 assert (err <= tol).all(), (name, s, m, n, float((err / tol).max()))
@@ -241,3 +241,14 @@ def test_long_sequence_in_many_shares():
     args = m.device([40, 10])
     outs = [again.attend(q, k, v, *args, rope=m.rope, max_new=40) for _ in range(3)]
     assert all(torch.equal(x, y) for o in outs[1:] for x, y in zip(outs[0], o))
+
+
+@pytest.mark.parametrize("name", CASES)
+@pytest.mark.parametrize("most", [1, 5, 20, 64])
+def test_many_sequences_of_all_lengths(name, most):
+    """More items than CTAs, empty caches and empty trees among them: a CTA works on several, one after the other."""
+    n_seqs = 70 if most < 20 else 40
+    m = make(name, n_seqs, seed=3)
+    m.append([int(x) for x in m.rng.integers(0, 1400, n_seqs) * (m.rng.random(n_seqs) < 0.7)])
+    for _ in range(2):
+        m.attend([int(x) for x in m.rng.integers(0, most + 1, n_seqs)], max_new=most)
