@@ -347,7 +347,8 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  * Counts, page numbers, rows and parents that cannot be used (out of range, more new tokens than max_new, beyond seq_len or beyond the
  * rope's positions, which have to cover n_tokens + the new tokens of a sequence) are found on the device: lrsa_workspace_status
  * returns LRSA_ERR_INVALID_ARG.  A sequence with bad counts is left out, whatever is read or written stays inside the tensors.
- * The workspace's figure holds for both calls and any n_seqs.
+ * lrsa_paged_shape: the workspace of an attend of n_new tokens of n_seqs sequences, at most max_new each (it grows with n_new and n_seqs; any
+ * output may be NULL); with max_new = 0 that of an append.
  */
 typedef struct lrsa_paged {
   int32_t page, n_pages, n_seqs, table_width;
@@ -361,7 +362,8 @@ typedef struct lrsa_rows {
   int64_t head_stride;       /* in elements */
   int64_t token_stride;
 } lrsa_rows_t;
-int lrsa_paged_shape(const lrsa_params_t* params, int32_t page, int32_t* table_width, int32_t* w_cap, size_t* workspace_bytes);
+int lrsa_paged_shape(const lrsa_params_t* params, int32_t page, int32_t n_seqs, int32_t n_new, int32_t max_new, int32_t* table_width,
+                     int32_t* w_cap, size_t* workspace_bytes);
 int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t* paged, const lrsa_rows_t* k_new, const lrsa_rows_t* v_new,
                       int32_t n_rows, const int32_t* cu_new, int32_t n_new, const int32_t* rows, const lrsa_rope_t* rope, int32_t* kept,
                       void* workspace, size_t workspace_bytes, void* cuda_stream);

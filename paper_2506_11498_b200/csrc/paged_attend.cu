@@ -26,6 +26,8 @@ constexpr int kMaxNew = 128;             // new tokens of a sequence: one key ti
 constexpr int kFewRows = 16;             // rows of the kernel for few
 constexpr int kMaxPlaces = 2 * kSms;     // CTAs of a launch
 
+struct Start;
+struct Divided;
 struct AttendArgs {
   PageGeom p;
   RopeArgs rope;
@@ -35,7 +37,13 @@ struct AttendArgs {
   const __nv_bfloat16 *k_pages, *v_pages;
   const int32_t* parent;                 // optional
   float *lse, *part;
-  void* divided;                         // [places] Divided
+  Start* starts;                         // [places]
+  Divided* divided;                      // [places]
+  // The kernel for many rows: what its first launch makes of the new tokens.
+  uint4* family;                         // [n_new] the new tokens that a new token sees
+  int* odd;                              // [n_seqs][Hkv] an infinity or NaN among its new values
+  __nv_bfloat16 *q_parts[2];             // [Hkv][n_new * G][D] rotated queries: rounded, and what that leaves
+  __nv_bfloat16 *k_parts[2], *v_finite;  // [Hkv][n_new][D] the new keys likewise; the new values with zeros for what is not finite
   int* status;
   int G, max_new, limit, rows;           // rows: of a row tile
   int places, min_tiles;                 // CTAs that share the work, and the fewest tiles that are a CTA's worth
@@ -189,10 +197,9 @@ struct alignas(16) Divided {
   int runs, part0, first;   // runs (0: none such); where the first one's result is, and the CTA of the second: those behind it are at 2 first, 2 first + 2, ...
   int h, rt, m, tok0, pad;
 };
-// By one thread of every CTA.
-__device__ __forceinline__ void note_divided(const AttendArgs& a, const Line& line, const Start& st) {
+// By one thread for every CTA.
+__device__ __forceinline__ void note_divided(const AttendArgs& a, const Line& line, const Start& st, int cta) {
   Divided d = {};
-  const int cta = blockIdx.x;
   if (st.left > 0 && st.t > 0) {
     const SeqWork w = seq_work(a, st.s);
     const long long i0 = line.begin(cta) - st.t;   // the item's first tile in the line
@@ -207,7 +214,7 @@ __device__ __forceinline__ void note_divided(const AttendArgs& a, const Line& li
       d.tok0 = w.c.tok0;
     }
   }
-  reinterpret_cast<Divided*>(a.divided)[cta] = d;
+  a.divided[cta] = d;
 }
 
 // A partial result: O [D / 4][rows] of four channels each, then the maxima (log2 domain) and sums of the rows.
@@ -221,15 +228,6 @@ __device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(TH
 __device__ __forceinline__ void bit_set(uint4& m, int i) {
   const uint32_t b = 1u << (i & 31);
   if (i < 32) m.x |= b; else if (i < 64) m.y |= b; else if (i < 96) m.z |= b; else m.w |= b;
-}
-template <int THREADS>
-__device__ __forceinline__ bool meet_and_vote(bool ok) {   // true: all of them are
-  uint32_t bad;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-      "bar.red.or.pred p, 1, %2, q;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-      : "=r"(bad) : "r"(ok ? 0 : 1), "n"(THREADS) : "memory");
-  return bad == 0;
 }
 template <int THREADS>
 __device__ __forceinline__ void find_family(const AttendArgs& a, int tok0, int m, int tid, Family& f) {
@@ -344,7 +342,7 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
   if (warp == 0) {
     const Line line = make_line(a, lane);
     const Start s = find_begin(a, line, blockIdx.x, lane);
-    if (lane == 0) { start = s; note_divided(a, line, s); }
+    if (lane == 0) { start = s; note_divided(a, line, s, blockIdx.x); }
   }
   __syncthreads();
   const bool two = a.rope.half > 0;
@@ -623,77 +621,158 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
 }
 
 // ---- joining the runs ----
-// A block joins 32 rows (16 of the kernel for few) of a divided item: O of its runs brought to one maximum, added in the order of the CTAs.  Grid: the CTAs
-// of the attention times the row groups of a row tile, and one block that checks.
+// A block joins eight rows of a divided item at a time: O of its runs brought to one maximum, added in the order of the CTAs.  The blocks share
+// the divided items' row groups, which each of them lists for itself; one block more checks.
 template <int D>
 __global__ void __launch_bounds__(256) paged_merge_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int kRuns = 32;                // maxima and sums of so many runs at a time in shared memory
-  __shared__ float2 ml[kRuns][32];
-  const int tid = threadIdx.x;
+  constexpr int kRuns = 64, kRows = 8, kStep = 256 / kRows, kMost = D / 4 / kStep > 0 ? D / 4 / kStep : 1;
+  static_assert(kMost == 1, "a float4 a thread");
+  __shared__ float2 ml[kRuns][kRows];      // maxima and sums of so many runs at a time
+  __shared__ short head[kMaxPlaces];       // the CTAs that wrote an item down
+  __shared__ int before[kMaxPlaces + 1];   // row groups of the items before
+  __shared__ int warp_sum[8][2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_front();
   if (blockIdx.x == gridDim.x - 1) { check_attend(a); return; }
-  const Divided d = reinterpret_cast<const Divided*>(a.divided)[blockIdx.x % a.places];
-  const int span = min(a.rows, 32), row0 = blockIdx.x / a.places * span, R = d.m * a.G - d.rt * a.rows;
-  if (d.runs == 0 || row0 >= R) return;
-  const int lane_row = tid % span, row = row0 + lane_row, step = 256 / span;   // rows of neighbouring threads are neighbours
-  constexpr int kMost = D / 32;            // float4 of a thread: 4 (2 with 16 rows)
-  auto part_of = [&](int i) { return part_at(a, i == 0 ? d.part0 : 2 * (d.first + i - 1), D); };
-  float M = -INFINITY, ls = 0.f;
-  float4 ov[kMost];
-#pragma unroll
-  for (int k = 0; k < kMost; ++k) ov[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = 0; i0 < d.runs; i0 += kRuns) {
-    const int n = min(kRuns, d.runs - i0);
+  const Divided* list = a.divided;
+  int items = 0, total = 0;
+  for (int c0 = 0; c0 < a.places; c0 += 256) {
+    int groups = 0;
+    if (c0 + tid < a.places) {
+      const Divided d = list[c0 + tid];
+      if (d.runs > 0) groups = (min(a.rows, d.m * a.G - d.rt * a.rows) + kRows - 1) / kRows;
+    }
+    const int n = warp_scan(groups > 0 ? 1 : 0, lane), g = warp_scan(groups, lane);
     __syncthreads();
-    for (int i = tid / span; i < n; i += step) {
-      const float* p = part_of(i0 + i) + a.rows * D + row;
-      ml[i][lane_row] = make_float2(__ldcg(p), __ldcg(p + a.rows));
-    }
+    if (lane == 31) { warp_sum[warp][0] = n; warp_sum[warp][1] = g; }
     __syncthreads();
-    const float before = M;
-    for (int i = 0; i < n; ++i) {
-      const float2 x = ml[i][lane_row];
-      if (x.y != 0.f) M = fmaxf(M, x.x);   // (nothing counted in a run: its maximum says nothing)
+    int n0 = items, g0 = total;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) { n0 += warp_sum[w][0]; g0 += warp_sum[w][1]; }
+      items += warp_sum[w][0];
+      total += warp_sum[w][1];
     }
-    const float f0 = before == -INFINITY ? 0.f : ex2(before - M);
-    ls *= f0;
-#pragma unroll
-    for (int k = 0; k < kMost; ++k) { ov[k].x *= f0; ov[k].y *= f0; ov[k].z *= f0; ov[k].w *= f0; }
-#pragma unroll 2
-    for (int i = 0; i < n; ++i) {
-      const float4* p = reinterpret_cast<const float4*>(part_of(i0 + i)) + row;
-      float4 x[kMost];
-#pragma unroll
-      for (int k = 0; k < kMost; ++k) {
-        const int c4 = tid / span + k * step;
-        x[k] = c4 < D / 4 ? __ldcg(p + c4 * a.rows) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (groups > 0) { head[n0 + n - 1] = (short)(c0 + tid); before[n0 + n - 1] = g0 + g - groups; }
+  }
+  const int lane_row = tid % kRows, c4 = tid / kRows;   // rows of neighbouring threads are neighbours
+  for (int at = blockIdx.x; at < total; at += gridDim.x - 1) {
+    __syncthreads();   // the list is there; `ml` has been read
+    int lo = 0, hi = items;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before[mid] <= at) lo = mid; else hi = mid;
+    }
+    const Divided d = list[head[lo]];
+    const int row = (at - before[lo]) * kRows + lane_row, R = d.m * a.G - d.rt * a.rows;
+    auto part_of = [&](int i) { return part_at(a, i == 0 ? d.part0 : 2 * (d.first + i - 1), D); };
+    float M = -INFINITY, ls = 0.f;
+    float4 ov = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < d.runs; i0 += kRuns) {
+      const int n = min(kRuns, d.runs - i0);
+      __syncthreads();
+      for (int i = c4; i < n; i += kStep) {
+        const float* p = part_of(i0 + i) + a.rows * D + row;
+        ml[i][lane_row] = make_float2(__ldcg(p), __ldcg(p + a.rows));
       }
-      const float2 w = ml[i][lane_row];
-      const float f = w.y != 0.f ? ex2(w.x - M) : 0.f;
-      ls = fmaf(w.y, f, ls);
-      if (f != 0.f) {
-#pragma unroll
-        for (int k = 0; k < kMost; ++k) {
-          ov[k].x = fmaf(x[k].x, f, ov[k].x); ov[k].y = fmaf(x[k].y, f, ov[k].y);
-          ov[k].z = fmaf(x[k].z, f, ov[k].z); ov[k].w = fmaf(x[k].w, f, ov[k].w);
-        }
+      __syncthreads();
+      const float was = M;
+      for (int i = 0; i < n; ++i) {
+        const float2 x = ml[i][lane_row];
+        if (x.y != 0.f) M = fmaxf(M, x.x);   // (nothing counted in a run: its maximum says nothing)
+      }
+      const float f0 = was == -INFINITY ? 0.f : ex2(was - M);
+      ls *= f0;
+      ov.x *= f0; ov.y *= f0; ov.z *= f0; ov.w *= f0;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const float4 x = c4 < D / 4 ? __ldcg(reinterpret_cast<const float4*>(part_of(i0 + i)) + c4 * a.rows + row) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float2 w = ml[i][lane_row];
+        const float f = w.y != 0.f ? ex2(w.x - M) : 0.f;
+        ls = fmaf(w.y, f, ls);
+        if (f != 0.f) { ov.x = fmaf(x.x, f, ov.x); ov.y = fmaf(x.y, f, ov.y); ov.z = fmaf(x.z, f, ov.z); ov.w = fmaf(x.w, f, ov.w); }
       }
     }
+    if (row >= R || c4 >= D / 4) continue;
+    const int r = d.rt * a.rows + row, tok = r / a.G, q_head = d.h * a.G + r - tok * a.G;
+    const float inv = 1.f / ls;
+    *reinterpret_cast<uint2*>(a.o + q_head * a.o_head + (d.tok0 + tok) * a.o_tok + 4 * c4) =
+        make_uint2(pack_bf16(ov.x * inv, ov.y * inv), pack_bf16(ov.z * inv, ov.w * inv));
+    if (c4 == 0 && a.lse) a.lse[(size_t)q_head * a.p.n_new + d.tok0 + tok] = (M + log2f(ls)) * 0.6931471805599453f;
   }
-  if (row >= R) return;
-  const int r = d.rt * a.rows + row, tok = r / a.G, head = d.h * a.G + r - tok * a.G;
-  const float inv = 1.f / ls;
-  __nv_bfloat16* dst = a.o + head * a.o_head + (d.tok0 + tok) * a.o_tok;
-#pragma unroll
-  for (int k = 0; k < kMost; ++k) {
-    const int c4 = tid / span + k * step;
-    if (c4 < D / 4)
-      *reinterpret_cast<uint2*>(dst + 4 * c4) = make_uint2(pack_bf16(ov[k].x * inv, ov[k].y * inv), pack_bf16(ov[k].z * inv, ov[k].w * inv));
-  }
-  if (tid / span == 0 && a.lse) a.lse[(size_t)head * a.p.n_new + d.tok0 + tok] = (M + log2f(ls)) * 0.6931471805599453f;
 }
 
 // ---- many rows ----
+// The operands of the new tokens, once for all CTAs that work on their items (which would each spend 5 to 15 us on it): which new tokens each one
+// sees, queries and keys rotated and split in two bf16, values without infinities and NaN.  A block takes a query head of a sequence, or a KV head's
+// keys and values.  The first blocks also find where the runs of the CTAs begin.
+template <int D>
+__global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int UNITS = D / 16, kAhead = 2;
+  __shared__ Family fam;
+  __shared__ int odd;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  wait_front();
+  if (blockIdx.x == 0 && tid == 0) *a.status = 0;
+  if (warp == 7 && blockIdx.x < a.places) {
+    const Line line = make_line(a, lane);
+    const Start s = find_begin(a, line, blockIdx.x, lane);
+    if (lane == 0) { a.starts[blockIdx.x] = s; note_divided(a, line, s, blockIdx.x); }
+  }
+  const int heads = a.p.Hkv * (a.G + 1), s = blockIdx.x / heads, which = blockIdx.x - s * heads;
+  if (s >= a.p.n_seqs) return;
+  const SeqCounts c = seq_counts(a.p, s, a.max_new, a.limit);
+  if (c.m == 0) return;
+  if (tid == 0) odd = 0;
+  find_family<256>(a, c.tok0, c.m, tid, fam);
+  const int q_heads = a.p.Hkv * a.G;
+  const bool is_q = which < q_heads, two = a.rope.half > 0;
+  const int h = is_q ? which / a.G : which - q_heads, g = which - h * a.G;
+  const __nv_bfloat16* src = is_q ? a.q + which * a.q_head + c.tok0 * a.q_tok : a.k + h * a.k_head + c.tok0 * a.k_tok;
+  const long long src_tok = is_q ? a.q_tok : a.k_tok;
+  // rows of the result: G to a token for the queries
+  const size_t row0 = (size_t)h * a.p.n_new * (is_q ? a.G : 1) + (size_t)c.tok0 * (is_q ? a.G : 1) + (is_q ? g : 0);
+  __nv_bfloat16 *hi_out = is_q ? a.q_parts[0] : a.k_parts[0], *lo_out = is_q ? a.q_parts[1] : a.k_parts[1];
+  for (int i0 = tid; i0 < c.m * UNITS; i0 += kAhead * 256) {
+    RotUnit u[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int i = min(i0 + x * 256, c.m * UNITS - 1), tok = i / UNITS;
+      load_unit(u[x], src + tok * src_tok, i % UNITS, two ? c.n + depth_of(fam.mask[tok]) : 0, a.rope);
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int i = i0 + x * 256, tok = i / UNITS;
+      if (i >= c.m * UNITS) break;
+      uint4 hi[2], lo[2];
+      turn_unit(u[x], hi, lo);
+      const size_t at = (row0 + (size_t)tok * (is_q ? a.G : 1)) * (D / 8);
+      reinterpret_cast<uint4*>(hi_out)[at + u[x].c0] = hi[0];
+      reinterpret_cast<uint4*>(hi_out)[at + u[x].c1] = hi[1];
+      if (two) {
+        reinterpret_cast<uint4*>(lo_out)[at + u[x].c0] = lo[0];
+        reinterpret_cast<uint4*>(lo_out)[at + u[x].c1] = lo[1];
+      }
+    }
+  }
+  if (is_q) {
+    if (which == 0 && tid < c.m) a.family[c.tok0 + tid] = fam.mask[tid];
+    return;
+  }
+  bool any = false;
+  for (int i = tid; i < c.m * (D / 8); i += 256) {
+    const int tok = i / (D / 8), ch = i % (D / 8);
+    const uint4 y = *reinterpret_cast<const uint4*>(a.v + h * a.v_head + (c.tok0 + tok) * a.v_tok + 8 * ch);
+    any |= odd_chunk(y);
+    reinterpret_cast<uint4*>(a.v_finite)[((size_t)h * a.p.n_new + c.tok0 + tok) * (D / 8) + ch] = finite_chunk(y);
+  }
+  if (any) odd = 1;
+  __syncthreads();
+  if (tid == 0) a.odd[(size_t)s * a.p.Hkv + h] = odd;
+}
+
+constexpr int kFar = 3;   // tiles that are asked for (into L2) ahead of their turn in the ring
+
 template <int D, int TQ>
 struct TileCfg {
   static constexpr int kSub = D / 64;                       // 64-column (128-byte) sub-tiles
@@ -701,29 +780,30 @@ struct TileCfg {
   static constexpr int kStages = D == 64 ? 8 : TQ == 1 ? 5 : 3;   // ring slots
   static constexpr int kQRegion = 2 * kTileBytes;           // rounded, and what that leaves; later the output rows, padded by 16 bytes each
   static constexpr int kRing = TQ * kQRegion, kTail = kRing + kStages * kTileBytes;
-  static constexpr int kSoft = 128 * TQ, kThreads = 128 + kSoft;
+  static constexpr int kThreads = 128 + 128 * TQ;
   static constexpr uint32_t kColO = 0, kColS = TQ * 128, kCols = 2 * TQ * 128;   // tensor memory: O of the row tiles, S with P over it
 };
-struct TileMaps { CUtensorMap k, v; };   // [n_pages * Hkv][page][D], box: 64 channels of a page's rows of a head
-struct TileTail {                        // behind the operand tiles in shared memory
-  uint64_t q_full, new_free[2], kv_full[8], kv_empty[8], s_full[2], pv_done[2], p_full[2][2];
-  Family fam;
+struct TileMaps {
+  CUtensorMap k, v;                // [n_pages * Hkv][page][D], box: 64 channels of a page's rows of a head
+  CUtensorMap q[2], kn[2], vn;     // what paged_operands_kernel made, box: 64 channels of 128 rows
+};
+struct TileTail {                  // behind the operand tiles in shared memory
+  uint64_t q_full, q_free, kv_full[8], kv_empty[8], s_full[2], pv_done[2], p_full[2][2];
   Start start;
   uint32_t tmem;
-  int abort, odd;
+  int abort;
 };
 
 // TQ row tiles of 128 rows (query heads and tokens) over runs of key tiles, one CTA an SM: the structure of the forward (attn_fwd_sm100.cu).  Warp 0
-// brings the pages of a tile, a TMA box for every page and 64 channels, through a ring of K and V tiles; warp 1 issues the products, per key
-// tile and row tile O_t += P_t V_j and then S_t of the next key tile; a warpgroup for each row tile does its softmax, a thread a row.  At the
-// start of an item these warps rotate Q and, where the run holds tile 0, the new tokens into their operand tiles (three ring slots: K, what its
-// rounding leaves, V).  S = Q K^T is formed with both parts of Q.
+// brings Q at the start of an item and the key tiles through a ring, of a page tile a TMA box for every page and 64 channels; warp 1
+// issues the products, per key tile and row tile O_t += P_t V_j and then S_t of the next key tile; a warpgroup for each row tile does its softmax, a
+// thread a row.  S = Q K^T is formed with both parts of Q, for the new tokens (tile 0: three ring slots) with both of K.
 // Pages end where they end: the slots behind the last row of a page, or of the sequence, get no weight, and their V rows are set to zero in
 // shared memory (what lies there belongs to nobody and may be infinite) by the softmax warps of the few tiles that have such slots.
 template <int D, int TQ>
 __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel(const __grid_constant__ TileMaps maps, const __grid_constant__ AttendArgs a) {
   using Cfg = TileCfg<D, TQ>;
-  constexpr int NS = Cfg::kStages, SOFT = Cfg::kSoft;
+  constexpr int NS = Cfg::kStages;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   TileTail& sh = *reinterpret_cast<TileTail*>(smem_raw + Cfg::kTail);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -731,9 +811,11 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
   if (tid == 0) {
     prefetch_tensormap(&maps.k);
     prefetch_tensormap(&maps.v);
-    sh.abort = sh.odd = 0;
+    for (int i = 0; i < 2; ++i) { prefetch_tensormap(&maps.q[i]); prefetch_tensormap(&maps.kn[i]); }
+    prefetch_tensormap(&maps.vn);
+    sh.abort = 0;
     mbar_init(smem_u32(&sh.q_full), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.new_free[i]), 1);
+    mbar_init(smem_u32(&sh.q_free), 4 * TQ);     // one arrival per softmax warp
     for (int i = 0; i < NS; ++i) { mbar_init(smem_u32(&sh.kv_full[i]), 1); mbar_init(smem_u32(&sh.kv_empty[i]), 1); }
     for (int t = 0; t < TQ; ++t) {
       mbar_init(smem_u32(&sh.s_full[t]), 1);
@@ -744,18 +826,14 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
   }
   if (warp == 1) { tmem_alloc(smem_u32(&sh.tmem), Cfg::kCols); tmem_relinquish(); }
   tc_fence_before_sync();
+  wait_front();
+  if (tid == 0) {
+    sh.start = a.starts[blockIdx.x];
+    if (sQ & 1023u) sh.start.left = 0;           // (the operand tiles want 1024 bytes, as declared)
+  }
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = sh.tmem;
-  wait_front();
-  if (blockIdx.x == 0 && tid == 0) *a.status = 0;   // (a wait that runs out does so seconds later)
-  if (warp == 0) {
-    const Line line = make_line(a, lane);
-    Start s = find_begin(a, line, blockIdx.x, lane);
-    if (sQ & 1023u) s.left = 0;                     // (the operand tiles want 1024 bytes, as declared)
-    if (lane == 0) { sh.start = s; note_divided(a, line, s); }
-  }
-  __syncthreads();
   volatile int* abort = &sh.abort;
   const int shift = a.p.shift, per = kKeys >> shift;
   const bool two = a.rope.half > 0;
@@ -773,7 +851,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
       // ---------------- TMA producer: a lane a box ----------------
       const int pi = lane % per, sub = lane / per;      // page of the tile, 64 channels of its rows: at most 16 lanes
       Entry e;
-      int filled = 0, news = 0;                         // entries, tiles of new tokens so far
+      int filled = 0, items = 0;                        // entries, items so far
       bool ok = true;
       while (ok && cursor.next(a, it)) {
         const SeqPages pg = seq_pages(a.p, it.n);
@@ -784,43 +862,74 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           x = (unsigned)x < (unsigned)a.p.n_pages ? x : 0;
           return __shfl_sync(0xffffffffu, x, pi);
         };
+        // into the next entry: waits for its slot, announces the bytes; lane 0 has done so when the others go on
+        auto claim = [&]() {
+          if (ok && filled >= NS) ok = mbar_wait_warp(smem_u32(&sh.kv_empty[e.slot]), e.phase ^ 1, abort);
+          if (ok && lane == 0) mbar_expect_tx(smem_u32(&sh.kv_full[e.slot]), Cfg::kTileBytes);
+          __syncwarp();
+          return ok;
+        };
+        auto pass = [&]() { e.next(); ++filled; };
+        // Q: both parts of the row tiles that have rows (rows behind the item's are other items', and nobody looks at theirs)
+        const int row_tiles = TQ == 2 && it.rt * a.rows + kTile < it.m * a.G ? 2 : 1, parts = two ? 2 : 1;
+        if (items > 0) ok = mbar_wait_warp(smem_u32(&sh.q_free), (items - 1) & 1, abort);
+        if (!ok) break;
+        ++items;
+        if (lane == 0) mbar_expect_tx(smem_u32(&sh.q_full), row_tiles * parts * Cfg::kTileBytes);
+        __syncwarp();
+        if (lane < row_tiles * parts * Cfg::kSub) {
+          const int x = lane % Cfg::kSub, lo = lane / Cfg::kSub % parts, t = lane / Cfg::kSub / parts;
+          tma_load_3d(sQ + t * Cfg::kQRegion + lo * Cfg::kTileBytes + x * Cfg::kSubBytes, &maps.q[lo], x * 64, it.tok0 * a.G + it.rt * a.rows + t * kTile,
+                      it.h, smem_u32(&sh.q_full));
+        }
         int tile = it.t0;
         if (tile == 0) {
-          // Written by the softmax warps, who are told when the three slots are free.  (This warp waits for every entry: a wait tells a phase from
-          // the one in front of it only, and a role that skips one may take an older phase for its own, or miss two.)
-          for (int i = 0; i < 3; ++i, ++filled, e.next())
-            if (ok && filled >= NS) ok = mbar_wait_warp(smem_u32(&sh.kv_empty[e.slot]), e.phase ^ 1, abort);
-          if (!ok) break;
-          if (lane == 0) mbar_arrive(smem_u32(&sh.new_free[news & 1]));
-          ++news;
+          for (int i = 0; i < 3 && claim(); ++i, pass()) {
+            const CUtensorMap* map = i == 0 ? &maps.kn[0] : i == 1 ? &maps.kn[two ? 1 : 0] : &maps.vn;   // (unrotated keys leave no rest: never multiplied)
+            if (lane < Cfg::kSub)
+              tma_load_3d(sRing + e.slot * Cfg::kTileBytes + lane * Cfg::kSubBytes, map, lane * 64, it.tok0, it.h, smem_u32(&sh.kv_full[e.slot]));
+          }
           ++tile;
         }
-        int next = tile < it.t1 ? page_at(tile) : 0;
+        // the page numbers of the next tiles; their rows are brought into L2 kFar tiles ahead of the ring, which holds little more than a tile
+        int far[kFar];
+        auto fetch = [&](int page) {
+          if (sub < Cfg::kSub) {
+            tma_prefetch_3d(&maps.k, sub * 64, 0, page * a.p.Hkv + it.h);
+            tma_prefetch_3d(&maps.v, sub * 64, 0, page * a.p.Hkv + it.h);
+          }
+        };
+#pragma unroll
+        for (int i = 0; i < kFar; ++i) {
+          far[i] = tile + i < it.t1 ? page_at(tile + i) : 0;
+          if (i > 0 && tile + i < it.t1) fetch(far[i]);
+        }
         for (; tile < it.t1 && ok; ++tile) {
-          const int page = next;
-          if (tile + 1 < it.t1) next = page_at(tile + 1);
+          const int page = far[0];
+#pragma unroll
+          for (int i = 0; i + 1 < kFar; ++i) far[i] = far[i + 1];
+          if (tile + kFar < it.t1) {
+            far[kFar - 1] = page_at(tile + kFar);
+            fetch(far[kFar - 1]);
+          }
 #pragma unroll
           for (int which = 0; which < 2; ++which) {
-            if (ok && filled >= NS) ok = mbar_wait_warp(smem_u32(&sh.kv_empty[e.slot]), e.phase ^ 1, abort);
-            if (!ok) break;
-            const uint32_t full = smem_u32(&sh.kv_full[e.slot]);
-            if (lane == 0) mbar_expect_tx(full, Cfg::kTileBytes);
-            __syncwarp();
+            if (!claim()) break;
             if (sub < Cfg::kSub)
               tma_load_3d(sRing + e.slot * Cfg::kTileBytes + sub * Cfg::kSubBytes + (pi << shift) * 128, which ? &maps.v : &maps.k, sub * 64, 0,
-                          page * a.p.Hkv + it.h, full);
-            e.next();
-            ++filled;
+                          page * a.p.Hkv + it.h, smem_u32(&sh.kv_full[e.slot]));
+            pass();
           }
         }
       }
       if (!ok) {
-        // loads in flight land before the CTA's shared memory is released (a bounded wait: entries that nobody fills run it out)
-        for (int i = 0; i < NS; ++i) {
+        // loads in flight land before the CTA's shared memory is released (bounded waits)
+        auto drain = [&](uint64_t* bar, int phase) {
           const long long t0 = clock64();
-          const int phase = i < e.slot ? e.phase : e.phase ^ 1;   // of the slot's last entry
-          while (!mbar_try_wait(smem_u32(&sh.kv_full[i]), phase) && clock64() - t0 < 2000000) {}
-        }
+          while (!mbar_try_wait(smem_u32(bar), phase) && clock64() - t0 < 2000000) {}
+        };
+        if (items > 0) drain(&sh.q_full, (items - 1) & 1);
+        for (int i = 0; i < NS && i < filled; ++i) drain(&sh.kv_full[i], i < e.slot ? e.phase : e.phase ^ 1);   // of the slot's last entry
       }
     } else if (warp == 1) {
       // ---------------- issuer (the products run in the order of issue, sm100_ptx.h) ----------------
@@ -843,18 +952,17 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
             umma_ss4(tmem + Cfg::kColS + t * kTile, desc_advance(dQ, h * Cfg::kSubBytes), desc_advance(dK, h * Cfg::kSubBytes), idesc_qk,
                      more || h > 0 ? 1u : 0u, leader);
         };
-        int rest = -1;              // slot of what the rounding of the new keys left, where the next tile has one
         Entry v;                    // of the tile whose P comes next
         for (int j = -1; j < n && ok; ++j) {
           if (j >= 0) {
             ok = mbar_wait_warp(smem_u32(&sh.kv_full[v.slot]), v.phase, abort);
             if (!ok) break;
           }
-          Entry k = e;
-          const bool more = j + 1 < n;
+          Entry k = e, rest = e;    // rest: of what the rounding of the new keys left, where the next tile has it
+          const bool more = j + 1 < n, fresh = it.t0 + j + 1 == 0;
           if (more) {
             e.next();
-            if (it.t0 + j + 1 == 0) { rest = e.slot; e.next(); } else rest = -1;
+            if (fresh) { rest = e; e.next(); }
           }
           const uint64_t dV = desc_advance(descV0, v.slot * Cfg::kTileBytes);
           bool k_here = false;
@@ -877,6 +985,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
             if (more) {
               if (!k_here) {
                 ok = mbar_wait_warp(smem_u32(&sh.kv_full[k.slot]), k.phase, abort);
+                if (ok && fresh) ok = mbar_wait_warp(smem_u32(&sh.kv_full[rest.slot]), rest.phase, abort);
                 if (!ok) break;
                 k_here = true;
               }
@@ -884,7 +993,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
               scores(t, 0, k.slot, false);
               if (two) {
                 scores(t, 1, k.slot, true);
-                if (rest >= 0) scores(t, 0, rest, true);
+                if (fresh) scores(t, 0, rest.slot, true);
               }
               umma_commit(smem_u32(&sh.s_full[t]), leader);
             }
@@ -893,7 +1002,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           if (j >= 0) umma_commit(smem_u32(&sh.kv_empty[v.slot]), leader);
           if (more) {
             umma_commit(smem_u32(&sh.kv_empty[k.slot]), leader);
-            if (rest >= 0) umma_commit(smem_u32(&sh.kv_empty[rest]), leader);
+            if (fresh) umma_commit(smem_u32(&sh.kv_empty[rest.slot]), leader);
             v = e;
             e.next();
           }
@@ -904,74 +1013,21 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
     if constexpr (TQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ---------------- softmax + epilogue: warpgroup t owns row tile t, one thread per row ----------------
     constexpr int CPR = D / 8;
-    const int t = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane, st = tid - 128;
+    const int t = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16, S_addr = tmem + lane_addr + Cfg::kColS + t * kTile, O_addr = tmem + lane_addr + Cfg::kColO + t * kTile;
     const float c = a.scale_log2;
-    // Operand tiles: chunk x of row r at sub-tile x / 8, row r, place (x % 8) ^ (r % 8)
-    auto place = [&](int offset, int r, int x) {
-      return reinterpret_cast<uint4*>(smem_raw + offset + (x >> 3) * Cfg::kSubBytes + r * 128 + (((x & 7) ^ (r & 7)) << 4));
-    };
     bool ok = true;
     Entry e;
-    int news = 0, count = 0;       // tiles of new tokens, and of this warpgroup, so far
-    while (cursor.next(a, it)) {
-      const int n = it.t1 - it.t0, R = it.m * a.G, r0 = it.rt * a.rows;
-      const bool mine = r0 + t * kTile < R;      // this warpgroup has rows
+    int count = 0, items = 0;      // tiles of this warpgroup, items so far
+    while (ok && cursor.next(a, it)) {
+      // (a warpgroup without rows waits here too: it must not tell that it is done with an item ahead of the others)
+      ok = mbar_wait_warp(smem_u32(&sh.q_full), items++ & 1, abort);
+      if (!ok) break;
+      const int n = it.t1 - it.t0, R = it.m * a.G, r0 = it.rt * a.rows + t * kTile;
+      const bool mine = r0 < R;    // this warpgroup has rows
       const SeqPages pg = seq_pages(a.p, it.n);
-      ok = meet_and_vote<SOFT>(ok);              // everybody is done with the item in front: Q's tiles and `odd` may be written
-      if (!ok) break;                            // (all of them leave together: a warp that left alone would be waited for at the barrier)
-      if (st == 0) sh.odd = 0;
-      find_family<SOFT>(a, it.tok0, it.m, st, sh.fam);
-      for (int i = st; i < TQ * kTile * CPR; i += SOFT) {
-        const int r = i / CPR, x = i % CPR;
-        if (r0 + (r & ~(kTile - 1)) >= R) break;   // a row tile without rows
-        uint4 hi = make_uint4(0, 0, 0, 0), lo = hi;
-        if (r0 + r < R) {
-          const int tok = (r0 + r) / a.G, head = it.h * a.G + r0 + r - tok * a.G;
-          const __nv_bfloat16* src = a.q + head * a.q_head + (it.tok0 + tok) * a.q_tok;
-          hi = two ? rotated_chunk(src, x, it.n + depth_of(sh.fam.mask[tok]), a.rope, lo) : *reinterpret_cast<const uint4*>(src + 8 * x);
-        }
-        const int at = (r >> 7) * Cfg::kQRegion;
-        *place(at, r & 127, x) = hi;
-        if (two) *place(at + Cfg::kTileBytes, r & 127, x) = lo;
-      }
-      uint32_t fresh[3];   // barriers of the slots of the new tokens
-      if (it.t0 == 0) {
-        int slot[3];
-        Entry f = e;
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          slot[i] = Cfg::kRing + f.slot * Cfg::kTileBytes;
-          fresh[i] = smem_u32(&sh.kv_full[f.slot]);
-          f.next();
-        }
-        // (two barriers in turn: with eight slots the next item's may be free before this one's have been asked for, a third's may not)
-        ok = mbar_wait_warp(smem_u32(&sh.new_free[news & 1]), news >> 1 & 1, abort);
-        ++news;
-        bool any = false;
-        for (int i = st; ok && i < kTile * CPR; i += SOFT) {
-          const int r = i / CPR, x = i % CPR;
-          uint4 hi = make_uint4(0, 0, 0, 0), lo = hi, y = hi;
-          if (r < it.m) {
-            const __nv_bfloat16 *kr = a.k + it.h * a.k_head + (it.tok0 + r) * a.k_tok, *vr = a.v + it.h * a.v_head + (it.tok0 + r) * a.v_tok;
-            hi = two ? rotated_chunk(kr, x, it.n + depth_of(sh.fam.mask[r]), a.rope, lo) : *reinterpret_cast<const uint4*>(kr + 8 * x);
-            y = *reinterpret_cast<const uint4*>(vr + 8 * x);
-            any |= odd_chunk(y);
-            y = finite_chunk(y);
-          }
-          *place(slot[0], r, x) = hi;
-          if (two) *place(slot[1], r, x) = lo;
-          *place(slot[2], r, x) = y;
-        }
-        if (any) sh.odd = 1;
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // for the products that read them
-      meet<SOFT>();
-      if (st == 0) {
-        mbar_arrive(smem_u32(&sh.q_full));
-        if (it.t0 == 0)
-          for (int i = 2; i >= 0; --i) mbar_arrive(fresh[i]);   // (K last: the products wait for it and for V, not for the one between)
-      }
+      uint4 own = make_uint4(0, 0, 0, 0);
+      if (it.t0 == 0 && mine) own = a.family[it.tok0 + min((r0 + row) / a.G, it.m - 1)];
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n && ok; ++j) {
         const int tile = it.t0 + j;
@@ -984,32 +1040,32 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
         tc_fence_after_sync();
         // the slots that this row sees; the same for all rows but among the new tokens
         bool whole = false;
-        uint32_t see[4] = {0, 0, 0, 0};
-        if (tile == 0) {
-          const uint4 own = sh.fam.mask[min((r0 + t * kTile + row) / a.G, it.m - 1)];
-          see[0] = own.x; see[1] = own.y; see[2] = own.z; see[3] = own.w;
-        } else {
+        uint32_t see[4] = {own.x, own.y, own.z, own.w};
+        bool used = row < it.m;      // V row `row` of the tile belongs to somebody
+        if (tile > 0) {
           const int f0 = (tile - 1) * per, front = (pg.sinks + (1 << shift) - 1) >> shift, recent = front + pg.w * a.p.kp;
           whole = (f0 >= front && f0 + per <= recent && a.p.kp << shift == a.p.K) || (f0 >= recent && (f0 + per - recent) << shift <= pg.ra);
           if (!whole) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const int key = 32 * q + lane;
-              int count;
-              page_column(a.p, pg, f0 + (key >> shift), count);
-              see[q] = __ballot_sync(0xffffffffu, (key & ((1 << shift) - 1)) < count);
+              int rows;
+              page_column(a.p, pg, f0 + (key >> shift), rows);
+              see[q] = __ballot_sync(0xffffffffu, (key & ((1 << shift) - 1)) < rows);
             }
-            // rows of V that belong to nobody: zero (the products with them start behind this thread's arrival below)
-            ok = mbar_wait_warp(smem_u32(&sh.kv_full[v.slot]), v.phase, abort);
-            if (!ok) break;
-            const uint32_t word = quad == 0 ? see[0] : quad == 1 ? see[1] : quad == 2 ? see[2] : see[3];
-            if (!(word >> lane & 1u)) {
-              unsigned char* dst = smem_raw + Cfg::kRing + v.slot * Cfg::kTileBytes + row * 128;
-#pragma unroll
-              for (int x = 0; x < CPR; ++x) *reinterpret_cast<uint4*>(dst + (x >> 3) * Cfg::kSubBytes + ((x & 7) << 4)) = make_uint4(0, 0, 0, 0);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            used = ((quad == 0 ? see[0] : quad == 1 ? see[1] : quad == 2 ? see[2] : see[3]) >> lane & 1u) != 0;
           }
+        }
+        if (!whole) {
+          // rows of V that belong to nobody: zero (the products with them start behind this thread's arrival below)
+          ok = mbar_wait_warp(smem_u32(&sh.kv_full[v.slot]), v.phase, abort);
+          if (!ok) break;
+          if (!used) {
+            unsigned char* dst = smem_raw + Cfg::kRing + v.slot * Cfg::kTileBytes + row * 128;
+#pragma unroll
+            for (int x = 0; x < CPR; ++x) *reinterpret_cast<uint4*>(dst + (x >> 3) * Cfg::kSubBytes + ((x & 7) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         uint32_t s[kTile];
 #pragma unroll
@@ -1091,13 +1147,12 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
       if (ok && mine) ok = mbar_wait_warp(smem_u32(&sh.pv_done[t]), (count - 1) & 1, abort);
       if (ok && mine) {
         tc_fence_after_sync();
-        const int rr = r0 + t * kTile + row;
-        const bool add_odd = it.t0 == 0 && sh.odd;
-        const uint4 seen = sh.fam.mask[min(rr / a.G, it.m - 1)];
+        const int rr = r0 + row;
+        const bool add_odd = it.t0 == 0 && a.odd[(size_t)it.s * a.p.Hkv + it.h];
         float* part = it.part >= 0 ? part_at(a, it.part, D) : nullptr;
         const float inv = 1.0f / l;
         constexpr int kStride = D * 2 + 16;
-        unsigned char* stage = smem_raw + t * Cfg::kQRegion + quad * 32 * kStride;   // rows of this warp, over Q, which is no longer needed
+        unsigned char* stage = smem_raw + t * Cfg::kQRegion + quad * 32 * kStride;   // rows of this warp, over Q_t, which is no longer needed
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
           uint32_t o[32];
@@ -1106,7 +1161,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           if (add_odd) {
 #pragma unroll 1
             for (int i = 0; i < 32; ++i) {
-              const float add = odd_values(a, it, seen, 32 * q + i);
+              const float add = odd_values(a, it, own, 32 * q + i);
 #pragma unroll
               for (int x = 0; x < 32; ++x)
                 if (x == i) o[x] = __float_as_uint(__uint_as_float(o[x]) + add);
@@ -1137,15 +1192,19 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           __syncwarp();
           // whole rows: neighbouring lanes take neighbouring chunks
           for (int r = lane / CPR; r < 32; r += 32 / CPR) {
-            const int x = r0 + t * kTile + quad * 32 + r;
+            const int x = r0 + quad * 32 + r;
             if (x >= R) break;
             const int tok = x / a.G, head = it.h * a.G + x - tok * a.G;
             reinterpret_cast<uint4*>(a.o + head * a.o_head + (it.tok0 + tok) * a.o_tok)[lane % CPR] =
                 *reinterpret_cast<const uint4*>(stage + r * kStride + (lane % CPR) * 16);
           }
+          __syncwarp();
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the next Q is written there by TMA
         }
         tc_fence_before_sync();   // O and S have been read: the next item's products may write them
       }
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(smem_u32(&sh.q_free));
     }
   }
   tc_fence_before_sync();
@@ -1161,19 +1220,43 @@ bool rows_ok(const lrsa_rows_t* r) {
 // Fewest key tiles that are a CTA's worth.
 constexpr int kMinTilesFew = 2, kMinTiles = 2;
 
-constexpr size_t kDividedBytes = (kMaxPlaces * sizeof(Divided) + 255) / 256 * 256;
-size_t attend_ws_bytes(int d) { return sizeof(WsHeader) + kDividedBytes + (size_t)2 * kSms * 2 * kTile * (d + 2) * sizeof(float); }
-static_assert(2 * kMaxPlaces * kFewRows <= 2 * kSms * 2 * kTile, "partial results of the kernel for few rows");
+// The parts of the workspace.  few: of a call that the kernel for few rows takes.
+struct AttendWs { size_t starts, divided, part, family, odd, q[2], k[2], v, total; };
+AttendWs attend_ws(const Geom& g, long long n_seqs, long long n_new, bool few) {
+  AttendWs w;
+  size_t off = sizeof(WsHeader);
+  auto take = [&off](size_t bytes) { const size_t at = off; off += align_up(bytes, 256); return at; };
+  w.starts = take(kMaxPlaces * sizeof(Start));
+  w.divided = take(kMaxPlaces * sizeof(Divided));
+  w.part = take((few ? (size_t)2 * kMaxPlaces * kFewRows : (size_t)2 * kSms * 2 * kTile) * (g.d + 2) * sizeof(float));
+  if (few) n_seqs = n_new = 0;
+  w.family = take(n_new * sizeof(uint4));
+  w.odd = take(n_seqs * g.Hkv * sizeof(int));
+  for (size_t& q : w.q) q = take((size_t)n_new * g.Hq * g.d * 2);
+  for (size_t& k : w.k) k = take((size_t)n_new * g.Hkv * g.d * 2);
+  w.v = take((size_t)n_new * g.Hkv * g.d * 2);
+  w.total = off;
+  return w;
+}
 
 template <int D, int TQ>
 int launch_tile(AttendArgs& a, cudaStream_t st) {
   using Cfg = TileCfg<D, TQ>;
   a.rows = TQ * kTile; a.places = kSms; a.min_tiles = kMinTiles;
   TileMaps maps;
-  const long long outer = (long long)a.p.n_pages * a.p.Hkv;
+  const long long outer = (long long)a.p.n_pages * a.p.Hkv, Hkv = a.p.Hkv, T = a.p.n_new > 0 ? a.p.n_new : 1;
   int rc = make_tmap_bf16(&maps.k, a.k_pages, D, 1 << a.p.shift, outer, 1 << a.p.shift);
   if (rc == LRSA_OK) rc = make_tmap_bf16(&maps.v, a.v_pages, D, 1 << a.p.shift, outer, 1 << a.p.shift);
+  for (int i = 0; i < 2; ++i) {
+    if (rc == LRSA_OK) rc = make_tmap_bf16(&maps.q[i], a.q_parts[i], D, T * a.G, Hkv, kTile);
+    if (rc == LRSA_OK) rc = make_tmap_bf16(&maps.kn[i], a.k_parts[i], D, T, Hkv, kTile);
+  }
+  if (rc == LRSA_OK) rc = make_tmap_bf16(&maps.vn, a.v_finite, D, T, Hkv, kTile);
   if (rc != LRSA_OK) return rc;
+  const long long blocks = (long long)a.p.n_seqs * Hkv * (a.G + 1), grid = blocks > a.places ? blocks : a.places;
+  if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
+  LRSA_CUDA_CHECK(launch_dependent(paged_operands_kernel<D>, dim3((unsigned)grid), dim3(256), 0, st, 1, a));
+  launch_counter().n++;
   constexpr size_t smem = Cfg::kTail + sizeof(TileTail);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
   LRSA_CUDA_CHECK(cudaFuncSetAttribute(paged_tile_kernel<D, TQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
@@ -1196,7 +1279,7 @@ int launch_attend(AttendArgs a, long long max_rows, cudaStream_t st) {
                                         : launch_tile<D, 2>(a, st);
   if (rc != LRSA_OK) return rc;
   launch_counter().n++;
-  LRSA_CUDA_CHECK(launch_dependent(paged_merge_kernel<D>, dim3(a.places * ((a.rows + 31) / 32) + 1), dim3(256), 0, st, 1, a));
+  LRSA_CUDA_CHECK(launch_dependent(paged_merge_kernel<D>, dim3(4 * kSms), dim3(256), 0, st, 1, a));
   launch_counter().n++;
   return LRSA_OK;
 }
@@ -1208,16 +1291,18 @@ using namespace lrsa;
 
 extern "C" {
 
-int lrsa_paged_shape(const lrsa_params_t* params, int32_t page, int32_t* table_width, int32_t* w_cap, size_t* workspace_bytes) {
+int lrsa_paged_shape(const lrsa_params_t* params, int32_t page, int32_t n_seqs, int32_t n_new, int32_t max_new, int32_t* table_width, int32_t* w_cap,
+                     size_t* workspace_bytes) {
   lrsa_paged_t paged = {};
   paged.page = page;
+  if (n_seqs < 0 || n_new < 0 || max_new < 0) return LRSA_ERR_INVALID_ARG;
   Geom g;
   PageGeom p;
   const int rc = make_pages(params, &paged, &g, &p);
   if (rc != LRSA_OK) return rc;
   if (table_width) *table_width = p.width;
   if (w_cap) *w_cap = p.w_cap;
-  if (workspace_bytes) *workspace_bytes = attend_ws_bytes(g.d);
+  if (workspace_bytes) *workspace_bytes = max_new > 0 ? attend_ws(g, n_seqs, n_new, (long long)max_new * g.G <= kFewRows).total : sizeof(WsHeader);
   return LRSA_OK;
 }
 
@@ -1242,7 +1327,9 @@ int lrsa_paged_attend(const lrsa_params_t* params, const lrsa_paged_t* paged, co
   if (((bits(paged->k_pages) | bits(paged->v_pages)) & 15u) ||
       ((bits(paged->table) | bits(paged->n_tokens) | bits(cu_new) | bits(parent) | bits(lse)) & 3u) || (bits(workspace) & 255u))
     return LRSA_ERR_INVALID_ARG;
-  if (workspace_bytes < attend_ws_bytes(g.d)) return LRSA_ERR_WORKSPACE_TOO_SMALL;
+  const long long max_rows = (long long)max_new * g.G;
+  const AttendWs ws = attend_ws(g, paged->n_seqs, n_new, max_rows <= kFewRows);
+  if (workspace_bytes < ws.total) return LRSA_ERR_WORKSPACE_TOO_SMALL;
   a.p.cu = cu_new; a.p.n_new = n_new;
   a.k_pages = static_cast<const __nv_bfloat16*>(paged->k_pages); a.v_pages = static_cast<const __nv_bfloat16*>(paged->v_pages);
   if (n_new > 0) {
@@ -1253,12 +1340,20 @@ int lrsa_paged_attend(const lrsa_params_t* params, const lrsa_paged_t* paged, co
   }
   a.parent = parent; a.lse = lse;
   a.status = &static_cast<WsHeader*>(workspace)->status;
-  a.divided = static_cast<unsigned char*>(workspace) + sizeof(WsHeader);
-  a.part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + sizeof(WsHeader) + kDividedBytes);
+  auto at = [workspace](size_t offset) { return static_cast<void*>(static_cast<unsigned char*>(workspace) + offset); };
+  a.starts = static_cast<Start*>(at(ws.starts));
+  a.divided = static_cast<Divided*>(at(ws.divided));
+  a.part = static_cast<float*>(at(ws.part));
+  a.family = static_cast<uint4*>(at(ws.family));
+  a.odd = static_cast<int*>(at(ws.odd));
+  for (int i = 0; i < 2; ++i) {
+    a.q_parts[i] = static_cast<__nv_bfloat16*>(at(ws.q[i]));
+    a.k_parts[i] = static_cast<__nv_bfloat16*>(at(ws.k[i]));
+  }
+  a.v_finite = static_cast<__nv_bfloat16*>(at(ws.v));
   a.G = g.G; a.max_new = max_new;
   a.limit = a.rope.half > 0 ? a.rope.n_pos : 0x7fffffff;
   a.scale = g.scale; a.scale_log2 = g.scale * 1.4426950408889634f;
-  const long long max_rows = (long long)max_new * g.G;
   auto st = static_cast<cudaStream_t>(cuda_stream);
   return g.d == 128 ? launch_attend<128>(a, max_rows, st) : launch_attend<64>(a, max_rows, st);
 }

@@ -76,20 +76,74 @@ __device__ __forceinline__ uint4 rotated_chunk(const __nv_bfloat16* row, int c, 
   turned_channels(row, c, pos, r, y);
   return pack_channels(y);
 }
+// What the rounding to hi left of y, rounded to bf16.
+__device__ __forceinline__ uint4 rest_of(const float (&y)[8], const uint4& hi) {
+  const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
+  float z[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float a = y[2 * e] - bf16_lo(h[e]), b = y[2 * e + 1] - bf16_hi(h[e]);
+    z[2 * e] = fabsf(a) < INFINITY ? a : 0.f;           // (an infinity or NaN is all in the first)
+    z[2 * e + 1] = fabsf(b) < INFINITY ? b : 0.f;
+  }
+  return pack_channels(z);
+}
 // The chunk rotated, as the sum of two bf16: rounded, and what that leaves (2^-17 of a channel is lost).  For operands of products.
 __device__ __forceinline__ uint4 rotated_chunk(const __nv_bfloat16* row, int c, int pos, const RopeArgs& r, uint4& rest) {
   float y[8];
   turned_channels(row, c, pos, r, y);
   const uint4 hi = pack_channels(y);
-  const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float a = y[2 * e] - bf16_lo(h[e]), b = y[2 * e + 1] - bf16_hi(h[e]);
-    y[2 * e] = fabsf(a) < INFINITY ? a : 0.f;           // (an infinity or NaN is all in the first)
-    y[2 * e + 1] = fabsf(b) < INFINITY ? b : 0.f;
-  }
-  rest = pack_channels(y);
+  rest = rest_of(y, hi);
   return hi;
+}
+
+// The same for two chunks at a time, which is what a row's D / 16 units are: partners of one another, or neighbours.  Loads and arithmetic
+// apart, so that a thread may ask for several units before it works on one.
+struct RotUnit {
+  uint4 x, y;          // chunks c0 and c1
+  float4 cs[2], sn[2];
+  int c0, c1, kind;    // 0: not rotated, 1: partners, 2: pairs of neighbours
+};
+__device__ __forceinline__ void load_unit(RotUnit& u, const __nv_bfloat16* row, int unit, int pos, const RopeArgs& r) {
+  const int m = r.half >> 3;
+  u.kind = unit >= m ? 0 : r.interleaved ? 2 : 1;
+  u.c0 = u.kind == 1 ? unit : 2 * unit;
+  u.c1 = u.kind == 1 ? unit + m : u.c0 + 1;
+  u.x = *reinterpret_cast<const uint4*>(row + 8 * u.c0);
+  u.y = *reinterpret_cast<const uint4*>(row + 8 * u.c1);
+  if (u.kind != 0) {
+    const float4* cs = reinterpret_cast<const float4*>(r.cos + (size_t)pos * r.half + 8 * unit);
+    const float4* sn = reinterpret_cast<const float4*>(r.sin + (size_t)pos * r.half + 8 * unit);
+    u.cs[0] = cs[0]; u.cs[1] = cs[1]; u.sn[0] = sn[0]; u.sn[1] = sn[1];
+  }
+}
+// hi: the chunks rounded to bf16; lo: what that leaves, rounded to bf16
+__device__ __forceinline__ void turn_unit(const RotUnit& u, uint4 (&hi)[2], uint4 (&lo)[2]) {
+  hi[0] = u.x; hi[1] = u.y;
+  lo[0] = lo[1] = make_uint4(0, 0, 0, 0);
+  if (u.kind == 0) return;
+  const uint32_t xs[4] = {u.x.x, u.x.y, u.x.z, u.x.w}, ys[4] = {u.y.x, u.y.y, u.y.z, u.y.w};
+  const float c[8] = {u.cs[0].x, u.cs[0].y, u.cs[0].z, u.cs[0].w, u.cs[1].x, u.cs[1].y, u.cs[1].z, u.cs[1].w};
+  const float s[8] = {u.sn[0].x, u.sn[0].y, u.sn[0].z, u.sn[0].w, u.sn[1].x, u.sn[1].y, u.sn[1].z, u.sn[1].w};
+  float a[8], b[8];
+  if (u.kind == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = e & 1 ? bf16_hi(xs[e >> 1]) : bf16_lo(xs[e >> 1]), q = e & 1 ? bf16_hi(ys[e >> 1]) : bf16_lo(ys[e >> 1]);
+      a[e] = turn(p, q, c[e], -s[e]);
+      b[e] = turn(q, p, c[e], s[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[2 * e] = turn(bf16_lo(xs[e]), bf16_hi(xs[e]), c[e], -s[e]);
+      a[2 * e + 1] = turn(bf16_hi(xs[e]), bf16_lo(xs[e]), c[e], s[e]);
+      b[2 * e] = turn(bf16_lo(ys[e]), bf16_hi(ys[e]), c[4 + e], -s[4 + e]);
+      b[2 * e + 1] = turn(bf16_hi(ys[e]), bf16_lo(ys[e]), c[4 + e], s[4 + e]);
+    }
+  }
+  hi[0] = pack_channels(a); hi[1] = pack_channels(b);
+  lo[0] = rest_of(a, hi[0]); lo[1] = rest_of(b, hi[1]);
 }
 
 // ---- pages ----

@@ -156,7 +156,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
         rp, gp, wp = ctypes.POINTER(lrsa_rope_t), ctypes.POINTER(lrsa_paged_t), ctypes.POINTER(lrsa_rows_t)
         L.lrsa_rotate.argtypes = [pp, vp, vp, vp, vp, rp, i32p, i32, vp]
-        L.lrsa_paged_shape.argtypes = [pp, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
+        L.lrsa_paged_shape.argtypes = [pp, i32, i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]
         L.lrsa_paged_append.argtypes = [pp, gp, wp, wp, i32, vp, i32, vp, rp, vp, vp, sz, vp]
         L.lrsa_paged_attend.argtypes = [pp, gp, wp, wp, wp, vp, i32, i32, vp, rp, wp, fp, vp, sz, vp]
         for name in ("lrsa_rotate", "lrsa_paged_shape", "lrsa_paged_append", "lrsa_paged_attend"):
@@ -743,15 +743,35 @@ class PagedCache:
 
     def __init__(self, params: Params, n_pages: int, page: int = 64, device="cuda"):
         self.params, self.page, self.n_pages = params, page, n_pages
-        width, cap, ws = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_size_t(0)
-        _check(lib().lrsa_paged_shape(params.ref(), page, ctypes.byref(width), ctypes.byref(cap), ctypes.byref(ws)), "lrsa_paged_shape")
+        width, cap = ctypes.c_int32(0), ctypes.c_int32(0)
+        _check(lib().lrsa_paged_shape(params.ref(), page, 0, 0, 0, ctypes.byref(width), ctypes.byref(cap), None), "lrsa_paged_shape")
         if n_pages < 1:
             raise LrsaError(1, f"PagedCache: {n_pages} pages")
         self.table_width, self.w_cap = width.value, cap.value
         self._shape = torch.Size((n_pages, params.n_kv_heads, page, params.head_dim))
         self.k_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
         self.v_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
-        self.ws = new_workspace(ws.value, device)
+        self.ws = new_workspace(self.workspace_bytes(1, 1, 1), device)
+        self._need, self._old = {}, []
+
+    def workspace_bytes(self, n_seqs: int, n_new: int, max_new: int) -> int:
+        """What an attend of n_new tokens of n_seqs sequences, at most max_new each, takes."""
+        out = ctypes.c_size_t(0)
+        _check(lib().lrsa_paged_shape(self.params.ref(), self.page, n_seqs, n_new, max_new, None, None, ctypes.byref(out)), "lrsa_paged_shape")
+        return out.value
+
+    def _workspace(self, near, stream, *sizes):
+        """The workspace, at least as large as an attend of these sizes needs.  One that was outgrown stays where it is: a captured
+        call may hold its address."""
+        need = self._need.get(sizes)
+        if need is None:
+            if len(self._need) > 4096:
+                self._need.clear()
+            need = self._need[sizes] = self.workspace_bytes(*sizes)
+        if self.ws.numel() < need:
+            self._old.append(self.ws)
+            self.ws = _made(stream, near, new_workspace, need, near.device)
+        return self.ws
 
     def columns(self, n_tokens: int):
         """Columns of the page table that a sequence of n_tokens has reached: those that need a page."""
@@ -836,10 +856,11 @@ class PagedCache:
             lse = _made(stream, q, torch.empty, (p.n_q_heads, n), dtype=torch.float32, device=q.device)
         else:
             _expect(where, "lse", lse, (p.n_q_heads, n), torch.float32, dev)
-        cp, ws = p.struct(), self.ws
-        status = call.paged_attend(ctypes.addressof(cp), *pages, *qa, *ka, *va, cu_new.data_ptr(), n,
-                                   max(1, min(n, self.MOST_NEW)) if max_new is None else max_new, _p(parent), *_rope_args(where, rope, dev),
-                                   *oa, lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
+        if max_new is None:
+            max_new = max(1, min(n, self.MOST_NEW))
+        cp, ws = p.struct(), self._workspace(q, stream, pages[2], n, max_new)
+        status = call.paged_attend(ctypes.addressof(cp), *pages, *qa, *ka, *va, cu_new.data_ptr(), n, max_new, _p(parent),
+                                   *_rope_args(where, rope, dev), *oa, lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
         if status:
             _check(status, where)
         return o, lse
