@@ -46,7 +46,7 @@ struct AttendArgs {
   __nv_bfloat16 *k_parts[2], *v_finite;  // [Hkv][n_new][D] the new keys likewise; the new values with zeros for what is not finite
   int* status;
   int G, max_new, limit, rows;           // rows: of a row tile
-  int places, min_tiles;                 // CTAs that share the work, and the fewest tiles that are a CTA's worth
+  int places, min_tiles, extra;          // CTAs that share the work; the fewest tiles that are a CTA's worth; what beginning an item costs, in tiles
   float scale, scale_log2;
 };
 
@@ -113,48 +113,52 @@ __device__ __forceinline__ T warp_scan(T x, int lane) {   // inclusive
   }
   return x;
 }
-// All key tiles, and the CTAs that share them: CTA i takes [i total / ctas, (i + 1) total / ctas) of the line.  By a whole warp.
+// The line of all items, each as long as its tiles and `extra` for what it costs a CTA to begin another one; CTA i takes [i total / ctas,
+// (i + 1) total / ctas) of it.
 struct Line {
   long long total;
   int ctas;
   __device__ __forceinline__ long long begin(int i) const { return total * i / ctas; }
-  // the CTA whose run holds tile g
+  // the CTA whose run holds place g
   __device__ __forceinline__ int cta_of(long long g) const { return (int)(((g + 1) * ctas - 1) / total); }
 };
-__device__ __forceinline__ Line make_line(const AttendArgs& a, int lane) {
+// Where a CTA's run begins: item, place in it, length of the run; and the counts of the item's sequence.  Items of a sequence: heads, row tiles
+// innermost (they read the same pages).
+struct Start { int s, item, t, left, n, m, tok0, tiles; };
+// By a whole warp.  left = 0: the CTA has nothing to do.
+__device__ __forceinline__ Start find_start(const AttendArgs& a, int cta, int lane, Line& line) {
   long long total = 0;
+  SeqWork w = {};
   for (int s = lane; s < a.p.n_seqs; s += 32) {
-    const SeqWork w = seq_work(a, s);
-    total += (long long)w.tiles * w.row_tiles;
+    w = seq_work(a, s);
+    total += (long long)(w.tiles + a.extra) * w.row_tiles;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  Line r;
-  r.total = total * a.p.Hkv;
-  r.ctas = (int)min((long long)a.places, (r.total + a.min_tiles - 1) / a.min_tiles);
-  return r;
-}
-// Where a CTA's run begins, and how long it is.  Items of a sequence: heads, row tiles innermost (they read the same pages).
-struct Start { int s, item, t, left; };
-// (by a whole warp; left = 0: the CTA has nothing to do)
-__device__ __forceinline__ Start find_begin(const AttendArgs& a, const Line& line, int cta, int lane) {
-  Start r = {0, 0, 0, 0};
+  line.total = total * a.p.Hkv;
+  line.ctas = (int)min((long long)a.places, (line.total + a.min_tiles - 1) / a.min_tiles);
+  Start r = {};
   if (cta >= line.ctas) return r;
   const long long g0 = line.begin(cta);
   r.left = (int)(line.begin(cta + 1) - g0);
   long long before = 0;
   for (int s0 = 0; s0 < a.p.n_seqs; s0 += 32) {
-    SeqWork w = {};
-    if (s0 + lane < a.p.n_seqs) w = seq_work(a, s0 + lane);
-    const long long mine = (long long)w.tiles * w.row_tiles * a.p.Hkv, incl = warp_scan(mine, lane);
+    if (a.p.n_seqs > 32) {   // (otherwise w is there)
+      w = SeqWork{};
+      if (s0 + lane < a.p.n_seqs) w = seq_work(a, s0 + lane);
+    }
+    const long long mine = (long long)(w.tiles + a.extra) * w.row_tiles * a.p.Hkv, incl = warp_scan(mine, lane);
     const unsigned hit = __ballot_sync(0xffffffffu, g0 < before + incl);
     if (hit) {
       const int l = __ffs(hit) - 1;
       const long long at = g0 - before - __shfl_sync(0xffffffffu, incl - mine, l);
-      const int tiles = __shfl_sync(0xffffffffu, w.tiles, l);
       r.s = s0 + l;
-      r.item = (int)(at / tiles);
-      r.t = (int)(at - (long long)r.item * tiles);
+      r.n = __shfl_sync(0xffffffffu, w.c.n, l);
+      r.m = __shfl_sync(0xffffffffu, w.c.m, l);
+      r.tok0 = __shfl_sync(0xffffffffu, w.c.tok0, l);
+      r.tiles = __shfl_sync(0xffffffffu, w.tiles, l);
+      r.item = (int)(at / (r.tiles + a.extra));
+      r.t = (int)(at - (long long)r.item * (r.tiles + a.extra));
       return r;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
@@ -165,53 +169,55 @@ __device__ __forceinline__ Start find_begin(const AttendArgs& a, const Line& lin
 // The runs of a CTA one after the other.  Every role of a CTA has a cursor of its own.
 struct Cursor {
   Start at;
-  SeqWork w;
+  int row_tiles;
   bool first;
-  __device__ __forceinline__ Cursor(const AttendArgs& a, const Start& start) : at(start), first(true) {
-    if (at.left > 0) w = seq_work(a, at.s);
-  }
+  __device__ __forceinline__ Cursor(const AttendArgs& a, const Start& start) : at(start), first(true) { row_tiles = (at.m * a.G + a.rows - 1) / a.rows; }
   __device__ __forceinline__ bool next(const AttendArgs& a, Share& out) {
-    if (at.left <= 0) return false;
-    while (at.item >= w.row_tiles * a.p.Hkv) {   // (there is a sequence with work behind this one: left > 0)
-      if (++at.s >= a.p.n_seqs) return false;
-      w = seq_work(a, at.s);
-      at.item = 0;
+    for (;;) {
+      if (at.left <= 0) return false;
+      while (at.item >= row_tiles * a.p.Hkv) {   // (there is a sequence with work behind this one: left > 0)
+        if (++at.s >= a.p.n_seqs) return false;
+        const SeqWork w = seq_work(a, at.s);
+        at.n = w.c.n; at.m = w.c.m; at.tok0 = w.c.tok0; at.tiles = w.tiles;
+        row_tiles = w.row_tiles;
+        at.item = 0;
+      }
+      out.s = at.s;
+      out.h = at.item / row_tiles;
+      out.rt = at.item - out.h * row_tiles;
+      out.n = at.n; out.m = at.m; out.tok0 = at.tok0;
+      const int end = min(at.tiles + a.extra, at.t + at.left);
+      out.t0 = max(at.t - a.extra, 0);
+      out.t1 = end - a.extra;
+      out.part = out.t0 == 0 && out.t1 == at.tiles ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
+      at.left -= end - at.t;
+      at.t = 0;
+      ++at.item;
+      first = false;
+      if (out.t1 > out.t0) return true;          // (the run may end before the item's first tile)
     }
-    out.s = at.s;
-    out.h = at.item / w.row_tiles;
-    out.rt = at.item - out.h * w.row_tiles;
-    out.n = w.c.n; out.m = w.c.m; out.tok0 = w.c.tok0;
-    out.t0 = at.t;
-    out.t1 = min(w.tiles, at.t + at.left);
-    out.part = out.t0 == 0 && out.t1 == w.tiles ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
-    at.left -= out.t1 - out.t0;
-    at.t = 0;
-    ++at.item;
-    first = false;
-    return true;
   }
 };
 
 // An item that several CTAs work on, written down by the first of them whose run begins inside of it.
 struct alignas(16) Divided {
   int runs, part0, first;   // runs (0: none such); where the first one's result is, and the CTA of the second: those behind it are at 2 first, 2 first + 2, ...
-  int h, rt, m, tok0, pad;
+  int h, row0, rows, tok0, pad;   // KV head; first row of the row tile, and how many rows it has
 };
 // By one thread for every CTA.
 __device__ __forceinline__ void note_divided(const AttendArgs& a, const Line& line, const Start& st, int cta) {
   Divided d = {};
-  if (st.left > 0 && st.t > 0) {
-    const SeqWork w = seq_work(a, st.s);
-    const long long i0 = line.begin(cta) - st.t;   // the item's first tile in the line
-    const int c0 = line.cta_of(i0);
+  if (st.left > 0 && st.t > a.extra) {
+    const long long i0 = line.begin(cta) - st.t;   // the item's place in the line
+    const int c0 = line.cta_of(i0 + a.extra), row_tiles = (st.m * a.G + a.rows - 1) / a.rows;
     if (c0 + 1 == cta) {
-      d.runs = line.cta_of(i0 + w.tiles - 1) - c0 + 1;
-      d.part0 = 2 * c0 + (line.begin(c0) == i0 ? 0 : 1);
+      d.runs = line.cta_of(i0 + a.extra + st.tiles - 1) - c0 + 1;
+      d.part0 = 2 * c0 + (line.begin(c0) >= i0 ? 0 : 1);
       d.first = cta;
-      d.h = st.item / w.row_tiles;
-      d.rt = st.item - d.h * w.row_tiles;
-      d.m = w.c.m;
-      d.tok0 = w.c.tok0;
+      d.h = st.item / row_tiles;
+      d.row0 = (st.item - d.h * row_tiles) * a.rows;
+      d.rows = min(a.rows, st.m * a.G - d.row0);
+      d.tok0 = st.tok0;
     }
   }
   a.divided[cta] = d;
@@ -286,18 +292,19 @@ __device__ __noinline__ float odd_values(const AttendArgs& a, const Share& it, u
   return sum;
 }
 
-// One CTA of the last launch looks at everything that the others take from the device (the first launch has cleared the status word).
-__device__ void check_attend(const AttendArgs& a) {
+// The warps of the last launch look at everything that the kernels take from the device, a sequence a warp, the last blocks first.  They read
+// inputs only: those were there when the launch in front of this one passed its own wait, so this one need not wait for its end.
+__device__ bool attend_inputs_bad(const AttendArgs& a) {
   const PageGeom& p = a.p;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int lane = threadIdx.x & 31, warps = blockDim.x / 32;
   bool bad = false;
-  for (int s = warp; s < p.n_seqs; s += blockDim.x / 32) {
+  for (int s = (gridDim.x - 1 - blockIdx.x) * warps + threadIdx.x / 32; s < p.n_seqs; s += gridDim.x * warps) {
     const SeqCounts c = seq_counts(p, s, a.max_new, a.limit);
     bad |= !c.ok;
     if (c.m == 0) continue;
     const SeqPages r = seq_pages(p, c.n);
     const int32_t* row = p.table + (size_t)s * p.width;
-#pragma unroll 4
+#pragma unroll 8
     for (int f = lane; f < r.pages; f += 32) {
       int count;
       bad |= (unsigned)row[page_column(p, r, f, count)] >= (unsigned)p.n_pages;
@@ -308,8 +315,7 @@ __device__ void check_attend(const AttendArgs& a) {
         bad |= up < -1 || up >= i;
       }
   }
-  bad = __syncthreads_or(bad);
-  if (tid == 0 && bad) atomicCAS(a.status, (int)LRSA_OK, (int)LRSA_ERR_INVALID_ARG);
+  return bad;
 }
 
 // ---- few rows ----
@@ -340,8 +346,8 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
   wait_front();
   if (blockIdx.x == 0 && tid == 0) *a.status = 0;
   if (warp == 0) {
-    const Line line = make_line(a, lane);
-    const Start s = find_begin(a, line, blockIdx.x, lane);
+    Line line;
+    const Start s = find_start(a, blockIdx.x, lane, line);
     if (lane == 0) { start = s; note_divided(a, line, s, blockIdx.x); }
   }
   __syncthreads();
@@ -359,9 +365,34 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
   Cursor cursor(a, start);
   Share it;
   while (cursor.next(a, it)) {
+    // the warp's first pages (their numbers are on the way while Q is made)
+    const SeqPages pg = seq_pages(a.p, it.n);
+    const int32_t* table = a.p.table + (size_t)it.s * a.p.width;
+    const size_t head_row = (size_t)it.h << a.p.shift;
+    const int b0 = (max(it.t0, 1) - 1) * BPT, b1 = (it.t1 - 1) * BPT;
+    struct Group { int page, count, row; };    // page number, rows that count of this group, first row of it in the page
+    auto look = [&](int blk, int u) {
+      const int slot = (blk * U + u) * 16;
+      Group r;
+      r.row = slot & in_page;
+      const int col = page_column(a.p, pg, slot >> a.p.shift, r.count);
+      r.page = table[col];
+      r.count = (unsigned)r.page < (unsigned)a.p.n_pages ? min(r.count - r.row, 16) : 0;
+      return r;
+    };
+    Group next[U];
+    if (b0 + warp < b1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = look(b0 + warp, u);
+    }
     const int R = it.m * a.G;
     if (tid == 0) odd = 0;
-    find_family<256>(a, it.tok0, it.m, tid, fam);
+    if (it.m > 1) {
+      find_family<256>(a, it.tok0, it.m, tid, fam);
+    } else {
+      if (tid == 0) fam.mask[0] = make_uint4(1, 0, 0, 0);
+      __syncthreads();
+    }
     for (int i = tid; i < NH * KC * 32; i += 256) {   // Q of row 8h + g: the chunks that this lane takes of every key row
       const int h = i / (KC * 32), j = i / 32 % KC, r = 8 * h + (i & 31) / 4, c = (i & 3) + 4 * j;
       uint4 x = make_uint4(0, 0, 0, 0), rest = x;
@@ -514,25 +545,6 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
       block(kq, vq, there, see, rest);
     }
     // the pages
-    const SeqPages pg = seq_pages(a.p, it.n);
-    const int32_t* table = a.p.table + (size_t)it.s * a.p.width;
-    const size_t head_row = (size_t)it.h << a.p.shift;
-    const int b0 = (max(it.t0, 1) - 1) * BPT, b1 = (it.t1 - 1) * BPT;
-    struct Group { int page, count, row; };    // page number, rows that count of this group, first row of it in the page
-    auto look = [&](int blk, int u) {
-      const int slot = (blk * U + u) * 16;
-      Group r;
-      r.row = slot & in_page;
-      const int col = page_column(a.p, pg, slot >> a.p.shift, r.count);
-      r.page = table[col];
-      r.count = (unsigned)r.page < (unsigned)a.p.n_pages ? min(r.count - r.row, 16) : 0;
-      return r;
-    };
-    Group next[U];
-    if (b0 + warp < b1) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) next[u] = look(b0 + warp, u);
-    }
     for (int blk = b0 + warp; blk < b1; blk += NW) {
       uint4 kq[U][2][KC], vq[U][4][VC];
       uint32_t there[U];
@@ -622,90 +634,109 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
 
 // ---- joining the runs ----
 // A block joins eight rows of a divided item at a time: O of its runs brought to one maximum, added in the order of the CTAs.  The blocks share
-// the divided items' row groups, which each of them lists for itself; one block more checks.
+// the divided items' row groups, which each of them lists for itself.
 template <int D>
-__global__ void __launch_bounds__(256) paged_merge_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int kRuns = 64, kRows = 8, kStep = 256 / kRows, kMost = D / 4 / kStep > 0 ? D / 4 / kStep : 1;
-  static_assert(kMost == 1, "a float4 a thread");
+__global__ void __launch_bounds__(256, 4) paged_merge_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int kRuns = 64, kRows = 8, kStep = 256 / kRows, kAhead = 4;
+  static_assert(D / 4 <= kStep, "a float4 a thread");
   __shared__ float2 ml[kRuns][kRows];      // maxima and sums of so many runs at a time
-  __shared__ short head[kMaxPlaces];       // the CTAs that wrote an item down
-  __shared__ int before[kMaxPlaces + 1];   // row groups of the items before
+  __shared__ Divided list[kMaxPlaces];
+  __shared__ int before[kMaxPlaces];       // row groups of the items before
   __shared__ int warp_sum[8][2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool bad = attend_inputs_bad(a);
   wait_front();
-  if (blockIdx.x == gridDim.x - 1) { check_attend(a); return; }
-  const Divided* list = a.divided;
+  if (bad) atomicCAS(a.status, (int)LRSA_OK, (int)LRSA_ERR_INVALID_ARG);
   int items = 0, total = 0;
-  for (int c0 = 0; c0 < a.places; c0 += 256) {
-    int groups = 0;
-    if (c0 + tid < a.places) {
-      const Divided d = list[c0 + tid];
-      if (d.runs > 0) groups = (min(a.rows, d.m * a.G - d.rt * a.rows) + kRows - 1) / kRows;
+  static_assert(kMaxPlaces <= 512, "two a thread");
+  Divided d[2] = {};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (2 * tid + u < a.places) d[u] = a.divided[2 * tid + u];
+  {
+    int groups[2], both = 0, n = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      groups[u] = d[u].runs > 0 ? (d[u].rows + kRows - 1) / kRows : 0;
+      both += groups[u];
+      n += groups[u] > 0;
     }
-    const int n = warp_scan(groups > 0 ? 1 : 0, lane), g = warp_scan(groups, lane);
+    const int n_incl = warp_scan(n, lane), g_incl = warp_scan(both, lane);
+    if (lane == 31) { warp_sum[warp][0] = n_incl; warp_sum[warp][1] = g_incl; }
     __syncthreads();
-    if (lane == 31) { warp_sum[warp][0] = n; warp_sum[warp][1] = g; }
-    __syncthreads();
-    int n0 = items, g0 = total;
+    int n0 = n_incl - n, g0 = g_incl - both;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
       if (w < warp) { n0 += warp_sum[w][0]; g0 += warp_sum[w][1]; }
       items += warp_sum[w][0];
       total += warp_sum[w][1];
     }
-    if (groups > 0) { head[n0 + n - 1] = (short)(c0 + tid); before[n0 + n - 1] = g0 + g - groups; }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (groups[u] > 0) { list[n0] = d[u]; before[n0++] = g0; g0 += groups[u]; }
   }
   const int lane_row = tid % kRows, c4 = tid / kRows;   // rows of neighbouring threads are neighbours
-  for (int at = blockIdx.x; at < total; at += gridDim.x - 1) {
+  for (int at = blockIdx.x; at < total; at += gridDim.x) {
     __syncthreads();   // the list is there; `ml` has been read
     int lo = 0, hi = items;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (before[mid] <= at) lo = mid; else hi = mid;
     }
-    const Divided d = list[head[lo]];
-    const int row = (at - before[lo]) * kRows + lane_row, R = d.m * a.G - d.rt * a.rows;
+    const Divided d = list[lo];
+    const int row = (at - before[lo]) * kRows + lane_row;
     auto part_of = [&](int i) { return part_at(a, i == 0 ? d.part0 : 2 * (d.first + i - 1), D); };
+    auto o_of = [&](int i) {
+      return i < d.runs && c4 < D / 4 ? __ldcg(reinterpret_cast<const float4*>(part_of(i)) + c4 * a.rows + row) : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
     float M = -INFINITY, ls = 0.f;
     float4 ov = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i0 = 0; i0 < d.runs; i0 += kRuns) {
       const int n = min(kRuns, d.runs - i0);
-      __syncthreads();
+      if (i0 > 0) __syncthreads();
       for (int i = c4; i < n; i += kStep) {
         const float* p = part_of(i0 + i) + a.rows * D + row;
         ml[i][lane_row] = make_float2(__ldcg(p), __ldcg(p + a.rows));
       }
+      float4 x[kAhead];   // of the next runs, asked for before the maximum is known
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) x[u] = o_of(i0 + u);
       __syncthreads();
       const float was = M;
       for (int i = 0; i < n; ++i) {
-        const float2 x = ml[i][lane_row];
-        if (x.y != 0.f) M = fmaxf(M, x.x);   // (nothing counted in a run: its maximum says nothing)
+        const float2 y = ml[i][lane_row];
+        if (y.y != 0.f) M = fmaxf(M, y.x);   // (nothing counted in a run: its maximum says nothing)
       }
       const float f0 = was == -INFINITY ? 0.f : ex2(was - M);
       ls *= f0;
       ov.x *= f0; ov.y *= f0; ov.z *= f0; ov.w *= f0;
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
-        const float4 x = c4 < D / 4 ? __ldcg(reinterpret_cast<const float4*>(part_of(i0 + i)) + c4 * a.rows + row) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float2 w = ml[i][lane_row];
-        const float f = w.y != 0.f ? ex2(w.x - M) : 0.f;
-        ls = fmaf(w.y, f, ls);
-        if (f != 0.f) { ov.x = fmaf(x.x, f, ov.x); ov.y = fmaf(x.y, f, ov.y); ov.z = fmaf(x.z, f, ov.z); ov.w = fmaf(x.w, f, ov.w); }
+      for (int i = 0; i < n; i += kAhead) {
+        float4 y[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) { y[u] = x[u]; if (i + kAhead < n) x[u] = o_of(i0 + i + kAhead + u); }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          if (i + u >= n) break;
+          const float2 w = ml[i + u][lane_row];
+          const float f = w.y != 0.f ? ex2(w.x - M) : 0.f;
+          ls = fmaf(w.y, f, ls);
+          if (f != 0.f) { ov.x = fmaf(y[u].x, f, ov.x); ov.y = fmaf(y[u].y, f, ov.y); ov.z = fmaf(y[u].z, f, ov.z); ov.w = fmaf(y[u].w, f, ov.w); }
+        }
       }
     }
-    if (row >= R || c4 >= D / 4) continue;
-    const int r = d.rt * a.rows + row, tok = r / a.G, q_head = d.h * a.G + r - tok * a.G;
+    const int r = d.row0 + row, tok = r / a.G, head = d.h * a.G + r - tok * a.G;
+    if (row >= d.rows || c4 >= D / 4) continue;
     const float inv = 1.f / ls;
-    *reinterpret_cast<uint2*>(a.o + q_head * a.o_head + (d.tok0 + tok) * a.o_tok + 4 * c4) =
+    *reinterpret_cast<uint2*>(a.o + head * a.o_head + (d.tok0 + tok) * a.o_tok + 4 * c4) =
         make_uint2(pack_bf16(ov.x * inv, ov.y * inv), pack_bf16(ov.z * inv, ov.w * inv));
-    if (c4 == 0 && a.lse) a.lse[(size_t)q_head * a.p.n_new + d.tok0 + tok] = (M + log2f(ls)) * 0.6931471805599453f;
+    if (c4 == 0 && a.lse) a.lse[(size_t)head * a.p.n_new + d.tok0 + tok] = (M + log2f(ls)) * 0.6931471805599453f;
   }
 }
 
 // ---- many rows ----
 // The operands of the new tokens, once for all CTAs that work on their items (which would each spend 5 to 15 us on it): which new tokens each one
 // sees, queries and keys rotated and split in two bf16, values without infinities and NaN.  A block takes a query head of a sequence, or a KV head's
-// keys and values.  The first blocks also find where the runs of the CTAs begin.
+// keys, or its values.  The last blocks find where the runs of the CTAs begin, a warp for each.
 template <int D>
 __global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int UNITS = D / 16, kAhead = 2;
@@ -714,18 +745,37 @@ __global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_front();
   if (blockIdx.x == 0 && tid == 0) *a.status = 0;
-  if (warp == 7 && blockIdx.x < a.places) {
-    const Line line = make_line(a, lane);
-    const Start s = find_begin(a, line, blockIdx.x, lane);
-    if (lane == 0) { a.starts[blockIdx.x] = s; note_divided(a, line, s, blockIdx.x); }
+  const int heads = a.p.Hkv * (a.G + 2), plan0 = a.p.n_seqs * heads, s = blockIdx.x / heads, which = blockIdx.x - s * heads;
+  if ((int)blockIdx.x >= plan0) {
+    const int cta = (blockIdx.x - plan0) * 8 + warp;
+    if (cta < a.places) {
+      Line line;
+      const Start st = find_start(a, cta, lane, line);
+      if (lane == 0) { a.starts[cta] = st; note_divided(a, line, st, cta); }
+    }
+    return;
   }
-  const int heads = a.p.Hkv * (a.G + 1), s = blockIdx.x / heads, which = blockIdx.x - s * heads;
-  if (s >= a.p.n_seqs) return;
   const SeqCounts c = seq_counts(a.p, s, a.max_new, a.limit);
   if (c.m == 0) return;
-  if (tid == 0) odd = 0;
-  find_family<256>(a, c.tok0, c.m, tid, fam);
   const int q_heads = a.p.Hkv * a.G;
+  if (which >= q_heads + a.p.Hkv) {
+    const int h = which - q_heads - a.p.Hkv;
+    if (tid == 0) odd = 0;
+    __syncthreads();
+    bool any = false;
+#pragma unroll 4
+    for (int i = tid; i < c.m * (D / 8); i += 256) {
+      const int tok = i / (D / 8), ch = i % (D / 8);
+      const uint4 y = *reinterpret_cast<const uint4*>(a.v + h * a.v_head + (c.tok0 + tok) * a.v_tok + 8 * ch);
+      any |= odd_chunk(y);
+      reinterpret_cast<uint4*>(a.v_finite)[((size_t)h * a.p.n_new + c.tok0 + tok) * (D / 8) + ch] = finite_chunk(y);
+    }
+    if (any) odd = 1;
+    __syncthreads();
+    if (tid == 0) a.odd[(size_t)s * a.p.Hkv + h] = odd;
+    return;
+  }
+  find_family<256>(a, c.tok0, c.m, tid, fam);
   const bool is_q = which < q_heads, two = a.rope.half > 0;
   const int h = is_q ? which / a.G : which - q_heads, g = which - h * a.G;
   const __nv_bfloat16* src = is_q ? a.q + which * a.q_head + c.tok0 * a.q_tok : a.k + h * a.k_head + c.tok0 * a.k_tok;
@@ -755,20 +805,7 @@ __global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_consta
       }
     }
   }
-  if (is_q) {
-    if (which == 0 && tid < c.m) a.family[c.tok0 + tid] = fam.mask[tid];
-    return;
-  }
-  bool any = false;
-  for (int i = tid; i < c.m * (D / 8); i += 256) {
-    const int tok = i / (D / 8), ch = i % (D / 8);
-    const uint4 y = *reinterpret_cast<const uint4*>(a.v + h * a.v_head + (c.tok0 + tok) * a.v_tok + 8 * ch);
-    any |= odd_chunk(y);
-    reinterpret_cast<uint4*>(a.v_finite)[((size_t)h * a.p.n_new + c.tok0 + tok) * (D / 8) + ch] = finite_chunk(y);
-  }
-  if (any) odd = 1;
-  __syncthreads();
-  if (tid == 0) a.odd[(size_t)s * a.p.Hkv + h] = odd;
+  if (which == 0 && tid < c.m) a.family[c.tok0 + tid] = fam.mask[tid];
 }
 
 constexpr int kFar = 3;   // tiles that are asked for (into L2) ahead of their turn in the ring
@@ -778,7 +815,7 @@ struct TileCfg {
   static constexpr int kSub = D / 64;                       // 64-column (128-byte) sub-tiles
   static constexpr int kSubBytes = kTile * 128, kTileBytes = kSub * kSubBytes;
   static constexpr int kStages = D == 64 ? 8 : TQ == 1 ? 5 : 3;   // ring slots
-  static constexpr int kQRegion = 2 * kTileBytes;           // rounded, and what that leaves; later the output rows, padded by 16 bytes each
+  static constexpr int kQRegion = 2 * kTileBytes;           // rounded, and what that leaves
   static constexpr int kRing = TQ * kQRegion, kTail = kRing + kStages * kTileBytes;
   static constexpr int kThreads = 128 + 128 * TQ;
   static constexpr uint32_t kColO = 0, kColS = TQ * 128, kCols = 2 * TQ * 128;   // tensor memory: O of the row tiles, S with P over it
@@ -815,7 +852,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
     prefetch_tensormap(&maps.vn);
     sh.abort = 0;
     mbar_init(smem_u32(&sh.q_full), 1);
-    mbar_init(smem_u32(&sh.q_free), 4 * TQ);     // one arrival per softmax warp
+    mbar_init(smem_u32(&sh.q_free), 1);
     for (int i = 0; i < NS; ++i) { mbar_init(smem_u32(&sh.kv_full[i]), 1); mbar_init(smem_u32(&sh.kv_empty[i]), 1); }
     for (int t = 0; t < TQ; ++t) {
       mbar_init(smem_u32(&sh.s_full[t]), 1);
@@ -902,7 +939,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
 #pragma unroll
         for (int i = 0; i < kFar; ++i) {
           far[i] = tile + i < it.t1 ? page_at(tile + i) : 0;
-          if (i > 0 && tile + i < it.t1) fetch(far[i]);
+          if ((i > 0 || it.t0 == 0) && tile + i < it.t1) fetch(far[i]);   // (behind the new tokens' tile the ring is full)
         }
         for (; tile < it.t1 && ok; ++tile) {
           const int page = far[0];
@@ -999,6 +1036,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
             }
           }
           if (!ok) break;
+          if (j + 2 == n) umma_commit(smem_u32(&sh.q_free), leader);   // the item's last scores: the next Q may come while this item ends
           if (j >= 0) umma_commit(smem_u32(&sh.kv_empty[v.slot]), leader);
           if (more) {
             umma_commit(smem_u32(&sh.kv_empty[k.slot]), leader);
@@ -1018,11 +1056,8 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
     const float c = a.scale_log2;
     bool ok = true;
     Entry e;
-    int count = 0, items = 0;      // tiles of this warpgroup, items so far
+    int count = 0;                 // tiles of this warpgroup so far
     while (ok && cursor.next(a, it)) {
-      // (a warpgroup without rows waits here too: it must not tell that it is done with an item ahead of the others)
-      ok = mbar_wait_warp(smem_u32(&sh.q_full), items++ & 1, abort);
-      if (!ok) break;
       const int n = it.t1 - it.t0, R = it.m * a.G, r0 = it.rt * a.rows + t * kTile;
       const bool mine = r0 < R;    // this warpgroup has rows
       const SeqPages pg = seq_pages(a.p, it.n);
@@ -1151,8 +1186,8 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
         const bool add_odd = it.t0 == 0 && a.odd[(size_t)it.s * a.p.Hkv + it.h];
         float* part = it.part >= 0 ? part_at(a, it.part, D) : nullptr;
         const float inv = 1.0f / l;
-        constexpr int kStride = D * 2 + 16;
-        unsigned char* stage = smem_raw + t * Cfg::kQRegion + quad * 32 * kStride;   // rows of this warp, over Q_t, which is no longer needed
+        const int tok = rr / a.G, head = it.h * a.G + rr - tok * a.G;
+        uint4* dst = rr < R ? reinterpret_cast<uint4*>(a.o + head * a.o_head + (it.tok0 + tok) * a.o_tok) : nullptr;
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
           uint32_t o[32];
@@ -1171,40 +1206,26 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
 #pragma unroll
             for (int x = 0; x < 8; ++x)
               reinterpret_cast<uint4*>(part)[(8 * q + x) * a.rows + t * kTile + row] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-          } else {
+          } else if (dst) {
+            // (a thread writes its own row: staged in shared memory the rows would leave in whole lines, but the only place for them is Q's, where the
+            // next item's is on its way by now)
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               float f[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[8 * x + i]) * inv;
-              *reinterpret_cast<uint4*>(stage + lane * kStride + (q * 4 + x) * 16) = pack_channels(f);
+              dst[q * 4 + x] = pack_channels(f);
             }
           }
         }
         if (part) {
           part[a.rows * D + t * kTile + row] = m * c;
           part[a.rows * (D + 1) + t * kTile + row] = l;
-        } else {
-          if (rr < R && a.lse) {
-            const int tok = rr / a.G, head = it.h * a.G + rr - tok * a.G;
-            a.lse[(size_t)head * a.p.n_new + it.tok0 + tok] = m * a.scale + logf(l);
-          }
-          __syncwarp();
-          // whole rows: neighbouring lanes take neighbouring chunks
-          for (int r = lane / CPR; r < 32; r += 32 / CPR) {
-            const int x = r0 + quad * 32 + r;
-            if (x >= R) break;
-            const int tok = x / a.G, head = it.h * a.G + x - tok * a.G;
-            reinterpret_cast<uint4*>(a.o + head * a.o_head + (it.tok0 + tok) * a.o_tok)[lane % CPR] =
-                *reinterpret_cast<const uint4*>(stage + r * kStride + (lane % CPR) * 16);
-          }
-          __syncwarp();
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the next Q is written there by TMA
+        } else if (dst && a.lse) {
+          a.lse[(size_t)head * a.p.n_new + it.tok0 + tok] = m * a.scale + logf(l);
         }
         tc_fence_before_sync();   // O and S have been read: the next item's products may write them
       }
-      __syncwarp();
-      if (ok && lane == 0) mbar_arrive(smem_u32(&sh.q_free));
     }
   }
   tc_fence_before_sync();
@@ -1219,6 +1240,8 @@ bool rows_ok(const lrsa_rows_t* r) {
 
 // Fewest key tiles that are a CTA's worth.
 constexpr int kMinTilesFew = 2, kMinTiles = 2;
+// What it costs a CTA to begin another item, in key tiles.
+constexpr int kExtraFew = 1, kExtra = 3;
 
 // The parts of the workspace.  few: of a call that the kernel for few rows takes.
 struct AttendWs { size_t starts, divided, part, family, odd, q[2], k[2], v, total; };
@@ -1242,7 +1265,7 @@ AttendWs attend_ws(const Geom& g, long long n_seqs, long long n_new, bool few) {
 template <int D, int TQ>
 int launch_tile(AttendArgs& a, cudaStream_t st) {
   using Cfg = TileCfg<D, TQ>;
-  a.rows = TQ * kTile; a.places = kSms; a.min_tiles = kMinTiles;
+  a.rows = TQ * kTile; a.places = kSms; a.min_tiles = kMinTiles; a.extra = kExtra;
   TileMaps maps;
   const long long outer = (long long)a.p.n_pages * a.p.Hkv, Hkv = a.p.Hkv, T = a.p.n_new > 0 ? a.p.n_new : 1;
   int rc = make_tmap_bf16(&maps.k, a.k_pages, D, 1 << a.p.shift, outer, 1 << a.p.shift);
@@ -1253,7 +1276,7 @@ int launch_tile(AttendArgs& a, cudaStream_t st) {
   }
   if (rc == LRSA_OK) rc = make_tmap_bf16(&maps.vn, a.v_finite, D, T, Hkv, kTile);
   if (rc != LRSA_OK) return rc;
-  const long long blocks = (long long)a.p.n_seqs * Hkv * (a.G + 1), grid = blocks > a.places ? blocks : a.places;
+  const long long grid = (long long)a.p.n_seqs * Hkv * (a.G + 2) + (a.places + 7) / 8;
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   LRSA_CUDA_CHECK(launch_dependent(paged_operands_kernel<D>, dim3((unsigned)grid), dim3(256), 0, st, 1, a));
   launch_counter().n++;
@@ -1266,7 +1289,7 @@ int launch_tile(AttendArgs& a, cudaStream_t st) {
 
 template <int D, int NH>
 int launch_few(AttendArgs& a, cudaStream_t st) {
-  a.rows = kFewRows; a.places = NH == 1 ? 2 * kSms : kSms; a.min_tiles = kMinTilesFew;
+  a.rows = kFewRows; a.places = NH == 1 ? 2 * kSms : kSms; a.min_tiles = kMinTilesFew; a.extra = kExtraFew;
   LRSA_CUDA_CHECK(launch_dependent(paged_few_kernel<D, NH>, dim3(a.places), dim3(256), 0, st, 1, a));
   return LRSA_OK;
 }

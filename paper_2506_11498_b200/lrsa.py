@@ -751,8 +751,8 @@ class PagedCache:
         self._shape = torch.Size((n_pages, params.n_kv_heads, page, params.head_dim))
         self.k_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
         self.v_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
-        self.ws = new_workspace(self.workspace_bytes(1, 1, 1), device)
         self._need, self._old = {}, []
+        self.ws = new_workspace(self.workspace_bytes(1, 1, 1), device)
 
     def workspace_bytes(self, n_seqs: int, n_new: int, max_new: int) -> int:
         """What an attend of n_new tokens of n_seqs sequences, at most max_new each, takes."""
@@ -785,30 +785,53 @@ class PagedCache:
         return cols + list(range(first, first + max(rest // p.lag - 1, 0) * kept))
 
     def _pages(self, where, name, first, table, n_tokens, cu_new):
-        """(device, what csrc/pycall.c takes of the cache), when everything is what the kernels read and write."""
+        """(device, what csrc/pycall.c takes of the cache), when everything is what the kernels read and write.  The pages are looked at
+        when they have been replaced, or lie elsewhere than they did."""
         dev = _device(where, name, first)
-        k, v, ws = self.k_pages, self.v_pages, self.ws
-        if k.shape != self._shape or v.shape != self._shape or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or \
-                not k.is_contiguous() or not v.is_contiguous() or k.get_device() != dev or v.get_device() != dev or ws.get_device() != dev:
-            raise LrsaError(1, f"{where}: the pages of the cache must be contiguous bfloat16 tensors of shape {tuple(self._shape)}, they and the "
-                               f"workspace on cuda:{dev}")
+        at_k, at_v = self.k_pages.data_ptr(), self.v_pages.data_ptr()
+        if self._seen != (at_k, at_v, dev):
+            self._look(where, dev)
+            object.__setattr__(self, "_seen", (at_k, at_v, dev))
         n = table.shape[0] if table.dim() == 2 else 0
-        _expect(where, "table", table, (n, self.table_width), torch.int32, dev)
-        _expect(where, "n_tokens", n_tokens, (n,), torch.int32, dev)
-        _expect(where, "cu_new", cu_new, (n + 1,), torch.int32, dev)
-        return dev, (self.page, self.n_pages, n, self.table_width, k.data_ptr(), v.data_ptr(), table.data_ptr(), n_tokens.data_ptr())
+        i32 = torch.int32
+        if table.dtype is not i32 or table.shape != (n, self.table_width) or not table.is_contiguous() or table.get_device() != dev:
+            _expect(where, "table", table, (n, self.table_width), i32, dev)
+        if n_tokens.dtype is not i32 or n_tokens.shape != (n,) or not n_tokens.is_contiguous() or n_tokens.get_device() != dev:
+            _expect(where, "n_tokens", n_tokens, (n,), i32, dev)
+        if cu_new.dtype is not i32 or cu_new.shape != (n + 1,) or not cu_new.is_contiguous() or cu_new.get_device() != dev:
+            _expect(where, "cu_new", cu_new, (n + 1,), i32, dev)
+        return dev, (self.page, self.n_pages, n, self.table_width, at_k, at_v, table.data_ptr(), n_tokens.data_ptr())
 
-    def _rows(self, where, name, t, heads, n, dev):
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_seen", None)
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k not in ("_seen", "_held")}   # (addresses of this process)
+
+    def _look(self, where, dev):
+        """Raises LRSA_ERR_INVALID_ARG unless the pages are what the kernels read and write."""
+        for name, t in (("k_pages", self.k_pages), ("v_pages", self.v_pages)):
+            _expect(where, name + " of the cache", t, self._shape, torch.bfloat16, dev)
+            if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
+                raise LrsaError(1, f"{where}: {name} of the cache has lost its memory")
+        if self.ws.get_device() != dev:
+            raise LrsaError(1, f"{where}: the workspace of the cache is on {self.ws.device}")
+        # aliases: while they are held no other memory can be at these addresses
+        object.__setattr__(self, "_held", (self.k_pages.detach(), self.v_pages.detach()))
+
+    @staticmethod
+    def _rows(where, name, t, shape, dev):
         """(address, strides) of rows [heads, n, d] with any strides between heads and tokens."""
-        if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.shape[0] != heads or t.shape[1] != n or t.shape[2] != self.params.head_dim or \
-                t.get_device() != dev:
-            raise LrsaError(1, f"{where}: {name} must be a bfloat16 tensor of shape {(heads, n, self.params.head_dim)} on cuda:{dev}, got "
-                               f"{t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev:
+            raise LrsaError(1, f"{where}: {name} must be a bfloat16 tensor of shape {shape} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on "
+                               f"{t.device}")
         head, token, channel = t.stride()
-        head, token = head if heads > 1 else 0, token if n > 1 else 0
         at = t.data_ptr()
-        if channel != 1 or head % 8 or token % 8 or at % 16:
-            raise LrsaError(1, f"{where}: the rows of {name} must be contiguous and 16-byte aligned, got strides {t.stride()}")
+        if channel != 1 or (head | token) & 7 or at & 15:
+            head, token = head if shape[0] > 1 else 0, token if shape[1] > 1 else 0    # (of one head or token a stride is never used)
+            if channel != 1 or (head | token) & 7 or at & 15:
+                raise LrsaError(1, f"{where}: the rows of {name} must be contiguous and 16-byte aligned, got strides {t.stride()}")
         return at, head, token
 
     def append(self, k_new, v_new, table, n_tokens, cu_new, rows=None, rope=None, kept=None, stream=None):
@@ -818,7 +841,8 @@ class PagedCache:
         p, where, call = self.params, "lrsa_paged_append", _calls()
         dev, pages = self._pages(where, "k_new", k_new, table, n_tokens, cu_new)
         n_rows = k_new.shape[1] if k_new.dim() == 3 else 0
-        k, v = self._rows(where, "k_new", k_new, p.n_kv_heads, n_rows, dev), self._rows(where, "v_new", v_new, p.n_kv_heads, n_rows, dev)
+        shape = (p.n_kv_heads, n_rows, p.head_dim)
+        k, v = self._rows(where, "k_new", k_new, shape, dev), self._rows(where, "v_new", v_new, shape, dev)
         n_new = n_rows
         if rows is not None:
             n_new = rows.shape[0] if rows.dim() == 1 else -1
@@ -840,22 +864,29 @@ class PagedCache:
         p, where, call = self.params, "lrsa_paged_attend", _calls()
         dev, pages = self._pages(where, "q", q, table, n_tokens, cu_new)
         n = q.shape[1] if q.dim() == 3 else 0
-        qa, ka, va = (self._rows(where, name, t, heads, n, dev) for name, t, heads in
-                      (("q", q, p.n_q_heads), ("k", k, p.n_kv_heads), ("v", v, p.n_kv_heads)))
+        Hq, d = p.n_q_heads, p.head_dim
+        shape, kv_shape = (Hq, n, d), (p.n_kv_heads, n, d)
+        qa, ka, va = self._rows(where, "q", q, shape, dev), self._rows(where, "k", k, kv_shape, dev), self._rows(where, "v", v, kv_shape, dev)
         if parent is not None:
             _expect(where, "parent", parent, (n,), torch.int32, dev)
         if o is None:
-            if n > 1 and qa[2] > qa[1]:     # token by token
-                o = _made(stream, q, torch.empty, (n, p.n_q_heads, p.head_dim), dtype=q.dtype, device=q.device).transpose(0, 1)
+            dense = qa[1:] == (d, Hq * d) or qa[1:] == (n * d, d)
+            if dense and stream is None:
+                o = torch.empty_like(q)
+            elif n > 1 and qa[2] > qa[1]:     # token by token
+                o = _made(stream, q, torch.empty, (n, Hq, d), dtype=q.dtype, device=q.device).transpose(0, 1)
             else:
-                o = _made(stream, q, torch.empty, (p.n_q_heads, n, p.head_dim), dtype=q.dtype, device=q.device)
-        oa = self._rows(where, "o", o, p.n_q_heads, n, dev)
-        if (p.n_q_heads > 1 and oa[1] < p.head_dim) or (n > 1 and oa[2] < p.head_dim):
-            raise LrsaError(1, f"{where}: rows of o overlap, strides {o.stride()}")
-        if lse is None:
-            lse = _made(stream, q, torch.empty, (p.n_q_heads, n), dtype=torch.float32, device=q.device)
+                o = _made(stream, q, torch.empty, shape, dtype=q.dtype, device=q.device)
+            oa = (o.data_ptr(),) + o.stride()[:2]
         else:
-            _expect(where, "lse", lse, (p.n_q_heads, n), torch.float32, dev)
+            oa = self._rows(where, "o", o, shape, dev)
+            if (Hq > 1 and oa[1] < d) or (n > 1 and oa[2] < d):
+                raise LrsaError(1, f"{where}: rows of o overlap, strides {o.stride()}")
+        if lse is None:
+            lse = torch.empty((Hq, n), dtype=torch.float32, device=q.device) if stream is None else \
+                _made(stream, q, torch.empty, (Hq, n), dtype=torch.float32, device=q.device)
+        else:
+            _expect(where, "lse", lse, (Hq, n), torch.float32, dev)
         if max_new is None:
             max_new = max(1, min(n, self.MOST_NEW))
         cp, ws = p.struct(), self._workspace(q, stream, pages[2], n, max_new)
