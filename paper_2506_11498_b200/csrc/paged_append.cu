@@ -9,7 +9,7 @@
 // of window w into the first CTA's shared memory; that one scores and selects; all of them move kept rows.  Two forms:
 //   one launch (few new tokens a sequence: every step of a server): a cluster per (sequence, KV head) cuts what there is to cut, mostly
 //     nothing, then writes the new rows.  The recent pages that it writes are those of the window it has just cut.
-//   two launches (prompts): a cluster per window, then the rows.
+//   several launches (prompts): the new keys rotated into the workspace, a cluster per window, then the rows.
 // The counts are on the device: a cluster finds its sequence and window by running over the sequences' counts.
 #include "infer_sm100.h"
 #include "paged_sm100.h"
@@ -48,6 +48,7 @@ struct AppendArgs {
   PageGeom p;
   RopeArgs rope;
   const __nv_bfloat16 *k, *v;
+  __nv_bfloat16* turned;                    // two launches and more: [Hkv][n_new][D], the new tokens' keys rotated (null: they come rotated)
   long long k_head, k_tok, v_head, v_tok;   // strides
   int n_rows;                               // rows of k and v
   const int32_t* rows;                      // optional: row of every new token
@@ -55,7 +56,7 @@ struct AppendArgs {
   int32_t* kept;                            // optional
   int* status;                              // written by the last cluster (null: not by this launch)
   int most, limit;                          // bounds of the counts
-  int ddof, with_rows;                      // with_rows: one launch
+  int ddof;
   int clusters;                             // clusters that work (the one behind them checks)
 };
 
@@ -73,13 +74,14 @@ __device__ __forceinline__ int new_row(const AppendArgs& a, const Seq& q, int i)
   return a.rows ? usable(a.rows[t], a.n_rows) : t;
 }
 
-// The row of the token at position p, of K (z = 0) or V.  `turn`: K of a new token, still to be rotated.
-template <int D>
+// The row of the token at position p, of K (z = 0) or V.  `turn` (TURN only): K of a new token, still to be rotated.
+template <int D, bool TURN>
 __device__ __forceinline__ const __nv_bfloat16* token_row(const AppendArgs& a, const Seq& q, int p, int z, bool& turn) {
-  turn = p >= q.n;
+  turn = false;
   if (p >= q.n) {
+    if (!TURN && z == 0 && a.turned) return a.turned + ((size_t)q.h * a.p.n_new + q.tok0 + (p - q.n)) * D;
     const int r = new_row(a, q, p - q.n);
-    turn = z == 0 && a.rope.half > 0;
+    turn = TURN && z == 0 && a.rope.half > 0;
     return z == 0 ? a.k + q.h * a.k_head + r * a.k_tok : a.v + q.h * a.v_head + r * a.v_tok;
   }
   int row;
@@ -150,7 +152,7 @@ __device__ __forceinline__ void rotate_held(uint4 (&x)[D / 32], const __nv_bfloa
 
 // Rows of a round: each warp takes eight tokens at a time, four such groups; four lanes share a row.
 // What a window's rows are for: their channels' ranges, or their spreads.
-template <int D, class F>
+template <int D, bool TURN, class F>
 __device__ __forceinline__ void walk_window(const AppendArgs& a, const Seq& q, int w, int i0, int i1, F use) {
   constexpr int KC = D / 32, T = 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, z = warp & 1, wz = warp >> 1;
@@ -160,12 +162,12 @@ __device__ __forceinline__ void walk_window(const AppendArgs& a, const Seq& q, i
     bool turn[T];
     const __nv_bfloat16* row[T];
 #pragma unroll
-    for (int s = 0; s < T; ++s) row[s] = token_row<D>(a, q, p0 + min(r0 + 8 * s + g, i1 - 1), z, turn[s]);
+    for (int s = 0; s < T; ++s) row[s] = token_row<D, TURN>(a, q, p0 + min(r0 + 8 * s + g, i1 - 1), z, turn[s]);
 #pragma unroll
     for (int s = 0; s < T; ++s)
 #pragma unroll
       for (int j = 0; j < KC; ++j) x[s][j] = *reinterpret_cast<const uint4*>(row[s] + (t + 4 * j) * 8);
-    if (z == 0 && a.rope.half > 0) {
+    if (TURN && z == 0 && a.rope.half > 0) {
 #pragma unroll
       for (int s = 0; s < T; ++s)
         if (turn[s])
@@ -176,7 +178,7 @@ __device__ __forceinline__ void walk_window(const AppendArgs& a, const Seq& q, i
 }
 
 // Cuts window w of the sequence (all CTAs of the cluster).
-template <int D>
+template <int D, bool TURN>
 __device__ void cut_window(const AppendArgs& a, const Seq& q, int w, int rank, int C, AppendShared<D>& sh, float* spread) {
   constexpr int KC = D / 32, T = 4;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, z = warp & 1;
@@ -188,7 +190,7 @@ __device__ void cut_window(const AppendArgs& a, const Seq& q, int w, int rank, i
   for (int j = 0; j < KC; ++j)
 #pragma unroll
     for (int p = 0; p < 4; ++p) { mn[j][p] = 0x7F807F80u; mx[j][p] = 0xFF80FF80u; }
-  walk_window<D>(a, q, w + 1, i0, i1, [&](int, uint4 (&x)[T][KC]) {
+  walk_window<D, TURN>(a, q, w + 1, i0, i1, [&](int, uint4 (&x)[T][KC]) {
 #pragma unroll
     for (int s = 0; s < T; ++s)
 #pragma unroll
@@ -248,7 +250,7 @@ __device__ void cut_window(const AppendArgs& a, const Seq& q, int w, int rank, i
   // Eq. 6, 7: spreads of window w, to the first CTA.  The sums are formed chunk by chunk and the chunks added in a tree over the
   // distances 8, 4, 2, 1, as in lrsa_score_select: equal scores fall on the same side.
   const float inv_dof = 1.0f / (float)(D - a.ddof);
-  walk_window<D>(a, q, w, i0, i1, [&](int r0, uint4 (&x)[T][KC]) {
+  walk_window<D, TURN>(a, q, w, i0, i1, [&](int r0, uint4 (&x)[T][KC]) {
     float v[T][2], first2[T][2];
 #pragma unroll
     for (int k = 0; k < KC; ++k) {
@@ -352,7 +354,7 @@ __device__ void cut_window(const AppendArgs& a, const Seq& q, int w, int rank, i
     i = min(max(i, 0), L - 1);
     const int p = a.p.S + w * L + i, page = page_of(a, q.s, col0 + (j >> a.p.shift));
     bool turn, none;
-    const __nv_bfloat16 *kr = token_row<D>(a, q, p, 0, turn), *vr = token_row<D>(a, q, p, 1, none);
+    const __nv_bfloat16 *kr = token_row<D, TURN>(a, q, p, 0, turn), *vr = token_row<D, TURN>(a, q, p, 1, none);
     const uint4 kx = turn ? rotated_chunk(kr, ch, p, a.rope) : *reinterpret_cast<const uint4*>(kr + 8 * ch);
     const uint4 vx = *reinterpret_cast<const uint4*>(vr + 8 * ch);
     if ((unsigned)page < (unsigned)a.p.n_pages) {
@@ -377,15 +379,16 @@ __device__ __forceinline__ Staying staying(const PageGeom& p, int n, int m) {
 __device__ __forceinline__ int stay_pos(const Staying& r, int n, int j) { return j < r.sinks ? n + j : r.first + (j - r.sinks); }
 
 // Row j of the staying ones of head q.h: chunk ch.
-template <int D>
+template <int D, bool TURN>
 __device__ __forceinline__ void put_row(const AppendArgs& a, const Seq& q, const Staying& r, int j, int ch) {
   constexpr int CPR = D / 8;
   const int p = stay_pos(r, q.n, j), src = new_row(a, q, p - q.n);
   int row;
   const int page = page_of(a, q.s, token_column(a.p, p, row));
-  const __nv_bfloat16 *kr = a.k + q.h * a.k_head + src * a.k_tok, *vr = a.v + q.h * a.v_head + src * a.v_tok;
+  const __nv_bfloat16* vr = a.v + q.h * a.v_head + src * a.v_tok;
+  const __nv_bfloat16* kr = !TURN && a.turned ? a.turned + ((size_t)q.h * a.p.n_new + q.tok0 + (p - q.n)) * D : a.k + q.h * a.k_head + src * a.k_tok;
   const uint4 vx = *reinterpret_cast<const uint4*>(vr + 8 * ch);
-  const uint4 kx = a.rope.half > 0 ? rotated_chunk(kr, ch, p, a.rope) : *reinterpret_cast<const uint4*>(kr + 8 * ch);
+  const uint4 kx = TURN && a.rope.half > 0 ? rotated_chunk(kr, ch, p, a.rope) : *reinterpret_cast<const uint4*>(kr + 8 * ch);
   if ((unsigned)page >= (unsigned)a.p.n_pages) return;
   const size_t at = ((((size_t)page * a.p.Hkv + q.h) << a.p.shift) + row) * CPR + ch;
   reinterpret_cast<uint4*>(a.k_pages)[at] = kx;
@@ -441,8 +444,50 @@ __device__ void check_append(const AppendArgs& a) {
   if (tid == 0) *a.status = bad ? LRSA_ERR_INVALID_ARG : LRSA_OK;
 }
 
-// Clusters of C CTAs: with_rows: one for each (sequence, head); otherwise one for each (window to be cut, head).
+// The keys of all new tokens rotated, for the forms with several launches: a window's rows are read twice there (for its own scores, and as the
+// reference of the one in front), and rotating them each time, in four of eight warps, took 72 us for a 32K prompt of 4 heads, d = 128, where
+// this takes 8 and the cuts, which read the result from L2, 27.  As in lrsa_rotate a thread takes two chunks of a token for all heads, with the
+// angles loaded once.
 template <int D>
+__global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__ AppendArgs a) {
+  constexpr int UNITS = D / 16, TOK = 256 / UNITS, kAhead = 4;
+  const int unit = threadIdx.x % UNITS, tok = blockIdx.x * TOK + threadIdx.x / UNITS;
+  wait_front();
+  if (tok >= a.p.n_new) return;
+  int lo = 0, hi = a.p.n_seqs;   // the last sequence that begins at or before the token
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.p.cu[mid] <= tok) lo = mid; else hi = mid;
+  }
+  const SeqCounts c = seq_counts(a.p, lo, a.most, a.limit);
+  if (tok < c.tok0 || tok >= c.tok0 + c.m) return;   // behind the last one, or a sequence with bad counts
+  const int src = a.rows ? usable(a.rows[tok], a.n_rows) : tok;
+  const __nv_bfloat16* row = a.k + src * a.k_tok;
+  RotUnit u;
+  load_unit(u, row, unit, c.n + tok - c.tok0, a.rope);
+  for (int h0 = 0; h0 < a.p.Hkv; h0 += kAhead) {
+    uint4 x[kAhead], y[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const __nv_bfloat16* r = row + min(h0 + i, a.p.Hkv - 1) * a.k_head;
+      x[i] = *reinterpret_cast<const uint4*>(r + 8 * u.c0);
+      y[i] = *reinterpret_cast<const uint4*>(r + 8 * u.c1);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (h0 + i >= a.p.Hkv) break;
+      u.x = x[i]; u.y = y[i];
+      uint4 hi2[2], lo2[2];
+      turn_unit(u, hi2, lo2);
+      uint4* dst = reinterpret_cast<uint4*>(a.turned + ((size_t)(h0 + i) * a.p.n_new + tok) * D);
+      dst[u.c0] = hi2[0];
+      dst[u.c1] = hi2[1];
+    }
+  }
+}
+
+// Clusters of C CTAs: ROWS: one for each (sequence, head); otherwise one for each (window to be cut, head).
+template <int D, bool ROWS>
 __global__ void __launch_bounds__(kAppThreads, 2) paged_cut_kernel(const __grid_constant__ AppendArgs a, int C) {
   extern __shared__ __align__(16) float app_spread[];   // [2][L]
   __shared__ __align__(16) AppendShared<D> sh;
@@ -454,7 +499,7 @@ __global__ void __launch_bounds__(kAppThreads, 2) paged_cut_kernel(const __grid_
   }
   Seq q;
   int w0, w1;
-  if (a.with_rows) {
+  if (ROWS) {
     q.s = cluster / a.p.Hkv;
     q.h = cluster - q.s * a.p.Hkv;
     const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);
@@ -496,13 +541,13 @@ __global__ void __launch_bounds__(kAppThreads, 2) paged_cut_kernel(const __grid_
     w1 = w0 + 1;
   }
   for (int w = w0; w < w1; ++w) {
-    cut_window<D>(a, q, w, rank, C, sh, app_spread);
+    cut_window<D, ROWS>(a, q, w, rank, C, sh, app_spread);
     cluster_sync();   // the first CTA's positions have been read
   }
-  if (!a.with_rows) return;
+  if (!ROWS) return;
   constexpr int CPR = D / 8;
   const Staying r = staying(a.p, q.n, q.m);
-  for (int i = rank * kAppThreads + threadIdx.x; i < r.count * CPR; i += C * kAppThreads) put_row<D>(a, q, r, i / CPR, i % CPR);
+  for (int i = rank * kAppThreads + threadIdx.x; i < r.count * CPR; i += C * kAppThreads) put_row<D, true>(a, q, r, i / CPR, i % CPR);
 }
 
 // The rows of prompts.  Grid: `blocks` for every sequence; a block takes rows in turn, all heads of them.
@@ -521,15 +566,23 @@ __global__ void __launch_bounds__(kAppThreads) paged_rows_kernel(const __grid_co
   for (long long i = (long long)blk * kAppThreads + threadIdx.x; i < items; i += (long long)blocks * kAppThreads) {
     const int j = (int)(i / per_row), e = (int)(i - (long long)j * per_row);
     q.h = e / CPR;
-    put_row<D>(a, q, r, j, e % CPR);
+    put_row<D, false>(a, q, r, j, e % CPR);
   }
 }
+
+// One launch while a sequence gets a few tokens on average: a cluster then writes the few rows of a head by itself and cuts a window at most.
+bool one_launch(long long n_seqs, long long n_new) { return n_new <= 64 * n_seqs; }
 
 bool rows_ok(const lrsa_rows_t* r) {
   return r && r->data && !(reinterpret_cast<uintptr_t>(r->data) & 15u) && r->head_stride % 8 == 0 && r->token_stride % 8 == 0;
 }
 
 }  // namespace
+
+size_t append_ws_bytes(const Geom& g, long long n_seqs, long long n_new) {
+  return sizeof(WsHeader) + (one_launch(n_seqs, n_new) ? 0 : (size_t)n_new * g.Hkv * g.d * sizeof(__nv_bfloat16));
+}
+
 }  // namespace lrsa
 
 using namespace lrsa;
@@ -553,7 +606,7 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   if (((bits(paged->k_pages) | bits(paged->v_pages)) & 15u) ||
       ((bits(paged->table) | bits(paged->n_tokens) | bits(cu_new) | bits(rows) | bits(kept)) & 3u) || (bits(workspace) & 255u))
     return LRSA_ERR_INVALID_ARG;
-  if (workspace_bytes < sizeof(WsHeader)) return LRSA_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < append_ws_bytes(g, paged->n_seqs, n_new)) return LRSA_ERR_WORKSPACE_TOO_SMALL;
   if (g.L > kAppMaxL) return LRSA_ERR_UNSUPPORTED;
   auto st = static_cast<cudaStream_t>(cuda_stream);
   a.p.cu = cu_new; a.p.n_new = n_new;
@@ -568,9 +621,15 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   a.limit = a.rope.half > 0 && a.rope.n_pos < g.N ? a.rope.n_pos : g.N;
   a.ddof = g.ddof;
   const int n_seqs = paged->n_seqs;
-  // One launch while a sequence gets a few tokens on average: a cluster then writes the few rows of a head by itself and cuts a window at most.
-  a.with_rows = n_new <= 64LL * n_seqs;
-  const long long windows = a.with_rows ? n_seqs : (long long)n_new / g.L + (n_seqs < n_new ? n_seqs : n_new);
+  const bool one = one_launch(n_seqs, n_new);
+  if (!one && a.rope.half > 0) {
+    a.turned = reinterpret_cast<__nv_bfloat16*>(static_cast<unsigned char*>(workspace) + sizeof(WsHeader));
+    const int tok = 256 / (g.d / 16);
+    LRSA_CUDA_CHECK(launch_dependent(g.d == 128 ? paged_turn_kernel<128> : paged_turn_kernel<64>, dim3((unsigned)((n_new + tok - 1) / tok)), dim3(256), 0,
+                                     st, 1, a));
+    launch_counter().n++;
+  }
+  const long long windows = one ? n_seqs : (long long)n_new / g.L + (n_seqs < n_new ? n_seqs : n_new);
   // A window's rows are read by C CTAs, as many as find room at a time.
   int C = 1;
   while (C < 8 && windows * g.Hkv * 2 * C <= 2 * kSms && g.L / (2 * C) >= 128) C *= 2;
@@ -578,11 +637,11 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   a.clusters = (int)clusters;
   const size_t smem = (size_t)2 * g.L * sizeof(float);
-  auto cut = g.d == 128 ? paged_cut_kernel<128> : paged_cut_kernel<64>;
+  auto cut = g.d == 128 ? (one ? paged_cut_kernel<128, true> : paged_cut_kernel<128, false>) : (one ? paged_cut_kernel<64, true> : paged_cut_kernel<64, false>);
   if (smem > 16 * 1024) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cut, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   LRSA_CUDA_CHECK(launch_dependent(cut, dim3((unsigned)grid), dim3(kAppThreads), smem, st, C, a, C));
   launch_counter().n++;
-  if (a.with_rows) return LRSA_OK;
+  if (one) return LRSA_OK;
   const long long stay = (long long)g.S + 2 * g.L < n_new ? (long long)g.S + 2 * g.L : n_new;   // rows of a sequence at most
   const int per_block = kAppThreads / (g.d / 8) * 2;
   long long blocks = (stay * g.Hkv + per_block - 1) / per_block;

@@ -1325,7 +1325,7 @@ int lrsa_paged_shape(const lrsa_params_t* params, int32_t page, int32_t n_seqs, 
   if (rc != LRSA_OK) return rc;
   if (table_width) *table_width = p.width;
   if (w_cap) *w_cap = p.w_cap;
-  if (workspace_bytes) *workspace_bytes = max_new > 0 ? attend_ws(g, n_seqs, n_new, (long long)max_new * g.G <= kFewRows).total : sizeof(WsHeader);
+  if (workspace_bytes) *workspace_bytes = max_new > 0 ? attend_ws(g, n_seqs, n_new, (long long)max_new * g.G <= kFewRows).total : append_ws_bytes(g, n_seqs, n_new);
   return LRSA_OK;
 }
 

@@ -162,6 +162,8 @@ struct PageGeom {
   const int32_t* cu;             // [n_seqs + 1]: where the new tokens of a sequence begin
   int n_new;                     // new tokens that there is room for (cu[n_seqs] may be less)
 };
+// paged_append.cu : the workspace of an append.
+size_t append_ws_bytes(const Geom& g, long long n_seqs, long long n_new);
 // Checks the caller's description and fills everything but cu and n_new.  An lrsa_status.
 int make_pages(const lrsa_params_t* params, const lrsa_paged_t* paged, Geom* g, PageGeom* out);
 

@@ -755,13 +755,13 @@ class PagedCache:
         self.ws = new_workspace(self.workspace_bytes(1, 1, 1), device)
 
     def workspace_bytes(self, n_seqs: int, n_new: int, max_new: int) -> int:
-        """What an attend of n_new tokens of n_seqs sequences, at most max_new each, takes."""
+        """What an attend of n_new tokens of n_seqs sequences, at most max_new each, takes; max_new = 0: an append."""
         out = ctypes.c_size_t(0)
         _check(lib().lrsa_paged_shape(self.params.ref(), self.page, n_seqs, n_new, max_new, None, None, ctypes.byref(out)), "lrsa_paged_shape")
         return out.value
 
     def _workspace(self, near, stream, *sizes):
-        """The workspace, at least as large as an attend of these sizes needs.  One that was outgrown stays where it is: a captured
+        """The workspace, at least as large as a call of these sizes needs.  One that was outgrown stays where it is: a captured
         call may hold its address."""
         need = self._need.get(sizes)
         if need is None:
@@ -849,7 +849,7 @@ class PagedCache:
             _expect(where, "rows", rows, (n_new,), torch.int32, dev)
         if kept is not None:
             _expect(where, "kept", kept, (pages[2], p.n_kv_heads, self.w_cap, p.top_k), torch.int32, dev)
-        cp, ws = p.struct(), self.ws
+        cp, ws = p.struct(), self._workspace(k_new, stream, pages[2], n_new, 0)
         status = call.paged_append(ctypes.addressof(cp), *pages, *k, *v, n_rows, cu_new.data_ptr(), n_new, _p(rows),
                                    *_rope_args(where, rope, dev), _p(kept), ws.data_ptr(), ws.numel(), _stream_of(stream, dev))
         if status:
