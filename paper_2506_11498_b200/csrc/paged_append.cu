@@ -57,7 +57,8 @@ struct AppendArgs {
   int* status;                              // written by the last cluster (null: not by this launch)
   int most, limit;                          // bounds of the counts
   int ddof;
-  int clusters;                             // clusters that work (the one behind them checks)
+  int clusters;                             // clusters that cut; the one behind them checks, those behind that write the rows of fresh sequences
+  int row_blocks;                           // blocks that share the rows of a sequence
 };
 
 // What a CTA works on: sequence, head, its counts.
@@ -346,23 +347,37 @@ __device__ void cut_window(const AppendArgs& a, const Seq& q, int w, int rank, i
   const int ch = lane % CPR;
   const uint32_t from = in_cluster(list, 0);
   const int col0 = a.p.sp + 2 * a.p.lp + w * a.p.kp;
-  for (int j0 = me * ROWS; j0 < K; j0 += warps * ROWS) {
-    const int j = j0 + lane / CPR;
-    if (j >= K) break;
-    int i;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(i) : "r"(from + 4 * j) : "memory");
-    i = min(max(i, 0), L - 1);
-    const int p = a.p.S + w * L + i, page = page_of(a, q.s, col0 + (j >> a.p.shift));
-    bool turn, none;
-    const __nv_bfloat16 *kr = token_row<D, TURN>(a, q, p, 0, turn), *vr = token_row<D, TURN>(a, q, p, 1, none);
-    const uint4 kx = turn ? rotated_chunk(kr, ch, p, a.rope) : *reinterpret_cast<const uint4*>(kr + 8 * ch);
-    const uint4 vx = *reinterpret_cast<const uint4*>(vr + 8 * ch);
-    if ((unsigned)page < (unsigned)a.p.n_pages) {
-      const size_t at = ((((size_t)page * a.p.Hkv + q.h) << a.p.shift) + (j & ((1 << a.p.shift) - 1))) * CPR + ch;
-      reinterpret_cast<uint4*>(a.k_pages)[at] = kx;
-      reinterpret_cast<uint4*>(a.v_pages)[at] = vx;
+  // (four rows a thread at a time: positions, then rows: one by one each is a chain of round trips)
+  constexpr int kAhead = 4;
+  for (int j0 = me * ROWS + lane / CPR; j0 < K; j0 += kAhead * warps * ROWS) {
+    int pos[kAhead], page[kAhead];
+    uint4 kx[kAhead], vx[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = min(j0 + u * warps * ROWS, K - 1);
+      int i;
+      asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(i) : "r"(from + 4 * j) : "memory");
+      pos[u] = a.p.S + w * L + min(max(i, 0), L - 1);
+      page[u] = page_of(a, q.s, col0 + (j >> a.p.shift));
     }
-    if (a.kept && ch == 0) a.kept[(((size_t)q.s * a.p.Hkv + q.h) * a.p.w_cap + w) * K + j] = p;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      bool turn, none;
+      const __nv_bfloat16 *kr = token_row<D, TURN>(a, q, pos[u], 0, turn), *vr = token_row<D, TURN>(a, q, pos[u], 1, none);
+      kx[u] = TURN && turn ? rotated_chunk(kr, ch, pos[u], a.rope) : *reinterpret_cast<const uint4*>(kr + 8 * ch);
+      vx[u] = *reinterpret_cast<const uint4*>(vr + 8 * ch);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u * warps * ROWS;
+      if (j >= K) break;
+      if ((unsigned)page[u] < (unsigned)a.p.n_pages) {
+        const size_t at = ((((size_t)page[u] * a.p.Hkv + q.h) << a.p.shift) + (j & ((1 << a.p.shift) - 1))) * CPR + ch;
+        reinterpret_cast<uint4*>(a.k_pages)[at] = kx[u];
+        reinterpret_cast<uint4*>(a.v_pages)[at] = vx[u];
+      }
+      if (a.kept && ch == 0) a.kept[(((size_t)q.s * a.p.Hkv + q.h) * a.p.w_cap + w) * K + j] = pos[u];
+    }
   }
 }
 
@@ -377,6 +392,9 @@ __device__ __forceinline__ Staying staying(const PageGeom& p, int n, int m) {
   return r;
 }
 __device__ __forceinline__ int stay_pos(const Staying& r, int n, int j) { return j < r.sinks ? n + j : r.first + (j - r.sinks); }
+
+// A sequence of which no window that may be cut is in the pages: its rows can be written while its windows are cut.
+__device__ __forceinline__ bool fresh(const PageGeom& p, int n) { return n <= p.S; }
 
 // Row j of the staying ones of head q.h: chunk ch.
 template <int D, bool TURN>
@@ -393,6 +411,21 @@ __device__ __forceinline__ void put_row(const AppendArgs& a, const Seq& q, const
   const size_t at = ((((size_t)page * a.p.Hkv + q.h) << a.p.shift) + row) * CPR + ch;
   reinterpret_cast<uint4*>(a.k_pages)[at] = kx;
   reinterpret_cast<uint4*>(a.v_pages)[at] = vx;
+}
+
+// The staying rows of a sequence, all heads of them, by the blocks first, first + step, ...
+template <int D, bool TURN>
+__device__ __forceinline__ void put_rows(const AppendArgs& a, Seq& q, int first, int step) {
+  constexpr int CPR = D / 8;
+  const Staying r = staying(a.p, q.n, q.m);
+  const int per_row = a.p.Hkv * CPR;
+  const long long items = (long long)r.count * per_row;
+#pragma unroll 2
+  for (long long i = (long long)first * kAppThreads + threadIdx.x; i < items; i += (long long)step * kAppThreads) {
+    const int j = (int)(i / per_row), e = (int)(i - (long long)j * per_row);
+    q.h = e / CPR;
+    put_row<D, TURN>(a, q, r, j, e % CPR);
+  }
 }
 
 // One CTA looks at everything that the others take from the device, and writes the status word.  A thread looks at the few pages of
@@ -454,6 +487,20 @@ __global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__
   const int unit = threadIdx.x % UNITS, tok = blockIdx.x * TOK + threadIdx.x / UNITS;
   wait_front();
   if (tok >= a.p.n_new) return;
+  const int src = a.rows ? usable(a.rows[tok], a.n_rows) : tok;
+  const __nv_bfloat16* row = a.k + src * a.k_tok;
+  RotUnit u;
+  place_unit(u, unit, a.rope);
+  uint4 x[kAhead], y[kAhead];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const __nv_bfloat16* r = row + min(h0 + i, a.p.Hkv - 1) * a.k_head;
+      x[i] = __ldcs(reinterpret_cast<const uint4*>(r + 8 * u.c0));
+      y[i] = __ldcs(reinterpret_cast<const uint4*>(r + 8 * u.c1));
+    }
+  };
+  load(0);                       // on their way while the token's sequence is looked for
   int lo = 0, hi = a.p.n_seqs;   // the last sequence that begins at or before the token
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -461,18 +508,9 @@ __global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__
   }
   const SeqCounts c = seq_counts(a.p, lo, a.most, a.limit);
   if (tok < c.tok0 || tok >= c.tok0 + c.m) return;   // behind the last one, or a sequence with bad counts
-  const int src = a.rows ? usable(a.rows[tok], a.n_rows) : tok;
-  const __nv_bfloat16* row = a.k + src * a.k_tok;
-  RotUnit u;
-  load_unit(u, row, unit, c.n + tok - c.tok0, a.rope);
+  load_angles(u, unit, c.n + tok - c.tok0, a.rope);
   for (int h0 = 0; h0 < a.p.Hkv; h0 += kAhead) {
-    uint4 x[kAhead], y[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const __nv_bfloat16* r = row + min(h0 + i, a.p.Hkv - 1) * a.k_head;
-      x[i] = *reinterpret_cast<const uint4*>(r + 8 * u.c0);
-      y[i] = *reinterpret_cast<const uint4*>(r + 8 * u.c1);
-    }
+    if (h0 > 0) load(h0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (h0 + i >= a.p.Hkv) break;
@@ -493,11 +531,22 @@ __global__ void __launch_bounds__(kAppThreads, 2) paged_cut_kernel(const __grid_
   __shared__ __align__(16) AppendShared<D> sh;
   const int cluster = blockIdx.x / C, rank = blockIdx.x - cluster * C;
   wait_front();
+  Seq q;
   if (cluster >= a.clusters) {
-    if (rank == 0 && a.status) check_append(a);
+    if (cluster == a.clusters) {
+      if (rank == 0) check_append(a);
+      return;
+    }
+    if constexpr (!ROWS) {   // the rows of fresh sequences
+      const int blk = blockIdx.x - (a.clusters + 1) * C;
+      q.s = blk / a.row_blocks;
+      if (q.s >= a.p.n_seqs) return;
+      const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);
+      q.n = c.n; q.m = c.m; q.tok0 = c.tok0;
+      if (fresh(a.p, q.n)) put_rows<D, false>(a, q, blk - q.s * a.row_blocks, a.row_blocks);
+    }
     return;
   }
-  Seq q;
   int w0, w1;
   if (ROWS) {
     q.s = cluster / a.p.Hkv;
@@ -550,24 +599,16 @@ __global__ void __launch_bounds__(kAppThreads, 2) paged_cut_kernel(const __grid_
   for (int i = rank * kAppThreads + threadIdx.x; i < r.count * CPR; i += C * kAppThreads) put_row<D, true>(a, q, r, i / CPR, i % CPR);
 }
 
-// The rows of prompts.  Grid: `blocks` for every sequence; a block takes rows in turn, all heads of them.
+// The rows of prompts that go on from what is in the cache.  Grid: row_blocks for every sequence.
 template <int D>
-__global__ void __launch_bounds__(kAppThreads) paged_rows_kernel(const __grid_constant__ AppendArgs a, int blocks) {
-  constexpr int CPR = D / 8;
-  const int blk = blockIdx.x % blocks;
+__global__ void __launch_bounds__(kAppThreads) paged_rows_kernel(const __grid_constant__ AppendArgs a) {
+  const int blocks = a.row_blocks;
   Seq q;
   q.s = blockIdx.x / blocks;
   wait_front();
   const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);
   q.n = c.n; q.m = c.m; q.tok0 = c.tok0;
-  const Staying r = staying(a.p, q.n, q.m);
-  const int per_row = a.p.Hkv * CPR;
-  const long long items = (long long)r.count * per_row;
-  for (long long i = (long long)blk * kAppThreads + threadIdx.x; i < items; i += (long long)blocks * kAppThreads) {
-    const int j = (int)(i / per_row), e = (int)(i - (long long)j * per_row);
-    q.h = e / CPR;
-    put_row<D, false>(a, q, r, j, e % CPR);
-  }
+  if (!fresh(a.p, q.n)) put_rows<D, false>(a, q, blockIdx.x % blocks, blocks);
 }
 
 // One launch while a sequence gets a few tokens on average: a cluster then writes the few rows of a head by itself and cuts a window at most.
@@ -633,7 +674,13 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   // A window's rows are read by C CTAs, as many as find room at a time.
   int C = 1;
   while (C < 8 && windows * g.Hkv * 2 * C <= 2 * kSms && g.L / (2 * C) >= 128) C *= 2;
-  const long long clusters = windows * g.Hkv, grid = (clusters + 1) * C;
+  // The rows of a sequence that stay, in blocks of four rounds: where the cuts leave room, beside them.
+  const long long stay = (long long)g.S + 2 * g.L < n_new ? (long long)g.S + 2 * g.L : n_new;
+  const int per_block = kAppThreads / (g.d / 8) * 4;
+  a.row_blocks = (int)((stay * g.Hkv + per_block - 1) / per_block);
+  if (a.row_blocks < 1) a.row_blocks = 1;
+  const long long clusters = windows * g.Hkv, row_clusters = one ? 0 : ((long long)a.row_blocks * n_seqs + C - 1) / C;
+  const long long grid = (clusters + 1 + row_clusters) * C;
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   a.clusters = (int)clusters;
   const size_t smem = (size_t)2 * g.L * sizeof(float);
@@ -642,13 +689,8 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   LRSA_CUDA_CHECK(launch_dependent(cut, dim3((unsigned)grid), dim3(kAppThreads), smem, st, C, a, C));
   launch_counter().n++;
   if (one) return LRSA_OK;
-  const long long stay = (long long)g.S + 2 * g.L < n_new ? (long long)g.S + 2 * g.L : n_new;   // rows of a sequence at most
-  const int per_block = kAppThreads / (g.d / 8) * 2;
-  long long blocks = (stay * g.Hkv + per_block - 1) / per_block;
-  if (blocks > 8 * kSms) blocks = 8 * kSms;
-  if (blocks * n_seqs > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
-  LRSA_CUDA_CHECK(launch_dependent(g.d == 128 ? paged_rows_kernel<128> : paged_rows_kernel<64>, dim3((unsigned)(blocks * n_seqs)), dim3(kAppThreads),
-                                   0, st, 1, a, (int)blocks));
+  LRSA_CUDA_CHECK(launch_dependent(g.d == 128 ? paged_rows_kernel<128> : paged_rows_kernel<64>, dim3((unsigned)((long long)a.row_blocks * n_seqs)),
+                                   dim3(kAppThreads), 0, st, 1, a));
   launch_counter().n++;
   return LRSA_OK;
 }

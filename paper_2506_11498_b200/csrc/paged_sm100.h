@@ -104,18 +104,23 @@ struct RotUnit {
   float4 cs[2], sn[2];
   int c0, c1, kind;    // 0: not rotated, 1: partners, 2: pairs of neighbours
 };
-__device__ __forceinline__ void load_unit(RotUnit& u, const __nv_bfloat16* row, int unit, int pos, const RopeArgs& r) {
+__device__ __forceinline__ void place_unit(RotUnit& u, int unit, const RopeArgs& r) {
   const int m = r.half >> 3;
   u.kind = unit >= m ? 0 : r.interleaved ? 2 : 1;
   u.c0 = u.kind == 1 ? unit : 2 * unit;
   u.c1 = u.kind == 1 ? unit + m : u.c0 + 1;
+}
+__device__ __forceinline__ void load_angles(RotUnit& u, int unit, int pos, const RopeArgs& r) {
+  if (u.kind == 0) return;
+  const float4* cs = reinterpret_cast<const float4*>(r.cos + (size_t)pos * r.half + 8 * unit);
+  const float4* sn = reinterpret_cast<const float4*>(r.sin + (size_t)pos * r.half + 8 * unit);
+  u.cs[0] = cs[0]; u.cs[1] = cs[1]; u.sn[0] = sn[0]; u.sn[1] = sn[1];
+}
+__device__ __forceinline__ void load_unit(RotUnit& u, const __nv_bfloat16* row, int unit, int pos, const RopeArgs& r) {
+  place_unit(u, unit, r);
   u.x = *reinterpret_cast<const uint4*>(row + 8 * u.c0);
   u.y = *reinterpret_cast<const uint4*>(row + 8 * u.c1);
-  if (u.kind != 0) {
-    const float4* cs = reinterpret_cast<const float4*>(r.cos + (size_t)pos * r.half + 8 * unit);
-    const float4* sn = reinterpret_cast<const float4*>(r.sin + (size_t)pos * r.half + 8 * unit);
-    u.cs[0] = cs[0]; u.cs[1] = cs[1]; u.sn[0] = sn[0]; u.sn[1] = sn[1];
-  }
+  load_angles(u, unit, pos, r);
 }
 // hi: the chunks rounded to bf16; lo: what that leaves, rounded to bf16
 __device__ __forceinline__ void turn_unit(const RotUnit& u, uint4 (&hi)[2], uint4 (&lo)[2]) {
