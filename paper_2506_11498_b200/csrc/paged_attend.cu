@@ -1143,8 +1143,9 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           l *= f;
           if (need) m = mx;
         }
-        const float nmc = m == -INFINITY ? 0.f : -m * c;
-        const uint64_t c2 = f2_pack(c, c), nmc2 = f2_pack(nmc, nmc);
+        // (s - m) c, not s c - m c in one step: there the rounding of m c is left over, and where scores are beyond 2^31 it is an exponent that overflows
+        const float nm = m == -INFINITY ? 0.f : -m;
+        const uint64_t c2 = f2_pack(c, c), nm2 = f2_pack(nm, nm);
         uint64_t sum2 = f2_pack(0.f, 0.f), sum2b = f2_pack(0.f, 0.f);
         // exponentials as a software pipeline, P over S in two halves, as in the forward
         constexpr int kPairs = kTile / 4, kLag = 4;
@@ -1156,7 +1157,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
             if (ii < kPairs) {
               const int i = half * kPairs + ii;
               float x0, x1;
-              f2_unpack(f2_fma(f2_pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, nmc2), x0, x1);
+              f2_unpack(f2_mul(f2_add(f2_pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), nm2), c2), x0, x1);
               s[2 * i] = __float_as_uint(ex2_ordered(x0));
               s[2 * i + 1] = __float_as_uint(ex2_ordered(x1));
             }

@@ -740,6 +740,7 @@ class PagedCache:
     attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status()."""
 
     MOST_NEW = 128   # new tokens of a sequence in an attend
+    _seen = None     # where the pages were when they were last looked at
 
     def __init__(self, params: Params, n_pages: int, page: int = 64, device="cuda"):
         self.params, self.page, self.n_pages = params, page, n_pages
@@ -788,6 +789,8 @@ class PagedCache:
         """(device, what csrc/pycall.c takes of the cache), when everything is what the kernels read and write.  The pages are looked at
         when they have been replaced, or lie elsewhere than they did."""
         dev = _device(where, name, first)
+        if self._seen is None:
+            self._look(where, dev)
         at_k, at_v = self.k_pages.data_ptr(), self.v_pages.data_ptr()
         if self._seen != (at_k, at_v, dev):
             self._look(where, dev)
@@ -812,6 +815,8 @@ class PagedCache:
     def _look(self, where, dev):
         """Raises LRSA_ERR_INVALID_ARG unless the pages are what the kernels read and write."""
         for name, t in (("k_pages", self.k_pages), ("v_pages", self.v_pages)):
+            if not isinstance(t, torch.Tensor) or t.device != self.ws.device:
+                raise LrsaError(1, f"{where}: {name} of the cache must be a tensor on {self.ws.device}")
             _expect(where, name + " of the cache", t, self._shape, torch.bfloat16, dev)
             if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
                 raise LrsaError(1, f"{where}: {name} of the cache has lost its memory")

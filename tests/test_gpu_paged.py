@@ -252,3 +252,386 @@ def test_many_sequences_of_all_lengths(name, most):
     m.append([int(x) for x in m.rng.integers(0, 1400, n_seqs) * (m.rng.random(n_seqs) < 0.7)])
     for _ in range(2):
         m.attend([int(x) for x in m.rng.integers(0, most + 1, n_seqs)], max_new=most)
+
+
+WIDE = {   # odd groups, windows longer than the scoring kernel's clusters take, tiny ones
+    "g20": (lrsa.Params(1, 20, 1, 900, 64, 64, 16, 4), 16, 64, False),
+    "g130": (lrsa.Params(1, 130, 1, 900, 128, 64, 16, 4), 32, 64, False),
+    "g300": (lrsa.Params(1, 600, 2, 900, 64, 100, 7, 0), 64, 0, False),
+    "mha24": (lrsa.Params(1, 24, 24, 900, 64, 33, 33, 2), 128, 32, True),
+    "l1": (lrsa.Params(1, 4, 2, 300, 64, 1, 1, 0), 16, 16, False),
+    "all_sinks": (lrsa.Params(1, 4, 2, 300, 128, 200, 3, 290), 64, 128, False),
+}
+
+
+@pytest.mark.parametrize("name", WIDE)
+def test_wide_groups_and_odd_windows(name):
+    p, page, dim, interleaved = WIDE[name]
+    m = Model(p, page, 3, dim, interleaved, seed=4)
+    m.append([p.seq_len // 3, 1, p.seq_len - 20])
+    m.check_pages()
+    m.attend([1, 1, 1])
+    m.attend([3, 0, 7])
+    m.append([5, 2, 12], pick=list(range(0, 38, 2)))
+    m.check_pages()
+    m.attend([2, 17, 1], tree=False)
+
+
+@pytest.mark.parametrize("d, L", [(64, 9000), (128, 5001)])
+def test_long_windows(d, L):
+    p = lrsa.Params(1, 2, 1, 5 * L, d, L, L // 8, 3)
+    m = Model(p, 128, 2, dim=d, seed=6)
+    m.append([3 + 3 * L + 17, 3 + 2 * L - 1])
+    m.append([1, 1])
+    m.check_pages()
+    m.attend([1, 30])
+
+
+def test_a_thousand_sequences():
+    p = lrsa.Params(1, 4, 2, 400, 64, 32, 8, 2)
+    m = Model(p, 16, 1000, dim=64, seed=7)
+    m.append([int(x) for x in m.rng.integers(0, 150, 1000)])
+    m.append([int(x) for x in m.rng.integers(0, 3, 1000)])
+    m.attend([1] * 1000)
+    m.attend([int(x) for x in m.rng.integers(0, 12, 1000)], max_new=12)
+
+
+def test_pages_far_into_a_large_pool():
+    """More than 2^31 elements of K in front of the pages in use."""
+    p = lrsa.Params(1, 8, 4, 900, 128, 128, 32, 4)
+    m = Model(p, 64, 2, dim=128, seed=8)
+    n_pages = (1 << 31) // (4 * 64 * 128) + 40
+    small = m.cache
+    m.cache = lrsa.PagedCache(p, 1, page=64)
+    m.cache.n_pages, m.cache._shape = n_pages, torch.Size((n_pages, 4, 64, 128))
+    m.cache.k_pages = torch.empty(m.cache._shape, dtype=torch.bfloat16, device="cuda")
+    m.cache.v_pages = torch.empty_like(m.cache.k_pages)
+    m.free = list(range(n_pages - 38, n_pages))
+    m.append([700, 33])
+    m.append([1, 300])
+    used = sorted({int(x) for x in m.table.ravel() if x >= 0})
+    assert min(used) * 4 * 64 * 128 >= 1 << 31
+    for t, host in ((m.cache.k_pages, m.K), (m.cache.v_pages, m.V)):
+        for s, n in enumerate(m.n):
+            for pos in range(min(n, p.n_sink)):
+                col, row = ref.place(p, 64, pos)
+                assert np.array_equal(f64(t[m.table[s, col], :, row]), host[s][:, pos])
+    m.attend([1, 1])
+    m.attend([40, 3])
+    del small
+
+
+def test_infinities_and_nan_of_tokens_that_are_not_seen():
+    """A row's result does not depend on drafts that it does not see, whatever they hold; a value that it sees does what it does in the formula."""
+    for p, new in ((lrsa.Params(1, 4, 2, 600, 64, 64, 16, 4), 6), (lrsa.Params(1, 4, 2, 600, 128, 64, 16, 4), 3),
+                   (lrsa.Params(1, 14, 2, 600, 128, 64, 16, 4), 30), (lrsa.Params(1, 8, 1, 600, 64, 64, 16, 4), 40)):
+        m = Model(p, 16, 1, dim=64, seed=9)
+        m.append([300])
+        G = p.n_q_heads // p.n_kv_heads
+        q, k, v = (m.rows(h, new, False).cuda() for h in (p.n_q_heads, p.n_kv_heads, p.n_kv_heads))
+        parent = i32([-1] + [0 if i == 1 else -1 if i == 2 else i - 2 for i in range(1, new)])    # two chains: 0, 1, 3, 5 ... and 2, 4, 6 ...
+        table, n_tokens, cu = m.device([new])
+        args = (table, n_tokens, cu, parent, m.rope)
+        want, want_lse = m.cache.attend(q, k, v, *args)
+        k2, v2 = k.clone(), v.clone()
+        k2[:, 2, 3], v2[:, 2, 5], v2[:, 2, 6], v2[:, 2, 7] = float("nan"), float("inf"), float("nan"), float("-inf")
+        for bad_k in (k, k2):
+            o, lse = m.cache.attend(q, bad_k, v2, *args)
+            for i in [0, 1] + list(range(3, new, 2)):
+                assert torch.equal(o[:, i], want[:, i]) and torch.equal(lse[:, i], want_lse[:, i])
+            for i in range(2, new, 2):
+                if bad_k is k:
+                    assert torch.equal(lse[:, i], want_lse[:, i])
+                    clean = [c for c in range(p.head_dim) if c not in (5, 6, 7)]
+                    assert torch.equal(o[:, i, clean], want[:, i, clean])
+                    assert (o[:, i, 5] == float("inf")).all() and torch.isnan(o[:, i, 6]).all() and (o[:, i, 7] == float("-inf")).all()
+                else:
+                    assert torch.isnan(o[:, i]).all() and torch.isnan(lse[:, i]).all()
+        # both signs in one channel of two tokens of a line
+        v3 = v.clone()
+        v3[:, 0, 9], v3[:, 1, 9] = float("inf"), float("-inf")
+        o, _ = m.cache.attend(q, k, v3, *args)
+        assert (o[:, 0, 9] == float("inf")).all() and torch.isnan(o[:, 1, 9]).all() and torch.equal(o[:, 2::2], want[:, 2::2])
+        # what is not finite in the cache is everybody's, in its channel
+        col, row = ref.place(p, 16, 299)
+        m.cache.v_pages[int(m.table[0, col]), :, row, 11] = float("inf")
+        o, lse = m.cache.attend(q, k, v, *args)
+        assert (o[:, :, 11] == float("inf")).all() and torch.equal(lse, want_lse)
+        assert G >= 1
+
+
+def test_scores_that_overflow_and_rows_of_zeros():
+    p = lrsa.Params(1, 4, 2, 600, 64, 64, 16, 4)
+    for new in (2, 20):
+        m = Model(p, 32, 1, seed=10)
+        m.append([200])
+        q, k, v = (m.rows(h, new, False).cuda() for h in (4, 2, 2))
+        table, n_tokens, cu = m.device([new])
+        q[:, 0] = 0                                       # every key counts alike
+        q[1, 1] *= 1e20
+        o, lse = m.cache.attend(q, k, v, table, n_tokens, cu)
+        w = ref.cut(p, 200)
+        n = 4 + w * 16 + 200 - 4 - w * 64 + 1
+        assert np.abs(f64(lse[:, 0]) - math.log(n)).max() < 1e-5
+        assert torch.isfinite(o[[0, 2, 3]]).all() and torch.isfinite(lse[1, 1])      # one key has it all
+        m.cache.k_pages.mul_(0)
+        m.cache.v_pages.mul_(0)
+        m.cache.k_pages.nan_to_num_()
+        m.cache.v_pages.nan_to_num_()
+        k0 = torch.full_like(k, -3e38)
+        o, lse = m.cache.attend(torch.ones_like(q), k0, v, table, n_tokens, cu)      # the new tokens' scores are -infinity, the others' 0
+        assert (o == 0).all() and np.abs(f64(lse) - math.log(n - 1)).max() < 1e-5
+
+
+BAD = {   # what is wrong with which of three sequences
+    "negative tokens": lambda a: a["n_tokens"].__setitem__(1, -1),
+    "too many tokens": lambda a: a["n_tokens"].__setitem__(1, 2000),
+    "counts go back": lambda a: a["cu_new"].__setitem__(2, a["cu_new"][1] - 1),
+    "counts beyond the rows": lambda a: a["cu_new"].__setitem__(3, 1000),
+    "a page that is not there": lambda a: a["table"].__setitem__((1, slice(None)), 1 << 30),
+    "a negative page": lambda a: a["table"].__setitem__((1, slice(None)), -1),
+}
+
+
+@pytest.mark.parametrize("what", BAD)
+@pytest.mark.parametrize("new", [1, 3, 20])
+def test_counts_and_pages_that_cannot_be_used(what, new):
+    p = lrsa.Params(1, 8, 2, 1500, 64, 64, 16, 4)
+    m = Model(p, 16, 3, dim=64, seed=11)
+    m.append([500, 300, 100])
+    for s in range(3):
+        m.reach(s, m.n[s] + new)
+    table, n_tokens, cu = m.device([new] * 3)
+    q, k, v = (m.rows(h, 3 * new).transpose(0, 1).contiguous().cuda().transpose(0, 1) for h in (8, 2, 2))
+    good, _ = m.cache.attend(q, k, v, table, n_tokens, cu, rope=m.rope, max_new=new)
+    assert m.cache.status() == 0
+    args = dict(table=table.clone(), n_tokens=n_tokens.clone(), cu_new=cu.clone())
+    BAD[what](args)
+    o, _ = m.cache.attend(q, k, v, **args, rope=m.rope, max_new=new)
+    assert m.cache.status() == 1
+    if what != "counts beyond the rows":
+        assert torch.equal(o[:, :new], good[:, :new])            # the first sequence is as it was
+    pages = m.cache.k_pages.clone(), m.cache.v_pages.clone()
+    m.cache.append(k, v, **args, rope=m.rope)
+    assert m.cache.status() == 1
+    # nothing is written but the pages of the other sequences
+    fine = [0, 1] if what == "counts beyond the rows" else [0, 2]
+    mine = sorted({int(x) for x in m.table[fine].ravel() if x >= 0})
+    others = [i for i in range(m.cache.n_pages) if i not in mine]
+    for x, y in zip(pages, (m.cache.k_pages, m.cache.v_pages)):
+        assert torch.equal(x[others].view(torch.int16), y[others].view(torch.int16))
+    m.cache.attend(q, k, v, table, n_tokens, cu, rope=m.rope, max_new=new)
+    assert m.cache.status() == 0
+
+
+def test_other_numbers_on_the_device_that_cannot_be_used():
+    p = lrsa.Params(1, 8, 2, 400, 64, 64, 16, 4)
+    m = Model(p, 16, 2, dim=64, seed=12)
+    m.append([380, 100])
+    for s in range(2):
+        m.reach(s, 400 if s == 0 else 140)
+    q, k, v = (m.rows(h, 40, False).cuda() for h in (8, 2, 2))
+    table, n, cu = m.device([20, 20])
+    for max_new in (20, 40):
+        m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=max_new)
+        assert m.cache.status() == 0
+    m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=19)              # more of them than was said
+    assert m.cache.status() == 1
+    m.cache.attend(q, k, v, table, n, cu, max_new=20)                            # without a rope positions may go on
+    m.cache.attend(q, k, v, table, n + 20, cu, max_new=20)
+    assert m.cache.status() == 0
+    m.cache.attend(q, k, v, table, i32([381, 100]), cu, rope=m.rope, max_new=20)  # the rope's last position
+    assert m.cache.status() == 1
+    for bad in (1, 20, -2):
+        parent = i32(list(range(-1, 19)) * 2)
+        parent[1] = bad
+        m.cache.attend(q, k, v, table, n, cu, parent=parent, rope=m.rope, max_new=20)
+        assert m.cache.status() == 1
+    for bad in (40, -1):
+        rows = torch.arange(40, dtype=torch.int32, device="cuda")
+        rows[3] = bad
+        m.cache.append(k, v, table, n, cu, rows=rows, rope=m.rope)
+        assert m.cache.status() == 1
+    m.cache.append(k, v, table, i32([381, 100]), cu, rope=m.rope)                 # beyond seq_len
+    assert m.cache.status() == 1
+    m.cache.append(k, v, table, n, cu, rope=m.rope)
+    assert m.cache.status() == 0
+
+
+def test_rows_behind_the_last_sequence_stay():
+    p = lrsa.Params(1, 8, 2, 400, 64, 64, 16, 4)
+    for new in (1, 20):
+        m = Model(p, 16, 2, dim=64, seed=13)
+        m.append([100, 50])
+        q, k, v = (m.rows(h, 2 * new + 9, False).cuda() for h in (8, 2, 2))
+        k[:, 2 * new:], v[:, 2 * new:] = float("nan"), float("nan")
+        table, n, cu = m.device([new, new])
+        o, lse = torch.full_like(q, 7.0), torch.full((8, 2 * new + 9), 7.0, device="cuda")
+        m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=new, o=o, lse=lse)
+        assert (o[:, 2 * new:] == 7).all() and (lse[:, 2 * new:] == 7).all() and torch.isfinite(o).all()
+
+
+def step(m, q, k, v, table, n, cu, parent, rows, cu_kept, taken):
+    """A step of a server: drafts are attended, some are accepted and enter the cache."""
+    o, lse = m.cache.attend(q, k, v, table, n, cu, parent=parent, rope=m.rope, max_new=12)
+    m.cache.append(k, v, table, n, cu_kept, rows=rows, rope=m.rope)
+    n += taken
+    return o, lse
+
+
+@pytest.mark.parametrize("heads", [(4, 2), (14, 2)])
+def test_a_captured_step_serves_the_later_ones(heads):
+    """The counts are on the device: one graph, replayed while sequences of different lengths grow over windows' ends."""
+    p = lrsa.Params(1, *heads, 1200, 64, 48, 12, 4)
+    a, b = Model(p, 16, 3, dim=64, seed=14), Model(p, 16, 3, dim=64, seed=14)
+    rng = np.random.default_rng(0)
+    for m in (a, b):
+        m.append([300, 40, 3])
+        for s in range(3):
+            m.reach(s, 1100)
+    b.table = a.table
+    b.cache.k_pages.copy_(a.cache.k_pages)
+    b.cache.v_pages.copy_(a.cache.v_pages)
+    table = i32(a.table.tolist())
+    n_a, n_b = i32(a.n), i32(a.n)
+    T = 24
+    bufs = dict(q=a.rows(heads[0], T, False).cuda(), k=a.rows(heads[1], T, False).cuda(), v=a.rows(heads[1], T, False).cuda(),
+                cu=i32([0, 8, 20, 24]), parent=i32([-1] * T), rows=i32([0] * T), cu_kept=i32([0, 1, 2, 3]), taken=i32([1, 1, 1]))
+    n_warm = n_a.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a.cache.attend(bufs["q"], bufs["k"], bufs["v"], table, n_warm, bufs["cu"], parent=bufs["parent"], rope=a.rope, max_new=12)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(a, bufs["q"], bufs["k"], bufs["v"], table, n_a, bufs["cu"], bufs["parent"], bufs["rows"], bufs["cu_kept"], bufs["taken"])
+    for i in range(40):
+        new = [int(x) for x in rng.integers(1, 9, 3)]
+        cu = np.concatenate([[0], np.cumsum(new)])
+        parent, rows, kept = [], [], []
+        for s, x in enumerate(new):
+            up = [int(rng.integers(-1, j)) if j else -1 for j in range(x)]
+            line, j = [], x - 1
+            while j >= 0:
+                line.append(int(cu[s]) + j)
+                j = up[j]
+            parent += up
+            rows += line[::-1]
+            kept.append(len(line))
+        for name, value in (("cu", cu), ("cu_kept", np.concatenate([[0], np.cumsum(kept)])), ("taken", kept)):
+            bufs[name].copy_(i32([int(x) for x in value]))
+        bufs["parent"].copy_(i32(parent + [0] * (T - len(parent))))
+        bufs["rows"].copy_(i32(rows + [0] * (T - len(rows))))
+        for name, h in (("q", heads[0]), ("k", heads[1]), ("v", heads[1])):
+            bufs[name].copy_(a.rows(h, T, False))
+        graph.replay()
+        o, lse = step(b, bufs["q"], bufs["k"], bufs["v"], table, n_b, bufs["cu"], bufs["parent"], bufs["rows"], bufs["cu_kept"], bufs["taken"])
+        used = int(cu[-1])
+        assert torch.equal(n_a, n_b)
+        assert torch.equal(out[0][:, :used], o[:, :used]) and torch.equal(out[1][:, :used], lse[:, :used]), i
+        assert a.cache.status() == 0 and b.cache.status() == 0
+    for x, y in ((a.cache.k_pages, b.cache.k_pages), (a.cache.v_pages, b.cache.v_pages)):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+def test_on_another_stream():
+    p = lrsa.Params(1, 14, 2, 900, 128, 64, 16, 4)
+    m = Model(p, 32, 2, dim=128, seed=15)
+    m.append([400, 77])
+    q, k, v = (m.rows(h, 20, False).cuda() for h in (14, 2, 2))
+    table, n, cu = m.device([12, 8])
+    want = m.cache.attend(q, k, v, table, n, cu, rope=m.rope)
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        side.wait_stream(torch.cuda.current_stream())
+        got = m.cache.attend(q, k, v, table, n, cu, rope=m.rope, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+def test_two_caches_at_once():
+    """Layers share the table and the counts, nothing else."""
+    p = lrsa.Params(1, 14, 2, 900, 128, 64, 16, 4)
+    ms = [Model(p, 32, 2, dim=128, seed=16) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in ms]
+    for m in ms:
+        m.append([400, 77])
+    calls = []
+    for m in ms:
+        q, k, v = (m.rows(h, 40, False).cuda() for h in (14, 2, 2))
+        calls.append((q, k, v) + m.device([30, 10]))
+    want = [m.cache.attend(*c, rope=m.rope) for m, c in zip(ms, calls)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for m, c, st in zip(ms, calls, streams):
+            with torch.cuda.stream(st):
+                got.append(m.cache.attend(*c, rope=m.rope))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_from_a_prompt_to_tokens():
+    """The operators as they are used together: rotation, selection and attention of a prompt, its rows into the cache, then token by
+    token; each token's output against the row that lrsa_attn_fwd gives it when all of them are the prompt."""
+    B, Hq, Hkv, d, L, K, S = 1, 8, 2, 128, 64, 16, 4
+    N, prompt = 520, 300
+    rope = lrsa.Rope.of_base(10000.0, d, N)
+    gen = torch.Generator().manual_seed(17)
+    Q, Kx, V = (torch.randn(B, h, N, d, generator=gen).bfloat16().cuda() for h in (Hq, Hkv, Hkv))
+    whole = lrsa.Params(B, Hq, Hkv, N, d, L, K, S)
+    Qr, Kr = lrsa.lrsa_rotate(whole, Q, Kx, rope)
+    idx, _ = lrsa.lrsa_score_select(whole, Kr, V)
+    O, LSE = lrsa.lrsa_attn_fwd(whole, Qr, Kr, V, idx)
+    cache = lrsa.PagedCache(whole, 64, page=16)
+    table = torch.full((1, cache.table_width), -1, dtype=torch.int32)
+    cols = cache.columns(N)
+    table[0, cols] = torch.randperm(64, generator=gen)[:len(cols)].int()
+    table, n = table.cuda(), i32([0])
+    cache.append(Kr[0, :, :prompt], V[0, :, :prompt], table, n, i32([0, prompt]))     # rotated already
+    n += prompt
+    t = prompt
+    while t < N:
+        m = min(1 if t % 3 else 7, N - t, L - (t - S) % L)        # a chain inside a chunk sees what the mask shows it
+        part = slice(t, t + m)
+        o, lse = cache.attend(Q[0, :, part], Kx[0, :, part], V[0, :, part], table, n, i32([0, m]), rope=rope, max_new=m)
+        # bf16 probabilities and outputs on both sides (2^-8 each of terms of size 1 or less); the forward's queries are rounded
+        assert (o.float() - O[0, :, part].float()).abs().max() < 2e-2 and (lse - LSE[0, :, part]).abs().max() < 5e-3, t
+        cache.append(Kx[0, :, part], V[0, :, part], table, n, i32([0, m]), rope=rope)
+        n += m
+        t += m
+        assert cache.status() == 0
+
+
+def test_training_through_the_rotation():
+    """Gradients of the unrotated queries and keys, against autograd in 64 bits through rotation and masked attention."""
+    from oracle import lrsa_oracle as orc
+    B, Hq, Hkv, N, d, L, K, S = 1, 4, 2, 200, 64, 32, 8, 4
+    p = lrsa.Params(B, Hq, Hkv, N, d, L, K, S)
+    cos, sin = ref.angles(N, d)
+    rope = lrsa.Rope(torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda(), True)
+    gen = torch.Generator().manual_seed(18)
+    Q, Kx, V, dO = (torch.randn(B, h, N, d, generator=gen).bfloat16() for h in (Hq, Hkv, Hkv, Hq))
+    Qr, Kr = lrsa.lrsa_rotate(p, Q.cuda(), Kx.cuda(), rope)
+    idx, _ = lrsa.lrsa_score_select(p, Kr, V.cuda())
+    O, LSE = lrsa.lrsa_attn_fwd(p, Qr, Kr, V.cuda(), idx)
+    dQr, dKr, dV = lrsa.lrsa_attn_bwd(p, Qr, Kr, V.cuda(), O, dO.cuda(), LSE, idx)
+    dQ, dK = lrsa.lrsa_rotate(p, dQr, dKr, rope, inverse=True)
+    op = orc.OracleParams(B, Hq, Hkv, N, d, L, K, S)
+    hidx = idx.cpu().numpy()
+    q, k, v = (x.double().requires_grad_() for x in (Q, Kx, V))
+    c, s = torch.from_numpy(cos).double(), torch.from_numpy(sin).double()
+
+    def turn(x):
+        a, b = x[..., 0::2], x[..., 1::2]
+        return torch.stack([a * c - b * s, b * c + a * s], -1).flatten(-2)
+
+    x = turn(q) @ turn(k).repeat_interleave(Hq // Hkv, 1).transpose(-1, -2) / math.sqrt(d)
+    vis = torch.stack([torch.from_numpy(np.stack([orc.visible_row(op, hidx, 0, h // (Hq // Hkv), t) for t in range(N)])) for h in range(Hq)])
+    o = torch.softmax(x.masked_fill(~vis.bool(), -math.inf), -1) @ v.repeat_interleave(Hq // Hkv, 1)
+    o.backward(dO.double())
+    for name, got, want in (("dQ", dQ, q.grad), ("dK", dK, k.grad), ("dV", dV, v.grad)):
+        err = (got.double().cpu() - want).norm() / want.norm()
+        assert err < 1.5e-2, (name, float(err))     # the backward's bound on this norm, 1e-2, and one more rounding to bf16
