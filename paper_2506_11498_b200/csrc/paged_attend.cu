@@ -223,6 +223,10 @@ __device__ __forceinline__ void note_divided(const AttendArgs& a, const Line& li
   a.divided[cta] = d;
 }
 
+// Key tile j of a run in the order in which the kernel for many rows takes them: the new tokens' last (their operands come from the launch in front
+// and take three ring slots; the pages' first tile is on its way at once).
+__device__ __forceinline__ int tile_of(const Share& it, int j) { return it.t0 > 0 ? it.t0 + j : j + 1 < it.t1 ? j + 1 : 0; }
+
 // A partial result: O [D / 4][rows] of four channels each, then the maxima (log2 domain) and sums of the rows.
 __device__ __forceinline__ float* part_at(const AttendArgs& a, int part, int D) { return a.part + (size_t)part * a.rows * (D + 2); }
 
@@ -234,6 +238,15 @@ __device__ __forceinline__ void meet() { asm volatile("bar.sync 1, %0;" ::"n"(TH
 __device__ __forceinline__ void bit_set(uint4& m, int i) {
   const uint32_t b = 1u << (i & 31);
   if (i < 32) m.x |= b; else if (i < 64) m.y |= b; else if (i < 96) m.z |= b; else m.w |= b;
+}
+template <int THREADS>
+__device__ __forceinline__ bool meet_and_vote(bool ok) {   // true: all of them are
+  uint32_t bad;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, 1, %2, q;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(bad) : "r"(ok ? 0 : 1), "n"(THREADS) : "memory");
+  return bad == 0;
 }
 template <int THREADS>
 __device__ __forceinline__ void find_family(const AttendArgs& a, int tok0, int m, int tid, Family& f) {
@@ -456,14 +469,15 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
             s[u][e] = ((there[u] & see[h][e & 1]) >> (g + 8 * (e >> 1)) & 1u) ? s[u][e] * a.scale_log2 : -INFINITY;
             mx[e & 1] = fmaxf(mx[e & 1], s[u][e]);
           }
-        // the maxima are raised only when they grew by more than 2^8 (then O is rescaled)
+        // a row's maximum is raised only when it grew by more than 2^8 (then O is rescaled), whatever the other rows' do: a row's bits do not
+        // depend on new tokens that it does not see
         if (__any_sync(0xffffffffu, mx[0] > m[h][0] + 8.f || mx[1] > m[h][1] + 8.f)) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
-            const float mn = fmaxf(m[h][e], mx[e]);
-            const float f = m[h][e] == -INFINITY ? 0.f : ex2(m[h][e] - mn);
+            const float mn = mx[e] > m[h][e] + 8.f ? mx[e] : m[h][e];
+            const float f = mn == m[h][e] ? 1.f : m[h][e] == -INFINITY ? 0.f : ex2(m[h][e] - mn);
             m[h][e] = mn;
             l[h][e] *= f;
 #pragma unroll
@@ -808,8 +822,6 @@ __global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_consta
   if (which == 0 && tid < c.m) a.family[c.tok0 + tid] = fam.mask[tid];
 }
 
-constexpr int kFar = 3;   // tiles that are asked for (into L2) ahead of their turn in the ring
-
 template <int D, int TQ>
 struct TileCfg {
   static constexpr int kSub = D / 64;                       // 64-column (128-byte) sub-tiles
@@ -817,8 +829,8 @@ struct TileCfg {
   static constexpr int kStages = D == 64 ? 8 : TQ == 1 ? 5 : 3;   // ring slots
   static constexpr int kQRegion = 2 * kTileBytes;           // rounded, and what that leaves
   static constexpr int kRing = TQ * kQRegion, kTail = kRing + kStages * kTileBytes;
-  static constexpr int kThreads = 128 + 128 * TQ;
-  static constexpr uint32_t kColO = 0, kColS = TQ * 128, kCols = 2 * TQ * 128;   // tensor memory: O of the row tiles, S with P over it
+  static constexpr int kThreads = 384;
+  static constexpr uint32_t kColO = 0, kColS = 256, kCols = 512;   // tensor memory: O of the warpgroups, S with P over it, 128 columns each
 };
 struct TileMaps {
   CUtensorMap k, v;                // [n_pages * Hkv][page][D], box: 64 channels of a page's rows of a head
@@ -829,12 +841,16 @@ struct TileTail {                  // behind the operand tiles in shared memory
   Start start;
   uint32_t tmem;
   int abort;
+  float2 ml[2][kTile];           // TQ = 1: maxima and sums of the warpgroups' rows
 };
 
-// TQ row tiles of 128 rows (query heads and tokens) over runs of key tiles, one CTA an SM: the structure of the forward (attn_fwd_sm100.cu).  Warp 0
-// brings Q at the start of an item and the key tiles through a ring, of a page tile a TMA box for every page and 64 channels; warp 1
-// issues the products, per key tile and row tile O_t += P_t V_j and then S_t of the next key tile; a warpgroup for each row tile does its softmax, a
-// thread a row.  S = Q K^T is formed with both parts of Q, for the new tokens (tile 0: three ring slots) with both of K.
+// 128 TQ rows (query heads and tokens) over runs of key tiles, one CTA an SM: the structure of the forward (attn_fwd_sm100.cu).  Warp 0 brings Q at
+// the start of an item and the key tiles through a ring, of a page tile a TMA box for every page and 64 channels; warp 1 issues the products;
+// two warpgroups do the softmax, a thread a row.  S = Q K^T is formed with both parts of Q, for the new tokens (three ring slots) with both of K.
+//   TQ = 2: a warpgroup has a row tile, a key tile serves both: per key tile O_t += P_t V_j and then S_t of the next one, for t = 0, 1.
+//   TQ = 1: the warpgroups take the key tiles of the one row tile in turns, each with its own S, O, maximum and sum, and their results are
+//           joined at the end of an item (both can read all of O in tensor memory).  A tile's chain of products and exponentials takes 2.3 us
+//           (d = 128), so one warpgroup alone would leave the SM waiting.
 // Pages end where they end: the slots behind the last row of a page, or of the sequence, get no weight, and their V rows are set to zero in
 // shared memory (what lies there belongs to nobody and may be infinite) by the softmax warps of the few tiles that have such slots.
 template <int D, int TQ>
@@ -854,7 +870,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
     mbar_init(smem_u32(&sh.q_full), 1);
     mbar_init(smem_u32(&sh.q_free), 1);
     for (int i = 0; i < NS; ++i) { mbar_init(smem_u32(&sh.kv_full[i]), 1); mbar_init(smem_u32(&sh.kv_empty[i]), 1); }
-    for (int t = 0; t < TQ; ++t) {
+    for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&sh.s_full[t]), 1);
       mbar_init(smem_u32(&sh.pv_done[t]), 1);
       for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.p_full[t][i]), 4);
@@ -874,20 +890,20 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
   volatile int* abort = &sh.abort;
   const int shift = a.p.shift, per = kKeys >> shift;
   const bool two = a.rope.half > 0;
-  // The ring: a page tile takes two entries (K, V), the new tokens' tile three (K, rest of K, V).  Entry e is in slot e % NS.
+  // The ring: a page tile takes two entries (K, V), the new tokens' tile, which is the last of an item's, three (K, rest of K, V).  Entry number i is
+  // in slot i % NS, in its i / NS-th use.
   struct Entry {
-    int slot = 0, phase = 0;
-    __device__ __forceinline__ void next() { if (++slot == NS) { slot = 0; phase ^= 1; } }
+    int slot, phase;
+    __device__ __forceinline__ explicit Entry(int i) : slot(i % NS), phase(i / NS & 1) {}
   };
   Cursor cursor(a, sh.start);
   Share it;
 
   if (warp < 4) {
-    if constexpr (TQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");   // 128 x 72 + 256 x 216 = 384 x 168
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");   // 128 x 72 + 256 x 216 = 384 x 168
     if (warp == 0) {
       // ---------------- TMA producer: a lane a box ----------------
       const int pi = lane % per, sub = lane / per;      // page of the tile, 64 channels of its rows: at most 16 lanes
-      Entry e;
       int filled = 0, items = 0;                        // entries, items so far
       bool ok = true;
       while (ok && cursor.next(a, it)) {
@@ -900,13 +916,12 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           return __shfl_sync(0xffffffffu, x, pi);
         };
         // into the next entry: waits for its slot, announces the bytes; lane 0 has done so when the others go on
-        auto claim = [&]() {
+        auto claim = [&](const Entry& e) {
           if (ok && filled >= NS) ok = mbar_wait_warp(smem_u32(&sh.kv_empty[e.slot]), e.phase ^ 1, abort);
           if (ok && lane == 0) mbar_expect_tx(smem_u32(&sh.kv_full[e.slot]), Cfg::kTileBytes);
           __syncwarp();
           return ok;
         };
-        auto pass = [&]() { e.next(); ++filled; };
         // Q: both parts of the row tiles that have rows (rows behind the item's are other items', and nobody looks at theirs)
         const int row_tiles = TQ == 2 && it.rt * a.rows + kTile < it.m * a.G ? 2 : 1, parts = two ? 2 : 1;
         if (items > 0) ok = mbar_wait_warp(smem_u32(&sh.q_free), (items - 1) & 1, abort);
@@ -919,43 +934,29 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           tma_load_3d(sQ + t * Cfg::kQRegion + lo * Cfg::kTileBytes + x * Cfg::kSubBytes, &maps.q[lo], x * 64, it.tok0 * a.G + it.rt * a.rows + t * kTile,
                       it.h, smem_u32(&sh.q_full));
         }
-        int tile = it.t0;
-        if (tile == 0) {
-          for (int i = 0; i < 3 && claim(); ++i, pass()) {
-            const CUtensorMap* map = i == 0 ? &maps.kn[0] : i == 1 ? &maps.kn[two ? 1 : 0] : &maps.vn;   // (unrotated keys leave no rest: never multiplied)
-            if (lane < Cfg::kSub)
-              tma_load_3d(sRing + e.slot * Cfg::kTileBytes + lane * Cfg::kSubBytes, map, lane * 64, it.tok0, it.h, smem_u32(&sh.kv_full[e.slot]));
-          }
-          ++tile;
-        }
-        // the page numbers of the next tiles; their rows are brought into L2 kFar tiles ahead of the ring, which holds little more than a tile
-        int far[kFar];
-        auto fetch = [&](int page) {
-          if (sub < Cfg::kSub) {
-            tma_prefetch_3d(&maps.k, sub * 64, 0, page * a.p.Hkv + it.h);
-            tma_prefetch_3d(&maps.v, sub * 64, 0, page * a.p.Hkv + it.h);
-          }
-        };
-#pragma unroll
-        for (int i = 0; i < kFar; ++i) {
-          far[i] = tile + i < it.t1 ? page_at(tile + i) : 0;
-          if ((i > 0 || it.t0 == 0) && tile + i < it.t1) fetch(far[i]);   // (behind the new tokens' tile the ring is full)
-        }
-        for (; tile < it.t1 && ok; ++tile) {
-          const int page = far[0];
-#pragma unroll
-          for (int i = 0; i + 1 < kFar; ++i) far[i] = far[i + 1];
-          if (tile + kFar < it.t1) {
-            far[kFar - 1] = page_at(tile + kFar);
-            fetch(far[kFar - 1]);
-          }
+        // (Bringing the rows of later tiles into L2 ahead of the ring was slower: 92.0 us without, 93.1 one tile ahead, 99.1 four, of sixteen trees of 32
+        // tokens at up to 32K.)
+        int next = max(it.t0, 1) < it.t1 ? page_at(max(it.t0, 1)) : 0;
+        for (int tile = max(it.t0, 1); tile < it.t1 && ok; ++tile) {
+          const int page = next;
+          if (tile + 1 < it.t1) next = page_at(tile + 1);
 #pragma unroll
           for (int which = 0; which < 2; ++which) {
-            if (!claim()) break;
+            const Entry e(filled);
+            if (!claim(e)) break;
             if (sub < Cfg::kSub)
               tma_load_3d(sRing + e.slot * Cfg::kTileBytes + sub * Cfg::kSubBytes + (pi << shift) * 128, which ? &maps.v : &maps.k, sub * 64, 0,
                           page * a.p.Hkv + it.h, smem_u32(&sh.kv_full[e.slot]));
-            pass();
+            ++filled;
+          }
+        }
+        if (it.t0 == 0 && ok) {
+          for (int i = 0; i < 3; ++i, ++filled) {
+            const Entry e(filled);
+            if (!claim(e)) break;
+            const CUtensorMap* map = i == 0 ? &maps.kn[0] : i == 1 ? &maps.kn[two ? 1 : 0] : &maps.vn;   // (unrotated keys leave no rest: never multiplied)
+            if (lane < Cfg::kSub)
+              tma_load_3d(sRing + e.slot * Cfg::kTileBytes + lane * Cfg::kSubBytes, map, lane * 64, it.tok0, it.h, smem_u32(&sh.kv_full[e.slot]));
           }
         }
       }
@@ -966,7 +967,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
           while (!mbar_try_wait(smem_u32(bar), phase) && clock64() - t0 < 2000000) {}
         };
         if (items > 0) drain(&sh.q_full, (items - 1) & 1);
-        for (int i = 0; i < NS && i < filled; ++i) drain(&sh.kv_full[i], i < e.slot ? e.phase : e.phase ^ 1);   // of the slot's last entry
+        for (int i = max(0, filled - NS); i < filled; ++i) drain(&sh.kv_full[Entry(i).slot], Entry(i).phase);
       }
     } else if (warp == 1) {
       // ---------------- issuer (the products run in the order of issue, sm100_ptx.h) ----------------
@@ -975,101 +976,109 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
       const uint64_t descQ0 = make_smem_desc_sw128(sQ, 16, 1024);
       const uint32_t leader = elect_one();
       bool ok = true;
-      Entry e;
-      int q_phase = 0, count[2] = {0, 0};   // tiles so far of each row tile: the parity of its P
+      int q_phase = 0, base = 0, count[2] = {0, 0};   // base: the item's first entry; count: tiles so far of each warpgroup, the parity of its P
       while (ok && cursor.next(a, it)) {
         const int n = it.t1 - it.t0, tiles = TQ == 2 && it.rt * a.rows + kTile < it.m * a.G ? 2 : 1;
         ok = mbar_wait_warp(smem_u32(&sh.q_full), q_phase, abort);
         q_phase ^= 1;
-        // S_t (+)= part `lo` of Q_t times the K tile in a slot
-        auto scores = [&](int t, int lo, int slot, bool more) {
-          const uint64_t dQ = desc_advance(descQ0, t * Cfg::kQRegion + lo * Cfg::kTileBytes), dK = desc_advance(descK0, slot * Cfg::kTileBytes);
+        // S_t (+)= part `lo` of Q_q times the K tile in a slot
+        auto product = [&](int t, int q, int lo, int slot, bool more) {
+          const uint64_t dQ = desc_advance(descQ0, q * Cfg::kQRegion + lo * Cfg::kTileBytes), dK = desc_advance(descK0, slot * Cfg::kTileBytes);
 #pragma unroll
           for (int h = 0; h < Cfg::kSub; ++h)
             umma_ss4(tmem + Cfg::kColS + t * kTile, desc_advance(dQ, h * Cfg::kSubBytes), desc_advance(dK, h * Cfg::kSubBytes), idesc_qk,
                      more || h > 0 ? 1u : 0u, leader);
         };
-        Entry v;                    // of the tile whose P comes next
-        for (int j = -1; j < n && ok; ++j) {
-          if (j >= 0) {
-            ok = mbar_wait_warp(smem_u32(&sh.kv_full[v.slot]), v.phase, abort);
+        auto is_new = [&](int j) { return tile_of(it, j) == 0; };
+        auto entry_k = [&](int j) { return Entry(base + 2 * j); };
+        auto entry_rest = [&](int j) { return Entry(base + 2 * j + 1); };
+        auto entry_v = [&](int j) { return Entry(base + 2 * j + (is_new(j) ? 2 : 1)); };
+        auto wait_k = [&](int j) {
+          ok = mbar_wait_warp(smem_u32(&sh.kv_full[entry_k(j).slot]), entry_k(j).phase, abort);
+          if (ok && is_new(j)) ok = mbar_wait_warp(smem_u32(&sh.kv_full[entry_rest(j).slot]), entry_rest(j).phase, abort);
+          return ok;
+        };
+        auto scores = [&](int j, int t, int q) {
+          tc_fence_after_sync();
+          product(t, q, 0, entry_k(j).slot, false);
+          if (two) {
+            product(t, q, 1, entry_k(j).slot, true);
+            if (is_new(j)) product(t, q, 0, entry_rest(j).slot, true);
+          }
+          umma_commit(smem_u32(&sh.s_full[t]), leader);
+        };
+        auto free_k = [&](int j) {
+          umma_commit(smem_u32(&sh.kv_empty[entry_k(j).slot]), leader);
+          if (is_new(j)) umma_commit(smem_u32(&sh.kv_empty[entry_rest(j).slot]), leader);
+          if (j + 1 == n) umma_commit(smem_u32(&sh.q_free), leader);   // the item's last scores: the next Q may come while this item ends
+        };
+        // O_t += P_t V_j, as the halves of P come
+        auto values = [&](int j, int t, bool more) {
+          const uint64_t dV = desc_advance(descV0, entry_v(j).slot * Cfg::kTileBytes);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (ok) ok = mbar_wait_warp(smem_u32(&sh.p_full[t][half]), count[t] & 1, abort);
+            if (!ok) return;
+            tc_fence_after_sync();
+            umma_ts4<8, 16, 24, 2048>(tmem + Cfg::kColO + t * kTile, tmem + Cfg::kColS + t * kTile + half * 32, desc_advance(dV, half * 4 * 2048),
+                                     idesc_pv, half > 0 || more ? 1u : 0u, leader);
+          }
+          umma_commit(smem_u32(&sh.pv_done[t]), leader);
+          ++count[t];
+        };
+        if constexpr (TQ == 2) {
+          for (int j = -1; j < n && ok; ++j) {
+            if (j >= 0) ok = mbar_wait_warp(smem_u32(&sh.kv_full[entry_v(j).slot]), entry_v(j).phase, abort);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (!ok || t >= tiles) break;
+              if (j >= 0) values(j, t, j > 0);
+              if (ok && j + 1 < n && (t > 0 || wait_k(j + 1))) scores(j + 1, t, t);
+            }
             if (!ok) break;
+            if (j >= 0) umma_commit(smem_u32(&sh.kv_empty[entry_v(j).slot]), leader);
+            if (j + 1 < n) free_k(j + 1);
           }
-          Entry k = e, rest = e;    // rest: of what the rounding of the new keys left, where the next tile has it
-          const bool more = j + 1 < n, fresh = it.t0 + j + 1 == 0;
-          if (more) {
-            e.next();
-            if (fresh) { rest = e; e.next(); }
-          }
-          const uint64_t dV = desc_advance(descV0, v.slot * Cfg::kTileBytes);
-          bool k_here = false;
-#pragma unroll
-          for (int t = 0; t < TQ; ++t) {
-            if (t >= tiles || !ok) break;
+        } else {
+          // tile j is warpgroup j % 2's; two tiles' scores are ahead of the values
+          for (int j = -2; j < n && ok; ++j) {
             if (j >= 0) {
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                if (ok) ok = mbar_wait_warp(smem_u32(&sh.p_full[t][half]), count[t] & 1, abort);
-                if (!ok) break;
-                tc_fence_after_sync();
-                umma_ts4<8, 16, 24, 2048>(tmem + Cfg::kColO + t * kTile, tmem + Cfg::kColS + t * kTile + half * 32, desc_advance(dV, half * 4 * 2048),
-                                         idesc_pv, (half > 0 || j > 0) ? 1u : 0u, leader);
-              }
+              ok = mbar_wait_warp(smem_u32(&sh.kv_full[entry_v(j).slot]), entry_v(j).phase, abort);
               if (!ok) break;
-              umma_commit(smem_u32(&sh.pv_done[t]), leader);
-              ++count[t];
+              if (j & 1) values(j, 1, j > 1); else values(j, 0, j > 1);
+              if (!ok) break;
+              umma_commit(smem_u32(&sh.kv_empty[entry_v(j).slot]), leader);
             }
-            if (more) {
-              if (!k_here) {
-                ok = mbar_wait_warp(smem_u32(&sh.kv_full[k.slot]), k.phase, abort);
-                if (ok && fresh) ok = mbar_wait_warp(smem_u32(&sh.kv_full[rest.slot]), rest.phase, abort);
-                if (!ok) break;
-                k_here = true;
-              }
-              tc_fence_after_sync();
-              scores(t, 0, k.slot, false);
-              if (two) {
-                scores(t, 1, k.slot, true);
-                if (fresh) scores(t, 0, rest.slot, true);
-              }
-              umma_commit(smem_u32(&sh.s_full[t]), leader);
+            if (j + 2 < n) {
+              if (!wait_k(j + 2)) break;
+              scores(j + 2, j & 1, 0);
+              free_k(j + 2);
             }
-          }
-          if (!ok) break;
-          if (j + 2 == n) umma_commit(smem_u32(&sh.q_free), leader);   // the item's last scores: the next Q may come while this item ends
-          if (j >= 0) umma_commit(smem_u32(&sh.kv_empty[v.slot]), leader);
-          if (more) {
-            umma_commit(smem_u32(&sh.kv_empty[k.slot]), leader);
-            if (fresh) umma_commit(smem_u32(&sh.kv_empty[rest.slot]), leader);
-            v = e;
-            e.next();
           }
         }
+        base += 2 * n + (it.t0 == 0 ? 1 : 0);
       }
     }
   } else {
-    if constexpr (TQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    // ---------------- softmax + epilogue: warpgroup t owns row tile t, one thread per row ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    // ---------------- softmax + epilogue: one thread per row; warpgroup t has row tile t (TQ = 2) or every other key tile (TQ = 1) ----------------
     constexpr int CPR = D / 8;
     const int t = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16, S_addr = tmem + lane_addr + Cfg::kColS + t * kTile, O_addr = tmem + lane_addr + Cfg::kColO + t * kTile;
     const float c = a.scale_log2;
     bool ok = true;
-    Entry e;
-    int count = 0;                 // tiles of this warpgroup so far
+    int base = 0, count = 0, others = 0;   // the item's first entry; tiles so far of this warpgroup, and (TQ = 1) of the other one
     while (ok && cursor.next(a, it)) {
-      const int n = it.t1 - it.t0, R = it.m * a.G, r0 = it.rt * a.rows + t * kTile;
+      const int n = it.t1 - it.t0, R = it.m * a.G, r0 = it.rt * a.rows + (TQ == 2 ? t * kTile : 0);
       const bool mine = r0 < R;    // this warpgroup has rows
       const SeqPages pg = seq_pages(a.p, it.n);
       uint4 own = make_uint4(0, 0, 0, 0);
       if (it.t0 == 0 && mine) own = a.family[it.tok0 + min((r0 + row) / a.G, it.m - 1)];
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < n && ok; ++j) {
-        const int tile = it.t0 + j;
-        for (int i = tile == 0 ? 2 : 1; i > 0; --i) e.next();   // e: the entry of V
-        const Entry v = e;
-        e.next();
-        if (!mine) continue;
+      const int first = TQ == 2 ? 0 : t, step = TQ == 2 ? 1 : 2;
+      for (int j = first; j < n && mine && ok; j += step) {
+        const int tile = tile_of(it, j);
+        const Entry v(base + 2 * j + (tile == 0 ? 2 : 1));
         ok = mbar_wait_warp(smem_u32(&sh.s_full[t]), count & 1, abort);
         if (!ok) break;
         tc_fence_after_sync();
@@ -1123,7 +1132,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
         const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
         // the maximum is only raised when it grew by more than 2^8 (then O is rescaled in tensor memory); -inf while no score has counted
         const bool need = mx > m && (mx - m) * c > 8.f;
-        if (j == 0) {
+        if (j == first) {
           m = mx;
         } else if (__any_sync(0xffffffffu, need)) {
           ok = mbar_wait_warp(smem_u32(&sh.pv_done[t]), (count - 1) & 1, abort);   // O holds every earlier tile
@@ -1180,53 +1189,88 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
         l += sum0 + sum1;
         ++count;
       }
-      if (ok && mine) ok = mbar_wait_warp(smem_u32(&sh.pv_done[t]), (count - 1) & 1, abort);
+      base += 2 * n + (it.t0 == 0 ? 1 : 0);
+      // the products are done: of TQ = 1 both warpgroups', whose maxima and sums meet in shared memory
+      if (ok && mine && n > first) ok = mbar_wait_warp(smem_u32(&sh.pv_done[t]), (count - 1) & 1, abort);
+      float f0 = 1.f, f1 = 0.f;   // TQ = 1: what brings O of the two to one maximum
+      if constexpr (TQ == 1) {
+        const int theirs = t == 0 ? n / 2 : (n + 1) / 2;   // the other warpgroup's tiles of the item
+        others += theirs;
+        if (ok && theirs > 0) ok = mbar_wait_warp(smem_u32(&sh.pv_done[t ^ 1]), (others - 1) & 1, abort);
+        sh.ml[t][row] = make_float2(m, l);
+        ok = meet_and_vote<256>(ok);
+        if (!ok) break;            // (all of them leave together: a warp that left alone would be waited for at the barrier)
+        const float2 x = sh.ml[0][row], y = sh.ml[1][row];
+        const float mx = x.y != 0.f ? (y.y != 0.f ? fmaxf(x.x, y.x) : x.x) : y.x;
+        f0 = x.y != 0.f ? ex2((x.x - mx) * c) : 0.f;
+        f1 = y.y != 0.f ? ex2((y.x - mx) * c) : 0.f;
+        m = mx;
+        l = fmaf(x.y, f0, y.y * f1);
+      }
       if (ok && mine) {
         tc_fence_after_sync();
         const int rr = r0 + row;
         const bool add_odd = it.t0 == 0 && a.odd[(size_t)it.s * a.p.Hkv + it.h];
         float* part = it.part >= 0 ? part_at(a, it.part, D) : nullptr;
         const float inv = 1.0f / l;
-        const int tok = rr / a.G, head = it.h * a.G + rr - tok * a.G;
+        const int tok = rr / a.G, head = it.h * a.G + rr - tok * a.G, part_row = TQ == 2 ? t * kTile + row : row;
         uint4* dst = rr < R ? reinterpret_cast<uint4*>(a.o + head * a.o_head + (it.tok0 + tok) * a.o_tok) : nullptr;
+        // columns of this warpgroup: all of its row tile's, or half of the common one's
+        constexpr int W = TQ == 2 ? 32 : 16, kParts = (TQ == 2 ? D : D / 2) / W;
 #pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-          uint32_t o[32];
-          tmem_ld32(O_addr + q * 32, o);
-          tmem_wait_ld();
+        for (int qq = 0; qq < kParts; ++qq) {
+          const int q = TQ == 2 ? qq : t * kParts + qq;
+          uint32_t o[W];
+          if constexpr (TQ == 2) {
+            tmem_ld32(O_addr + q * W, o);
+            tmem_wait_ld();
+          } else {
+            uint32_t o1[W];
+            tmem_ld16(tmem + lane_addr + Cfg::kColO + q * W, o);
+            if (n > 1) tmem_ld16(tmem + lane_addr + Cfg::kColO + kTile + q * W, o1);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              const float z = f0 != 0.f ? __uint_as_float(o[i]) * f0 : 0.f;
+              o[i] = __float_as_uint(n > 1 && f1 != 0.f ? fmaf(__uint_as_float(o1[i]), f1, z) : z);
+            }
+          }
           if (add_odd) {
 #pragma unroll 1
-            for (int i = 0; i < 32; ++i) {
-              const float add = odd_values(a, it, own, 32 * q + i);
+            for (int i = 0; i < W; ++i) {
+              const float add = odd_values(a, it, own, W * q + i);
 #pragma unroll
-              for (int x = 0; x < 32; ++x)
+              for (int x = 0; x < W; ++x)
                 if (x == i) o[x] = __float_as_uint(__uint_as_float(o[x]) + add);
             }
           }
           if (part) {
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
-              reinterpret_cast<uint4*>(part)[(8 * q + x) * a.rows + t * kTile + row] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            for (int x = 0; x < W / 4; ++x)
+              reinterpret_cast<uint4*>(part)[(W / 4 * q + x) * a.rows + part_row] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
           } else if (dst) {
             // (a thread writes its own row: staged in shared memory the rows would leave in whole lines, but the only place for them is Q's, where the
             // next item's is on its way by now)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
+            for (int x = 0; x < W / 8; ++x) {
               float f[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[8 * x + i]) * inv;
-              dst[q * 4 + x] = pack_channels(f);
+              dst[q * (W / 8) + x] = pack_channels(f);
             }
           }
         }
-        if (part) {
-          part[a.rows * D + t * kTile + row] = m * c;
-          part[a.rows * (D + 1) + t * kTile + row] = l;
-        } else if (dst && a.lse) {
-          a.lse[(size_t)head * a.p.n_new + it.tok0 + tok] = m * a.scale + logf(l);
+        if (TQ == 2 || t == 0) {
+          if (part) {
+            part[a.rows * D + part_row] = m * c;
+            part[a.rows * (D + 1) + part_row] = l;
+          } else if (dst && a.lse) {
+            a.lse[(size_t)head * a.p.n_new + it.tok0 + tok] = m * a.scale + logf(l);
+          }
         }
         tc_fence_before_sync();   // O and S have been read: the next item's products may write them
       }
+      if constexpr (TQ == 1) meet<256>();   // ... when both warpgroups have
     }
   }
   tc_fence_before_sync();
@@ -1242,7 +1286,7 @@ bool rows_ok(const lrsa_rows_t* r) {
 // Fewest key tiles that are a CTA's worth.
 constexpr int kMinTilesFew = 2, kMinTiles = 2;
 // What it costs a CTA to begin another item, in key tiles.
-constexpr int kExtraFew = 1, kExtra = 3;
+constexpr int kExtraFew = 2, kExtra = 3;
 
 // The parts of the workspace.  few: of a call that the kernel for few rows takes.
 struct AttendWs { size_t starts, divided, part, family, odd, q[2], k[2], v, total; };
