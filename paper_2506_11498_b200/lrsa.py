@@ -705,31 +705,36 @@ def lrsa_rotate(params: Params, Q, K, rope: Rope, positions=None, inverse: bool 
     """Position rotation of Q [B,Hq,N,d] and K [B,Hkv,N,d] (either may be None), in front of lrsa_score_select and lrsa_attn_fwd;
     inverse: its gradient, behind lrsa_attn_bwd.  positions: int32 [N]; none: a token's index in its sequence.  Q_out, K_out may be
     Q, K themselves.  Returns (Q_out, K_out)."""
-    p, where, call = params, "lrsa_rotate", _calls()
+    p, where, call = params, "lrsa_rotate", _call or _calls()
     first = Q if Q is not None else K
     if first is None:
         raise LrsaError(1, f"{where}: neither Q nor K")
-    dev, out = _device(where, "Q" if Q is not None else "K", first), []
-    for name, x, y, heads in (("Q", Q, Q_out, p.n_q_heads), ("K", K, K_out, p.n_kv_heads)):
-        if x is None:
-            if y is not None:
-                raise LrsaError(1, f"{where}: {name}_out without {name}")
-        else:
-            shape = (p.batch, heads, p.seq_len, p.head_dim)
-            _expect(where, name, x, shape, torch.bfloat16, dev)
-            if y is None:
-                y = _made(stream, x, torch.empty_like, x)
-            elif y is not x:
-                _expect(where, name + "_out", y, shape, torch.bfloat16, dev)
-        out.append(y)
+    dev = _device(where, "Q" if Q is not None else "K", first)
+    q_at, q_to, Q_out = _turned(where, "Q", Q, Q_out, (p.batch, p.n_q_heads, p.seq_len, p.head_dim), dev, stream)
+    k_at, k_to, K_out = _turned(where, "K", K, K_out, (p.batch, p.n_kv_heads, p.seq_len, p.head_dim), dev, stream)
     if positions is not None:
         _expect(where, "positions", positions, (p.seq_len,), torch.int32, dev)
     cp = p.struct()
-    status = call.rotate(ctypes.addressof(cp), _p(Q), _p(K), _p(out[0]), _p(out[1]), *_rope_args(where, rope, dev), _p(positions),
-                         int(inverse), _stream_of(stream, dev))
+    status = call.rotate(ctypes.addressof(cp), q_at, k_at, q_to, k_to, *_rope_args(where, rope, dev), _p(positions), int(inverse),
+                         _stream_of(stream, dev))
     if status:
         _check(status, where)
-    return tuple(out)
+    return Q_out, K_out
+
+
+def _turned(where, name, x, y, shape, dev, stream):
+    """(address of x, address of y, y) of a tensor to be rotated; y is made where there is none."""
+    if x is None:
+        if y is not None:
+            raise LrsaError(1, f"{where}: {name}_out without {name}")
+        return None, None, None
+    if x.dtype is not torch.bfloat16 or x.shape != shape or not x.is_contiguous() or x.get_device() != dev:
+        _expect(where, name, x, shape, torch.bfloat16, dev)
+    if y is None:
+        y = torch.empty_like(x) if stream is None else _made(stream, x, torch.empty_like, x)
+    elif y is not x:
+        _expect(where, name + "_out", y, shape, torch.bfloat16, dev)
+    return x.data_ptr(), y.data_ptr(), y
 
 
 class PagedCache:
@@ -843,7 +848,7 @@ class PagedCache:
         """The new tokens enter the cache: k_new, v_new bf16 [Hkv, tokens, d] with any strides, K rotated on the way unless rope is
         None.  rows (int32): new token i is row rows[i] of k_new and v_new (the accepted ones of drafts).  kept (int32 [sequences, Hkv,
         w_cap, top_k]) receives the kept positions of the windows that are cut."""
-        p, where, call = self.params, "lrsa_paged_append", _calls()
+        p, where, call = self.params, "lrsa_paged_append", _call or _calls()
         dev, pages = self._pages(where, "k_new", k_new, table, n_tokens, cu_new)
         n_rows = k_new.shape[1] if k_new.dim() == 3 else 0
         shape = (p.n_kv_heads, n_rows, p.head_dim)
@@ -866,7 +871,7 @@ class PagedCache:
         token of its sequence each one continues, -1: the cache; none: the one in front of it.  max_new: the most tokens of a
         sequence (at most 128; fewer than 17 rows, heads of a group times max_new, take the kernel for few).  Returns (o [Hq, tokens, d],
         lse fp32 [Hq, tokens]); o lies in memory as q does, token by token or head by head."""
-        p, where, call = self.params, "lrsa_paged_attend", _calls()
+        p, where, call = self.params, "lrsa_paged_attend", _call or _calls()
         dev, pages = self._pages(where, "q", q, table, n_tokens, cu_new)
         n = q.shape[1] if q.dim() == 3 else 0
         Hq, d = p.n_q_heads, p.head_dim
