@@ -635,3 +635,42 @@ def test_training_through_the_rotation():
     for name, got, want in (("dQ", dQ, q.grad), ("dK", dK, k.grad), ("dV", dV, v.grad)):
         err = (got.double().cpu() - want).norm() / want.norm()
         assert err < 1.5e-2, (name, float(err))     # the backward's bound on this norm, 1e-2, and one more rounding to bf16
+
+
+def test_no_new_tokens():
+    p = lrsa.Params(1, 14, 2, 400, 64, 64, 16, 4)
+    m = Model(p, 16, 2, dim=64, seed=19)
+    m.append([100, 50])
+    before = m.cache.k_pages.clone()
+    table, n, cu = m.device([0, 0])
+    for T in (0, 5):                       # no rows at all, or room for some
+        q, k, v = (m.rows(h, T, False).cuda() for h in (14, 2, 2))
+        for max_new in (1, 20):
+            o, lse = m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=max_new)
+            assert o.shape == (14, T, 64) and lse.shape == (14, T) and m.cache.status() == 0
+        m.cache.append(k, v, table, n, cu, rope=m.rope)
+        assert m.cache.status() == 0 and torch.equal(before.view(torch.int16), m.cache.k_pages.view(torch.int16))
+
+
+def test_launches_and_the_binding_without_its_module(monkeypatch):
+    p = lrsa.Params(1, 14, 2, 900, 128, 64, 16, 4)
+    m = Model(p, 32, 2, dim=128, seed=20)
+    m.append([400, 77])
+    assert lrsa.lrsa_last_launch_count() == 3
+    for s in range(2):
+        m.reach(s, m.n[s] + 12)
+    q, k, v = (m.rows(h, 20, False).cuda() for h in (14, 2, 2))
+    for new, launches in (([1, 1], 2), ([12, 8], 3)):
+        args = m.device(new)
+        with monkeypatch.context() as c:
+            outs = []
+            for call in (lrsa._calls(), lrsa._CtypesCalls(lrsa.lib())):
+                c.setattr(lrsa, "_call", call)
+                o, lse = m.cache.attend(q, k, v, *args, rope=m.rope, max_new=max(new))
+                assert lrsa.lrsa_last_launch_count() == launches
+                m.cache.append(k, v, *args, rope=m.rope)
+                assert lrsa.lrsa_last_launch_count() == 1
+                pages = m.cache.k_pages.clone()
+                x, _ = lrsa.lrsa_rotate(lrsa.Params(1, 14, 2, 20, 128, 16, 4, 0), q[None], None, m.rope)
+                outs.append((o[:, :sum(new)], lse[:, :sum(new)], pages.view(torch.int16), x))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
