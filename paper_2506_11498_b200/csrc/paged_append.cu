@@ -8,8 +8,11 @@
 // A cluster of CTAs cuts one window at a time: channel ranges of window w + 1, exchanged through shared memory; spreads of the rows
 // of window w into the first CTA's shared memory; that one scores and selects; all of them move kept rows.  Two forms:
 //   one launch (few new tokens a sequence: every step of a server): a cluster per (sequence, KV head) cuts what there is to cut, mostly
-//     nothing, then writes the new rows.  The recent pages that it writes are those of the window it has just cut.
-//   several launches (prompts): the new keys rotated into the workspace, a cluster per window, then the rows.
+//     nothing, then writes the new rows.  The recent pages that it writes are those of the window it has just cut.  A token of 16 sequences
+//     (4 heads, d = 128) 2.6 us in a graph; bound by the launch and four round trips (counts, page number, row, store).
+//   several launches (prompts): the new keys rotated into the workspace; a cluster per window, and the rows of sequences that begin; the rows of
+//     those that go on.  Bound by reading the windows twice (32K: 9 and 8 of the 33 us of a cut, 7.4 TB/s, mostly L2), and by the chain between:
+//     finding the window 1, selecting 4, moving rows 2.5, barriers.
 // The counts are on the device: a cluster finds its sequence and window by running over the sequences' counts.
 #include "infer_sm100.h"
 #include "paged_sm100.h"
@@ -478,9 +481,10 @@ __device__ void check_append(const AppendArgs& a) {
 }
 
 // The keys of all new tokens rotated, for the forms with several launches: a window's rows are read twice there (for its own scores, and as the
-// reference of the one in front), and rotating them each time, in four of eight warps, took 72 us for a 32K prompt of 4 heads, d = 128, where
-// this takes 8 and the cuts, which read the result from L2, 27.  As in lrsa_rotate a thread takes two chunks of a token for all heads, with the
-// angles loaded once.
+// reference of the one in front), and rotating them each time, in four of eight warps, made the cuts of a 32K prompt of 4 heads, d = 128, take
+// 72 us.  This takes 15 (50 MB read, 34 written) and the cuts 38 with the rows beside them; the call 80 before, 51 now.  As in
+// lrsa_rotate a thread takes two chunks of a token for all heads, with the angles loaded once.  (Finding the windows' ranges here too, so that a cut
+// reads its rows once: 47 us for this and 33 for the cuts.)
 template <int D>
 __global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int UNITS = D / 16, TOK = 256 / UNITS, kAhead = 4;
@@ -671,9 +675,14 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
     launch_counter().n++;
   }
   const long long windows = one ? n_seqs : (long long)n_new / g.L + (n_seqs < n_new ? n_seqs : n_new);
-  // A window's rows are read by C CTAs, as many as find room at a time.
+  // A window's rows are read by C CTAs, as many as find room at a time; of drafts, where few clusters have a window to cut and the others are soon
+  // gone, twice as many.  us, C = 1 | 2 | 4 | 8: 32K prompt, 4 heads, windows of 1024 64 | 51 | 57 | 80; eight prompts of 0.7 to 9K, 8 heads, of 512
+  // 50 | 60 | 83 | 140; one of 2295, 4 heads, of 512 22 | 18.5 | 16.3 | 16.0; a token of 16 sequences, 4 heads, of 1024 2.5 | 2.5 | 2.6 | 4.2; up to 16 drafts
+  // of 40 sequences, 4 heads, of 512 30 | 24 | 19.6 | 20.8, up to 6 of nine, 8 heads, of 333 27.6 | 22.9 | 19.9 | 21.0.
+  const bool drafts = one && n_new > n_seqs;
+  const long long room = (drafts ? 4 : 2) * kSms;
   int C = 1;
-  while (C < 8 && windows * g.Hkv * 2 * C <= 2 * kSms && g.L / (2 * C) >= 128) C *= 2;
+  while (C < 8 && windows * g.Hkv * 2 * C <= room && g.L / (2 * C) >= (drafts ? 80 : 128)) C *= 2;
   // The rows of a sequence that stay, in blocks of four rounds: where the cuts leave room, beside them.
   const long long stay = (long long)g.S + 2 * g.L < n_new ? (long long)g.S + 2 * g.L : n_new;
   const int per_block = kAppThreads / (g.d / 8) * 4;

@@ -344,6 +344,9 @@ __device__ __forceinline__ uint4 load_once(const void* p) {   // read once: no p
 //   O^T = V^T P^T  lane (g, t) loads chunk g (+ 8) of rows 2t, 2t + 1, 2t + 8, 2t + 9; P^T is turned by movmatrix
 // A group of sixteen keys lies in one page; the page number of a warp's next group is asked for while this one is computed.  Rows that do
 // not count are not read.  The new tokens are a group of their own, for the first warp of the run that holds tile 0.
+// Bound by the rows it reads where there are many: a token each for 16 sequences of 4K to 32K (28/4 heads, d = 128, 173 MB) takes 44 us, of which the
+// loop over the rows is 26 (6.6 TB/s); the others are finding the run 2.2, Q 1.7, joining the warps 3, runs that begin another item up to 5, the merge
+// behind it 4.  One sequence of 3.6K (8/8, d = 64) takes 12.5 us in a graph: a chain of round trips, with the merge.
 template <int D, int NH>
 __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int U = 128 / D;                // 16-key groups per block
@@ -849,8 +852,13 @@ struct TileTail {                  // behind the operand tiles in shared memory
 // two warpgroups do the softmax, a thread a row.  S = Q K^T is formed with both parts of Q, for the new tokens (three ring slots) with both of K.
 //   TQ = 2: a warpgroup has a row tile, a key tile serves both: per key tile O_t += P_t V_j and then S_t of the next one, for t = 0, 1.
 //   TQ = 1: the warpgroups take the key tiles of the one row tile in turns, each with its own S, O, maximum and sum, and their results are
-//           joined at the end of an item (both can read all of O in tensor memory).  A tile's chain of products and exponentials takes 2.3 us
-//           (d = 128), so one warpgroup alone would leave the SM waiting.
+//           joined at the end of an item (both can read all of O in tensor memory).  A tile's chain of products and exponentials takes 2.3 us,
+//           so one warpgroup alone would leave the SM waiting: 16 trees of 16 tokens at up to 20K, 16/4 heads, d = 64, 52 us with one, 45 with two (d = 128, 8 of 32/4 at
+//           60K: 90 and 89, a tile then takes 1.75 us where its bytes would take 1.46).
+// What bounds it.  TQ = 2, d = 128: 2.15 us a key tile (a plain copy's rate would bring it in 1.46, its 48 products take 1.87 at 1965 MHz): beside 128 KB
+// of Q the ring has three slots, so K of the next tile but one comes 1.4 us after the slot of V is free, and then its scores take 0.75.  16 trees of 32 tokens at
+// up to 32K (28/4) 92 us: launch in front 5, first tile 7, twenty tiles 43 to 60, a second item 8, merge 8.  Four trees of 64 tokens at 120K (32/8): 430 us, at
+// 1.65 GHz under the power limit; without the second part of Q 371.
 // Pages end where they end: the slots behind the last row of a page, or of the sequence, get no weight, and their V rows are set to zero in
 // shared memory (what lies there belongs to nobody and may be infinite) by the softmax warps of the few tiles that have such slots.
 template <int D, int TQ>
