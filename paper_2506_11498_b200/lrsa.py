@@ -742,7 +742,8 @@ class PagedCache:
     v_pages, bf16 [n_pages, Hkv, page, d], which may be replaced by others of that shape, type and device.  What the layers of a
     model share is the caller's, on the device: the page table (int32 [sequences, table_width]), the tokens in the cache (n_tokens, int32
     [sequences]) and where the new tokens of a sequence begin (cu_new, int32 [sequences + 1]).  Neither call changes them, so a step is
-    attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status()."""
+    attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status().
+    The calls of a cache share its workspace, so they run one after the other, captured ones too; different caches share nothing."""
 
     MOST_NEW = 128   # new tokens of a sequence in an attend
     _seen = None     # where the pages were when they were last looked at
@@ -768,7 +769,7 @@ class PagedCache:
 
     def _workspace(self, near, stream, *sizes):
         """The workspace, at least as large as a call of these sizes needs.  One that was outgrown stays where it is: a captured
-        call may hold its address."""
+        call may hold its address.  (The next is twice as large at least: all that were outgrown take no more than it does.)"""
         need = self._need.get(sizes)
         if need is None:
             if len(self._need) > 4096:
@@ -776,7 +777,7 @@ class PagedCache:
             need = self._need[sizes] = self.workspace_bytes(*sizes)
         if self.ws.numel() < need:
             self._old.append(self.ws)
-            self.ws = _made(stream, near, new_workspace, need, near.device)
+            self.ws = _made(stream, near, new_workspace, max(need, 2 * self.ws.numel()), near.device)
         return self.ws
 
     def columns(self, n_tokens: int):

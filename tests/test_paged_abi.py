@@ -255,6 +255,15 @@ def test_a_workspace_that_was_outgrown_stays_where_it_was(calls):
     assert cache.ws is small and calls[-1][1][32] == small.numel()
 
 
+def test_workspaces_of_growing_calls_take_little(calls):
+    cache = lrsa.PagedCache(P, 5, device="cpu")
+    for T in range(4000, 60000, 4000):               # prompts, each longer than the last
+        cache.append(**good(cache, T)[0], stream=STREAM)
+        assert cache.ws.numel() >= cache.workspace_bytes(3, T, 0)
+    assert cache._old and cache.ws.numel() <= 2 * cache.workspace_bytes(3, T, 0)
+    assert sum(x.numel() for x in cache._old) <= cache.ws.numel()
+
+
 def test_ropes():
     r = lrsa.Rope.of_base(10000.0, 64, 100, device="cpu")
     cos, sin = ref.angles(100, 64)
