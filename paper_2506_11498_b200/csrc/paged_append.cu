@@ -529,8 +529,8 @@ __global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__
 }
 
 // Clusters of C CTAs: ROWS: one for each (sequence, head); otherwise one for each (window to be cut, head).
-template <int D, bool ROWS>
-__global__ void __launch_bounds__(kAppThreads, 2) paged_cut_kernel(const __grid_constant__ AppendArgs a, int C) {
+template <int D, bool ROWS, int PER_SM>
+__global__ void __launch_bounds__(kAppThreads, PER_SM) paged_cut_kernel(const __grid_constant__ AppendArgs a, int C) {
   extern __shared__ __align__(16) float app_spread[];   // [2][L]
   __shared__ __align__(16) AppendShared<D> sh;
   const int cluster = blockIdx.x / C, rank = blockIdx.x - cluster * C;
@@ -693,7 +693,13 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   a.clusters = (int)clusters;
   const size_t smem = (size_t)2 * g.L * sizeof(float);
-  auto cut = g.d == 128 ? (one ? paged_cut_kernel<128, true> : paged_cut_kernel<128, false>) : (one ? paged_cut_kernel<64, true> : paged_cut_kernel<64, false>);
+  // CTAs of an SM: a cut is a chain of round trips, so where more of them wait than two an SM can hold, three take turns (80 registers instead of
+  // 100 and 126, fewer rows on their way in each).  us, two | three: eight prompts of 0.7 to 9K, 8 heads, windows of 512, d = 64 49.6 | 39.4,
+  // d = 128 75 | 67; 48 of 0.2 to 0.7K, windows of 128, 72 | 66 and 89 | 82.  Where all are held at once: 32K prompt, 4 heads, d = 128
+  // 50 | 57, two of 15 to 20K, 4 heads, windows of 1024, d = 64 45 | 53.
+  const bool three = !one && clusters * C > 2 * kSms && 3 * (smem + 17 * 1024) <= 227 * 1024;
+  auto cut = g.d == 128 ? (one ? paged_cut_kernel<128, true, 2> : three ? paged_cut_kernel<128, false, 3> : paged_cut_kernel<128, false, 2>)
+                        : (one ? paged_cut_kernel<64, true, 2> : three ? paged_cut_kernel<64, false, 3> : paged_cut_kernel<64, false, 2>);
   if (smem > 16 * 1024) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cut, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   LRSA_CUDA_CHECK(launch_dependent(cut, dim3((unsigned)grid), dim3(kAppThreads), smem, st, C, a, C));
   launch_counter().n++;

@@ -254,6 +254,17 @@ def test_many_sequences_of_all_lengths(name, most):
         m.attend([int(x) for x in m.rng.integers(0, most + 1, n_seqs)], max_new=most)
 
 
+@pytest.mark.parametrize("name", CASES)
+def test_more_cuts_than_run_at_once(name):
+    """Prompts, and more tokens behind them, of so many windows that their cuts take turns on the SMs."""
+    m = make(name, 40, seed=8)
+    first = [int(x) for x in m.rng.integers(300, 900, 40)]
+    m.append(first)
+    m.check_pages()
+    m.append([int(x) for x in m.rng.integers(200, 600, 40)])
+    m.check_pages()
+
+
 WIDE = {   # odd groups, windows longer than the scoring kernel's clusters take, tiny ones
     "g20": (lrsa.Params(1, 20, 1, 900, 64, 64, 16, 4), 16, 64, False),
     "g130": (lrsa.Params(1, 130, 1, 900, 128, 64, 16, 4), 32, 64, False),
