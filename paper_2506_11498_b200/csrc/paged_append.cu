@@ -677,10 +677,14 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   const long long windows = one ? n_seqs : (long long)n_new / g.L + (n_seqs < n_new ? n_seqs : n_new);
   // A window's rows are read by C CTAs, as many as find room at a time; of drafts, where few clusters have a window to cut and the others are soon
   // gone, twice as many.  us, C = 1 | 2 | 4 | 8: 32K prompt, 4 heads, windows of 1024 64 | 51 | 57 | 80; eight prompts of 0.7 to 9K, 8 heads, of 512
-  // 50 | 60 | 83 | 140; one of 2295, 4 heads, of 512 22 | 18.5 | 16.3 | 16.0; a token of 16 sequences, 4 heads, of 1024 2.5 | 2.5 | 2.6 | 4.2; up to 16 drafts
+  // 50 (40 with three CTAs an SM, below) | 60 | 83 | 140; one of 2295, 4 heads, of 512 22 | 18.5 | 16.3 | 16.0; a token of 16 sequences, 4 heads, of 1024 2.5 | 2.5 | 2.6 | 4.2; up to 16 drafts
   // of 40 sequences, 4 heads, of 512 30 | 24 | 19.6 | 20.8, up to 6 of nine, 8 heads, of 333 27.6 | 22.9 | 19.9 | 21.0.
   const bool drafts = one && n_new > n_seqs;
-  const long long room = (drafts ? 4 : 2) * kSms;
+  // Prompts may fill three CTAs an SM: 208 cuts (13K, 8 heads, windows of 512, d = 64) 27.2 us with one CTA each, 25.6 with two; 100 (25K, 4 heads, of
+  // 1024, d = 128) 44.5 with two, 43.4 with four; two prompts of 15 to 20K, 4 heads, of 1024, d = 64, 45.1 and 38.7.
+  const size_t smem = (size_t)2 * g.L * sizeof(float);
+  const bool fit3 = 3 * (smem + 17 * 1024) <= 227 * 1024;   // three windows' spreads in an SM's shared memory
+  const long long room = (drafts ? 4 : !one && fit3 ? 3 : 2) * kSms;
   int C = 1;
   while (C < 8 && windows * g.Hkv * 2 * C <= room && g.L / (2 * C) >= (drafts ? 80 : 128)) C *= 2;
   // The rows of a sequence that stay, in blocks of four rounds: where the cuts leave room, beside them.
@@ -692,12 +696,11 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   const long long grid = (clusters + 1 + row_clusters) * C;
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   a.clusters = (int)clusters;
-  const size_t smem = (size_t)2 * g.L * sizeof(float);
   // CTAs of an SM: a cut is a chain of round trips, so where more of them wait than two an SM can hold, three take turns (80 registers instead of
   // 100 and 126, fewer rows on their way in each).  us, two | three: eight prompts of 0.7 to 9K, 8 heads, windows of 512, d = 64 49.6 | 39.4,
   // d = 128 75 | 67; 48 of 0.2 to 0.7K, windows of 128, 72 | 66 and 89 | 82.  Where all are held at once: 32K prompt, 4 heads, d = 128
-  // 50 | 57, two of 15 to 20K, 4 heads, windows of 1024, d = 64 45 | 53.
-  const bool three = !one && clusters * C > 2 * kSms && 3 * (smem + 17 * 1024) <= 227 * 1024;
+  // 50 | 57, four of 3 to 8K, 2 heads, windows of 1000, d = 64 20 | 23.
+  const bool three = !one && fit3 && clusters * C > 2 * kSms;
   auto cut = g.d == 128 ? (one ? paged_cut_kernel<128, true, 2> : three ? paged_cut_kernel<128, false, 3> : paged_cut_kernel<128, false, 2>)
                         : (one ? paged_cut_kernel<64, true, 2> : three ? paged_cut_kernel<64, false, 3> : paged_cut_kernel<64, false, 2>);
   if (smem > 16 * 1024) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cut, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
