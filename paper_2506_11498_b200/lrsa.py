@@ -663,18 +663,38 @@ class KVStore:
 
 class Rope:
     """The angles of a position rotation: cos, sin fp32 [positions, pairs], whatever base or scaling they were made with.  The first
-    2 * pairs channels of a row are rotated, pairs (i, i + pairs), or neighbours (2i, 2i + 1) where `interleaved`."""
+    2 * pairs channels of a row are rotated, pairs (i, i + pairs), or neighbours (2i, 2i + 1) where `interleaved`.  The tables may be written
+    between calls, or replaced by others (both: longer ones for a longer context); the next call takes them.  A captured call goes on with
+    the memory that it was captured with."""
+
+    _seen = None     # addresses and shapes of the tables when they were last looked at
 
     def __init__(self, cos, sin, interleaved: bool = False):
+        self.cos, self.sin, self.interleaved = cos, sin, interleaved
+        self._look("Rope")
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value.detach() if isinstance(value, torch.Tensor) else value)
+        object.__setattr__(self, "_seen", None)
+        object.__setattr__(self, "_held", None)
+
+    def _look(self, where):
+        """Raises LRSA_ERR_INVALID_ARG unless the tables are what the kernels read."""
+        cos, sin = self.cos, self.sin
         for name, t in (("cos", cos), ("sin", sin)):
-            if t.dtype is not torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.data_ptr() % 16 or t.shape != cos.shape or \
-                    t.device != cos.device:
-                raise LrsaError(1, f"Rope: {name} must be a contiguous, 16-byte aligned float32 tensor [positions, pairs], the same for both")
+            if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.dim() != 2 or not t.is_contiguous() or \
+                    t.shape != cos.shape or t.device != cos.device or t.data_ptr() % 16:
+                raise LrsaError(1, f"{where}: {name} of a rope must be a contiguous, 16-byte aligned float32 tensor [positions, pairs], "
+                                   "the same for both")
+            if t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size():
+                raise LrsaError(1, f"{where}: {name} of the rope has lost its memory")
         if cos.shape[0] < 1 or cos.shape[1] < 8 or cos.shape[1] % 8:
-            raise LrsaError(1, f"Rope: {cos.shape[1]} pairs of {cos.shape[0]} positions (pairs: a multiple of 8)")
-        self.cos, self.sin, self.interleaved = cos.detach(), sin.detach(), bool(interleaved)
-        self._dev = cos.get_device()
-        self._args = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(self.interleaved))
+            raise LrsaError(1, f"{where}: {cos.shape[1]} pairs of {cos.shape[0]} positions (pairs: a multiple of 8)")
+        set_ = object.__setattr__
+        set_(self, "_dev", cos.get_device())
+        set_(self, "_args", (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(self.interleaved))))
+        set_(self, "_held", (cos.detach(), sin.detach()))   # while they are held no other memory can be at these addresses
+        set_(self, "_seen", (cos.data_ptr(), sin.data_ptr(), cos.shape, sin.shape))
 
     @staticmethod
     def of_base(base: float, dim: int, n_positions: int, interleaved: bool = False, device="cuda") -> "Rope":
@@ -696,6 +716,9 @@ _NO_ROPE = (None, None, 0, 0, 0)
 def _rope_args(where, rope, dev):
     if rope is None:
         return _NO_ROPE
+    cos, sin, seen = rope.cos, rope.sin, rope._seen
+    if seen is None or cos.data_ptr() != seen[0] or sin.data_ptr() != seen[1] or cos.shape != seen[2] or sin.shape != seen[3]:
+        rope._look(where)
     if rope._dev != dev:
         raise LrsaError(1, f"{where}: the rope is on {rope.cos.device}")
     return rope._args

@@ -1,0 +1,76 @@
+"""The binding of the rotation and the paged cache on the CPU, with recorded calls: what the library is given after the caller has replaced
+something, and what is told and held meanwhile."""
+import pytest
+import torch
+
+from paper_2506_11498_b200 import lrsa
+from tests.test_paged_abi import INVALID, P, STREAM, _built, bf, calls, good, i32  # noqa: F401  (fixtures)
+
+ROPE_AT = {"paged_append": 19, "paged_attend": 22, "rotate": 5}     # where the five values of a rope begin
+
+
+def every_call(cache, rope):
+    a, b = good(cache)
+    return [lambda: cache.append(**{**a, "rope": rope}, stream=STREAM), lambda: cache.attend(**{**b, "rope": rope}, stream=STREAM),
+            lambda: lrsa.lrsa_rotate(P, bf(1, 8, 4000, 128), None, rope, positions=i32(4000), stream=STREAM)]
+
+
+def given(calls):
+    """The rope of the last three calls."""
+    return [args[ROPE_AT[name]:ROPE_AT[name] + 5] for name, args in calls[-3:]]
+
+
+def test_tables_of_a_rope_that_were_replaced(calls):
+    """Longer tables, other angles of the same shape, the other pairing: the next call takes them."""
+    cache, rope = lrsa.PagedCache(P, 5, device="cpu"), lrsa.Rope(torch.zeros(64, 64), torch.zeros(64, 64))
+    for rows in (64, 4096, 64):
+        rope.cos, rope.sin = torch.ones(rows, 64), torch.ones(rows, 64)
+        rope.interleaved = rows == 4096
+        for call in every_call(cache, rope):
+            call()
+        assert given(calls) == [(rope.cos.data_ptr(), rope.sin.data_ptr(), rows, 128, int(rows == 4096))] * 3
+
+
+def test_tables_of_a_rope_that_were_resized(calls):
+    cache = lrsa.PagedCache(P, 5, device="cpu")
+    for rows in (8, 5000):      # in their memory, and beyond it
+        rope = lrsa.Rope(torch.zeros(64, 64), torch.zeros(64, 64))
+        every_call(cache, rope)[0]()
+        rope.cos.resize_(rows, 64)
+        rope.sin.resize_(rows, 64)
+        for call in every_call(cache, rope):
+            call()
+        assert given(calls) == [(rope.cos.data_ptr(), rope.sin.data_ptr(), rows, 128, 0)] * 3
+
+
+@pytest.mark.parametrize("used", [False, True], ids=["fresh", "used"])
+@pytest.mark.parametrize("name", ["cos", "sin"])
+def test_tables_of_a_rope_that_cannot_be_used(calls, name, used):
+    cache = lrsa.PagedCache(P, 5, device="cpu")
+    other = {"cos": "sin", "sin": "cos"}[name]
+    for bad in (torch.zeros(64, 64).double(), torch.zeros(65, 64), torch.zeros(64, 72), torch.zeros(64, 128)[:, ::2], torch.zeros(64 * 64),
+                torch.zeros(64, 64, device="meta"), torch.zeros(64 * 64 + 1)[1:].view(64, 64), None, 3.0):
+        rope = lrsa.Rope(torch.zeros(64, 64), torch.zeros(64, 64))
+        if used:
+            every_call(cache, rope)[0]()
+        n = len(calls)
+        setattr(rope, name, bad)
+        for call in every_call(cache, rope):
+            with pytest.raises(lrsa.LrsaError) as e:
+                call()
+            assert e.value.status == INVALID
+        assert len(calls) == n
+        setattr(rope, name, torch.zeros_like(getattr(rope, other)))
+        every_call(cache, rope)[0]()
+        assert len(calls) == n + 1
+
+
+def test_tables_of_a_rope_that_lost_their_memory(calls):
+    cache, rope = lrsa.PagedCache(P, 5, device="cpu"), lrsa.Rope(torch.zeros(64, 64), torch.zeros(64, 64))
+    every_call(cache, rope)[0]()
+    n = len(calls)
+    rope.sin.untyped_storage().resize_(0)
+    for call in every_call(cache, rope):
+        with pytest.raises(lrsa.LrsaError):
+            call()
+    assert len(calls) == n
