@@ -667,7 +667,7 @@ class Rope:
     between calls, or replaced by others (both: longer ones for a longer context); the next call takes them.  A captured call goes on with
     the memory that it was captured with."""
 
-    _seen = None     # addresses and shapes of the tables when they were last looked at
+    _seen = None     # addresses and shape of the tables when they were last looked at
 
     def __init__(self, cos, sin, interleaved: bool = False):
         self.cos, self.sin, self.interleaved = cos, sin, interleaved
@@ -694,7 +694,7 @@ class Rope:
         set_(self, "_dev", cos.get_device())
         set_(self, "_args", (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(self.interleaved))))
         set_(self, "_held", (cos.detach(), sin.detach()))   # while they are held no other memory can be at these addresses
-        set_(self, "_seen", (cos.data_ptr(), sin.data_ptr(), cos.shape, sin.shape))
+        set_(self, "_seen", (cos.data_ptr(), sin.data_ptr(), cos.shape))
 
     @staticmethod
     def of_base(base: float, dim: int, n_positions: int, interleaved: bool = False, device="cuda") -> "Rope":
@@ -717,7 +717,7 @@ def _rope_args(where, rope, dev):
     if rope is None:
         return _NO_ROPE
     cos, sin, seen = rope.cos, rope.sin, rope._seen
-    if seen is None or cos.data_ptr() != seen[0] or sin.data_ptr() != seen[1] or cos.shape != seen[2] or sin.shape != seen[3]:
+    if seen is None or cos.data_ptr() != seen[0] or sin.data_ptr() != seen[1] or cos.shape != seen[2]:
         rope._look(where)
     if rope._dev != dev:
         raise LrsaError(1, f"{where}: the rope is on {rope.cos.device}")
