@@ -667,7 +667,7 @@ class Rope:
     between calls, or replaced by others (both: longer ones for a longer context); the next call takes them.  A captured call goes on with
     the memory that it was captured with."""
 
-    _seen = None     # addresses and shape of the tables when they were last looked at
+    _args = None     # what csrc/pycall.c takes of the tables, as they were when they were last looked at
 
     def __init__(self, cos, sin, interleaved: bool = False):
         self.cos, self.sin, self.interleaved = cos, sin, interleaved
@@ -675,7 +675,7 @@ class Rope:
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value.detach() if isinstance(value, torch.Tensor) else value)
-        object.__setattr__(self, "_seen", None)
+        object.__setattr__(self, "_args", None)
         object.__setattr__(self, "_held", None)
 
     def _look(self, where):
@@ -690,11 +690,11 @@ class Rope:
                 raise LrsaError(1, f"{where}: {name} of the rope has lost its memory")
         if cos.shape[0] < 1 or cos.shape[1] < 8 or cos.shape[1] % 8:
             raise LrsaError(1, f"{where}: {cos.shape[1]} pairs of {cos.shape[0]} positions (pairs: a multiple of 8)")
-        set_ = object.__setattr__
-        set_(self, "_dev", cos.get_device())
-        set_(self, "_args", (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(self.interleaved))))
-        set_(self, "_held", (cos.detach(), sin.detach()))   # while they are held no other memory can be at these addresses
-        set_(self, "_seen", (cos.data_ptr(), sin.data_ptr(), cos.shape))
+        args = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(self.interleaved))
+        # (while the aliases are held no other memory can be at these addresses)
+        for name, value in (("_dev", cos.get_device()), ("_numel", cos.numel()), ("_held", (cos.detach(), sin.detach())), ("_args", args)):
+            object.__setattr__(self, name, value)
+        return args
 
     @staticmethod
     def of_base(base: float, dim: int, n_positions: int, interleaved: bool = False, device="cuda") -> "Rope":
@@ -716,12 +716,12 @@ _NO_ROPE = (None, None, 0, 0, 0)
 def _rope_args(where, rope, dev):
     if rope is None:
         return _NO_ROPE
-    cos, sin, seen = rope.cos, rope.sin, rope._seen
-    if seen is None or cos.data_ptr() != seen[0] or sin.data_ptr() != seen[1] or cos.shape != seen[2]:
-        rope._look(where)
+    args = rope._args
+    if args is None or rope.cos.data_ptr() != args[0] or rope.sin.data_ptr() != args[1] or rope.cos.numel() != rope._numel:
+        args = rope._look(where)
     if rope._dev != dev:
         raise LrsaError(1, f"{where}: the rope is on {rope.cos.device}")
-    return rope._args
+    return args
 
 
 def lrsa_rotate(params: Params, Q, K, rope: Rope, positions=None, inverse: bool = False, Q_out=None, K_out=None, stream=None):
@@ -824,9 +824,9 @@ class PagedCache:
         if self._seen != (at_k, at_v, dev):
             self._look(where, dev)
             object.__setattr__(self, "_seen", (at_k, at_v, dev))
-        n = table.shape[0] if table.dim() == 2 else 0
-        i32 = torch.int32
-        if table.dtype is not i32 or table.shape != (n, self.table_width) or not table.is_contiguous() or table.get_device() != dev:
+        shape, i32 = table.shape, torch.int32
+        n = shape[0] if len(shape) == 2 else 0
+        if table.dtype is not i32 or shape != (n, self.table_width) or not table.is_contiguous() or table.get_device() != dev:
             _expect(where, "table", table, (n, self.table_width), i32, dev)
         if n_tokens.dtype is not i32 or n_tokens.shape != (n,) or not n_tokens.is_contiguous() or n_tokens.get_device() != dev:
             _expect(where, "n_tokens", n_tokens, (n,), i32, dev)
