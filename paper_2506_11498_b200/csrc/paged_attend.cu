@@ -305,9 +305,9 @@ __device__ __noinline__ float odd_values(const AttendArgs& a, const Share& it, u
   return sum;
 }
 
-// What a part of a row's sum counts, brought to the maximum of all parts.  Where that leaves it no weight in 32 bits an infinity or NaN in it is
-// one all the same: it has some weight in the formula, and the parts depend on how the items are dealt out.
-__device__ __forceinline__ float weighed(float x, float f) { return f != 0.f ? x * f : fabsf(x) < INFINITY ? 0.f : x; }
+// The weight of a part of a row's sum beside the others (l: the sum of its probabilities, x: its maximum above theirs).  Where 32 bits leave it
+// none it has the least one there is: in the formula it has some, so an infinity or NaN in it is one of the row's, however the items are dealt out.
+__device__ __forceinline__ float weight_of(float l, float x) { return l != 0.f ? fmaxf(ex2(x), 0x1p-149f) : 0.f; }
 
 // The warps of the last launch look at everything that the kernels take from the device, a sequence a warp, the last blocks first.  They read
 // inputs only: those were there when the launch in front of this one passed its own wait, so this one need not wait for its end.
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
         float ls = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const float f = ex2(sm_m[w][r] - ref);
+          const float f = weight_of(sm_l[w][r], sm_m[w][r] - ref);
           const float4 x = *reinterpret_cast<const float4*>(&sm_o[w][r][4 * c4]);
           ov.x = fmaf(x.x, f, ov.x); ov.y = fmaf(x.y, f, ov.y); ov.z = fmaf(x.z, f, ov.z); ov.w = fmaf(x.w, f, ov.w);
           ls = fmaf(sm_l[w][r], f, ls);
@@ -728,11 +728,9 @@ __global__ void __launch_bounds__(256, 4) paged_merge_kernel(const __grid_consta
         const float2 y = ml[i][lane_row];
         if (y.y != 0.f) M = fmaxf(M, y.x);   // (nothing counted in a run: its maximum says nothing)
       }
-      if (was != -INFINITY) {
-        const float f0 = ex2(was - M);
-        ls *= f0;
-        ov.x = weighed(ov.x, f0); ov.y = weighed(ov.y, f0); ov.z = weighed(ov.z, f0); ov.w = weighed(ov.w, f0);
-      }
+      const float f0 = was == -INFINITY ? 0.f : weight_of(1.f, was - M);
+      ls *= f0;
+      ov.x *= f0; ov.y *= f0; ov.z *= f0; ov.w *= f0;
       for (int i = 0; i < n; i += kAhead) {
         float4 y[kAhead];
 #pragma unroll
@@ -741,14 +739,9 @@ __global__ void __launch_bounds__(256, 4) paged_merge_kernel(const __grid_consta
         for (int u = 0; u < kAhead; ++u) {
           if (i + u >= n) break;
           const float2 w = ml[i + u][lane_row];
-          if (w.y == 0.f) continue;
-          const float f = ex2(w.x - M);
+          const float f = weight_of(w.y, w.x - M);
           ls = fmaf(w.y, f, ls);
-          if (f != 0.f) {
-            ov.x = fmaf(y[u].x, f, ov.x); ov.y = fmaf(y[u].y, f, ov.y); ov.z = fmaf(y[u].z, f, ov.z); ov.w = fmaf(y[u].w, f, ov.w);
-          } else {
-            ov.x += weighed(y[u].x, 0.f); ov.y += weighed(y[u].y, 0.f); ov.z += weighed(y[u].z, 0.f); ov.w += weighed(y[u].w, 0.f);
-          }
+          if (f != 0.f) { ov.x = fmaf(y[u].x, f, ov.x); ov.y = fmaf(y[u].y, f, ov.y); ov.z = fmaf(y[u].z, f, ov.z); ov.w = fmaf(y[u].w, f, ov.w); }
         }
       }
     }
@@ -1211,8 +1204,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
       base += 2 * n + (it.t0 == 0 ? 1 : 0);
       // the products are done: of TQ = 1 both warpgroups', whose maxima and sums meet in shared memory
       if (ok && mine && n > first) ok = mbar_wait_warp(smem_u32(&sh.pv_done[t]), (count - 1) & 1, abort);
-      float f0 = 1.f, f1 = 0.f;   // TQ = 1: what brings O of the two to one maximum,
-      bool has0 = true, has1 = false;   // and whether anything counted in them
+      float f0 = 1.f, f1 = 0.f;   // TQ = 1: what brings O of the two to one maximum
       if constexpr (TQ == 1) {
         const int theirs = t == 0 ? n / 2 : (n + 1) / 2;   // the other warpgroup's tiles of the item
         others += theirs;
@@ -1221,11 +1213,9 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
         ok = meet_and_vote<256>(ok);
         if (!ok) break;            // (all of them leave together: a warp that left alone would be waited for at the barrier)
         const float2 x = sh.ml[0][row], y = sh.ml[1][row];
-        has0 = x.y != 0.f;
-        has1 = y.y != 0.f;
-        const float mx = has0 ? (has1 ? fmaxf(x.x, y.x) : x.x) : y.x;
-        f0 = has0 ? ex2((x.x - mx) * c) : 0.f;
-        f1 = has1 ? ex2((y.x - mx) * c) : 0.f;
+        const float mx = x.y != 0.f ? (y.y != 0.f ? fmaxf(x.x, y.x) : x.x) : y.x;
+        f0 = weight_of(x.y, (x.x - mx) * c);
+        f1 = weight_of(y.y, (y.x - mx) * c);
         m = mx;
         l = fmaf(x.y, f0, y.y * f1);
       }
@@ -1253,8 +1243,8 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
             tmem_wait_ld();
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-              const float z = has0 ? weighed(__uint_as_float(o[i]), f0) : 0.f, z1 = has1 ? __uint_as_float(o1[i]) : 0.f;
-              o[i] = __float_as_uint(f1 != 0.f ? fmaf(z1, f1, z) : z + weighed(z1, 0.f));
+              const float z = f0 != 0.f ? __uint_as_float(o[i]) * f0 : 0.f;
+              o[i] = __float_as_uint(n > 1 && f1 != 0.f ? fmaf(__uint_as_float(o1[i]), f1, z) : z);
             }
           }
           if (add_odd) {
