@@ -349,7 +349,9 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  *
  * Counts, page numbers, rows and parents that cannot be used (out of range, more new tokens than max_new, beyond seq_len or beyond the
  * rope's positions, which have to cover n_tokens + the new tokens of a sequence) are found on the device: lrsa_workspace_status
- * returns LRSA_ERR_INVALID_ARG.  A sequence with bad counts is left out, whatever is read or written stays inside the tensors.
+ * returns LRSA_ERR_INVALID_ARG.  A sequence with bad counts is left out (its rows of o stay as they were), whatever is read or written stays
+ * inside the tensors.  Where cu_new goes back, a sequence that begins in front of an earlier boundary may be left out too: no row becomes
+ * another sequence's.
  * lrsa_paged_shape: the workspace of an attend of n_new tokens of n_seqs sequences, at most max_new each (it grows with n_new and n_seqs; any
  * output may be NULL); with max_new = 0 that of an append.
  */

@@ -488,9 +488,9 @@ __device__ void check_append(const AppendArgs& a) {
 template <int D>
 __global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int UNITS = D / 16, TOK = 256 / UNITS, kAhead = 4;
-  const int unit = threadIdx.x % UNITS, tok = blockIdx.x * TOK + threadIdx.x / UNITS;
+  const int unit = threadIdx.x % UNITS, mine = blockIdx.x * TOK + threadIdx.x / UNITS;
+  const int tok = min(mine, a.p.n_new - 1);   // (the lanes of a warp stay together)
   wait_front();
-  if (tok >= a.p.n_new) return;
   const int src = a.rows ? usable(a.rows[tok], a.n_rows) : tok;
   const __nv_bfloat16* row = a.k + src * a.k_tok;
   RotUnit u;
@@ -505,14 +505,32 @@ __global__ void __launch_bounds__(256) paged_turn_kernel(const __grid_constant__
     }
   };
   load(0);                       // on their way while the token's sequence is looked for
+  bool back = false;             // boundaries that go back
+  for (int i = threadIdx.x & 31; i < a.p.n_seqs && a.p.n_seqs > 1; i += 32) back |= a.p.cu[i + 1] < a.p.cu[i];
   int lo = 0, hi = a.p.n_seqs;   // the last sequence that begins at or before the token
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (a.p.cu[mid] <= tok) lo = mid; else hi = mid;
   }
-  const SeqCounts c = seq_counts(a.p, lo, a.most, a.limit);
-  if (tok < c.tok0 || tok >= c.tok0 + c.m) return;   // behind the last one, or a sequence with bad counts
-  load_angles(u, unit, c.n + tok - c.tok0, a.rope);
+  SeqCounts c;
+  auto place = [&](int behind) {   // false: behind the last one, or a sequence with bad counts
+    c = seq_counts(a.p, lo, a.most, a.limit, behind);
+    const bool there = mine == tok && tok >= c.tok0 && tok < c.tok0 + c.m;
+    if (there) load_angles(u, unit, c.n + tok - c.tok0, a.rope);
+    return there;
+  };
+  bool there = place(0);
+  if (__any_sync(0xffffffffu, back)) {   // (asked when the angles are on their way)  Then: the last sequence up to which all begin there
+    int behind = 0;
+    lo = 0;
+    for (int s = 0, top = 0; s < a.p.n_seqs && max(top, a.p.cu[s]) <= tok; ++s) {
+      lo = s;
+      behind = top;
+      top = max(top, a.p.cu[s]);
+    }
+    there = place(behind);
+  }
+  if (!there) return;
   for (int h0 = 0; h0 < a.p.Hkv; h0 += kAhead) {
     if (h0 > 0) load(h0);
 #pragma unroll
@@ -545,9 +563,11 @@ __global__ void __launch_bounds__(kAppThreads, PER_SM) paged_cut_kernel(const __
       const int blk = blockIdx.x - (a.clusters + 1) * C;
       q.s = blk / a.row_blocks;
       if (q.s >= a.p.n_seqs) return;
+      const int first = first_boundary(a.p, q.s);
       const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);
+      if (!fresh(a.p, c.n) || begins_early(a.p, q.s, first)) return;
       q.n = c.n; q.m = c.m; q.tok0 = c.tok0;
-      if (fresh(a.p, q.n)) put_rows<D, false>(a, q, blk - q.s * a.row_blocks, a.row_blocks);
+      put_rows<D, false>(a, q, blk - q.s * a.row_blocks, a.row_blocks);
     }
     return;
   }
@@ -555,7 +575,7 @@ __global__ void __launch_bounds__(kAppThreads, PER_SM) paged_cut_kernel(const __
   if (ROWS) {
     q.s = cluster / a.p.Hkv;
     q.h = cluster - q.s * a.p.Hkv;
-    const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);
+    const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);   // (should ranges overlap, each sequence has its own rows all the same)
     q.n = c.n; q.m = c.m; q.tok0 = c.tok0;
     w0 = cut_windows(a.p, q.n);
     w1 = cut_windows(a.p, q.n + q.m);
@@ -564,14 +584,12 @@ __global__ void __launch_bounds__(kAppThreads, PER_SM) paged_cut_kernel(const __
     const int unit = cluster / a.p.Hkv, lane = threadIdx.x & 31;
     q.h = cluster - unit * a.p.Hkv;
     q.m = 0;
-    int before = 0;
+    int before = 0, behind = 0;
     for (int s0 = 0; s0 < a.p.n_seqs; s0 += 32) {
       SeqCounts c = {};
-      int cuts = 0;
-      if (s0 + lane < a.p.n_seqs) {
-        c = seq_counts(a.p, s0 + lane, a.most, a.limit);
-        cuts = cut_windows(a.p, c.n + c.m) - cut_windows(a.p, c.n);
-      }
+      if (s0 + lane < a.p.n_seqs) c = seq_counts(a.p, s0 + lane, a.most, a.limit);
+      if (c.tok0 < largest_in_front(a.p, s0, lane, behind)) c = SeqCounts{};
+      const int cuts = cut_windows(a.p, c.n + c.m) - cut_windows(a.p, c.n);
       int incl = cuts;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -610,9 +628,11 @@ __global__ void __launch_bounds__(kAppThreads) paged_rows_kernel(const __grid_co
   Seq q;
   q.s = blockIdx.x / blocks;
   wait_front();
+  const int first = first_boundary(a.p, q.s);
   const SeqCounts c = seq_counts(a.p, q.s, a.most, a.limit);
+  if (fresh(a.p, c.n) || begins_early(a.p, q.s, first)) return;
   q.n = c.n; q.m = c.m; q.tok0 = c.tok0;
-  if (!fresh(a.p, q.n)) put_rows<D, false>(a, q, blockIdx.x % blocks, blocks);
+  put_rows<D, false>(a, q, blockIdx.x % blocks, blocks);
 }
 
 // One launch while a sequence gets a few tokens on average: a cluster then writes the few rows of a head by itself and cuts a window at most.

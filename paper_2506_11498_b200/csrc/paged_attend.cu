@@ -96,9 +96,9 @@ struct Share {
   int part;             // where a partial result goes, -1: the run is the whole item
 };
 struct SeqWork { SeqCounts c; int tiles, row_tiles; };
-__device__ __forceinline__ SeqWork seq_work(const AttendArgs& a, int s) {
+__device__ __forceinline__ SeqWork seq_work(const AttendArgs& a, int s, int behind = 0) {
   SeqWork w;
-  w.c = seq_counts(a.p, s, a.max_new, a.limit);
+  w.c = seq_counts(a.p, s, a.max_new, a.limit, behind);
   const int per = kKeys >> a.p.shift;
   w.tiles = 1 + (seq_pages(a.p, w.c.n).pages + per - 1) / per;
   w.row_tiles = (w.c.m * a.G + a.rows - 1) / a.rows;
@@ -126,26 +126,40 @@ struct Line {
 // innermost (they read the same pages).
 struct Start { int s, item, t, left, n, m, tok0, tiles; };
 // By a whole warp.  left = 0: the CTA has nothing to do.
-__device__ __forceinline__ Start find_start(const AttendArgs& a, int cta, int lane, Line& line) {
+template <bool BACK>
+__device__ __forceinline__ Start find_start_in(const AttendArgs& a, int cta, int lane, Line& line, bool& back) {
   long long total = 0;
   SeqWork w = {};
-  for (int s = lane; s < a.p.n_seqs; s += 32) {
-    w = seq_work(a, s);
-    total += (long long)(w.tiles + a.extra) * w.row_tiles;
+  back = false;
+  if constexpr (BACK) {
+    for (int s0 = 0, behind = 0; s0 < a.p.n_seqs; s0 += 32) {
+      const int front = largest_in_front(a.p, s0, lane, behind);
+      w = SeqWork{};
+      if (s0 + lane < a.p.n_seqs) w = seq_work(a, s0 + lane, front);
+      total += (long long)(w.tiles + a.extra) * w.row_tiles;
+    }
+  } else {
+    for (int s = lane; s < a.p.n_seqs; s += 32) {
+      w = seq_work(a, s);
+      total += (long long)(w.tiles + a.extra) * w.row_tiles;
+      back |= a.p.cu[s + 1] < a.p.cu[s];
+    }
+    back = __any_sync(0xffffffffu, back);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   line.total = total * a.p.Hkv;
   line.ctas = (int)min((long long)a.places, (line.total + a.min_tiles - 1) / a.min_tiles);
   Start r = {};
-  if (cta >= line.ctas) return r;
+  if (cta >= line.ctas || back) return r;
   const long long g0 = line.begin(cta);
   r.left = (int)(line.begin(cta + 1) - g0);
   long long before = 0;
-  for (int s0 = 0; s0 < a.p.n_seqs; s0 += 32) {
+  for (int s0 = 0, behind = 0; s0 < a.p.n_seqs; s0 += 32) {
     if (a.p.n_seqs > 32) {   // (otherwise w is there)
+      const int front = BACK ? largest_in_front(a.p, s0, lane, behind) : 0;
       w = SeqWork{};
-      if (s0 + lane < a.p.n_seqs) w = seq_work(a, s0 + lane);
+      if (s0 + lane < a.p.n_seqs) w = seq_work(a, s0 + lane, front);
     }
     const long long mine = (long long)(w.tiles + a.extra) * w.row_tiles * a.p.Hkv, incl = warp_scan(mine, lane);
     const unsigned hit = __ballot_sync(0xffffffffu, g0 < before + incl);
@@ -166,18 +180,36 @@ __device__ __forceinline__ Start find_start(const AttendArgs& a, int cta, int la
   r.left = 0;   // (not reached)
   return r;
 }
+// Where boundaries go back, with those in front of every sequence.  (Apart, so that the others' code stays short.)
+__device__ __noinline__ void find_start_back(const AttendArgs& a, int cta, int lane, Line* line, Start* r) {
+  bool back;
+  *r = find_start_in<true>(a, cta, lane, *line, back);
+}
+__device__ __forceinline__ Start find_start(const AttendArgs& a, int cta, int lane, Line& line) {
+  bool back;
+  Start r = find_start_in<false>(a, cta, lane, line, back);
+  if (back) {
+    Line l;
+    Start x;
+    find_start_back(a, cta, lane, &l, &x);
+    line = l;
+    r = x;
+  }
+  return r;
+}
 // The runs of a CTA one after the other.  Every role of a CTA has a cursor of its own.
 struct Cursor {
   Start at;
-  int row_tiles;
+  int row_tiles, behind;   // behind: the largest boundary up to that of the sequence at hand
   bool first;
-  __device__ __forceinline__ Cursor(const AttendArgs& a, const Start& start) : at(start), first(true) { row_tiles = (at.m * a.G + a.rows - 1) / a.rows; }
+  __device__ __forceinline__ Cursor(const AttendArgs& a, const Start& start) : at(start), behind(start.tok0), first(true) { row_tiles = (at.m * a.G + a.rows - 1) / a.rows; }
   __device__ __forceinline__ bool next(const AttendArgs& a, Share& out) {
     for (;;) {
       if (at.left <= 0) return false;
       while (at.item >= row_tiles * a.p.Hkv) {   // (there is a sequence with work behind this one: left > 0)
         if (++at.s >= a.p.n_seqs) return false;
-        const SeqWork w = seq_work(a, at.s);
+        const SeqWork w = seq_work(a, at.s, behind);
+        behind = max(behind, a.p.cu[at.s]);
         at.n = w.c.n; at.m = w.c.m; at.tok0 = w.c.tok0; at.tiles = w.tiles;
         row_tiles = w.row_tiles;
         at.item = 0;
@@ -776,8 +808,9 @@ __global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_consta
     }
     return;
   }
+  const int first = first_boundary(a.p, s);
   const SeqCounts c = seq_counts(a.p, s, a.max_new, a.limit);
-  if (c.m == 0) return;
+  if (begins_early(a.p, s, first) || c.m == 0) return;   // (the whole block)
   const int q_heads = a.p.Hkv * a.G;
   if (which >= q_heads + a.p.Hkv) {
     const int h = which - q_heads - a.p.Hkv;

@@ -175,18 +175,44 @@ int make_pages(const lrsa_params_t* params, const lrsa_paged_t* paged, Geom* g, 
 __device__ __forceinline__ int cut_windows(const PageGeom& a, int n) { return n >= a.S ? max((n - a.S) / a.L - 1, 0) : 0; }
 
 // The tokens of sequence s in the cache (n) and the new ones [tok0, tok0 + m); m = 0 where the counts on the device are not usable.
-// most: new tokens that a sequence may have; limit: tokens it may have together.
+// most: new tokens that a sequence may have; limit: tokens it may have together; behind: the largest of the boundaries in front of
+// its own (where they go back, the ranges of two sequences could overlap: the later one is left out).
 struct SeqCounts { int n, tok0, m; bool ok; };
-__device__ __forceinline__ SeqCounts seq_counts(const PageGeom& a, int s, int most, int limit) {
+__device__ __forceinline__ SeqCounts seq_counts(const PageGeom& a, int s, int most, int limit, int behind = 0) {
   SeqCounts q;
   q.n = a.n_tokens[s];
   q.tok0 = a.cu[s];
   const int end = a.cu[s + 1];
-  q.ok = q.n >= 0 && q.n <= a.N && q.tok0 >= 0 && end >= q.tok0 && end <= a.n_new;
+  q.ok = q.n >= 0 && q.n <= a.N && q.tok0 >= max(behind, 0) && end >= q.tok0 && end <= a.n_new;
   q.m = q.ok ? end - q.tok0 : 0;
   if (q.m > most || q.m > limit - q.n) { q.ok = false; q.m = 0; }
   if (!q.ok) q.n = q.tok0 = 0;
   return q;
+}
+// True where a boundary in front of sequence s lies behind its own; by a whole warp.  first: first_boundary, asked for with the counts
+// (volatile: the compiler would ask for it where it is used, a round trip later).
+__device__ __forceinline__ int first_boundary(const PageGeom& a, int s) {
+  int x;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(x) : "l"(a.cu + min((int)threadIdx.x & 31, s)));
+  return x;
+}
+__device__ __forceinline__ bool begins_early(const PageGeom& a, int s, int first) {
+  const int begin = a.cu[s];
+  bool early = first > begin;
+  for (int i0 = 32 + (threadIdx.x & 31); i0 < s; i0 += 256) {
+#pragma unroll
+    for (int i = i0; i < i0 + 256; i += 32) early |= i < s && a.cu[i] > begin;   // (eight loads on their way)
+  }
+  return __any_sync(0xffffffffu, early);
+}
+// The largest boundary in front of every lane's sequence s0 + lane, by a whole warp; `behind`: in front of s0, moved on by 32.
+__device__ __forceinline__ int largest_in_front(const PageGeom& a, int s0, int lane, int& behind) {
+  int top = s0 + lane < a.n_seqs ? a.cu[s0 + lane] : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) top = max(top, __shfl_up_sync(0xffffffffu, top, o));   // (the lanes below o get their own)
+  const int front = __shfl_up_sync(0xffffffffu, top, 1), mine = lane > 0 ? max(behind, front) : behind;
+  behind = max(behind, __shfl_sync(0xffffffffu, top, 31));
+  return mine;
 }
 
 // Column of the table and row of that page of the uncompressed token at position p.

@@ -62,3 +62,176 @@ def test_an_infinity_in_the_pages_stays_one_however_little_it_weighs(heads, d, n
     assert torch.isfinite(lse).all()
     assert not torch.isfinite(o[..., 11]).any()
     assert torch.isfinite(o[..., [c for c in range(d) if c != 11]]).all()
+
+
+def twins(p, page, tokens, reach, **kw):
+    """Two caches that hold the same in the same pages, and the table."""
+    a, b = (Model(p, page, len(tokens), seed=3, **kw) for _ in "ab")
+    for m in (a, b):
+        m.append(tokens)
+    for s, n in enumerate(reach):
+        a.reach(s, n)
+    b.table = a.table
+    b.cache.k_pages.copy_(a.cache.k_pages)
+    b.cache.v_pages.copy_(a.cache.v_pages)
+    return a, b, i32(a.table.tolist())
+
+
+def same_pages(a, b):
+    return all(torch.equal(x.view(torch.int16), y.view(torch.int16))
+               for x, y in ((a.cache.k_pages, b.cache.k_pages), (a.cache.v_pages, b.cache.v_pages)))
+
+
+RANGES = {   # boundaries that go back
+    "the first one only": [0, 30, 10, 20, 40],
+    "first and last": [0, 10, 5, 30, 42],
+    "all behind a large one": [0, 15, 90, 20, 40],
+    "the second only": [-3, 4, 30, 22, 41],
+}
+
+
+def that_count(cu, room, most, apart=True):
+    """(sequence, begin, end) of those that begin at or behind every boundary in front of them; not apart: of all whose own two can be used."""
+    return [(s, cu[s], cu[s + 1]) for s in range(len(cu) - 1)
+            if max([0] + (cu[:s] if apart else [])) <= cu[s] <= cu[s + 1] <= room and cu[s + 1] - cu[s] <= most]
+
+
+@pytest.mark.parametrize("what", RANGES)
+@pytest.mark.parametrize("times, rope", [(1, 64), (10, 64), (10, 0)], ids=["one_launch", "several_launches", "several_no_rope"])
+def test_appends_whose_ranges_would_overlap(what, times, rope):
+    """A sequence's keys are its own, rotated for its own positions.  Of prompts the later ones are left out; few tokens are each sequence's."""
+    p = lrsa.Params(1, 8, 2, 1500, 64, 64, 16, 4)
+    tokens = [0, 150, 30, 3]
+    a, b, table = twins(p, 16, tokens, [n + 460 for n in tokens], dim=rope)
+    cu = [x * times for x in RANGES[what]]
+    T = 45 * times
+    k, v = (a.rows(2, T, False).cuda() for _ in "kv")
+    a.cache.append(k, v, table, i32(a.n), i32(cu), rope=a.rope)
+    assert a.cache.status() == 1
+    for s, begin, end in that_count(cu, T, T, apart=times > 1):     # one at a time
+        one = [begin] * (s + 1) + [end] * (4 - s)
+        b.cache.append(k, v, table, i32(b.n), i32(one), rope=b.rope)
+        assert b.cache.status() == 0
+    assert same_pages(a, b)
+
+
+@pytest.mark.parametrize("what", RANGES)
+@pytest.mark.parametrize("heads, most", [((2, 2), 6), ((4, 2), 6), ((8, 2), 30), ((14, 2), 30)], ids=["few", "few12", "tile", "tiles"])
+def test_attends_whose_ranges_would_overlap(what, heads, most):
+    p = lrsa.Params(1, *heads, 1500, 64, 64, 16, 4)
+    m = Model(p, 16, 4, dim=64, seed=4)
+    m.append([500, 0, 30, 150])
+    cu = [x * most // 30 for x in RANGES[what]]
+    T = 45 * most // 30
+    q, k, v = (m.rows(h, T, False).cuda() for h in (heads[0], 2, 2))
+    table = i32(m.table.tolist())
+    o, lse = torch.full_like(q, 7.0), torch.full((heads[0], T), 7.0, device="cuda")
+    m.cache.attend(q, k, v, table, i32(m.n), i32(cu), rope=m.rope, max_new=most, o=o, lse=lse)
+    assert m.cache.status() == 1
+    left = torch.ones(T, dtype=torch.bool)
+    for s, begin, end in that_count(cu, T, most):
+        one = [begin] * (s + 1) + [end] * (4 - s)
+        want, want_lse = m.cache.attend(q, k, v, table, i32(m.n), i32(one), rope=m.rope, max_new=most)
+        part = slice(begin, end)
+        left[part] = False
+        # (the items may be dealt out otherwise: on both sides a rounding of the probabilities and one of the sum, of values below 5)
+        assert end > begin and (o[:, part].float() - want[:, part].float()).abs().max() <= 4 * 5 * ref.HALF_STEP
+        assert torch.allclose(lse[:, part], want_lse[:, part], rtol=1e-5, atol=1e-5)
+    assert (o[:, left] == 7).all() and (lse[:, left] == 7).all()
+
+
+@pytest.mark.parametrize("n_seqs", [40, 300])
+def test_many_sequences_behind_a_boundary_that_goes_back(n_seqs):
+    """The boundaries in front are looked at by warps and blocks, 32 and 256 at a time."""
+    p = lrsa.Params(1, 4, 2, 900, 64, 64, 16, 4)
+    for at in (5, 33, n_seqs - 3):
+        for new in (3, 80):
+            tokens = [int(x) for x in np.random.default_rng(at).integers(0, 300, n_seqs)]
+            a, b, table = twins(p, 16, tokens, [n + 4 * new for n in tokens], dim=64)
+            k, v = (a.rows(2, new * n_seqs, False).cuda() for _ in "kv")
+            cu = [new * s for s in range(n_seqs + 1)]
+            cu[at] = new * (at - 3)
+            a.cache.append(k, v, table, i32(a.n), i32(cu), rope=a.rope)
+            assert a.cache.status() == 1
+            # the one in front has its end before its beginning, the one behind begins too early: of prompts both are left out
+            parts = [[new * min(s, at - 1) for s in range(n_seqs + 1)], [new * max(s, at + 1) for s in range(n_seqs + 1)]]
+            if new == 3:
+                parts.append([cu[at]] * (at + 1) + [cu[at + 1]] * (n_seqs - at))
+            for part in parts:
+                b.cache.append(k, v, table, i32(b.n), i32(part), rope=b.rope)
+                assert b.cache.status() == 0
+            assert same_pages(a, b)
+            if new == 3:
+                q = a.rows(4, new * n_seqs, False).cuda()
+                for heads_new in (3, 60):      # the kernel for few, the one for many
+                    o, _ = a.cache.attend(q, k, v, table, i32(a.n), i32(cu), rope=a.rope, max_new=heads_new, o=torch.full_like(q, 7.0))
+                    assert a.cache.status() == 1
+                    out = torch.zeros(new * n_seqs, dtype=torch.bool)
+                    out[new * (at - 1):new * (at + 1)] = True
+                    assert (o[:, out] == 7).all() and not (o[:, ~out] == 7).all(-1).any()
+
+
+BAD = {   # what is wrong with which of three sequences
+    "negative tokens": lambda a: a["n_tokens"].__setitem__(1, -1),
+    "too many tokens": lambda a: a["n_tokens"].__setitem__(1, 2000),
+    "counts go back": lambda a: a["cu_new"].__setitem__(2, a["cu_new"][1] - 1),
+    "counts beyond the rows": lambda a: a["cu_new"].__setitem__(3, 10000),
+    "a page that is not there": lambda a: a["table"].__setitem__((1, slice(None)), 1 << 30),
+    "a negative page": lambda a: a["table"].__setitem__((1, slice(None)), -1),
+    "a row that is not there": lambda a: a["rows"].__setitem__(300, 750),
+    "a negative row": lambda a: a["rows"].__setitem__(300, -1),
+}
+
+
+@pytest.mark.parametrize("what", BAD)
+def test_prompts_with_numbers_that_cannot_be_used(what):
+    """As the short calls: told by the status, nothing written but the pages of the other sequences, those to the bit."""
+    p = lrsa.Params(1, 8, 2, 1500, 64, 64, 16, 4)
+    a, b, table = twins(p, 16, [500, 300, 0], [750, 550, 250], dim=64)
+    k, v = (a.rows(2, 750, False).cuda() for _ in "kv")
+    fresh = lambda: dict(table=table.clone(), n_tokens=i32(a.n), cu_new=i32([0, 250, 500, 750]), rows=torch.arange(750, dtype=torch.int32, device="cuda"))
+    args = fresh()
+    BAD[what](args)
+    a.cache.append(k, v, **args, rope=a.rope)
+    assert lrsa.lrsa_last_launch_count() == 3 and a.cache.status() == 1
+    b.cache.append(k, v, **{**fresh(), "cu_new": i32([0, 250, 250, 250])}, rope=b.rope)
+    fine = {0} if what in ("counts go back", "counts beyond the rows") else {0, 2}
+    if 2 in fine:
+        b.cache.append(k, v, **{**fresh(), "cu_new": i32([500, 500, 500, 750])}, rope=b.rope)
+    if what == "counts beyond the rows":
+        b.cache.append(k, v, **{**fresh(), "cu_new": i32([250, 250, 500, 500])}, rope=b.rope)
+        fine = {0, 1}
+    others = [i for i in range(a.cache.n_pages) if i not in {int(x) for s in {0, 1, 2} - fine for x in a.table[s] if x >= 0}]
+    if "row" not in what:
+        others = list(range(a.cache.n_pages))      # (of a bad row another one is taken: its sequence's pages hold something)
+    for x, y in ((a.cache.k_pages, b.cache.k_pages), (a.cache.v_pages, b.cache.v_pages)):
+        assert torch.equal(x[others].view(torch.int16), y[others].view(torch.int16))
+    a.cache.append(k, v, **fresh(), rope=a.rope)
+    assert a.cache.status() == 0
+
+
+def test_prompts_on_another_stream_and_captured():
+    p = lrsa.Params(1, 8, 2, 1500, 64, 64, 16, 4)
+    a, b, table = twins(p, 16, [0, 300], [900, 1200], dim=64)
+    k, v = (a.rows(2, 800, False).cuda() for _ in "kv")
+    n, cu = i32(a.n), i32([0, 400, 800])
+    b.cache.append(k, v, table, n, cu, rope=b.rope)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a.cache.append(k, v, table, n, cu, rope=a.rope, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert a.cache.status() == 0 and same_pages(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.cache.append(k, v, table, n, cu, rope=a.rope)
+        n += cu.diff()
+    for step in (400, 300):
+        new = [step, 800 - step]
+        k.copy_(a.rows(2, 800, False))
+        v.copy_(a.rows(2, 800, False))
+        cu.copy_(i32([0, step, 800]))
+        n.copy_(i32([step, 500 - step]))
+        b.cache.append(k, v, table, n, cu, rope=b.rope)
+        graph.replay()
+        assert a.cache.status() == 0 and same_pages(a, b), new
+        assert n.tolist() == [step + new[0], 500 - step + new[1]]
