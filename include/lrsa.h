@@ -349,7 +349,7 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  *
  * Counts, page numbers, rows and parents that cannot be used (out of range, more new tokens than max_new, beyond seq_len or beyond the
  * rope's positions, which have to cover n_tokens + the new tokens of a sequence) are found on the device: lrsa_workspace_status
- * returns LRSA_ERR_INVALID_ARG.  A sequence with bad counts is left out (its rows of o stay as they were), whatever is read or written stays
+ * returns LRSA_ERR_INVALID_ARG for the last call on a workspace, lrsa_paged_status when any had such numbers since it was last asked.  A sequence with bad counts is left out (its rows of o stay as they were), whatever is read or written stays
  * inside the tensors.  Where cu_new goes back, a sequence that begins in front of an earlier boundary may be left out too: no row becomes
  * another sequence's.
  * lrsa_paged_shape: the workspace of an attend of n_new tokens of n_seqs sequences, at most max_new each (it grows with n_new and n_seqs; any
@@ -376,6 +376,12 @@ int lrsa_paged_attend(const lrsa_params_t* params, const lrsa_paged_t* paged, co
                       const lrsa_rows_t* v, const int32_t* cu_new, int32_t n_new, int32_t max_new, const int32_t* parent,
                       const lrsa_rope_t* rope, const lrsa_rows_t* o, float* lse, void* workspace, size_t workspace_bytes,
                       void* cuda_stream);
+/*
+ * What the calls of lrsa_paged_* on a workspace have found since this was last asked, replays of captured ones too: LRSA_OK, LRSA_ERR_TIMEOUT or
+ * LRSA_ERR_INVALID_ARG; starts anew.  (An append behind an attend clears the status word of lrsa_workspace_status.)  Whoever asks this has zeroed the
+ * first 256 bytes of the workspace when it was made.  Synchronises `cuda_stream`; the calls are in front of it there, or otherwise done.
+ */
+int lrsa_paged_status(void* workspace, void* cuda_stream);
 
 /*
  * Reads the status word that the last call using `workspace` left there.  Synchronises

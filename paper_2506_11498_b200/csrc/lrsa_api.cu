@@ -255,6 +255,17 @@ int lrsa_workspace_status(const void* workspace, void* cuda_stream) {
   return status == LRSA_OK || status == LRSA_ERR_INVALID_ARG ? status : LRSA_ERR_TIMEOUT;
 }
 
+int lrsa_paged_status(void* workspace, void* cuda_stream) {
+  if (!workspace || !aligned(workspace, 256)) return LRSA_ERR_INVALID_ARG;
+  int* word = &static_cast<WsHeader*>(workspace)->raised;
+  int raised = 0;
+  auto st = static_cast<cudaStream_t>(cuda_stream);
+  if (cudaMemcpyAsync(&raised, word, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess) return LRSA_ERR_CUDA;
+  if (cudaStreamSynchronize(st) != cudaSuccess) return LRSA_ERR_CUDA;
+  if (raised != 0 && cudaMemsetAsync(word, 0, sizeof(int), st) != cudaSuccess) return LRSA_ERR_CUDA;
+  return raised & kRaisedTimeout ? LRSA_ERR_TIMEOUT : raised & kRaisedInvalid ? LRSA_ERR_INVALID_ARG : LRSA_OK;
+}
+
 const char* lrsa_status_string(int status) {
   switch (status) {
     case LRSA_OK: return "ok";

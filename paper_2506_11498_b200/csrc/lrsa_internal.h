@@ -50,8 +50,10 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 struct WsHeader {
   int status;   // lrsa_status written by kernels (0 or LRSA_ERR_TIMEOUT)
   int ticket;   // dynamic work counter of the scoring kernel
-  int pad[62];
+  int raised;   // calls of the paged cache: what any of them found since it was read last (kRaised*); they never clear it
+  int pad[61];
 };
+constexpr int kRaisedInvalid = 1, kRaisedTimeout = 2;
 static_assert(sizeof(WsHeader) == 256, "header is 256 bytes");
 
 // Number of leading windows that query chunk c sees only through their kept tokens.

@@ -57,7 +57,7 @@ struct AppendArgs {
   const int32_t* rows;                      // optional: row of every new token
   __nv_bfloat16 *k_pages, *v_pages;
   int32_t* kept;                            // optional
-  int* status;                              // written by the last cluster (null: not by this launch)
+  WsHeader* head;                           // its status is written by the cluster that checks
   int most, limit;                          // bounds of the counts
   int ddof;
   int clusters;                             // clusters that cut; the one behind them checks, those behind that write the rows of fresh sequences
@@ -477,7 +477,9 @@ __device__ void check_append(const AppendArgs& a) {
     }
   }
   bad = __syncthreads_or(bad);
-  if (tid == 0) *a.status = bad ? LRSA_ERR_INVALID_ARG : LRSA_OK;
+  if (tid != 0) return;
+  a.head->status = bad ? LRSA_ERR_INVALID_ARG : LRSA_OK;
+  if (bad) keep_status(a.head, LRSA_ERR_INVALID_ARG);
 }
 
 // The keys of all new tokens rotated, for the forms with several launches: a window's rows are read twice there (for its own scores, and as the
@@ -681,7 +683,7 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   }
   a.n_rows = n_rows; a.rows = rows; a.kept = kept;
   a.k_pages = static_cast<__nv_bfloat16*>(paged->k_pages); a.v_pages = static_cast<__nv_bfloat16*>(paged->v_pages);
-  a.status = &static_cast<WsHeader*>(workspace)->status;
+  a.head = static_cast<WsHeader*>(workspace);
   a.most = n_new;
   a.limit = a.rope.half > 0 && a.rope.n_pos < g.N ? a.rope.n_pos : g.N;
   a.ddof = g.ddof;

@@ -44,7 +44,7 @@ struct AttendArgs {
   int* odd;                              // [n_seqs][Hkv] an infinity or NaN among its new values
   __nv_bfloat16 *q_parts[2];             // [Hkv][n_new * G][D] rotated queries: rounded, and what that leaves
   __nv_bfloat16 *k_parts[2], *v_finite;  // [Hkv][n_new][D] the new keys likewise; the new values with zeros for what is not finite
-  int* status;
+  WsHeader* head;
   int G, max_new, limit, rows;           // rows: of a row tile
   int places, min_tiles, extra;          // CTAs that share the work; the fewest tiles that are a CTA's worth; what beginning an item costs, in tiles
   float scale, scale_log2;
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
   __shared__ int odd;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   wait_front();
-  if (blockIdx.x == 0 && tid == 0) *a.status = 0;
+  if (blockIdx.x == 0 && tid == 0) a.head->status = LRSA_OK;
   if (warp == 0) {
     Line line;
     const Start s = find_start(a, blockIdx.x, lane, line);
@@ -699,7 +699,10 @@ __global__ void __launch_bounds__(256, 4) paged_merge_kernel(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool bad = attend_inputs_bad(a);
   wait_front();
-  if (bad) atomicCAS(a.status, (int)LRSA_OK, (int)LRSA_ERR_INVALID_ARG);
+  if (bad) {
+    atomicCAS(&a.head->status, (int)LRSA_OK, (int)LRSA_ERR_INVALID_ARG);
+    keep_status(a.head, LRSA_ERR_INVALID_ARG);
+  }
   int items = 0, total = 0;
   static_assert(kMaxPlaces <= 512, "two a thread");
   Divided d[2] = {};
@@ -797,7 +800,7 @@ __global__ void __launch_bounds__(256) paged_operands_kernel(const __grid_consta
   __shared__ int odd;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_front();
-  if (blockIdx.x == 0 && tid == 0) *a.status = 0;
+  if (blockIdx.x == 0 && tid == 0) a.head->status = LRSA_OK;
   const int heads = a.p.Hkv * (a.G + 2), plan0 = a.p.n_seqs * heads, s = blockIdx.x / heads, which = blockIdx.x - s * heads;
   if ((int)blockIdx.x >= plan0) {
     const int cta = (blockIdx.x - plan0) * 8 + warp;
@@ -1321,7 +1324,10 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem, Cfg::kCols);
-  if (tid == 0 && sh.abort) atomicExch(a.status, (int)LRSA_ERR_TIMEOUT);
+  if (tid == 0 && sh.abort) {
+    atomicExch(&a.head->status, (int)LRSA_ERR_TIMEOUT);
+    keep_status(a.head, LRSA_ERR_TIMEOUT);
+  }
 }
 
 bool rows_ok(const lrsa_rows_t* r) {
@@ -1452,7 +1458,7 @@ int lrsa_paged_attend(const lrsa_params_t* params, const lrsa_paged_t* paged, co
     a.v_head = v->head_stride; a.v_tok = v->token_stride; a.o_head = o->head_stride; a.o_tok = o->token_stride;
   }
   a.parent = parent; a.lse = lse;
-  a.status = &static_cast<WsHeader*>(workspace)->status;
+  a.head = static_cast<WsHeader*>(workspace);
   auto at = [workspace](size_t offset) { return static_cast<void*>(static_cast<unsigned char*>(workspace) + offset); };
   a.starts = static_cast<Start*>(at(ws.starts));
   a.divided = static_cast<Divided*>(at(ws.divided));

@@ -13,6 +13,11 @@ __device__ __forceinline__ void wait_front() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// What a call found is told by the status word, which the next call on the workspace clears, and by a word that is kept until it is read.
+__device__ __forceinline__ void keep_status(WsHeader* head, lrsa_status code) {
+  atomicOr(&head->raised, code == LRSA_ERR_TIMEOUT ? kRaisedTimeout : kRaisedInvalid);
+}
+
 // ---- rotation ----
 struct RopeArgs {
   const float *cos, *sin;   // [n_pos][half]

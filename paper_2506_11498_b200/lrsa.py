@@ -161,7 +161,8 @@ def lib() -> ctypes.CDLL:
         L.lrsa_paged_attend.argtypes = [pp, gp, wp, wp, wp, vp, i32, i32, vp, rp, wp, fp, vp, sz, vp]
         for name in ("lrsa_rotate", "lrsa_paged_shape", "lrsa_paged_append", "lrsa_paged_attend"):
             getattr(L, name).restype = ctypes.c_int
-        L.lrsa_workspace_status.argtypes = [vp, vp]
+        L.lrsa_workspace_status.argtypes = L.lrsa_paged_status.argtypes = [vp, vp]
+        L.lrsa_paged_status.restype = ctypes.c_int
         L.lrsa_score_select_static_status.argtypes = [vp]
         L.lrsa_score_select_static_status.restype = ctypes.c_int
         L.lrsa_status_string.argtypes = [ctypes.c_int]
@@ -257,6 +258,13 @@ def lrsa_workspace_bytes(params: Params):
 
 def new_workspace(nbytes: int, device="cuda") -> torch.Tensor:
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def _cleared_workspace(nbytes: int, device) -> torch.Tensor:
+    """A workspace with a header of zeros, as lrsa_paged_status wants it."""
+    ws = new_workspace(nbytes, device)
+    ws[:256].zero_()
+    return ws
 
 
 def _made(stream, near, make, *args, **kw):
@@ -765,7 +773,8 @@ class PagedCache:
     v_pages, bf16 [n_pages, Hkv, page, d], which may be replaced by others of that shape, type and device.  What the layers of a
     model share is the caller's, on the device: the page table (int32 [sequences, table_width]), the tokens in the cache (n_tokens, int32
     [sequences]) and where the new tokens of a sequence begin (cu_new, int32 [sequences + 1]).  Neither call changes them, so a step is
-    attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status().
+    attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status(),
+    until it has been asked.
     The calls of a cache share its workspace, so they run one after the other, captured ones too; different caches share nothing."""
 
     MOST_NEW = 128   # new tokens of a sequence in an attend
@@ -782,7 +791,7 @@ class PagedCache:
         self.k_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
         self.v_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
         self._need, self._old = {}, []
-        self.ws = new_workspace(self.workspace_bytes(1, 1, 1), device)
+        self.ws = _cleared_workspace(self.workspace_bytes(1, 1, 1), device)
 
     def workspace_bytes(self, n_seqs: int, n_new: int, max_new: int) -> int:
         """What an attend of n_new tokens of n_seqs sequences, at most max_new each, takes; max_new = 0: an append."""
@@ -800,7 +809,7 @@ class PagedCache:
             need = self._need[sizes] = self.workspace_bytes(*sizes)
         if self.ws.numel() < need:
             self._old.append(self.ws)
-            self.ws = _made(stream, near, new_workspace, max(need, 2 * self.ws.numel()), near.device)
+            self.ws = _made(stream, near, _cleared_workspace, max(need, 2 * self.ws.numel()), near.device)
         return self.ws
 
     def columns(self, n_tokens: int):
@@ -931,4 +940,8 @@ class PagedCache:
         return o, lse
 
     def status(self, stream=None) -> int:
-        return lrsa_workspace_status(self.ws, stream)
+        """What the calls of this cache have found since this was last asked, in whichever workspace they ran, replays of captured ones too: 0, 1
+        (counts, page numbers, rows or parents that cannot be used) or 5 (a bounded wait ran out).  Synchronises the stream; calls on others are
+        done by then, or told the next time.  (A workspace that a call makes while it is captured starts anew with every replay.)"""
+        at = _stream(stream)
+        return max(lib().lrsa_paged_status(ws.data_ptr(), at) for ws in (*self._old, self.ws))

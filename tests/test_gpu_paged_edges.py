@@ -235,3 +235,60 @@ def test_prompts_on_another_stream_and_captured():
         graph.replay()
         assert a.cache.status() == 0 and same_pages(a, b), new
         assert n.tolist() == [step + new[0], 500 - step + new[1]]
+
+
+def a_step(seed, heads=(8, 2)):
+    p = lrsa.Params(1, *heads, 1500, 64, 64, 16, 4)
+    m = Model(p, 16, 2, dim=64, seed=seed)
+    m.append([300, 40])
+    for s in range(2):
+        m.reach(s, 1400)
+    q, k, v = (m.rows(h, 40, False).cuda() for h in (heads[0], 2, 2))
+    return m, q, k, v, i32(m.table.tolist()), i32(m.n), i32([0, 20, 40])
+
+
+@pytest.mark.parametrize("most", [2, 20], ids=["few", "tile"])
+def test_what_an_attend_found_is_told_behind_its_append(most):
+    """A step is attend, then append: what only the attend can find, and an append that everything is right for."""
+    m, q, k, v, table, n, _ = a_step(5)
+    cu = i32([0, most, 2 * most])
+    parent = i32(list(range(-1, most - 1)) * 2)
+    wrong = parent.clone()
+    wrong[1] = 1
+    for bad in (dict(parent=wrong, max_new=most), dict(parent=parent, max_new=most - 1)):
+        m.cache.attend(q, k, v, table, n, cu, rope=m.rope, **{**bad, "parent": torch.cat([bad["parent"], bad["parent"].new_zeros(40 - 2 * most)])})
+        m.cache.append(k, v, table, n, cu, rope=m.rope)
+        m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=most)
+        assert lrsa.lrsa_workspace_status(m.cache.ws) == 0       # of the last call
+        assert m.cache.status() == 1 and m.cache.status() == 0
+    for _ in range(2):
+        m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=most)
+        m.cache.append(k, v, table, n, cu, rope=m.rope)
+    assert m.cache.status() == 0
+
+
+def test_what_a_captured_step_found_is_told_when_the_workspace_has_grown():
+    m, q, k, v, table, n, cu = a_step(6)
+    parent = i32(list(range(-1, 19)) * 2)
+    step = lambda: (m.cache.attend(q, k, v, table, n, cu, parent=parent, rope=m.rope, max_new=20), m.cache.append(k, v, table, n, cu, rope=m.rope))
+    step()
+    assert m.cache.status() == 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    small = m.cache.ws
+    big, big_cu = 500000, i32([0, 500000, 500000])          # (more tokens than a sequence may have: told, and nothing else done)
+    x = torch.zeros(2, 1, 64, dtype=torch.bfloat16, device="cuda").expand(-1, big, -1)
+    m.cache.append(x, x, table, n, big_cu, rope=m.rope)
+    assert m.cache.ws is not small and m.cache.status() == 1 and m.cache.status() == 0
+    graph.replay()
+    assert m.cache.status() == 0
+    parent[3] = 7
+    graph.replay()
+    parent[3] = 2
+    for _ in range(3):
+        graph.replay()                                      # ... and right again
+        step()
+    assert m.cache.status() == 1 and m.cache.status() == 0
+    graph.replay()
+    assert m.cache.status() == 0

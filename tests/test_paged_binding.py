@@ -74,3 +74,36 @@ def test_tables_of_a_rope_that_lost_their_memory(calls):
         with pytest.raises(lrsa.LrsaError):
             call()
     assert len(calls) == n
+
+
+def test_status_is_asked_of_every_workspace(calls, monkeypatch):
+    """A captured call goes on in the workspace that it was captured with, when the cache has a larger one."""
+    cache = lrsa.PagedCache(P, 5, device="cpu")
+    asked, told = [], {}
+
+    class Library:
+        def __getattr__(self, name):
+            return getattr(lrsa._lib, name)
+
+        def lrsa_paged_status(self, at, stream):
+            asked.append(at)
+            return told.pop(at, 0)
+
+    library = Library()
+    spaces = [cache.ws]
+    for new in (20, 60, 130):
+        cache.append(**good(cache, 1000 * new)[0], stream=STREAM)
+        spaces.append(cache.ws)
+    assert len({x.data_ptr() for x in spaces}) == 4 and all((x[:256] == 0).all() for x in spaces)
+    monkeypatch.setattr(lrsa, "lib", lambda: library)
+    for code in (1, 5):
+        for space in spaces:
+            told[space.data_ptr()] = code
+            assert cache.status(STREAM) == code and cache.status(STREAM) == 0
+    told.update({spaces[0].data_ptr(): 5, spaces[3].data_ptr(): 1})
+    assert cache.status(STREAM) == 5
+    assert set(asked) == {x.data_ptr() for x in spaces}
+
+
+def test_status_without_a_workspace():
+    assert lrsa.lib().lrsa_paged_status(None, None) == lrsa.lib().lrsa_paged_status(0x7f0000000080, None) == INVALID
