@@ -539,7 +539,7 @@ static int launch_dkv_t(const Geom& whole, const SeqBatch& b, const DkvBatch& db
   a.stats = p.stats; a.Dacc = p.Dacc; a.seg_map = p.seg_map; a.dKf = p.dKf; a.dVf = p.dVf;
   a.scale = whole.scale; a.scale_log2 = whole.scale * 1.4426950408889634f; a.status = p.status;
   auto kern = lrsa_bwd_dkv_kernel<D, NSEQ>;
-  LRSA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+  LRSA_CUDA_CHECK(allow_smem<Cfg::kSmem>(kern));
   const long long grid = (long long)a.seg0[b.n] * a.BHkv;
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)grid), dim3(Cfg::kThreads), Cfg::kSmem, st, 1, m, a));

@@ -575,7 +575,7 @@ static int launch_fwd_t(const Geom& whole, const SeqBatch& b, const __nv_bfloat1
   const long long grid = (long long)a.block0[b.n] * a.BH;
   if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   auto kern = lrsa_fwd_kernel<D, NSEQ, TQ>;
-  LRSA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+  LRSA_CUDA_CHECK(allow_smem<Cfg::kSmem>(kern));
   LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)grid), dim3(Cfg::kThreads), Cfg::kSmem, st, 1, m, a));
   launch_counter().n++;
   return LRSA_OK;

@@ -350,7 +350,7 @@ int launch_weights_t(const Geom& whole, const SeqBatch& b, const __nv_bfloat16* 
   a.split = weights_split(items, pairs);
   a.LSE = LSE; a.weight = weight; a.scale_log2 = whole.scale * 1.4426950408889634f; a.status = status; a.clear = clear;
   auto kern = lrsa_weights_kernel<D, NSEQ>;
-  LRSA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+  LRSA_CUDA_CHECK(allow_smem<Cfg::kSmem>(kern));
   LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)(items * a.split)), dim3(Cfg::kThreads), Cfg::kSmem, st, a.split, m, a));
   launch_counter().n++;
   return LRSA_OK;

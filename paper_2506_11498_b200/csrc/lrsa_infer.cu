@@ -705,10 +705,10 @@ template <int D>
 cudaError_t launch_split_t(const Geom& g, DecodeArgs& a, cudaStream_t st) {
   // K and V rows; the merge buffer (4 warps x 16 heads x (d + 2) floats) lies over them, or behind them when the
   // group has more than 16 query heads and the rows are read again
-  const size_t rows_bytes = (size_t)(2 * kDecKeys + kDecHeads) * (D * sizeof(__nv_bfloat16) + 16);   // K, V and Q rows, padded
-  const size_t merge_bytes = (size_t)4 * kDecHeads * (D + 2) * sizeof(float);
+  constexpr size_t rows_bytes = (size_t)(2 * kDecKeys + kDecHeads) * (D * sizeof(__nv_bfloat16) + 16);   // K, V and Q rows, padded
+  constexpr size_t merge_bytes = (size_t)4 * kDecHeads * (D + 2) * sizeof(float);
   const size_t smem = g.G > kDecHeads ? rows_bytes + merge_bytes : (rows_bytes > merge_bytes ? rows_bytes : merge_bytes);
-  const cudaError_t e = cudaFuncSetAttribute(decode_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = allow_smem<(int)(rows_bytes + merge_bytes)>(decode_split_kernel<D>);
   if (e != cudaSuccess) return e;
   return launch_dependent(decode_split_kernel<D>, dim3(a.n_split, g.B * g.Hkv), dim3(kDecThreads), smem, st, 1, a);
 }

@@ -144,6 +144,13 @@ cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, dim3 block, size_t s
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
+// Leave for launches of `kern` to ask for up to BYTES of dynamic shared memory.  The limit belongs to the function and is the same for all host threads:
+// one constant for a kernel, so that no call lowers it between another's leave and its launch.
+template <int BYTES, typename... P>
+cudaError_t allow_smem(void (*kern)(P...)) {
+  return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES);
+}
+
 // lrsa_api.cu : clusters of c CTAs (at most 16) that the device runs at a time with 2^p CTAs on an SM, n[p][c].
 struct ClusterRoom {
   int n[3][17];

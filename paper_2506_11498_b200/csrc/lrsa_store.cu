@@ -240,7 +240,7 @@ template <int D, int T, int M>
 int launch_rows_t(const StoreRows& a, int threads, long long grid, size_t smem, cudaStream_t st, bool cut) {
   auto rows = store_rows_kernel<D, T, M>;
   auto cuts = store_cut_kernel<D, T, M>;
-  if (smem > kSelSmemFree) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cuts, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelSmemMax));
+  if (smem > kSelSmemFree) LRSA_CUDA_CHECK(allow_smem<kSelSmemMax>(cuts));
   LRSA_CUDA_CHECK(cut ? launch_dependent(cuts, dim3((unsigned)grid), dim3(threads), smem, st, a.split, a)
                       : launch_dependent(rows, dim3((unsigned)grid), dim3(threads), 0, st, 1, a));
   launch_counter().n++;
@@ -1072,8 +1072,9 @@ DecodePlan store_plan(const Geom& g, int blocks, int max_splits = kDecMaxSplits)
 template <int D, int NH, int T>
 cudaError_t launch_store_decode_t(StoreDecodeArgs& a, const DecodePlan& pl, int BHkv, cudaStream_t st) {
   auto kern = store_decode_kernel<D, NH, T>;
-  const int merge = pl.warps * 8 * (D + 4) * 4, rings = pl.warps * kRing * kStage, smem = merge > rings ? merge : rings;
-  const cudaError_t es = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  constexpr int kWarps = dec_max_warps(NH) / 2;   // (store_plan's)
+  constexpr int merge = kWarps * 8 * (D + 4) * 4, rings = kWarps * kRing * kStage, smem = merge > rings ? merge : rings;
+  const cudaError_t es = allow_smem<smem>(kern);
   if (es != cudaSuccess) return es;
   if (pl.splits > 8) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);

@@ -725,7 +725,7 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   const bool three = !one && fit3 && clusters * C > 2 * kSms;
   auto cut = g.d == 128 ? (one ? paged_cut_kernel<128, true, 2> : three ? paged_cut_kernel<128, false, 3> : paged_cut_kernel<128, false, 2>)
                         : (one ? paged_cut_kernel<64, true, 2> : three ? paged_cut_kernel<64, false, 3> : paged_cut_kernel<64, false, 2>);
-  if (smem > 16 * 1024) LRSA_CUDA_CHECK(cudaFuncSetAttribute(cut, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  if (smem > 16 * 1024) LRSA_CUDA_CHECK(allow_smem<2 * kAppMaxL * (int)sizeof(float)>(cut));
   LRSA_CUDA_CHECK(launch_dependent(cut, dim3((unsigned)grid), dim3(kAppThreads), smem, st, C, a, C));
   launch_counter().n++;
   if (one) return LRSA_OK;

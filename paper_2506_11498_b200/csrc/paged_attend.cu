@@ -1378,7 +1378,7 @@ int launch_tile(AttendArgs& a, cudaStream_t st) {
   launch_counter().n++;
   constexpr size_t smem = Cfg::kTail + sizeof(TileTail);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
-  LRSA_CUDA_CHECK(cudaFuncSetAttribute(paged_tile_kernel<D, TQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  LRSA_CUDA_CHECK((allow_smem<(int)smem>(paged_tile_kernel<D, TQ>)));
   LRSA_CUDA_CHECK(launch_dependent(paged_tile_kernel<D, TQ>, dim3(a.places), dim3(Cfg::kThreads), smem, st, 1, maps, a));
   return LRSA_OK;
 }

@@ -91,7 +91,7 @@ __device__ __forceinline__ float warp_sum(float v) {
 // Top-K of the window by the last CTA to finish it.  smem: sk[L], sv[L] floats, then scratch.
 // Bytes of the selection scratch: sk[L], sv[L] (rounded up to 16 bytes), two histograms of 256 bins, 32 floats, 16 + 8 words.
 // Rounded up to 16 bytes: the cluster kernel has two of them one behind the other.
-__host__ __device__ inline size_t select_scratch_bytes(int L) {
+__host__ __device__ constexpr size_t select_scratch_bytes(int L) {
   return (((size_t)2 * L * 4 + 15) & ~(size_t)15) + 2 * 256 * 4 + 32 * 4 + 16 * 4 + 8 * 4;
 }
 
@@ -661,7 +661,7 @@ constexpr int kUnitMaxL = 25448;
 template <int D>
 constexpr int tok_per_unit() { return kSteps * (kThreads / (D / 8)); }
 
-size_t select_smem_bytes(int L, int d) {
+constexpr size_t select_smem_bytes(int L, int d) {
   const size_t phase1 = (size_t)(kThreads / 32) * 4 * d * sizeof(__nv_bfloat16);
   const size_t sel = select_scratch_bytes(L);
   return phase1 > sel ? phase1 : sel;
@@ -738,6 +738,8 @@ static ScoreArgs score_args(const Geom& g, const __nv_bfloat16* K, const __nv_bf
   return a;
 }
 
+constexpr size_t cluster_smem_bytes(int L, int d) { return (size_t)d * 16 + 2 * (4 * d * 2) + 8 * 2 * d * 2 + 2 * select_scratch_bytes(L); }
+
 static int launch_cluster(const Geom* gs, int n_seqs, const __nv_bfloat16* K, const __nv_bfloat16* V, int32_t* idx, float* score,
                           void* ws, cudaStream_t st, bool clear_status) {
   for (int s0 = 0; s0 < n_seqs;) {
@@ -767,11 +769,10 @@ static int launch_cluster(const Geom* gs, int n_seqs, const __nv_bfloat16* K, co
     }
     const long long grid = (long long)q.item0[q.n] * pl.C;
     if (grid > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
-    const size_t bytes = (size_t)g.d * 16 + 2 * (4 * g.d * 2) + 8 * 2 * g.d * 2 + 2 * select_scratch_bytes(g.L);
+    const size_t bytes = cluster_smem_bytes(g.L, g.d);
     auto kern = g.d == 128 ? (pl.run > 1 ? score_select_cluster_kernel<128, true> : score_select_cluster_kernel<128, false>)
                            : (pl.run > 1 ? score_select_cluster_kernel<64, true> : score_select_cluster_kernel<64, false>);
-    if (bytes > 48 * 1024)
-      LRSA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (bytes > 48 * 1024) LRSA_CUDA_CHECK((allow_smem<(int)cluster_smem_bytes(kClusterMaxL, 128)>(kern)));
     LRSA_CUDA_CHECK(launch_dependent(kern, dim3((unsigned)grid), dim3(kThreads), bytes, st, pl.C, a, q, pl.run, pl.C));
     launch_counter().n++;
     clear_status = false;
@@ -801,7 +802,7 @@ static int launch_unit(const Geom& g, const __nv_bfloat16* K, const __nv_bfloat1
   const long long units = (long long)a.BH * g.W * a.n_slices;
   if (units > 0x7fffffffLL) return LRSA_ERR_UNSUPPORTED;
   auto kern = g.d == 128 ? score_select_kernel<128> : score_select_kernel<64>;
-  LRSA_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  LRSA_CUDA_CHECK((allow_smem<(int)select_smem_bytes(kUnitMaxL, 128)>(kern)));
   kern<<<(unsigned)units, kThreads, smem, st>>>(a);
   LRSA_CUDA_CHECK(cudaGetLastError());
   launch_counter().n++;

@@ -27,7 +27,7 @@ static int launch_weight_select(const WeightSelectArgs& a, cudaStream_t st) {
   if (a.n == 0 || a.item0[a.n] == 0) return LRSA_OK;
   const size_t smem = (size_t)a.L * 4;
   if (smem > kSelSmemFree)
-    LRSA_CUDA_CHECK(cudaFuncSetAttribute(weight_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelSmemMax));
+    LRSA_CUDA_CHECK(allow_smem<kSelSmemMax>(weight_select_kernel));
   LRSA_CUDA_CHECK(launch_dependent(weight_select_kernel, dim3((unsigned)a.item0[a.n]), dim3(kSelThreads), smem, st, 1, a));
   launch_counter().n++;
   return LRSA_OK;

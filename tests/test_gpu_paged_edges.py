@@ -292,3 +292,48 @@ def test_what_a_captured_step_found_is_told_when_the_workspace_has_grown():
     assert m.cache.status() == 1 and m.cache.status() == 0
     graph.replay()
     assert m.cache.status() == 0
+
+
+def test_calls_of_two_threads_with_windows_of_different_lengths():
+    """Kernels that take shared memory by the length of a window, called side by side: appends of two caches, selections, decodes."""
+    import threading
+    failed, work = [], []
+    gate = threading.Barrier(2)
+    for lag, group in ((9000, 32), (2100, 10)):
+        p = lrsa.Params(1, 2 * group, 2, 4 * lag, 64, lag, lag // 4, 4)
+        cache = lrsa.PagedCache(p, 2 * (-(-4 * lag // 128) + 8), page=128)
+        table = torch.arange(cache.table_width, dtype=torch.int32, device="cuda")[None]
+        k, v = (torch.randn(2, 3 * lag + 10, 64, generator=torch.Generator().manual_seed(lag)).bfloat16().cuda() for _ in "kv")
+        some = lrsa.Params(1, 2 * group, 2, 1000, 64, 256, 64, 4)
+        kv = lrsa.KVCache(some)
+        x = k[None, :, :900].contiguous()
+        kv.append(x, x)
+        sel = lrsa.Params(1, 2 * group, 2, 3 * lag + 10, 64, lag, lag // 4, 4)
+        q = torch.randn(1, 2 * group, 64, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+        work.append((cache, k, v, table, i32([0]), i32([0, 3 * lag + 10]), kv, q, sel))
+
+    def run(i):
+        cache, k, v, table, n, cu, kv, q, sel = work[i]
+        stream = torch.cuda.Stream()
+        try:
+            with torch.cuda.stream(stream):
+                out = []
+                gate.wait()
+                for _ in range(200):
+                    cache.append(k, v, table, n, cu)
+                    idx, _ = lrsa.lrsa_score_select(sel, k[None], v[None])
+                    out.append((idx, kv.decode(q)[0]))
+            stream.synchronize()
+            for idx, o in out[1:]:
+                assert torch.equal(idx, out[0][0]) and torch.equal(o, out[0][1])
+            assert cache.status(stream) == 0
+        except Exception as e:
+            failed.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
