@@ -930,7 +930,7 @@ __global__ void __launch_bounds__(TileCfg<D, TQ>::kThreads, 1) paged_tile_kernel
   wait_front();
   if (tid == 0) {
     sh.start = a.starts[blockIdx.x];
-    if (sQ & 1023u) sh.start.left = 0;           // (the operand tiles want 1024 bytes, as declared)
+    if (sQ & 1023u) { sh.start.left = 0; sh.abort = 1; }   // (the operand tiles want 1024 bytes, as declared)
   }
   __syncthreads();
   tc_fence_after_sync();
