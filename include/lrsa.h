@@ -344,7 +344,7 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  * A token deeper than the end of the chunk of the first one sees the cache as the first one does.  What
  * a token does not see has no influence on it, infinities and NaN included.  Rotated queries and new keys are multiplied as sums of two bf16, probabilities
  * are rounded to bf16, sums and softmax are fp32.  (With a rope, an infinite channel of a key that is seen may give NaN where one product would give
- * a score of -infinity.)  o overlaps none of the inputs.
+ * a score of -infinity.)  The rows of o overlap neither one another nor those of q, k and v.
  *   q, o : bf16 [Hq, n_new, d];  k, v : bf16 [Hkv, n_new, d];  lse (optional): fp32 [Hq, n_new]
  *
  * Counts, page numbers, rows and parents that cannot be used (out of range, more new tokens than max_new, beyond seq_len or beyond the

@@ -1334,6 +1334,42 @@ bool rows_ok(const lrsa_rows_t* r) {
   return r && r->data && !(reinterpret_cast<uintptr_t>(r->data) & 15u) && r->head_stride % 8 == 0 && r->token_stride % 8 == 0;
 }
 
+// Whether |c + y step| < d for a y in [lo, hi].
+bool comes_near(long long c, long long step, long long lo, long long hi, long long d) {
+  auto near = [=](long long y) { const long long x = c + (y < lo ? lo : y > hi ? hi : y) * step; return x < d && -x < d; };
+  if (step == 0) return near(lo);
+  const long long y = -c / step;   // (towards zero: the nearest is this one or a neighbour)
+  return near(y - 1) || near(y) || near(y + 1);
+}
+// Whether two of the rows of o lie over one another: heads h, tokens t at h o_head + t o_tok, d elements each.
+bool rows_overlap(const AttendArgs& a, long long heads, long long n, long long d) {
+  const long long head = a.o_head < 0 ? -a.o_head : a.o_head, tok = a.o_tok < 0 ? -a.o_tok : a.o_tok;
+  if (n > 1 && tok < d) return true;
+  if (heads == 1 || (n > 1 ? (tok >= (heads - 1) * head + d && head >= d) || head >= (n - 1) * tok + d : head >= d)) return false;   // one inside the other
+  for (long long h = 1; h < heads; ++h)
+    if (comes_near(h * a.o_head, a.o_tok, 1 - n, n - 1, d)) return true;
+  return false;
+}
+// Whether a row of o lies over one of the rows at p.  Rows of both may take turns in one buffer (the output beside a fused projection's).
+bool rows_overlap(const AttendArgs& a, long long heads, long long n, long long d, const __nv_bfloat16* p, long long p_heads, long long p_head, long long p_tok) {
+  const long long apart = (reinterpret_cast<intptr_t>(a.o) - reinterpret_cast<intptr_t>(p)) / (long long)sizeof(__nv_bfloat16);
+  auto low = [n](long long h, long long head, long long tok) { return (head < 0 ? (h - 1) * head : 0) + (tok < 0 ? (n - 1) * tok : 0); };
+  auto high = [n](long long h, long long head, long long tok) { return (head > 0 ? (h - 1) * head : 0) + (tok > 0 ? (n - 1) * tok : 0); };
+  if (apart + high(heads, a.o_head, a.o_tok) + d <= low(p_heads, p_head, p_tok) || apart + low(heads, a.o_head, a.o_tok) >= high(p_heads, p_head, p_tok) + d)
+    return false;   // (all that is looked at where every tensor has memory of its own)
+  for (long long h = 0; h < heads; ++h)
+    for (long long g = 0; g < p_heads; ++g) {
+      const long long c = apart + h * a.o_head - g * p_head;
+      if (a.o_tok == p_tok) {
+        if (comes_near(c, a.o_tok, 1 - n, n - 1, d)) return true;
+      } else {
+        for (long long t = 0; t < n; ++t)
+          if (comes_near(c + t * a.o_tok, -p_tok, 0, n - 1, d)) return true;
+      }
+    }
+  return false;
+}
+
 // Fewest key tiles that are a CTA's worth.
 constexpr int kMinTilesFew = 2, kMinTiles = 2;
 // What it costs a CTA to begin another item, in key tiles.
@@ -1456,6 +1492,9 @@ int lrsa_paged_attend(const lrsa_params_t* params, const lrsa_paged_t* paged, co
     a.q = rows(q); a.k = rows(k); a.v = rows(v); a.o = rows(o);
     a.q_head = q->head_stride; a.q_tok = q->token_stride; a.k_head = k->head_stride; a.k_tok = k->token_stride;
     a.v_head = v->head_stride; a.v_tok = v->token_stride; a.o_head = o->head_stride; a.o_tok = o->token_stride;
+    if (rows_overlap(a, g.Hq, n_new, g.d) || rows_overlap(a, g.Hq, n_new, g.d, a.q, g.Hq, a.q_head, a.q_tok) ||
+        rows_overlap(a, g.Hq, n_new, g.d, a.k, g.Hkv, a.k_head, a.k_tok) || rows_overlap(a, g.Hq, n_new, g.d, a.v, g.Hkv, a.v_head, a.v_tok))
+      return LRSA_ERR_INVALID_ARG;
   }
   a.parent = parent; a.lse = lse;
   a.head = static_cast<WsHeader*>(workspace);

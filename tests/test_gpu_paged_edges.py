@@ -337,3 +337,33 @@ def test_calls_of_two_threads_with_windows_of_different_lengths():
     for t in threads:
         t.join()
     assert not failed, failed
+
+
+@pytest.mark.parametrize("new", [2, 20])
+def test_outputs_beside_the_inputs_in_one_buffer(new):
+    """Rows that take turns with those of q, k and v, and o in other orders."""
+    p = lrsa.Params(1, 8, 2, 900, 64, 64, 16, 4)
+    m = Model(p, 16, 2, dim=64, seed=7)
+    m.append([300, 40])
+    table, n, cu = m.device([new, new])
+    T = 2 * new
+    q, k, v = (m.rows(h, T, False).cuda() for h in (8, 2, 2))
+    want, _ = m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=new)
+    fused = torch.zeros(T, 20 + 4, 64, dtype=torch.bfloat16, device="cuda")
+    parts = [fused[:, a:b].transpose(0, 1) for a, b in ((0, 8), (8, 10), (10, 12), (12, 20))]
+    for x, y in zip(parts, (q, k, v)):
+        x.copy_(y)
+    kept = fused.clone()
+    o, _ = m.cache.attend(*parts[:3], table, n, cu, rope=m.rope, max_new=new, o=parts[3])
+    assert torch.equal(o, want) and o.data_ptr() == parts[3].data_ptr()
+    assert torch.equal(fused[:, :12], kept[:, :12]) and torch.equal(fused[:, 20:], kept[:, 20:])
+    by_head = torch.zeros(8, T + 3, 3 * 64, dtype=torch.bfloat16, device="cuda")
+    by_head[:, :T, 64:128] = q
+    o, _ = m.cache.attend(by_head[:, :T, 64:128], k, v, table, n, cu, rope=m.rope, max_new=new, o=by_head[:, :T, 128:])
+    assert torch.equal(o, want) and (by_head[:, T:] == 0).all() and (by_head[:, :, :64] == 0).all()
+    back = torch.zeros(2 * T, 8, 64, dtype=torch.bfloat16, device="cuda")
+    o, _ = m.cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=new, o=back[::2].transpose(0, 1))
+    assert torch.equal(o, want) and (back[1::2] == 0).all()
+    for bad in (q, by_head[:, :T, 64:128]):
+        with pytest.raises(lrsa.LrsaError):
+            m.cache.attend(bad, k, v, table, n, cu, rope=m.rope, max_new=new, o=bad)

@@ -107,3 +107,24 @@ def test_status_is_asked_of_every_workspace(calls, monkeypatch):
 
 def test_status_without_a_workspace():
     assert lrsa.lib().lrsa_paged_status(None, None) == lrsa.lib().lrsa_paged_status(0x7f0000000080, None) == INVALID
+
+
+def test_outputs_that_lie_over_one_another_or_over_the_inputs():
+    """By the library, which knows the strides of all of them: 8/2 heads, d = 128, 16 tokens."""
+    from tests.test_paged_abi import AT, attend, rows
+    far = dict(q=rows(AT), k=rows(AT + (1 << 20)), v=rows(AT + (2 << 20)), ws_bytes=1 << 30)
+    o = AT + (3 << 20)
+    own = [(128, 128), (0, 1024), (128, 0), (64, 1024), (128, 64), (128, 1016), (136, 136), (2040, 128), (1024, 1024), (256, 384), (-128, 128),
+           (128, -1016), (384, 256)]
+    for head, token in own:
+        assert attend(o=rows(o, head, token), **far) == INVALID, (head, token)
+    for at in (AT, AT + 16, AT + 2 * (15 * 1024 + 7 * 128), AT - 2 * (15 * 1024 + 8 * 128 - 8)):      # q itself, parts of it, its last row, its first
+        assert attend(o=rows(at), **far) == INVALID
+        assert attend(o=rows(at, 16 * 128, 128), **far) == INVALID       # head by head
+    for name in "kv":
+        for at in (far[name].data, far[name].data + 2 * (15 * 1024 + 128), far[name].data - 2 * (15 * 1024 + 7 * 128)):
+            assert attend(o=rows(at), **far) == INVALID
+    # beside them in one buffer, a few elements too near
+    fused = dict(q=rows(AT, 128, 2568), k=rows(AT + 2 * 1024, 128, 2568), v=rows(AT + 2 * 1280, 128, 2568), ws_bytes=1 << 30)
+    assert attend(o=rows(AT + 2 * 1528, 128, 2568), **fused) == attend(o=rows(AT + 2 * 1552, 128, 2568), **fused) == INVALID
+    assert attend(o=rows(AT + 2 * 1536, 128, 2560), **fused) == INVALID   # (the next pitch: only a later token's comes near)
