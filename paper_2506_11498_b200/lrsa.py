@@ -778,7 +778,8 @@ class PagedCache:
     The calls of a cache share its workspace, so they run one after the other, captured ones too; different caches share nothing."""
 
     MOST_NEW = 128   # new tokens of a sequence in an attend
-    _seen = None     # where the pages were when they were last looked at
+    _seen = None     # where the pages were when they were last looked at,
+    _held = None     # and aliases of them
 
     def __init__(self, params: Params, n_pages: int, page: int = 64, device="cuda"):
         self.params, self.page, self.n_pages = params, page, n_pages
@@ -846,6 +847,8 @@ class PagedCache:
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_seen", None)
+        if name in ("k_pages", "v_pages"):
+            object.__setattr__(self, "_held", None)   # (the caller may want the room of the old ones)
 
     def __getstate__(self):
         return {k: v for k, v in self.__dict__.items() if k not in ("_seen", "_held")}   # (addresses of this process)

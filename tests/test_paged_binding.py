@@ -1,5 +1,7 @@
 """The binding of the rotation and the paged cache on the CPU, with recorded calls: what the library is given after the caller has replaced
 something, and what is told and held meanwhile."""
+import gc
+
 import pytest
 import torch
 
@@ -128,3 +130,27 @@ def test_outputs_that_lie_over_one_another_or_over_the_inputs():
     fused = dict(q=rows(AT, 128, 2568), k=rows(AT + 2 * 1024, 128, 2568), v=rows(AT + 2 * 1280, 128, 2568), ws_bytes=1 << 30)
     assert attend(o=rows(AT + 2 * 1528, 128, 2568), **fused) == attend(o=rows(AT + 2 * 1552, 128, 2568), **fused) == INVALID
     assert attend(o=rows(AT + 2 * 1536, 128, 2560), **fused) == INVALID   # (the next pitch: only a later token's comes near)
+
+
+def holders(storage):
+    """Tensors anywhere in the process that hold a storage."""
+    return sum(type(x) is torch.Tensor and x.untyped_storage()._cdata == storage for x in gc.get_objects())
+
+
+@pytest.mark.parametrize("name", ["k_pages", "v_pages"])
+def test_pages_that_were_replaced_are_let_go(calls, name):
+    """A pool makes room for a larger one: nothing of the cache holds on to what was given up for it."""
+    cache = lrsa.PagedCache(P, 5, device="cpu")
+    cache.append(**good(cache)[0], stream=STREAM)
+    storage = getattr(cache, name).untyped_storage()._cdata
+    assert holders(storage) > 1
+    setattr(cache, name, None)
+    assert holders(storage) == 0
+
+
+def test_tables_of_a_rope_that_were_replaced_are_let_go(calls):
+    cache, rope = lrsa.PagedCache(P, 5, device="cpu"), lrsa.Rope(torch.zeros(64, 64), torch.zeros(64, 64))
+    every_call(cache, rope)[0]()
+    storage = rope.cos.untyped_storage()._cdata
+    rope.cos = None
+    assert holders(storage) == 0
