@@ -768,6 +768,13 @@ def _turned(where, name, x, y, shape, dev, stream):
     return x.data_ptr(), y.data_ptr(), y
 
 
+class _Space:
+    """A workspace, and those that it has outgrown (a captured call may hold their addresses)."""
+
+    def __init__(self, ws):
+        self.ws, self.old = ws, []
+
+
 class PagedCache:
     """Condensed KV cache of one layer for sequences of different lengths, in pages (lrsa_paged_* in the C header): k_pages and
     v_pages, bf16 [n_pages, Hkv, page, d], which may be replaced by others of that shape, type and device.  What the layers of a
@@ -775,13 +782,15 @@ class PagedCache:
     [sequences]) and where the new tokens of a sequence begin (cu_new, int32 [sequences + 1]).  Neither call changes them, so a step is
     attend (and append) for every layer, then n_tokens += the new tokens.  Counts and page numbers that cannot be used are told by status(),
     until it has been asked.
-    The calls of a cache share its workspace, so they run one after the other, captured ones too; different caches share nothing."""
+    The calls of a cache share its workspace, so they run one after the other, captured ones too; different caches share nothing, unless one is
+    made `beside` another: then that one's workspace, its status and this rule are those of both (the layers of a model, whose calls run
+    one after the other anyway; the attention of trees takes 40 MB at d = 128, a prompt of 32K tokens 34)."""
 
     MOST_NEW = 128   # new tokens of a sequence in an attend
     _seen = None     # where the pages were when they were last looked at,
     _held = None     # and aliases of them
 
-    def __init__(self, params: Params, n_pages: int, page: int = 64, device="cuda"):
+    def __init__(self, params: Params, n_pages: int, page: int = 64, device="cuda", beside: "PagedCache | None" = None):
         self.params, self.page, self.n_pages = params, page, n_pages
         width, cap = ctypes.c_int32(0), ctypes.c_int32(0)
         _check(lib().lrsa_paged_shape(params.ref(), page, 0, 0, 0, ctypes.byref(width), ctypes.byref(cap), None), "lrsa_paged_shape")
@@ -791,8 +800,25 @@ class PagedCache:
         self._shape = torch.Size((n_pages, params.n_kv_heads, page, params.head_dim))
         self.k_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
         self.v_pages = torch.zeros(self._shape, dtype=torch.bfloat16, device=device)
-        self._need, self._old = {}, []
-        self.ws = _cleared_workspace(self.workspace_bytes(1, 1, 1), device)
+        self._need = {}
+        if beside is None:
+            self._space = _Space(_cleared_workspace(self.workspace_bytes(1, 1, 1), device))
+        elif not isinstance(beside, PagedCache) or beside.ws.device != self.k_pages.device:
+            raise LrsaError(1, f"PagedCache: beside a cache on {self.k_pages.device}, got {getattr(getattr(beside, 'ws', None), 'device', beside)}")
+        else:
+            self._space = beside._space
+
+    @property
+    def ws(self):
+        return self._space.ws
+
+    @ws.setter
+    def ws(self, ws):
+        self._space.ws = ws
+
+    @property
+    def _old(self):
+        return self._space.old
 
     def workspace_bytes(self, n_seqs: int, n_new: int, max_new: int) -> int:
         """What an attend of n_new tokens of n_seqs sequences, at most max_new each, takes; max_new = 0: an append."""

@@ -367,3 +367,40 @@ def test_outputs_beside_the_inputs_in_one_buffer(new):
     for bad in (q, by_head[:, :T, 64:128]):
         with pytest.raises(lrsa.LrsaError):
             m.cache.attend(bad, k, v, table, n, cu, rope=m.rope, max_new=new, o=bad)
+
+
+def test_layers_that_share_a_workspace():
+    """The layers of a model, one step after the other, captured and not: each has what it has alone."""
+    ps = [lrsa.Params(1, 8, 2, 900, 64, 64, 16, 4), lrsa.Params(1, 14, 2, 900, 128, 64, 16, 4), lrsa.Params(1, 8, 2, 900, 64, 64, 16, 4)]
+    ms = [Model(p, 16, 2, dim=64, seed=8) for p in ps]
+    shared = [lrsa.PagedCache(p, m.cache.n_pages, page=16, beside=None) for p, m in zip(ps[:1], ms)]
+    shared += [lrsa.PagedCache(p, m.cache.n_pages, page=16, beside=shared[0]) for p, m in zip(ps[1:], ms[1:])]
+    steps = []
+    for m, cache in zip(ms, shared):
+        m.append([400, 77])
+        for s in range(2):
+            m.reach(s, m.n[s] + 40)
+        cache.k_pages, cache.v_pages = m.cache.k_pages.clone(), m.cache.v_pages.clone()
+        p = m.p
+        q, k, v = (m.rows(h, 40, False).cuda() for h in (p.n_q_heads, 2, 2))
+        steps.append((q, k, v, i32(m.table.tolist()), i32(m.n), i32([0, 30, 40])))
+    def run(caches):
+        out = []
+        for m, cache, (q, k, v, table, n, cu) in zip(ms, caches, steps):
+            out.append(cache.attend(q, k, v, table, n, cu, rope=m.rope, max_new=30))
+            cache.append(k, v, table, n, cu, rope=m.rope)
+        return out
+    want = run([m.cache for m in ms])
+    got = run(shared)
+    assert len({c.ws.data_ptr() for c in shared}) == 1
+    for (o, lse), (x, y), m, cache in zip(want, got, ms, shared):
+        assert torch.equal(o, x) and torch.equal(lse, y) and torch.equal(m.cache.k_pages.view(torch.int16), cache.k_pages.view(torch.int16))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again = run(shared)
+    for _ in range(3):
+        graph.replay()
+        assert all(torch.equal(x, z) and torch.equal(y, w) for (x, y), (z, w) in zip(got, again))
+    steps[1][4].fill_(-1)
+    graph.replay()
+    assert [c.status() for c in shared] == [1, 0, 0]      # told once, by whichever is asked

@@ -1,11 +1,13 @@
 """The binding of the rotation and the paged cache on the CPU, with recorded calls: what the library is given after the caller has replaced
 something, and what is told and held meanwhile."""
 import gc
+import pickle
 
 import pytest
 import torch
 
 from paper_2506_11498_b200 import lrsa
+from tests import paged_reference as ref
 from tests.test_paged_abi import INVALID, P, STREAM, _built, bf, calls, good, i32  # noqa: F401  (fixtures)
 
 ROPE_AT = {"paged_append": 19, "paged_attend": 22, "rotate": 5}     # where the five values of a rope begin
@@ -154,3 +156,25 @@ def test_tables_of_a_rope_that_were_replaced_are_let_go(calls):
     storage = rope.cos.untyped_storage()._cdata
     rope.cos = None
     assert holders(storage) == 0
+
+
+def test_the_layers_of_a_model_share_a_workspace(calls):
+    """Their calls run one after the other: a workspace each would hold as many times what one call takes."""
+    first = lrsa.PagedCache(P, 5, device="cpu")
+    layers = [first] + [lrsa.PagedCache(p, 5, device="cpu", beside=first) for p in (P, lrsa.Params(1, 16, 4, 900, 64, 100, 30, 3))]
+    assert len({x.ws.data_ptr() for x in layers}) == 1 and len({x.k_pages.data_ptr() for x in layers}) == 3
+    for i, cache in enumerate(layers[:2]):
+        cache.append(**good(cache, 20000 * (i + 1))[0], stream=STREAM)
+        assert all(x.ws is cache.ws and x._old is cache._old for x in layers)
+        assert calls[-1][1][25] == cache.ws.data_ptr()
+    layers[0].attend(**good(layers[0])[1], max_new=6, stream=STREAM)
+    assert calls[-1][1][31] == layers[2].ws.data_ptr() and calls[-1][1][32] == layers[2].ws.numel()
+    alone = lrsa.PagedCache(P, 5, device="cpu")
+    assert alone.ws is not first.ws
+    a, b = pickle.loads(pickle.dumps(layers[:2]))
+    assert a.ws is b.ws and a.ws.data_ptr() != first.ws.data_ptr()
+    for other in (lrsa.PagedCache(P, 5, device="cpu"), None):
+        if other is not None:
+            other.ws = other.ws.to("meta")
+        with pytest.raises(lrsa.LrsaError):
+            lrsa.PagedCache(P, 5, device="cpu", beside=other or object())
