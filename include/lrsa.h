@@ -341,7 +341,8 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  * are not in the cache.  parent (optional, int32 [n_new]): new token i continues new token parent[i] < i of its sequence, or (-1) the
  * cache; NULL: token i continues token i - 1.  A token sees what the cache shows its next token, the new tokens that it continues, and itself;
  * its position is n_tokens + the number of those that it continues.  q and k are rotated on the way (rope NULL: they are rotated already).
- * A token deeper than the end of the chunk of the first one sees the cache as the first one does.  What
+ * A token deeper than the end of the chunk of the first one sees the cache as the first one does (a window that the mask would show it condensed
+ * is whole): tokens at positions below S + (max((n_tokens - S) / lag - 1, 0) + 2) * lag have what single tokens would have.  What
  * a token does not see has no influence on it, infinities and NaN included.  Rotated queries and new keys are multiplied as sums of two bf16, probabilities
  * are rounded to bf16, sums and softmax are fp32.  (With a rope, an infinite channel of a key that is seen may give NaN where one product would give
  * a score of -infinity.)  The rows of o overlap neither one another nor those of q, k and v.

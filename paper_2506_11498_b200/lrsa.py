@@ -850,6 +850,13 @@ class PagedCache:
         first = sinks + 2 * ring
         return cols + list(range(first, first + max(rest // p.lag - 1, 0) * kept))
 
+    def room(self, n_tokens):
+        """How many tokens from n_tokens on (int32, on the device or the host) see in one attend what they would see one by one.  From there on
+        a window more is condensed, and a deeper draft has seen it whole: a server that accepts at most so many drafts, which it can tell on the
+        device, gets what single tokens give."""
+        p = self.params
+        return p.n_sink + (((n_tokens - p.n_sink) // p.lag - 1).clamp(min=0) + 2) * p.lag - n_tokens
+
     def _pages(self, where, name, first, table, n_tokens, cu_new):
         """(device, what csrc/pycall.c takes of the cache), when everything is what the kernels read and write.  The pages are looked at
         when they have been replaced, or lie elsewhere than they did."""

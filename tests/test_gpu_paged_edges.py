@@ -369,6 +369,46 @@ def test_outputs_beside_the_inputs_in_one_buffer(new):
             m.cache.attend(bad, k, v, table, n, cu, rope=m.rope, max_new=new, o=bad)
 
 
+def test_drafts_beyond_the_end_of_a_chunk_are_cut_on_the_device():
+    """A captured step of drafts, of which as many are accepted as there is room for: tokens and pages are those of single steps."""
+    p = lrsa.Params(1, 4, 2, 600, 64, 32, 8, 4)
+    tokens, new = [4 + 2 * 32 - 3, 40], 7
+    a, b, table = twins(p, 16, tokens, [500, 500], dim=64)
+    q, k, v = (a.rows(h, 2 * new, False).cuda() for h in (4, 2, 2))
+    n, nb, cu, slots = i32(tokens), i32(tokens), i32([0, new, 2 * new]), torch.arange(2 * new, dtype=torch.int32, device="cuda")
+    a.cache.attend(q, k, v, table, n, cu, rope=a.rope, max_new=new)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = a.cache.attend(q, k, v, table, n, cu, rope=a.rope, max_new=new)
+        taken = torch.minimum(cu.diff(), a.cache.room(n))
+        cu_kept = torch.cat([taken.new_zeros(1), taken.cumsum(0, dtype=torch.int32)])
+        s = (torch.searchsorted(cu_kept, slots, right=True) - 1).clamp(max=1)
+        a.cache.append(k, v, table, n, cu_kept, rows=(cu[s] + slots - cu_kept[s]).clamp(max=2 * new - 1), rope=a.rope)
+        n += taken
+    capped = 0
+    for i in range(14):
+        for x, h in ((q, 4), (k, 2), (v, 2)):
+            x.copy_(a.rows(h, 2 * new, False))
+        graph.replay()
+        most = taken.tolist()
+        capped += sum(x < new for x in most)
+        for j in range(max(most)):
+            rows = [s * new + j for s in range(2) if j < most[s]]
+            one = i32([0, 1 if j < most[0] else 0, len(rows)])
+            args = [x[:, rows].contiguous() for x in (q, k, v)]
+            want, want_lse = b.cache.attend(*args, table, nb, one, rope=b.rope, max_new=1)
+            # A draft sees the drafts in front of it with keys of two bf16, a single token has them from the cache, rounded to one: half a step of
+            # every channel, so at most 2^-8 |q| |k| / sqrt(d) of a score.  lse moves by no more than a score does, a probability by a factor of
+            # exp(2 of that) at most.  And both sides round the probabilities and the sum, of values below 5.
+            ds = ref.HALF_STEP * float(q.float().norm(dim=-1).max() * k.float().norm(dim=-1).max()) / 8
+            assert (o[:, rows].float() - want.float()).abs().max() <= 4 * 5 * ref.HALF_STEP + 5 * (np.exp(2 * ds) - 1)
+            assert (lse[:, rows] - want_lse).abs().max() <= ds + 1e-4, (i, j)
+            b.cache.append(*args[1:], table, nb, one, rope=b.rope)
+            nb += one.diff()
+        assert torch.equal(n, nb) and a.cache.status() == 0 and b.cache.status() == 0
+    assert capped > 3 and same_pages(a, b)
+
+
 def test_layers_that_share_a_workspace():
     """The layers of a model, one step after the other, captured and not: each has what it has alone."""
     ps = [lrsa.Params(1, 8, 2, 900, 64, 64, 16, 4), lrsa.Params(1, 14, 2, 900, 128, 64, 16, 4), lrsa.Params(1, 8, 2, 900, 64, 64, 16, 4)]

@@ -178,3 +178,13 @@ def test_the_layers_of_a_model_share_a_workspace(calls):
             other.ws = other.ws.to("meta")
         with pytest.raises(lrsa.LrsaError):
             lrsa.PagedCache(P, 5, device="cpu", beside=other or object())
+
+
+@pytest.mark.parametrize("p", [P, lrsa.Params(1, 4, 2, 300, 64, 7, 3, 0), lrsa.Params(1, 4, 2, 300, 64, 16, 16, 40)])
+def test_room_is_where_a_window_more_is_condensed(p):
+    cache = lrsa.PagedCache(p, 5, device="cpu")
+    n = torch.arange(250, dtype=torch.int32)
+    room = cache.room(n)
+    assert room.dtype is torch.int32
+    for a, r in zip(n.tolist(), room.tolist()):
+        assert r >= 1 and ref.cut(p, a + r - 1) == ref.cut(p, a) and ref.cut(p, a + r) == ref.cut(p, a) + 1
