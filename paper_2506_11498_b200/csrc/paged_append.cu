@@ -7,8 +7,8 @@
 //
 // A cluster of CTAs cuts one window at a time: channel ranges of window w + 1, exchanged through shared memory; spreads of the rows
 // of window w into the first CTA's shared memory; that one scores and selects; all of them move kept rows.  Two forms:
-//   one launch (few new tokens a sequence: every step of a server): a cluster per (sequence, KV head) cuts what there is to cut, mostly
-//     nothing, then writes the new rows.  The recent pages that it writes are those of the window it has just cut.  A token of 16 sequences
+//   one launch (every step of a server: a token or some drafts a sequence, as far as the host can tell, one_launch below): a cluster per (sequence,
+//     KV head) cuts what there is to cut, mostly nothing, one window after the other, then writes the new rows.  A token of 16 sequences
 //     (4 heads, d = 128) 2.6 us in a graph; bound by the launch and four round trips (counts, page number, row, store).
 //   several launches (prompts): the new keys rotated into the workspace; a cluster per window, and the rows of sequences that begin; the rows of
 //     those that go on.  Bound by reading the windows twice (32K: 9 and 8 of the 33 us of a cut, 7.4 TB/s, mostly L2), and by the chain between:
@@ -637,8 +637,12 @@ __global__ void __launch_bounds__(kAppThreads) paged_rows_kernel(const __grid_co
   put_rows<D, false>(a, q, blockIdx.x % blocks, blocks);
 }
 
-// One launch while a sequence gets a few tokens on average: a cluster then writes the few rows of a head by itself and cuts a window at most.
-bool one_launch(long long n_seqs, long long n_new) { return n_new <= 64 * n_seqs; }
+// One launch where the sequences get a few tokens each.  The host knows their sum only, and a sequence that gets most of it has its windows cut one
+// after the other by one cluster a head: so neither more than drafts on average, nor so many that one sequence could have more than eight cuts.
+// us in a graph, one launch | several, 4 heads, d = 128: drafts, 8 for each of 64 sequences, windows of 128 16.8 | 21.4, of 512 28 | 36; of 256, of 512
+// 55 | 97; 60 for each of 8, of 128 18.5 | 18.7.  63 tokens beside a prompt of 500, of 128 63 | 20, of 1024 48 | 53; of 1000 95 | 18 and 23 | 22; of
+// 4000 406 | 23 and 127 | 51.  (d = 64, 8 heads: 60 for each of 8 sequences 12.5 | 18; 8 for each of 256, of 128 41 | 67: the price of the rule.)
+bool one_launch(const Geom& g, long long n_seqs, long long n_new) { return n_new <= n_seqs || (n_new <= 16 * n_seqs && n_new <= 8LL * g.L); }
 
 bool rows_ok(const lrsa_rows_t* r) {
   return r && r->data && !(reinterpret_cast<uintptr_t>(r->data) & 15u) && r->head_stride % 8 == 0 && r->token_stride % 8 == 0;
@@ -647,7 +651,7 @@ bool rows_ok(const lrsa_rows_t* r) {
 }  // namespace
 
 size_t append_ws_bytes(const Geom& g, long long n_seqs, long long n_new) {
-  return sizeof(WsHeader) + (one_launch(n_seqs, n_new) ? 0 : (size_t)n_new * g.Hkv * g.d * sizeof(__nv_bfloat16));
+  return sizeof(WsHeader) + (one_launch(g, n_seqs, n_new) ? 0 : (size_t)n_new * g.Hkv * g.d * sizeof(__nv_bfloat16));
 }
 
 }  // namespace lrsa
@@ -688,7 +692,7 @@ extern "C" int lrsa_paged_append(const lrsa_params_t* params, const lrsa_paged_t
   a.limit = a.rope.half > 0 && a.rope.n_pos < g.N ? a.rope.n_pos : g.N;
   a.ddof = g.ddof;
   const int n_seqs = paged->n_seqs;
-  const bool one = one_launch(n_seqs, n_new);
+  const bool one = one_launch(g, n_seqs, n_new);
   if (!one && a.rope.half > 0) {
     a.turned = reinterpret_cast<__nv_bfloat16*>(static_cast<unsigned char*>(workspace) + sizeof(WsHeader));
     const int tok = 256 / (g.d / 16);

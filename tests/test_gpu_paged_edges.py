@@ -97,12 +97,12 @@ def that_count(cu, room, most, apart=True):
 
 
 @pytest.mark.parametrize("what", RANGES)
-@pytest.mark.parametrize("times, rope", [(1, 64), (10, 64), (10, 0)], ids=["one_launch", "several_launches", "several_no_rope"])
+@pytest.mark.parametrize("times, rope", [(1, 64), (12, 64), (12, 0)], ids=["one_launch", "several_launches", "several_no_rope"])
 def test_appends_whose_ranges_would_overlap(what, times, rope):
     """A sequence's keys are its own, rotated for its own positions.  Of prompts the later ones are left out; few tokens are each sequence's."""
     p = lrsa.Params(1, 8, 2, 1500, 64, 64, 16, 4)
     tokens = [0, 150, 30, 3]
-    a, b, table = twins(p, 16, tokens, [n + 460 for n in tokens], dim=rope)
+    a, b, table = twins(p, 16, tokens, [n + 540 for n in tokens], dim=rope)
     cu = [x * times for x in RANGES[what]]
     T = 45 * times
     k, v = (a.rows(2, T, False).cuda() for _ in "kv")
@@ -152,10 +152,11 @@ def test_many_sequences_behind_a_boundary_that_goes_back(n_seqs):
             cu = [new * s for s in range(n_seqs + 1)]
             cu[at] = new * (at - 3)
             a.cache.append(k, v, table, i32(a.n), i32(cu), rope=a.rope)
-            assert a.cache.status() == 1
+            few = lrsa.lrsa_last_launch_count() == 1
+            assert a.cache.status() == 1 and few == (new == 3 and n_seqs == 40)
             # the one in front has its end before its beginning, the one behind begins too early: of prompts both are left out
             parts = [[new * min(s, at - 1) for s in range(n_seqs + 1)], [new * max(s, at + 1) for s in range(n_seqs + 1)]]
-            if new == 3:
+            if few:
                 parts.append([cu[at]] * (at + 1) + [cu[at + 1]] * (n_seqs - at))
             for part in parts:
                 b.cache.append(k, v, table, i32(b.n), i32(part), rope=b.rope)
@@ -444,3 +445,18 @@ def test_layers_that_share_a_workspace():
     steps[1][4].fill_(-1)
     graph.replay()
     assert [c.status() for c in shared] == [1, 0, 0]      # told once, by whichever is asked
+
+
+@pytest.mark.parametrize("new, launches", [([1] * 16, 1), ([5] * 15 + [90], 1), ([300] + [1] * 15, 3), ([1] * 15 + [600], 3), ([0, 2] * 7 + [0, 250], 3)])
+def test_prompts_beside_the_tokens_of_other_sequences(new, launches):
+    """Where one sequence may have many windows to cut, they are cut side by side."""
+    m = Model(lrsa.Params(1, 8, 2, 2500, 64, 64, 16, 4), 16, 16, dim=64, seed=9)
+    m.append([int(x) for x in m.rng.integers(0, 500, 16)])
+    m.append(new)
+    for s in range(16):
+        m.reach(s, m.n[s] + max(new))
+    table, n, cu = m.device(new)
+    k, v = (m.rows(2, sum(new), False).cuda() for _ in "kv")
+    m.check_pages()
+    m.cache.append(k, v, table, n, cu, rope=m.rope)
+    assert lrsa.lrsa_last_launch_count() == launches and m.cache.status() == 0
