@@ -938,8 +938,10 @@ class PagedCache:
         """Attention of every sequence's next token, or of a tree of drafted ones, over the cache: q bf16 [Hq, tokens, d], k, v bf16
         [Hkv, tokens, d] with any strides, not in the cache, rotated on the way unless rope is None.  parent (int32 [tokens]): which
         token of its sequence each one continues, -1: the cache; none: the one in front of it.  max_new: the most tokens of a
-        sequence (at most 128; fewer than 17 rows, heads of a group times max_new, take the kernel for few).  Returns (o [Hq, tokens, d],
-        lse fp32 [Hq, tokens]); o lies in memory as q does, token by token or head by head."""
+        sequence (at most 128); fewer than 17 rows, heads of a group times max_new, take the kernel for few.  Without it any sequence may
+        have all of them: a step of single tokens says max_new=1, or it is taken for a tree (sixteen sequences with seven heads to a group: 112
+        rows, three launches for two and 40 MB of workspace for 5).  Returns (o [Hq, tokens, d], lse fp32 [Hq, tokens]); o lies in memory as q
+        does, token by token or head by head.  (Rows of a sequence that status() tells of may hold anything in an o that the call made.)"""
         p, where, call = self.params, "lrsa_paged_attend", _call or _calls()
         dev, pages = self._pages(where, "q", q, table, n_tokens, cu_new)
         n = q.shape[1] if q.dim() == 3 else 0
