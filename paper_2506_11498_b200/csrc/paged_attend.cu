@@ -1357,6 +1357,10 @@ bool rows_overlap(const AttendArgs& a, long long heads, long long n, long long d
   auto high = [n](long long h, long long head, long long tok) { return (head > 0 ? (h - 1) * head : 0) + (tok > 0 ? (n - 1) * tok : 0); };
   if (apart + high(heads, a.o_head, a.o_tok) + d <= low(p_heads, p_head, p_tok) || apart + low(heads, a.o_head, a.o_tok) >= high(p_heads, p_head, p_tok) + d)
     return false;   // (all that is looked at where every tensor has memory of its own)
+  if (a.o_tok == p_tok && p_tok > 0 && a.o_head >= 0 && p_head >= 0) {   // side by side within the pitch of a token
+    const long long column = (apart % p_tok + p_tok) % p_tok;
+    if (column >= (p_heads - 1) * p_head + d && column + (heads - 1) * a.o_head + d <= p_tok) return false;
+  }
   for (long long h = 0; h < heads; ++h)
     for (long long g = 0; g < p_heads; ++g) {
       const long long c = apart + h * a.o_head - g * p_head;

@@ -886,6 +886,12 @@ class PagedCache:
     def __getstate__(self):
         return {k: v for k, v in self.__dict__.items() if k not in ("_seen", "_held")}   # (addresses of this process)
 
+    def __setstate__(self, state):
+        state = dict(state)
+        if "_space" not in state:      # saved before caches could share one
+            state["_space"] = _Space(_cleared_workspace(state["ws"].numel(), state["ws"].device))
+        self.__dict__.update((k, v) for k, v in state.items() if k not in ("ws", "_old"))
+
     def _look(self, where, dev):
         """Raises LRSA_ERR_INVALID_ARG unless the pages are what the kernels read and write."""
         for name, t in (("k_pages", self.k_pages), ("v_pages", self.v_pages)):

@@ -188,3 +188,14 @@ def test_room_is_where_a_window_more_is_condensed(p):
     assert room.dtype is torch.int32
     for a, r in zip(n.tolist(), room.tolist()):
         assert r >= 1 and ref.cut(p, a + r - 1) == ref.cut(p, a) and ref.cut(p, a + r) == ref.cut(p, a) + 1
+
+
+def test_a_cache_that_was_saved_with_a_workspace_of_its_own_works(calls):
+    cache = lrsa.PagedCache(P, 5, device="cpu")
+    state = cache.__getstate__()
+    ws = torch.full_like(state.pop("_space").ws, 255)
+    again = lrsa.PagedCache.__new__(lrsa.PagedCache)
+    again.__setstate__({**state, "ws": ws, "_old": []})
+    assert again.ws.numel() == ws.numel() and (again.ws[:256] == 0).all() and again._old == []
+    again.append(**good(again)[0], stream=STREAM)
+    assert calls[-1][1][25] == again.ws.data_ptr() and calls[-1][1][5] == again.k_pages.data_ptr()
