@@ -343,8 +343,8 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  * its position is n_tokens + the number of those that it continues.  q and k are rotated on the way (rope NULL: they are rotated already).
  * A token deeper than the end of the chunk of the first one sees the cache as the first one does (a window that the mask would show it condensed
  * is whole): tokens at positions below S + (max((n_tokens - S) / lag - 1, 0) + 2) * lag have what single tokens would have.  What
- * a token does not see has no influence on it, infinities and NaN included.  Rotated queries and new keys are multiplied as sums of two bf16, probabilities
- * are rounded to bf16, sums and softmax are fp32.  (With a rope, an infinite channel of a key that is seen may give NaN where one product would give
+ * a token does not see has no influence on it, infinities and NaN included.  Rotated queries and new keys are multiplied as sums of two bf16, and so are
+ * probabilities for up to 16 rows (heads of a group times max_new); for more they are rounded to bf16.  Sums and softmax are fp32.  (With a rope, an infinite channel of a key that is seen may give NaN where one product would give
  * a score of -infinity.)  The rows of o overlap neither one another nor those of q, k and v.
  *   q, o : bf16 [Hq, n_new, d];  k, v : bf16 [Hkv, n_new, d];  lse (optional): fp32 [Hq, n_new]
  *

@@ -11,7 +11,10 @@
 // by atomics: results repeat bit by bit.
 // Precision.  A rotated query enters the products as the sum of two bf16 (2^-17 of a channel is lost; rounded to one, the error of o grows from
 // 2.0e-3 to 2.9e-3, root mean square, and that of lse to 1e-5 of it), and so does a rotated new key; the keys of the cache are bf16.  Scores, softmax and
-// sums are fp32; the probabilities are rounded to bf16 in front of V, as the product asks for (half a step: 2^-8 of a term).
+// sums are fp32.  The probabilities enter the product with V as sums of two bf16 in the kernel for few, where the tensor pipe has room (16 single tokens
+// of 28/4 heads at up to 32K 44.4 and 44.5 us, two tokens each 50.7 and 52.6; the error of o is the rounding of o, 1.7e-3).  In the kernel for many they are
+// rounded to bf16 as the forward's are (half a step: 2^-8 of a term; error of o 2.3e-3): in two parts the trees of 32 over 16 sequences took 107 us instead
+// of 88, a tree of 48 at 32K 43 instead of 37, the trees at 120K 530 instead of 410.
 #include "attn_common_sm100.h"
 #include "infer_sm100.h"
 #include "paged_sm100.h"
@@ -532,14 +535,24 @@ __global__ void __launch_bounds__(256, NH == 1 ? 2 : 1) paged_few_kernel(const _
             p[e] = ex2(s[u][e] - ref[e & 1]);
             l[h][e & 1] += p[e];
           }
-          const uint32_t b0 = transpose_8x8(pack_bf16(p[0], p[1])), b1 = transpose_8x8(pack_bf16(p[2], p[3]));
+          // P as the sum of two bf16, cut off and what that leaves (not nothing where P is something: an infinite value stays one)
+          uint32_t hi[2], lo[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float x = p[2 * i], y = p[2 * i + 1];
+            hi[i] = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+            lo[i] = pack_bf16(fmaxf(x - bf16_lo(hi[i]), x * 0x1p-40f), fmaxf(y - bf16_hi(hi[i]), y * 0x1p-40f));
+            hi[i] = transpose_8x8(hi[i]);
+            lo[i] = transpose_8x8(lo[i]);
+          }
 #pragma unroll
           for (int j = 0; j < VC; ++j)
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
               const uint32_t w0 = word_of(vq[u][0][j], f), w1 = word_of(vq[u][1][j], f), w2 = word_of(vq[u][2][j], f), w3 = word_of(vq[u][3][j], f);
-              mma_16816(o[h][4 * j + f], __byte_perm(w0, w1, 0x5410), __byte_perm(w0, w1, 0x7632), __byte_perm(w2, w3, 0x5410),
-                        __byte_perm(w2, w3, 0x7632), b0, b1);
+              const uint32_t v0 = __byte_perm(w0, w1, 0x5410), v1 = __byte_perm(w0, w1, 0x7632), v2 = __byte_perm(w2, w3, 0x5410), v3 = __byte_perm(w2, w3, 0x7632);
+              mma_16816(o[h][4 * j + f], v0, v1, v2, v3, hi[0], hi[1]);
+              mma_16816(o[h][4 * j + f], v0, v1, v2, v3, lo[0], lo[1]);
             }
         }
       }

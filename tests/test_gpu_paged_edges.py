@@ -1,11 +1,13 @@
 """The paged cache on the GPU where weights underflow, numbers on the device cannot be used, and steps are captured."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2506_11498_b200 import lrsa
 from tests import paged_reference as ref
-from tests.test_gpu_paged import Model, i32
+from tests.test_gpu_paged import Model, f64, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -460,3 +462,37 @@ def test_prompts_beside_the_tokens_of_other_sequences(new, launches):
     m.check_pages()
     m.cache.append(k, v, table, n, cu, rope=m.rope)
     assert lrsa.lrsa_last_launch_count() == launches and m.cache.status() == 0
+
+
+@pytest.mark.parametrize("heads, d, new", [((8, 8), 64, 1), ((14, 2), 128, 1), ((8, 1), 64, 2), ((8, 2), 128, 4)], ids=["mha", "gqa7", "rows16", "drafts"])
+@pytest.mark.parametrize("rope", [0, 64])
+def test_up_to_sixteen_rows_lose_nothing_but_the_rounding_of_o(heads, d, new, rope):
+    """Probabilities enter as sums of two bf16: what is left out of them, half a step of the second part (2^-7 of the first, so 2^-7 2^-8 of a
+    term), the least that the second part is (2^-40), the scores' and the sums' rounding (the bounds that ref.attend gives for lse, which moves a
+    probability by a factor), and one rounding of o."""
+    p = lrsa.Params(1, *heads, 3000, d, 256, 64, 4)
+    m = Model(p, 32, 3, dim=rope, seed=10)
+    m.append([2500, 40, 700])
+    sizes = [new] * 3
+    q, k, v = (m.rows(h, 3 * new, False) for h in (heads[0], heads[1], heads[1]))
+    table, n, cu = m.device(sizes)
+    o, _ = m.cache.attend(q.cuda(), k.cuda(), v.cuda(), table, n, cu, rope=m.rope, max_new=new)
+    for s in range(3):
+        part = slice(s * new, (s + 1) * new)
+        n_s, w = m.n[s], ref.cut(p, m.n[s])
+        sees = ref.ancestors(None, new)
+        pos = n_s + np.arange(new)
+        qs, ks, vs = m.turned(f64(q)[:, part], pos, False), m.turned(f64(k)[:, part], pos, False), f64(v)[:, part]
+        idx = m.selected(s)
+        keys, vals = [], []
+        for h in range(heads[1]):
+            seen = np.concatenate([np.arange(min(n_s, p.n_sink)), idx[h].ravel(), np.arange(min(n_s, p.n_sink + w * p.lag), n_s)]).astype(int)
+            keys.append(np.concatenate([m.K[s][h, seen], ks[h]]))
+            vals.append(np.concatenate([m.V[s][h, seen], vs[h]]))
+        sees = np.concatenate([np.ones((new, keys[0].shape[0] - new), bool), sees], 1)
+        args = qs, np.stack(keys), sees, 1 / math.sqrt(d)
+        want, _, _, lse_tol = ref.attend(args[0], args[1], np.stack(vals), *args[2:], rotated=rope > 0)
+        terms = ref.attend(args[0], args[1], np.abs(np.stack(vals)), *args[2:], rotated=rope > 0)[0]
+        tol = (2.0 ** -15 + 2.0 ** -39 + 2 * lse_tol[..., None] + 2.0 ** -18) * terms
+        err = np.abs(f64(o)[:, part] - want)
+        assert (err <= tol + ref.HALF_STEP * (np.abs(want) + tol)).all(), (s, float((err / (tol + ref.HALF_STEP * np.abs(want))).max()))
