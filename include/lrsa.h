@@ -297,7 +297,8 @@ int lrsa_store_rows(const lrsa_params_t* params, const lrsa_store_t* store, int3
  * head_dim.  Arithmetic in fp32, rounded to bf16 once.
  *
  * lrsa_rotate: Q and K (either may be NULL) rotated; with `inverse` by the opposite angles, which is the gradient of the rotation:
- * dQ, dK of lrsa_attn_bwd in, those of the unrotated Q, K out.  Out of place, or in place (the same pointer).
+ * dQ, dK of lrsa_attn_bwd in, those of the unrotated Q, K out.  Out of place, or in place (the same pointer); an output that lies over anything
+ * else of the call is refused.
  *   Q, Q_out : bf16 [B, Hq, N, d];  K, K_out : bf16 [B, Hkv, N, d]
  *   positions: optional int32 [N] on the device.  NULL: the position of a token is its index in its sequence (packed batches too),
  *              and n_pos covers the longest one.  A row whose given position is not in [0, n_pos) becomes NaN in the rotated channels.
@@ -344,14 +345,14 @@ int lrsa_rotate(const lrsa_params_t* params, const void* Q, const void* K, void*
  * A token deeper than the end of the chunk of the first one sees the cache as the first one does (a window that the mask would show it condensed
  * is whole): tokens at positions below S + (max((n_tokens - S) / lag - 1, 0) + 2) * lag have what single tokens would have.  What
  * a token does not see has no influence on it, infinities and NaN included.  Rotated queries and new keys are multiplied as sums of two bf16, and so are
- * probabilities for up to 16 rows (heads of a group times max_new); for more they are rounded to bf16.  Sums and softmax are fp32.  (With a rope, an infinite channel of a key that is seen may give NaN where one product would give
- * a score of -infinity.)  The rows of o overlap neither one another nor those of q, k and v.
+ * probabilities for up to 16 rows (heads of a group times max_new); for more they are rounded to bf16.  Sums and softmax are fp32.  (With a rope, an
+ * infinite channel of a key that is seen may give NaN where one product would give a score of -infinity.)  The rows of o overlap neither one another nor those of q, k and v.
  *   q, o : bf16 [Hq, n_new, d];  k, v : bf16 [Hkv, n_new, d];  lse (optional): fp32 [Hq, n_new]
  *
  * Counts, page numbers, rows and parents that cannot be used (out of range, more new tokens than max_new, beyond seq_len or beyond the
  * rope's positions, which have to cover n_tokens + the new tokens of a sequence) are found on the device: lrsa_workspace_status
- * returns LRSA_ERR_INVALID_ARG for the last call on a workspace, lrsa_paged_status when any had such numbers since it was last asked.  A sequence with bad counts is left out (its rows of o stay as they were), whatever is read or written stays
- * inside the tensors.  Where cu_new goes back, a sequence that begins in front of an earlier boundary may be left out too: no row becomes
+ * returns LRSA_ERR_INVALID_ARG for the last call on a workspace, lrsa_paged_status when any had such numbers since it was last asked.  A sequence
+ * with bad counts is left out (its rows of o stay as they were), whatever is read or written stays inside the tensors.  Where cu_new goes back, a sequence that begins in front of an earlier boundary may be left out too: no row becomes
  * another sequence's.
  * lrsa_paged_shape: the workspace of an attend of n_new tokens of n_seqs sequences, at most max_new each (it grows with n_new and n_seqs; any
  * output may be NULL); with max_new = 0 that of an append.

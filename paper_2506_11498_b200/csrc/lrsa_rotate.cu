@@ -136,6 +136,16 @@ extern "C" int lrsa_rotate(const lrsa_params_t* params, const void* Q, const voi
   const uintptr_t all = reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(Q_out) |
                         reinterpret_cast<uintptr_t>(K_out);
   if ((all & 15u) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return LRSA_ERR_INVALID_ARG;
+  // an output is its own input, or lies over nothing else of the call
+  const size_t row = (size_t)g.N * g.d * sizeof(__nv_bfloat16), size[2] = {(size_t)g.B * g.Hq * row, (size_t)g.B * g.Hkv * row};
+  const void *in[2] = {Q, K}, *out[2] = {Q_out, K_out};
+  auto over = [&](const void* p, int i, const void* r, int j) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(r);
+    return p && r && a < b + size[j] && b < a + size[i];
+  };
+  for (int i = 0; i < 2; ++i)
+    if ((out[i] != in[i] && over(out[i], i, in[i], i)) || over(out[i], i, in[1 - i], 1 - i)) return LRSA_ERR_INVALID_ARG;
+  if (over(Q_out, 0, K_out, 1)) return LRSA_ERR_INVALID_ARG;
   const int n_seqs = positions || g.n_seqs == 0 ? 1 : g.n_seqs;
   if (!positions) {
     int longest = g.N;

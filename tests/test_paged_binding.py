@@ -199,3 +199,17 @@ def test_a_cache_that_was_saved_with_a_workspace_of_its_own_works(calls):
     assert again.ws.numel() == ws.numel() and (again.ws[:256] == 0).all() and again._old == []
     again.append(**good(again)[0], stream=STREAM)
     assert calls[-1][1][25] == again.ws.data_ptr() and calls[-1][1][5] == again.k_pages.data_ptr()
+
+
+def test_rotations_whose_outputs_lie_over_other_tensors():
+    """In place is the same tensor; a part of it, or another of the call's tensors, would be read after it was written."""
+    import ctypes
+    from tests.test_paged_abi import AT, rope
+    q, k = 8 * 4000 * 128 * 2, 2 * 4000 * 128 * 2      # bytes
+    K, QO, KO = AT + (1 << 30), AT + (2 << 30), AT + (3 << 30)
+    r = rope()
+    call = lambda *at: lrsa.lib().lrsa_rotate(P.ref(), *at, ctypes.byref(r), None, 0, None)
+    for at in ((AT, K, AT + 256, KO), (AT, K, AT - 16, KO), (AT, K, AT + q - 16, KO), (AT, K, QO, K + 16), (AT, K, QO, K - k + 16),
+               (AT, K, K, KO), (AT, K, K - q + 16, KO), (AT, K, QO, AT), (AT, K, QO, AT + q - 16), (AT, K, QO, QO), (AT, K, QO, QO + q - 16),
+               (AT, AT, AT, KO), (AT, AT + 16, QO, AT + 16 + k - 16), (AT, None, AT + 16, None), (None, K, None, K + 16)):
+        assert call(*at) == INVALID, at
