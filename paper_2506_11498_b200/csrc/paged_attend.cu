@@ -910,7 +910,7 @@ struct TileTail {                  // behind the operand tiles in shared memory
 //           60K: 90 and 89, a tile then takes 1.75 us where its bytes would take 1.46).
 // What bounds it.  TQ = 2, d = 128: 2.15 us a key tile (a plain copy's rate would bring it in 1.46, its 48 products take 1.87 at 1965 MHz): beside 128 KB
 // of Q the ring has three slots, so K of the next tile but one comes 1.4 us after the slot of V is free, and then its scores take 0.75.  16 trees of 32 tokens at
-// up to 32K (28/4) 92 us: launch in front 5, first tile 7, twenty tiles 43 to 60, a second item 8, merge 8.  Four trees of 64 tokens at 120K (32/8): 430 us, at
+// up to 32K (28/4) 89 us: launch in front 5, first tile 7, twenty tiles 43 to 60, a second item 8, merge 8.  Four trees of 64 tokens at 120K (32/8): 414 us, at
 // 1.65 GHz under the power limit; without the second part of Q 371.
 // Pages end where they end: the slots behind the last row of a page, or of the sequence, get no weight, and their V rows are set to zero in
 // shared memory (what lies there belongs to nobody and may be infinite) by the softmax warps of the few tiles that have such slots.
